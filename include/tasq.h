@@ -587,6 +587,101 @@ typedef struct tasq_cost {
 int tasq_schedule_cost(const tasq_layer *layers, int L, const uint8_t *b_table, int S, int T,
                        int t_begin, int t_end, int act_bits, tasq_cost *out);
 
+/* ------------------------------------------------------------------------
+ * The attention half of a block: what stands between the quantized linears.
+ * Floating tensors are fp32, bfloat16 or IEEE half (TASQ_TYPE_*); sums,
+ * maxima, norms and statistics are fp32 and every result is rounded once.
+ * Strides are in elements and not negative, the innermost dimension is
+ * contiguous; the stride of a dimension of extent 1 is ignored.  An unknown
+ * type is TASQ_ERR_KIND.
+ * ------------------------------------------------------------------------ */
+enum { TASQ_TYPE_F32 = 0, TASQ_TYPE_BF16 = 1, TASQ_TYPE_F16 = 2 };
+
+/*
+ * Symmetric 8-bit activation codes with one scale per token:
+ *   sx[m] = max_k |x[m][k]| * RN(1 / 127),  X_out[m][k] = round(x[m][k] / sx[m]),
+ * decided in IEEE single precision (one product with the fp32 value nearest
+ * 1/127; a correctly rounded division, then ties to even), codes in
+ * [-127, 127]; a token whose scale is zero has codes 0.
+ *   x         [M][K] of x_type, row m at x + m * x_stride; finite values.
+ *             K % 8 == 0 with rows and X_out aligned to 16 and 8 bytes
+ *             takes vector loads, any other layout element loads.
+ *   X_out     int8 [M][K]; sx_out fp32 [M] (4-byte aligned).
+ * M == 0 enqueues nothing; K == 0 writes sx = 0.  Errors: TASQ_ERR_NULL,
+ * _DIM (negative sizes, x_stride < K), _OVERFLOW (K > TASQ_MAX_K), _KIND,
+ * _ALIGN (x not aligned to its elements), _HIP.
+ */
+int tasq_quantize_tokens(const void *x, int x_type, int M, int K, long long x_stride,
+                         int8_t *X_out, float *sx_out, void *stream);
+
+/*
+ * tasq_masked_linear on codes with one scale per token, and with a floating
+ * output of any type:
+ *   y[m][n] = (sum_k X[m][k] W_b[n][k]) * (sx[m] * sw[n]) + bias[n],
+ * the sum exact in int32.  X int8 [M][K], W int8 [N][K] row-major, sx fp32
+ * [M], sw fp32 [N], bias fp32 [N] or NULL, y_out [M][N] of y_type, all
+ * contiguous; b as in tasq_masked_linear.  K a multiple of 16 with X and W
+ * 16-byte aligned takes whole vector loads.  M == 0 or N == 0 enqueues
+ * nothing.  Errors: TASQ_ERR_NULL, _DIM, _BITS, _OVERFLOW, _KIND, _ALIGN (a
+ * floating array not aligned to its elements), _HIP.
+ */
+int tasq_masked_linear_tokens(const int8_t *X, const float *sx, const int8_t *W, const float *sw,
+                              const float *bias, int M, int N, int K, int b, void *y_out,
+                              int y_type, void *stream);
+
+/* Largest head dimension of tasq_norm_rotate, and most jobs of one call. */
+#define TASQ_MAX_NORM_DIM 256
+#define TASQ_MAX_NORM_JOBS 2
+
+/* One tensor of heads of tasq_norm_rotate: the queries or the keys. */
+typedef struct tasq_heads {
+    const void *x;              /* [batch][tokens][heads][dim] */
+    const void *dy;             /* backward: gradient of the output, shaped as x */
+    void *out;                  /* y, or backward dx: contiguous, shaped as x */
+    const float *weight;        /* fp32 [dim], or NULL for ones */
+    float *dweight;             /* backward: fp32 [dim], or NULL */
+    const float *cos, *sin;     /* fp32 [positions][rot / 2]; with rot > 0 */
+    const int32_t *position;    /* [batch][tokens], or NULL: token s is at s */
+    long long x_stride[3];      /* of batch, token and head */
+    long long dy_stride[3];
+    int32_t batch, tokens, heads;
+    int32_t positions;          /* rows of cos and sin */
+    int32_t rot;                /* rotated elements of a head, even, 0..dim */
+} tasq_heads;
+
+/*
+ * Root-mean-square norm of every head, then the rotation of its first rot
+ * elements by the angles of its token's position:
+ *   r = 1 / sqrt(mean_d x[d]^2 + eps),  n[d] = x[d] r weight[d],
+ *   y[i] = n[i] c - n[j] s,  y[j] = n[i] s + n[j] c
+ * for the pairs (i, j) = (i, i + rot/2), i < rot/2, or with interleaved
+ * (2f, 2f + 1), c and s the table's entry of frequency i (f) at the position;
+ * y[d] = n[d] from rot on.  A token whose position is outside the table is
+ * not rotated.
+ *   jobs  host array of n tensors (0..TASQ_MAX_NORM_JOBS), queries and keys,
+ *         in one launch; read during the call only.
+ *   type  of x, dy and out; dim even, 2..TASQ_MAX_NORM_DIM; eps >= 0.
+ * dim and rot multiples of 8 with 16-byte aligned tensors and strides (8-byte
+ * where pairs are rot/2 apart and the type has 16 bits) take vector loads.
+ * A tensor without elements enqueues nothing.  Errors: TASQ_ERR_NULL (x, out,
+ * or cos and sin with rot > 0), _DIM (a size, a stride, rot), _RANGE (n, eps),
+ * _KIND, _ALIGN (a pointer not aligned to its elements), _HIP.
+ */
+int tasq_norm_rotate(const tasq_heads *jobs, int n, int type, int dim, float eps,
+                     int interleaved, void *stream);
+
+/*
+ * Its gradient: out receives dx and, where dweight is given, dweight the sum
+ * over all heads of all tokens (in a fixed order: the same bits each time; a
+ * tensor without elements gives zeros).  workspace: 256-byte aligned device
+ * scratch of tasq_norm_rotate_workspace_bytes(n, dim) bytes
+ * (TASQ_ERR_WORKSPACE, _ALIGN otherwise).  Errors also: TASQ_ERR_NULL (dy).
+ */
+int tasq_norm_rotate_backward(const tasq_heads *jobs, int n, int type, int dim, float eps,
+                              int interleaved, void *workspace, size_t workspace_bytes,
+                              void *stream);
+size_t tasq_norm_rotate_workspace_bytes(int n, int dim);
+
 #ifdef __cplusplus
 }
 #endif

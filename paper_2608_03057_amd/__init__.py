@@ -14,6 +14,10 @@ from .api import (  # noqa: F401
     stage_of_step, run_schedule, run_schedule_noalloc, schedule_workspace_bytes,
     workspace_bytes, make_layer, status_string,
 )
+from .block import (  # noqa: F401
+    quantize_tokens, masked_linear_tokens, qk_norm_rotate, qk_norm_rotate_backward,
+    qk_norm_rotate_workspace_bytes,
+)
 from ._lib import (  # noqa: F401
     TasqError, VARIANT_AUTO, VARIANT_MASKED_I8, VARIANT_BITPLANE, VARIANT_PACKED, KIND_LINEAR,
     KIND_CONV3X3, TASQ_ACT_PARAMS_FLOATS,

@@ -37,6 +37,12 @@ VARIANT_PACKED = 3
 KIND_LINEAR = 0
 KIND_CONV3X3 = 1
 
+TYPE_F32 = 0
+TYPE_BF16 = 1
+TYPE_F16 = 2
+TASQ_MAX_NORM_DIM = 256
+TASQ_MAX_NORM_JOBS = 2
+
 # Every exported symbol the header declares.
 EXPORTS = (
     "tasq_masked_linear", "tasq_masked_conv3x3", "tasq_pack_planes", "tasq_planes_bytes",
@@ -46,6 +52,8 @@ EXPORTS = (
     "tasq_quantize_weights", "tasq_row_sums", "tasq_schedule_cost",
     "tasq_stage_of_step", "tasq_run_schedule", "tasq_run_schedule_noalloc",
     "tasq_workspace_bytes", "tasq_schedule_workspace_bytes", "tasq_status_string",
+    "tasq_quantize_tokens", "tasq_masked_linear_tokens",
+    "tasq_norm_rotate", "tasq_norm_rotate_backward", "tasq_norm_rotate_workspace_bytes",
 )
 
 
@@ -95,6 +103,17 @@ class WeightJob(ctypes.Structure):
     _fields_ = [("W", ctypes.c_void_p), ("N", ctypes.c_int32), ("K", ctypes.c_int32),
                 ("W_out", ctypes.c_void_p), ("alpha_out", ctypes.c_void_p),
                 ("z_out", ctypes.c_void_p), ("sw_out", ctypes.c_void_p)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("dy", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("dweight", ctypes.c_void_p),
+                ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p),
+                ("position", ctypes.c_void_p),
+                ("x_stride", ctypes.c_longlong * 3), ("dy_stride", ctypes.c_longlong * 3),
+                ("batch", ctypes.c_int32), ("tokens", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("positions", ctypes.c_int32),
+                ("rot", ctypes.c_int32)]
 
 
 class TasqError(RuntimeError):
@@ -156,6 +175,19 @@ def lib() -> ctypes.CDLL:
         L.tasq_workspace_bytes.restype = ctypes.c_size_t
         L.tasq_schedule_workspace_bytes.argtypes = [ctypes.POINTER(Layer), i32]
         L.tasq_schedule_workspace_bytes.restype = ctypes.c_size_t
+        i64, size = ctypes.c_longlong, ctypes.c_size_t
+        L.tasq_quantize_tokens.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
+        L.tasq_quantize_tokens.restype = i32
+        L.tasq_masked_linear_tokens.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i32,
+                                                vp]
+        L.tasq_masked_linear_tokens.restype = i32
+        L.tasq_norm_rotate.argtypes = [ctypes.POINTER(Heads), i32, i32, i32, f32, i32, vp]
+        L.tasq_norm_rotate.restype = i32
+        L.tasq_norm_rotate_backward.argtypes = [ctypes.POINTER(Heads), i32, i32, i32, f32, i32,
+                                                vp, size, vp]
+        L.tasq_norm_rotate_backward.restype = i32
+        L.tasq_norm_rotate_workspace_bytes.argtypes = [i32, i32]
+        L.tasq_norm_rotate_workspace_bytes.restype = size
         L.tasq_status_string.argtypes = [i32]
         L.tasq_status_string.restype = ctypes.c_char_p
         _lib = L

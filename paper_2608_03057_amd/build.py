@@ -39,6 +39,10 @@ SOURCES = [
     "splitk.hip",
     "kgroups.hip",
     "tiles.cpp",
+    "token_quant.hip",
+    "token_gemm.hip",
+    "head_norm.hip",
+    "block_api.cpp",
     "cost.cpp",
     "tasq_api.cpp",
 ]

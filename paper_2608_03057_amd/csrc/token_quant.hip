@@ -1,0 +1,163 @@
+// Symmetric 8-bit activation codes with one scale per token:
+//
+//   s[m] = max_k |x[m][k]| * RN(1 / 127),   Q[m][k] = round(x[m][k] / s[m]),
+//
+// decided in IEEE single precision (one product; a correctly rounded division,
+// then ties to even); a token of zeros has s = 0 and codes 0.
+//
+// One read of x: a row stays in the registers of the threads that loaded it
+// between its maximum and its codes.  Bound by memory.
+#include "block_internal.h"
+#include "floats.h"
+#include "quant.h"
+
+namespace tasq {
+
+namespace {
+
+// Scale of a row and its codes' divisor.
+struct TokenScale {
+    float s;
+    Divider div;
+    __device__ __forceinline__ explicit TokenScale(float top)
+        : s(__fmul_rn(top, 1.0f / 127.0f)), div(s)
+    {
+    }
+    __device__ __forceinline__ int code(float x) const
+    {
+        if (s == 0.0f)
+            return 0;
+        const float q = div.exact ? div(x) : __fdiv_rn(x, s);
+        return (int)fminf(fmaxf(__builtin_rintf(q), -127.0f), 127.0f);
+    }
+};
+
+// Maximum over the TPR threads of a row (TPR 64: a wave; 256: a workgroup).
+template <int TPR> __device__ __forceinline__ float row_max(float v)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1)
+        v = fmaxf(v, __shfl_xor(v, off));
+    if constexpr (TPR > 64) {
+        __shared__ float part[TPR / 64];
+        if ((threadIdx.x & 63) == 0)
+            part[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = part[0];
+#pragma unroll
+        for (int w = 1; w < TPR / 64; ++w)
+            v = fmaxf(v, part[w]);
+    }
+    return v;
+}
+
+// Rows of up to 8 * NV * TPR elements, K % 8 == 0, 16-byte aligned rows.
+template <class T, int TPR, int NV>
+__global__ void __launch_bounds__(256) k_quantize_tokens(const T *__restrict__ x, int M, int K,
+                                                         long long stride,
+                                                         int8_t *__restrict__ q,
+                                                         float *__restrict__ sx)
+{
+    const int m = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    if (m >= M)
+        return;                 // whole waves (TPR 64) or nobody (TPR 256)
+    const int t = threadIdx.x % TPR, chunks = K / 8;
+    const T *row = x + (size_t)m * stride;
+    float v[NV][8];
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (t + i * TPR < chunks) {
+            load_vec(row + 8 * (size_t)(t + i * TPR), v[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[i][e] = 0.0f;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            top = fmaxf(top, fabsf(v[i][e]));
+    const TokenScale ts(row_max<TPR>(top));
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (t + i * TPR < chunks) {
+            uint32_t w[2] = {0, 0};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                w[e >> 2] |= (uint32_t)(uint8_t)ts.code(v[i][e]) << (8 * (e & 3));
+            *reinterpret_cast<uint2 *>(q + (size_t)m * K + 8 * (size_t)(t + i * TPR)) =
+                make_uint2(w[0], w[1]);
+        }
+    }
+    if (t == 0)
+        sx[m] = ts.s;
+}
+
+// Rows of any length and alignment, read twice (the second time from L2).
+template <class T>
+__global__ void __launch_bounds__(256) k_quantize_tokens_any(const T *__restrict__ x, int K,
+                                                             long long stride,
+                                                             int8_t *__restrict__ q,
+                                                             float *__restrict__ sx)
+{
+    const int m = blockIdx.x;
+    const T *row = x + (size_t)m * stride;
+    float top = 0.0f;
+    for (int k = threadIdx.x; k < K; k += 256)
+        top = fmaxf(top, fabsf((float)row[k]));
+    const TokenScale ts(row_max<256>(top));
+    for (int k = threadIdx.x; k < K; k += 256)
+        q[(size_t)m * K + k] = (int8_t)ts.code((float)row[k]);
+    if (threadIdx.x == 0)
+        sx[m] = ts.s;
+}
+
+template <class T, int TPR, int NV>
+hipError_t launch_rows(const T *x, int M, int K, long long stride, int8_t *q, float *sx,
+                       hipStream_t stream)
+{
+    const int rows = 256 / TPR;
+    k_quantize_tokens<T, TPR, NV><<<(M + rows - 1) / rows, 256, 0, stream>>>(x, M, K, stride, q,
+                                                                           sx);
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_typed(const T *x, int M, int K, long long stride, int8_t *q, float *sx,
+                        hipStream_t stream)
+{
+    const bool aligned = K % 8 == 0 && (stride * sizeof(T)) % 16 == 0 &&
+                         reinterpret_cast<uintptr_t>(x) % 16 == 0 &&
+                         reinterpret_cast<uintptr_t>(q) % 8 == 0;
+    if (!aligned || K > 256 * 8 * 8) {
+        k_quantize_tokens_any<T><<<M, 256, 0, stream>>>(x, K, stride, q, sx);
+        return hipGetLastError();
+    }
+    if (K <= 64 * 8)
+        return launch_rows<T, 64, 1>(x, M, K, stride, q, sx, stream);
+    if (K <= 64 * 8 * 2)
+        return launch_rows<T, 64, 2>(x, M, K, stride, q, sx, stream);
+    if (K <= 64 * 8 * 4)
+        return launch_rows<T, 64, 4>(x, M, K, stride, q, sx, stream);
+    if (K <= 256 * 8 * 2)
+        return launch_rows<T, 256, 2>(x, M, K, stride, q, sx, stream);
+    if (K <= 256 * 8 * 4)
+        return launch_rows<T, 256, 4>(x, M, K, stride, q, sx, stream);
+    return launch_rows<T, 256, 8>(x, M, K, stride, q, sx, stream);
+}
+
+}  // namespace
+
+hipError_t launch_quantize_tokens(const void *x, int type, int M, int K, long long stride,
+                                  int8_t *q, float *sx, hipStream_t stream)
+{
+    return with_type(type, [&](auto zero) {
+        using T = decltype(zero);
+        return launch_typed<T>(static_cast<const T *>(x), M, K, stride, q, sx, stream);
+    });
+}
+
+}  // namespace tasq
