@@ -682,6 +682,71 @@ int tasq_norm_rotate_backward(const tasq_heads *jobs, int n, int type, int dim, 
                               void *stream);
 size_t tasq_norm_rotate_workspace_bytes(int n, int dim);
 
+/* Largest head dimension of attention. */
+#define TASQ_MAX_ATTENTION_DIM 128
+
+/*
+ * Softmax attention of q_len queries over kv_len keys and values, e.g. image
+ * tokens over an encoder's states (or over themselves, kv_len = q_len):
+ *   z[i][j] = scale q[i] . k[j],  lse[i] = log sum_j exp(z[i][j]),
+ *   out[i] = sum_j exp(z[i][j] - lse[i]) v[j],
+ * the sums over the keys that count: j < kv_lengths[batch] (clamped to
+ * [0, kv_len]) where given, and key_mask[batch][j] != 0 where given.  Keys
+ * and values that do not count are not used whatever they hold.  A query
+ * without keys gives out = 0 and lse = -infinity.  Query head h reads key
+ * head h / (heads / kv_heads).
+ *
+ * Scores, statistics and sums are fp32; the weights exp(z - max) (and in the
+ * backward pass the weights and the scores' gradients) are rounded to the
+ * tensors' type for the second product.
+ */
+typedef struct tasq_attention {
+    int32_t type;               /* of q, k, v, out and the gradients: BF16 or F16 */
+    int32_t batch, heads, kv_heads, q_len, kv_len;
+    int32_t dim;                /* a multiple of 8, 8..TASQ_MAX_ATTENTION_DIM */
+    float scale;                /* finite, > 0 */
+    const void *q;              /* [batch][q_len][heads][dim] */
+    const void *k, *v;          /* [batch][kv_len][kv_heads][dim] */
+    long long q_stride[3], k_stride[3], v_stride[3];    /* of batch, token, head */
+    const int32_t *kv_lengths;  /* device [batch], or NULL */
+    const uint8_t *key_mask;    /* device [batch][kv_len], or NULL */
+    void *out;                  /* [batch][q_len][heads][dim] contiguous */
+    float *lse;                 /* fp32 [batch][heads][q_len], or NULL (forward) */
+    const void *dout;           /* backward: gradient of out, shaped as q */
+    long long dout_stride[3];
+    void *dq, *dk, *dv;         /* backward: contiguous, shaped as q, k and v */
+    void *workspace;            /* device scratch, 256-byte aligned */
+    size_t workspace_bytes;
+} tasq_attention;
+
+/*
+ * Writes out, and lse where it is given.  With
+ * tasq_attention_workspace_bytes(a, 0) bytes of workspace, few rows over many
+ * keys are cut into ranges of keys that run side by side; a smaller
+ * workspace, or none, runs them uncut.
+ *
+ * Tensors are 16-byte aligned with strides that are multiples of 8
+ * (TASQ_ERR_ALIGN otherwise); a token stride is below 2^23 elements.  No
+ * queries: enqueues nothing.  Errors: TASQ_ERR_NULL, _DIM (a size, a stride,
+ * heads % kv_heads != 0, more than 2^30 rows or keys), _KIND, _RANGE (scale),
+ * _ALIGN, _HIP.
+ */
+int tasq_attention_forward(const tasq_attention *a, void *stream);
+
+/*
+ * Writes dq, dk and dv from dout and from the out and lse of the forward call
+ * (both are read only here).  Keys that do not count get gradients of zero,
+ * shared key heads the sum over their query heads; sums run in a fixed order,
+ * so that a call gives the same bits each time.  The workspace is required:
+ * tasq_attention_workspace_bytes(a, 1) bytes, of which 4 per query and head
+ * always (TASQ_ERR_WORKSPACE), the rest where ranges run side by side.
+ */
+int tasq_attention_backward(const tasq_attention *a, void *stream);
+
+/* Bytes of workspace for the call; reads the sizes and the type only, and is
+ * 0 where they are not valid. */
+size_t tasq_attention_workspace_bytes(const tasq_attention *a, int backward);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,7 +16,7 @@ from .api import (  # noqa: F401
 )
 from .block import (  # noqa: F401
     quantize_tokens, masked_linear_tokens, qk_norm_rotate, qk_norm_rotate_backward,
-    qk_norm_rotate_workspace_bytes,
+    qk_norm_rotate_workspace_bytes, attention, attention_backward, attention_workspace_bytes,
 )
 from ._lib import (  # noqa: F401
     TasqError, VARIANT_AUTO, VARIANT_MASKED_I8, VARIANT_BITPLANE, VARIANT_PACKED, KIND_LINEAR,

@@ -42,6 +42,7 @@ TYPE_BF16 = 1
 TYPE_F16 = 2
 TASQ_MAX_NORM_DIM = 256
 TASQ_MAX_NORM_JOBS = 2
+TASQ_MAX_ATTENTION_DIM = 128
 
 # Every exported symbol the header declares.
 EXPORTS = (
@@ -54,6 +55,7 @@ EXPORTS = (
     "tasq_workspace_bytes", "tasq_schedule_workspace_bytes", "tasq_status_string",
     "tasq_quantize_tokens", "tasq_masked_linear_tokens",
     "tasq_norm_rotate", "tasq_norm_rotate_backward", "tasq_norm_rotate_workspace_bytes",
+    "tasq_attention_forward", "tasq_attention_backward", "tasq_attention_workspace_bytes",
 )
 
 
@@ -114,6 +116,20 @@ class Heads(ctypes.Structure):
                 ("batch", ctypes.c_int32), ("tokens", ctypes.c_int32),
                 ("heads", ctypes.c_int32), ("positions", ctypes.c_int32),
                 ("rot", ctypes.c_int32)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("q_len", ctypes.c_int32),
+                ("kv_len", ctypes.c_int32), ("dim", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_longlong * 3), ("k_stride", ctypes.c_longlong * 3),
+                ("v_stride", ctypes.c_longlong * 3),
+                ("kv_lengths", ctypes.c_void_p), ("key_mask", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("dout", ctypes.c_void_p),
+                ("dout_stride", ctypes.c_longlong * 3), ("dq", ctypes.c_void_p),
+                ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 class TasqError(RuntimeError):
@@ -188,6 +204,12 @@ def lib() -> ctypes.CDLL:
         L.tasq_norm_rotate_backward.restype = i32
         L.tasq_norm_rotate_workspace_bytes.argtypes = [i32, i32]
         L.tasq_norm_rotate_workspace_bytes.restype = size
+        for name in ("tasq_attention_forward", "tasq_attention_backward"):
+            f = getattr(L, name)
+            f.argtypes = [ctypes.POINTER(Attention), vp]
+            f.restype = i32
+        L.tasq_attention_workspace_bytes.argtypes = [ctypes.POINTER(Attention), i32]
+        L.tasq_attention_workspace_bytes.restype = size
         L.tasq_status_string.argtypes = [i32]
         L.tasq_status_string.restype = ctypes.c_char_p
         _lib = L

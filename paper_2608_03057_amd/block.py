@@ -14,7 +14,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import _lib
-from ._lib import Heads, check
+from ._lib import Attention, Heads, check
 from .api import _need, _ptr, _stream
 
 _TYPES = {torch.float32: _lib.TYPE_F32, torch.bfloat16: _lib.TYPE_BF16,
@@ -181,3 +181,110 @@ def qk_norm_rotate_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: tor
     if rc:
         check(rc, "tasq_norm_rotate_backward")
     return gq, gk, dwq, dwk
+
+
+def _attention(q, k, v, kv_lengths, key_mask, scale) -> Attention:
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q, k and v must be [batch, tokens, heads, dim]")
+    B, SQ, H, D = q.shape
+    SK, HK = k.shape[1:3]
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"q must be bfloat16 or float16, got {q.dtype}")
+    _strided(q, q.dtype, q.shape, "q")
+    _strided(k, q.dtype, (B, SK, HK, D), "k")
+    _strided(v, q.dtype, (B, SK, HK, D), "v")
+    _need(kv_lengths, torch.int32, (B,), "kv_lengths")
+    if key_mask is not None:
+        if key_mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError("key_mask must be bool or uint8")
+        _need(key_mask, key_mask.dtype, (B, SK), "key_mask")
+    a = Attention()
+    a.type = _TYPES[q.dtype]
+    a.batch, a.heads, a.kv_heads, a.q_len, a.kv_len, a.dim = B, H, HK, SQ, SK, D
+    a.scale = D ** -0.5 if scale is None else scale
+    a.q, a.k, a.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
+    a.q_stride[:] = q.stride()[:3]
+    a.k_stride[:] = k.stride()[:3]
+    a.v_stride[:] = v.stride()[:3]
+    a.kv_lengths, a.key_mask = _ptr(kv_lengths), _ptr(key_mask)
+    return a
+
+
+def attention_workspace_bytes(q: torch.Tensor, k: torch.Tensor, *, backward: bool = False) -> int:
+    """Workspace with which attention (or its backward pass) of these shapes
+    runs ranges of a long axis side by side."""
+    a = _attention(q, k, k, None, None, None)
+    return _lib.lib().tasq_attention_workspace_bytes(ctypes.byref(a), backward)
+
+
+def _take_workspace(a: Attention, workspace, device, backward):
+    """Sets the workspace, allocated when None and of any use; returns what
+    has to live until the call has been made."""
+    if workspace is None:
+        nbytes = _lib.lib().tasq_attention_workspace_bytes(ctypes.byref(a), backward)
+        if not nbytes:
+            return None
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    ws = _workspace(workspace, nbytes, device, "attention")
+    a.workspace, a.workspace_bytes = ws.data_ptr(), nbytes
+    return ws
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
+              kv_lengths: Optional[torch.Tensor] = None,
+              key_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+              out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+              want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
+    """(out [B, SQ, H, D], lse fp32 [B, H, SQ] or None) of softmax attention of
+    queries q [B, SQ, H, D] over keys and values [B, SK, HK, D] of another
+    length, bfloat16 or half at any strides that are multiples of 8; H a
+    multiple of HK, whose heads are shared.  Keys count where they are below
+    kv_lengths (int32 [B]) and nonzero in key_mask (bool or uint8 [B, SK]); a
+    query without keys gives zeros.  scale defaults to D ** -0.5."""
+    a = _attention(q, k, v, kv_lengths, key_mask, scale)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None and want_lse:
+        lse = torch.empty((a.batch, a.heads, a.q_len), dtype=torch.float32, device=q.device)
+    _need(out, q.dtype, q.shape, "out")
+    _need(lse, torch.float32, (a.batch, a.heads, a.q_len), "lse")
+    a.out, a.lse = out.data_ptr(), _ptr(lse)
+    ws = _take_workspace(a, workspace, q.device, 0)  # noqa: F841
+    rc = _lib.lib().tasq_attention_forward(ctypes.byref(a), _stream())
+    if rc:
+        check(rc, "tasq_attention_forward")
+    return out, lse
+
+
+def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                       out: torch.Tensor, lse: torch.Tensor, *,
+                       kv_lengths: Optional[torch.Tensor] = None,
+                       key_mask: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                       dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                       dv: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None):
+    """Gradients (dq, dk, dv) of attention from the gradient dout of its
+    output, with the out and lse that the forward call gave for the same
+    arguments."""
+    a = _attention(q, k, v, kv_lengths, key_mask, scale)
+    _strided(dout, q.dtype, q.shape, "dout")
+    _need(out, q.dtype, q.shape, "out")
+    _need(lse, torch.float32, (a.batch, a.heads, a.q_len), "lse")
+    if dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if dk is None:
+        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    if dv is None:
+        dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    _need(dq, q.dtype, q.shape, "dq")
+    _need(dk, q.dtype, k.shape, "dk")
+    _need(dv, q.dtype, k.shape, "dv")
+    a.out, a.lse, a.dout = out.data_ptr(), lse.data_ptr(), dout.data_ptr()
+    a.dout_stride[:] = dout.stride()[:3]
+    a.dq, a.dk, a.dv = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
+    ws = _take_workspace(a, workspace, q.device, 1)  # noqa: F841
+    rc = _lib.lib().tasq_attention_backward(ctypes.byref(a), _stream())
+    if rc:
+        check(rc, "tasq_attention_backward")
+    return dq, dk, dv

@@ -42,6 +42,10 @@ SOURCES = [
     "token_quant.hip",
     "token_gemm.hip",
     "head_norm.hip",
+    "attn_fwd_bf16.hip",
+    "attn_fwd_f16.hip",
+    "attn_bwd_bf16.hip",
+    "attn_bwd_f16.hip",
     "block_api.cpp",
     "cost.cpp",
     "tasq_api.cpp",

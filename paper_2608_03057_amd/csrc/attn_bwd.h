@@ -1,0 +1,367 @@
+// Attention, backward, from the kept O and log-sum-exp:
+//   P = exp(scale Q K^T - lse),   dS = P (dO V^T - delta),
+//   delta = rowsum(dO O),
+//   dQ = scale dS K,   dK = scale dS^T Q,   dV = P^T dO.
+// Two kernels, both recomputing S and dP, so that every gradient is summed in
+// registers in a fixed order: k_attn_dq has the queries resident and streams
+// keys and values, k_attn_dkdv has the keys resident and streams queries and
+// output gradients (over all query heads that share the key head).  S, P, dP,
+// dS and the sums are fp32; P and dS are rounded to the inputs' type as the
+// operands of the products.
+//
+// A weight of a long row is small, and as fp32 or half it would lose bits or
+// vanish: the kernels hold P' = 2^kShift P (kShift is taken off the exponent's
+// lse) and dS' = P' (kScore dO V^T - kScore delta), and take the factors out of
+// the sums at the end.  bfloat16 has fp32's range, so both carry 2^32 and
+// weights down to 2^-158 count; half ends at 65504, so P carries 2^14 and dS,
+// which is as large as the gradients are, nothing.
+//
+// Where there are few resident tiles the streamed axis is cut into ranges
+// whose fp32 parts k_attn_sum adds up in order.
+#pragma once
+
+#include "attn.h"
+
+namespace tasq {
+
+template <class T> struct Range;
+template <> struct Range<bf16_t> {
+    static constexpr float kShift = 32.0f, kScore = 1.0f;
+    static constexpr float kOutP = 0x1p-32f, kOutS = 0x1p-32f;  // of sums of P' and dS'
+};
+template <> struct Range<f16_t> {
+    static constexpr float kShift = 14.0f, kScore = 0x1p-14f;
+    static constexpr float kOutP = 0x1p-14f, kOutS = 1.0f;
+};
+
+template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnCall a)
+{
+    constexpr int NT = 256, DB = Tile<KS>::DB;
+    __shared__ __attribute__((aligned(16))) char lds[2][2][Tile<KS>::kBytes];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int u = attn_unit(blockIdx.x, gridDim.x);
+    const int mt = u % a.row_tiles;
+    u /= a.row_tiles;
+    const int sp = u % a.splits;
+    u /= a.splits;
+    const int hk = u % a.kv_heads, b = u / a.kv_heads;
+    const int group = a.heads / a.kv_heads;
+
+    const int rows = group * a.q_len;
+    const int m = mt * 128 + wave * 32 + (lane & 31);
+    const bool ok = m < rows;
+    const int g = ok ? m / a.q_len : 0, s = ok ? m - g * a.q_len : 0;
+    const int head = hk * group + g;
+    const bool busy = mt * 128 + wave * 32 < rows;
+    const size_t at = (((size_t)b * a.q_len + s) * a.heads + head) * a.dim;
+    const size_t row = ((size_t)b * a.heads + head) * a.q_len + s;
+    u32x4 qf[KS], gf[KS];
+    load_columns<KS>(static_cast<const T *>(a.q) + b * a.q_stride[0] + s * a.q_stride[1] +
+                         head * a.q_stride[2],
+                     ok, a.dim, qf);
+    load_columns<KS>(static_cast<const T *>(a.dout) + b * a.dout_stride[0] +
+                         s * a.dout_stride[1] + head * a.dout_stride[2],
+                     ok, a.dim, gf);
+    float delta = 0.0f;
+    {
+        u32x4 of[KS];
+        load_columns<KS>(static_cast<const T *>(a.out) + at, ok, a.dim, of);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x2 x = unpack2<T>(of[ks][i]), y = unpack2<T>(gf[ks][i]);
+                delta += x.x * y.x + x.y * y.y;
+            }
+        delta = across_halves(delta, [](float p, float q) { return p + q; });
+        if (ok && lane < 32 && sp == 0)
+            a.delta[row] = delta;
+    }
+    // A row without keys (lse = -inf) has P = 0.
+    float lse2 = ok ? a.lse[row] * kLog2e - Range<T>::kShift : 0.0f;
+    if (lse2 == -__builtin_huge_valf())
+        lse2 = __builtin_huge_valf();
+    delta *= Range<T>::kScore;
+
+    const int n = key_count(a, b);
+    const int t0 = sp * a.split_tiles;
+    const int t1 = min((n + kAttnTile - 1) / kAttnTile, t0 + a.split_tiles);
+    const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2];
+    const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2];
+    const uint32_t kb = 2u * (uint32_t)a.k_stride[1], vb = 2u * (uint32_t)a.v_stride[1];
+
+    v16f_t dq[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+        dq[db] = v16f_t{};
+    Stage<KS, NT> kst, vst;
+    uint64_t live = 0, now = 0;
+    int next_byte = 0;
+    auto fetch = [&](int t) {
+        kst.load(k + (size_t)t * kAttnTile * a.k_stride[1], kb, a.dim, live);
+        vst.load(v + (size_t)t * kAttnTile * a.v_stride[1], vb, a.dim, live);
+    };
+    if (t0 < t1) {
+        now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
+        fetch(t0);
+        next_byte = mask_byte(a, b, n, t0 + 1);
+        kst.store(lds[0][0]);
+        vst.store(lds[0][1]);
+        __syncthreads();
+    }
+    for (int t = t0; t < t1; ++t) {
+        const char *kt = lds[(t - t0) & 1][0], *vt = lds[(t - t0) & 1][1];
+        if (t + 1 < t1) {
+            live = live_keys(a, n, t + 1, next_byte);
+            fetch(t + 1);
+            next_byte = mask_byte(a, b, n, t + 2);
+        }
+        if (busy && now) {
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) {
+                v16f_t sa = {}, pa = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    sa = mfma(T{}, Tile<KS>::rows(kt, rb, ks), qf[ks], sa);
+                    pa = mfma(T{}, Tile<KS>::rows(vt, rb, ks), gf[ks], pa);
+                }
+                float x[16];
+                const uint32_t bits = (uint32_t)(now >> (32 * rb)) >> (4 * (lane >> 5));
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float p = __builtin_amdgcn_exp2f(sa[i] * a.scale_log2 - lse2);
+                    if (now != ~0ull && !((bits >> (8 * (i / 4) + i % 4)) & 1))
+                        p = 0.0f;
+                    x[i] = p * (pa[i] * Range<T>::kScore - delta);
+                }
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2) {
+                    const u32x4 ds = pack_rows<T>(x, s2);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db)
+                        dq[db] =
+                            mfma(T{}, Tile<KS>::columns(kt, 32 * rb + 16 * s2, db), ds, dq[db]);
+                }
+            }
+        }
+        now = live;
+        if (t + 1 < t1) {
+            kst.store(lds[(t + 1 - t0) & 1][0]);
+            vst.store(lds[(t + 1 - t0) & 1][1]);
+        }
+        __syncthreads();
+    }
+    if (a.splits > 1)
+        store_columns_f32<DB>(a.part + (size_t)sp * a.batch * a.q_len * a.heads * a.dim + at, ok,
+                              a.dim, dq, a.scale * Range<T>::kOutS);
+    else
+        store_columns<T, DB>(static_cast<T *>(a.dq) + at, ok, a.dim, dq,
+                             a.scale * Range<T>::kOutS);
+}
+
+template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv(AttnCall a)
+{
+    constexpr int NT = 256, DB = Tile<KS>::DB;
+    __shared__ __attribute__((aligned(16))) char lds[2][2][Tile<KS>::kBytes];
+    __shared__ __attribute__((aligned(16))) float stat[2][2][kAttnTile];    // lse, delta
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int u = attn_unit(blockIdx.x, gridDim.x);
+    const int kt_ = u % a.key_tiles;
+    u /= a.key_tiles;
+    const int sp = u % a.kv_splits;
+    u /= a.kv_splits;
+    const int hk = u % a.kv_heads, b = u / a.kv_heads;
+    const int group = a.heads / a.kv_heads;
+
+    const int n = key_count(a, b);
+    const int key = kt_ * 128 + wave * 32 + (lane & 31);
+    const bool ok = key < a.kv_len;
+    const bool counts =
+        key < n && (!a.key_mask || a.key_mask[(size_t)b * a.kv_len + key] != 0);
+    const bool busy = __ballot(counts) != 0;
+    u32x4 kf[KS], vf[KS];
+    load_columns<KS>(static_cast<const T *>(a.k) + b * a.k_stride[0] + key * a.k_stride[1] +
+                         hk * a.k_stride[2],
+                     counts, a.dim, kf);
+    load_columns<KS>(static_cast<const T *>(a.v) + b * a.v_stride[0] + key * a.v_stride[1] +
+                         hk * a.v_stride[2],
+                     counts, a.dim, vf);
+
+    v16f_t dk[DB], dv[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+        dk[db] = dv[db] = v16f_t{};
+    // Tiles of 64 queries, the group's heads one after the other.
+    const int per_head = (a.q_len + kAttnTile - 1) / kAttnTile;
+    const int t0 = sp * a.kv_split_tiles;
+    const int t1 = kt_ * 128 < n ? min(group * per_head, t0 + a.kv_split_tiles) : t0;
+    Stage<KS, NT> qst, gst;
+    float st = 0.0f;
+    auto fetch = [&](int t) {
+        const int g = t / per_head, s0 = (t - g * per_head) * kAttnTile;
+        const int left = a.q_len - s0, head = hk * group + g;
+        const uint64_t live = left >= kAttnTile ? ~0ull : (1ull << left) - 1;
+        qst.load(static_cast<const T *>(a.q) + b * a.q_stride[0] + s0 * a.q_stride[1] +
+                     head * a.q_stride[2],
+                 2u * (uint32_t)a.q_stride[1], a.dim, live);
+        gst.load(static_cast<const T *>(a.dout) + b * a.dout_stride[0] + s0 * a.dout_stride[1] +
+                     head * a.dout_stride[2],
+                 2u * (uint32_t)a.dout_stride[1], a.dim, live);
+        if (wave < 2) {         // wave 0 has the rows' lse, wave 1 their delta
+            const float *p = wave == 0 ? a.lse : a.delta;
+            st = lane < left ? p[((size_t)b * a.heads + head) * a.q_len + s0 + lane]
+                             : -__builtin_huge_valf();
+            if (wave == 0) {    // rows past the end and rows without keys have P = 0
+                st = st * kLog2e - Range<T>::kShift;
+                if (st == -__builtin_huge_valf())
+                    st = __builtin_huge_valf();
+            } else {
+                st = lane < left ? st * Range<T>::kScore : 0.0f;
+            }
+        }
+    };
+    auto put = [&](int i) {
+        qst.store(lds[i][0]);
+        gst.store(lds[i][1]);
+        if (wave < 2)
+            stat[i][wave][lane] = st;
+    };
+    if (t0 < t1) {
+        fetch(t0);
+        put(0);
+        __syncthreads();
+    }
+    for (int t = t0; t < t1; ++t) {
+        const int cur = (t - t0) & 1;
+        const char *qt = lds[cur][0], *gt = lds[cur][1];
+        if (t + 1 < t1)
+            fetch(t + 1);
+        if (busy) {
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) {
+                v16f_t sa = {}, pa = {};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    sa = mfma(T{}, Tile<KS>::rows(qt, rb, ks), kf[ks], sa);
+                    pa = mfma(T{}, Tile<KS>::rows(gt, rb, ks), vf[ks], pa);
+                }
+                float p[16], x[16];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = 32 * rb + 8 * q + 4 * (lane >> 5);
+                    const float4 l = *reinterpret_cast<const float4 *>(&stat[cur][0][r]);
+                    const float4 d = *reinterpret_cast<const float4 *>(&stat[cur][1][r]);
+                    const float ls[4] = {l.x, l.y, l.z, l.w}, de[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        p[4 * q + i] =
+                            __builtin_amdgcn_exp2f(sa[4 * q + i] * a.scale_log2 - ls[i]);
+                        x[4 * q + i] =
+                            p[4 * q + i] * (pa[4 * q + i] * Range<T>::kScore - de[i]);
+                    }
+                }
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2) {
+                    const u32x4 pf = pack_rows<T>(p, s2), ds = pack_rows<T>(x, s2);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) {
+                        dv[db] =
+                            mfma(T{}, Tile<KS>::columns(gt, 32 * rb + 16 * s2, db), pf, dv[db]);
+                        dk[db] =
+                            mfma(T{}, Tile<KS>::columns(qt, 32 * rb + 16 * s2, db), ds, dk[db]);
+                    }
+                }
+            }
+        }
+        if (t + 1 < t1)
+            put(cur ^ 1);
+        __syncthreads();
+    }
+    // Keys that do not count have gradients of zero.
+    if (!counts) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            dk[db] = dv[db] = v16f_t{};
+    }
+    const size_t at = (((size_t)b * a.kv_len + key) * a.kv_heads + hk) * a.dim;
+    if (a.kv_splits > 1) {
+        const size_t all = (size_t)a.batch * a.kv_len * a.kv_heads * a.dim;
+        store_columns_f32<DB>(a.kv_part + 2 * sp * all + at, ok, a.dim, dk,
+                              a.scale * Range<T>::kOutS);
+        store_columns_f32<DB>(a.kv_part + (2 * sp + 1) * all + at, ok, a.dim, dv,
+                              Range<T>::kOutP);
+    } else {
+        store_columns<T, DB>(static_cast<T *>(a.dk) + at, ok, a.dim, dk,
+                             a.scale * Range<T>::kOutS);
+        store_columns<T, DB>(static_cast<T *>(a.dv) + at, ok, a.dim, dv, Range<T>::kOutP);
+    }
+}
+
+// out[i] = sum of `parts` fp32 parts, `step` elements apart, four at a time
+// (a head has a multiple of eight).
+template <class T>
+__global__ void __launch_bounds__(256) k_attn_sum(const float *__restrict__ part, size_t n,
+                                                  size_t step, int parts, T *__restrict__ out)
+{
+    const size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
+    if (i >= n)
+        return;
+    float s[4] = {};
+    for (int p = 0; p < parts; ++p) {
+        float v[4];
+        load_vec(part + p * step + i, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            s[e] += v[e];
+    }
+    store_vec(out + i, s);
+}
+
+template <class T>
+hipError_t attn_sum(const float *part, size_t n, size_t step, int parts, void *out,
+                    hipStream_t stream)
+{
+    k_attn_sum<T><<<(unsigned)((n / 4 + 255) / 256), 256, 0, stream>>>(part, n, step, parts,
+                                                                     static_cast<T *>(out));
+    return hipGetLastError();
+}
+
+template <class T, int KS> hipError_t attn_backward_ks(const AttnCall &a, hipStream_t stream)
+{
+    const long long rows = (long long)a.batch * a.kv_heads * a.splits * a.row_tiles;
+    const long long keys = (long long)a.batch * a.kv_heads * a.kv_splits * a.key_tiles;
+    hipError_t e = hipSuccess;
+    if (rows > 0) {
+        k_attn_dq<T, KS><<<(unsigned)rows, 256, 0, stream>>>(a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && keys > 0) {
+        k_attn_dkdv<T, KS><<<(unsigned)keys, 256, 0, stream>>>(a);
+        e = hipGetLastError();
+    }
+    const size_t nq = (size_t)a.batch * a.q_len * a.heads * a.dim;
+    const size_t nk = (size_t)a.batch * a.kv_len * a.kv_heads * a.dim;
+    if (e == hipSuccess && a.splits > 1)
+        e = attn_sum<T>(a.part, nq, nq, a.splits, a.dq, stream);
+    if (e == hipSuccess && a.kv_splits > 1)
+        e = attn_sum<T>(a.kv_part, nk, 2 * nk, a.kv_splits, a.dk, stream);
+    if (e == hipSuccess && a.kv_splits > 1)
+        e = attn_sum<T>(a.kv_part + nk, nk, 2 * nk, a.kv_splits, a.dv, stream);
+    return e;
+}
+
+template <class T> hipError_t attn_backward_typed(const AttnCall &a, hipStream_t stream)
+{
+    switch ((a.dim + 15) / 16) {
+    case 1:
+    case 2: return attn_backward_ks<T, 2>(a, stream);
+    case 3: return attn_backward_ks<T, 3>(a, stream);
+    case 4: return attn_backward_ks<T, 4>(a, stream);
+    case 5: return attn_backward_ks<T, 5>(a, stream);
+    case 6: return attn_backward_ks<T, 6>(a, stream);
+    case 7: return attn_backward_ks<T, 7>(a, stream);
+    default: return attn_backward_ks<T, 8>(a, stream);
+    }
+}
+
+}  // namespace tasq

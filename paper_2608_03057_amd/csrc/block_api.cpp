@@ -97,6 +97,170 @@ int norm_rotate(const tasq_heads *jobs, int n, int type, int dim, float eps, int
                                            static_cast<hipStream_t>(stream)));
 }
 
+// Ranges that `tiles` streamed tiles are cut into when `base` workgroups would
+// run uncut: enough to give each compute unit `per_cu` workgroups, at least
+// four tiles each.
+void plan_ranges(long long base, int tiles, int per_cu, int *ranges, int *range_tiles)
+{
+    *ranges = 1;
+    *range_tiles = tiles > 0 ? tiles : 1;
+    if (base <= 0 || tiles < 8)
+        return;
+    const long long want = 256LL * per_cu / base;
+    const int most = tiles / 4;
+    const int r = want < 2 ? 1 : want < most ? (int)want : most;
+    *range_tiles = (tiles + r - 1) / r;
+    *ranges = (tiles + *range_tiles - 1) / *range_tiles;
+}
+
+constexpr size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+// The launch's shape (with cuts if `cut`), and the bytes of its workspace.
+size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
+{
+    const int group = c.kv_heads ? c.heads / c.kv_heads : 0;
+    const long long pairs = (long long)c.batch * c.kv_heads;
+    const int key_tiles = (c.kv_len + 63) / 64;
+    c.row_tiles = (int)(((long long)group * c.q_len + 127) / 128);
+    plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, backward ? 2 : 3, &c.splits,
+                &c.split_tiles);
+    const size_t rows = (size_t)c.batch * c.heads * c.q_len;
+    size_t bytes = 0;
+    if (c.splits > 1) {
+        bytes += round256(c.splits * rows * c.dim * sizeof(float));
+        bytes += backward ? 0 : round256(c.splits * rows * sizeof(float));
+    }
+    if (backward) {
+        c.key_tiles = (c.kv_len + 127) / 128;
+        plan_ranges(cut ? pairs * c.key_tiles : 0, group * ((c.q_len + 63) / 64), 2,
+                    &c.kv_splits, &c.kv_split_tiles);
+        bytes += round256(rows * sizeof(float));
+        if (c.kv_splits > 1)
+            bytes += round256((size_t)c.kv_splits * 2 * c.batch * c.kv_len * c.kv_heads * c.dim *
+                              sizeof(float));
+    }
+    return bytes;
+}
+
+void lay_out_workspace(tasq::AttnCall &c, bool backward, void *workspace)
+{
+    char *p = static_cast<char *>(workspace);
+    const size_t rows = (size_t)c.batch * c.heads * c.q_len;
+    auto take = [&](size_t floats) {
+        float *r = reinterpret_cast<float *>(p);
+        p += round256(floats * sizeof(float));
+        return r;
+    };
+    if (c.splits > 1) {
+        c.part = take(c.splits * rows * c.dim);
+        if (!backward)
+            c.part_lse = take(c.splits * rows);
+    }
+    if (backward) {
+        c.delta = take(rows);
+        if (c.kv_splits > 1)
+            c.kv_part = take((size_t)c.kv_splits * 2 * c.batch * c.kv_len * c.kv_heads * c.dim);
+    }
+}
+
+// Strides of a [batch][tokens][heads][dim] operand, those of extents below 2
+// as zero.
+int take_strides(const long long *in, int batch, int tokens, int heads, long long *out)
+{
+    const int extent[3] = {batch, tokens, heads};
+    for (int i = 0; i < 3; ++i) {
+        out[i] = extent[i] > 1 ? in[i] : 0;
+        // A tile of 64 rows is addressed with 32-bit byte offsets.
+        if (out[i] < 0 || (i == 1 && out[i] >= (1LL << 23)))
+            return TASQ_ERR_DIM;
+        if (out[i] % 8)
+            return TASQ_ERR_ALIGN;
+    }
+    return TASQ_OK;
+}
+
+// Sizes and types: what tasq_attention_workspace_bytes needs to be valid.
+int check_attention_sizes(const tasq_attention *a, tasq::AttnCall &c)
+{
+    if (!a)
+        return TASQ_ERR_NULL;
+    if (a->type != TASQ_TYPE_BF16 && a->type != TASQ_TYPE_F16)
+        return TASQ_ERR_KIND;
+    if (a->batch < 0 || a->heads < 0 || a->kv_heads < 0 || a->q_len < 0 || a->kv_len < 0 ||
+        a->dim < 8 || a->dim > TASQ_MAX_ATTENTION_DIM || a->dim % 8 ||
+        (a->kv_heads ? a->heads % a->kv_heads : a->heads) != 0)
+        return TASQ_ERR_DIM;
+    // Rows, keys and workgroups are counted in 32 bits.
+    const long long most = 1LL << 30;
+    if (a->kv_len > most || (long long)a->heads * a->q_len > most ||
+        (long long)a->batch * a->kv_heads > (1 << 20) ||
+        (long long)a->batch * a->heads * (a->q_len / 32 + 1LL) > most ||
+        (long long)a->batch * a->kv_heads * (a->kv_len / 32 + 1LL) > most)
+        return TASQ_ERR_DIM;
+    c.type = a->type;
+    c.batch = a->batch;
+    c.heads = a->heads;
+    c.kv_heads = a->kv_heads;
+    c.q_len = a->q_len;
+    c.kv_len = a->kv_len;
+    c.dim = a->dim;
+    return TASQ_OK;
+}
+
+int attention(const tasq_attention *a, bool backward, void *stream)
+{
+    tasq::AttnCall c{};
+    if (int rc = check_attention_sizes(a, c))
+        return rc;
+    if (!(a->scale > 0.0f) || isinf(a->scale))
+        return TASQ_ERR_RANGE;
+    const bool queries = c.batch && c.heads && c.q_len, keys = c.batch && c.kv_heads && c.kv_len;
+    if (!queries && !(backward && keys))
+        return TASQ_OK;
+    if ((queries && (!a->q || !a->out)) || (keys && (!a->k || !a->v)))
+        return TASQ_ERR_NULL;
+    if (backward && ((queries && (!a->dout || !a->lse || !a->dq)) || (keys && (!a->dk || !a->dv))))
+        return TASQ_ERR_NULL;
+    const void *wide[] = {a->q, a->k, a->v, a->out, a->dout, a->dq, a->dk, a->dv};
+    for (int i = 0; i < (backward ? 8 : 4); ++i)
+        if (!aligned_to(wide[i], 16))
+            return TASQ_ERR_ALIGN;
+    if (!aligned_to(a->kv_lengths, 4) || !aligned_to(a->lse, 4) ||
+        !aligned_to(a->workspace, 256))
+        return TASQ_ERR_ALIGN;
+    int rc = take_strides(a->q_stride, c.batch, c.q_len, c.heads, c.q_stride);
+    if (!rc)
+        rc = take_strides(a->k_stride, c.batch, c.kv_len, c.kv_heads, c.k_stride);
+    if (!rc)
+        rc = take_strides(a->v_stride, c.batch, c.kv_len, c.kv_heads, c.v_stride);
+    if (!rc && backward)
+        rc = take_strides(a->dout_stride, c.batch, c.q_len, c.heads, c.dout_stride);
+    if (rc)
+        return rc;
+    c.q = a->q;
+    c.k = a->k;
+    c.v = a->v;
+    c.kv_lengths = a->kv_lengths;
+    c.key_mask = a->key_mask;
+    c.out = a->out;
+    c.lse = a->lse;
+    c.dout = a->dout;
+    c.dq = a->dq;
+    c.dk = a->dk;
+    c.dv = a->dv;
+    c.scale = a->scale;
+    c.scale_log2 = a->scale * 1.4426950408889634f;
+    const size_t have = a->workspace ? a->workspace_bytes : 0;
+    if (plan_attention(c, backward, true) > have && plan_attention(c, backward, false) > have)
+        return TASQ_ERR_WORKSPACE;
+    lay_out_workspace(c, backward, a->workspace);
+    const bool bf16 = c.type == TASQ_TYPE_BF16;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (backward)
+        return status(bf16 ? tasq::attn_backward_bf16(c, st) : tasq::attn_backward_f16(c, st));
+    return status(bf16 ? tasq::attn_forward_bf16(c, st) : tasq::attn_forward_f16(c, st));
+}
+
 }  // namespace
 
 extern "C" {
@@ -162,6 +326,24 @@ int tasq_norm_rotate_backward(const tasq_heads *jobs, int n, int type, int dim, 
 {
     return norm_rotate(jobs, n, type, dim, eps, interleaved, true, workspace, workspace_bytes,
                        stream);
+}
+
+size_t tasq_attention_workspace_bytes(const tasq_attention *a, int backward)
+{
+    tasq::AttnCall c{};
+    if (check_attention_sizes(a, c))
+        return 0;
+    return plan_attention(c, backward != 0, true);
+}
+
+int tasq_attention_forward(const tasq_attention *a, void *stream)
+{
+    return attention(a, false, stream);
+}
+
+int tasq_attention_backward(const tasq_attention *a, void *stream)
+{
+    return attention(a, true, stream);
 }
 
 }  // extern "C"

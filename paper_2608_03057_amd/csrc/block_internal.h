@@ -49,4 +49,29 @@ struct HeadCall {
 // part: n * kHeadGroups * dim floats (grad only).
 hipError_t launch_norm_rotate(const HeadCall &call, bool grad, float *part, hipStream_t stream);
 
+// Attention (attn_fwd.h, attn_bwd.h).  Rows are (query head of the group,
+// query) pairs of one key head; a workgroup has 128 rows, or 128 keys in
+// k_attn_dkdv.  plan_attention sets the launch's shape.
+struct AttnCall {
+    const void *q, *k, *v;
+    const int32_t *kv_lengths;  // [batch] or null
+    const uint8_t *key_mask;    // [batch][kv_len] or null
+    void *out;                  // [batch][q_len][heads][dim]
+    float *lse;                 // [batch][heads][q_len], null if not wanted
+    const void *dout;           // backward
+    void *dq, *dk, *dv;
+    long long q_stride[3], k_stride[3], v_stride[3], dout_stride[3];    // batch, token, head
+    int type, batch, heads, kv_heads, q_len, kv_len, dim;
+    float scale, scale_log2;    // scale, and scale * log2(e)
+    int row_tiles, splits, split_tiles;             // ranges of the keys, in tiles of 64
+    int key_tiles, kv_splits, kv_split_tiles;       // ranges of the rows (k_attn_dkdv)
+    float *part, *part_lse;     // [splits][batch][..] parts of out (or dq) and lse
+    float *kv_part;             // [kv_splits][2][batch][kv_len][kv_heads][dim]
+    float *delta;               // [batch][heads][q_len]
+};
+hipError_t attn_forward_bf16(const AttnCall &a, hipStream_t stream);
+hipError_t attn_forward_f16(const AttnCall &a, hipStream_t stream);
+hipError_t attn_backward_bf16(const AttnCall &a, hipStream_t stream);
+hipError_t attn_backward_f16(const AttnCall &a, hipStream_t stream);
+
 }  // namespace tasq

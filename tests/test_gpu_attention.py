@@ -1,0 +1,370 @@
+"""Attention and its gradient against the formulas in 64 bits.
+
+U is the unit roundoff of the type (2^-8 bfloat16, 2^-11 half), e = 256 * 2^-24
+* (1 + Z) the relative error of a weight exp(z - lse) computed in fp32: a score
+is a chain of at most 130 fp32 roundings relative to scale sum |q k| <= Z, Z
+also covers |lse|, and the exponential and the sum add a few more.
+
+Forward: every weight is rounded once (U) before it meets v, the result once:
+  |out - ref| <= (U + e) sum_j p |v| + U |ref| + tiny.
+Gradients, from the same out and lse that the call is given: with a = p (sum
+|do v| + sum |do out|), the magnitude behind a score's gradient ds,
+  |dv - ref| <= (U + e) sum_i p |do| + U |ref|,
+  |dq - ref| <= scale sum_j (U |ds| + 2 e a) |k| + U |ref|, and dk alike.
+In half, what is below the smallest normal number is rounded to a multiple of
+2^-24: each weight and each ds is then off by up to 2^-25 as well."""
+import math
+
+import pytest
+import torch
+
+import paper_2608_03057_amd as T
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+STEP = {torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25}
+
+
+def bmm(a, b):
+    return torch.matmul(a.contiguous(), b.contiguous())
+
+
+class Exact:
+    """The operator and its error bounds in 64 bits; heads first."""
+
+    def __init__(self, q, k, v, lengths=None, mask=None, scale=None):
+        B, SQ, H, D = q.shape
+        SK, HK = k.shape[1:3]
+        self.G, self.HK, self.scale = H // HK, HK, D ** -0.5 if scale is None else scale
+        self.dt = q.dtype
+        live = torch.ones(B, SK, dtype=torch.bool, device=q.device)
+        if lengths is not None:
+            live &= torch.arange(SK, device=q.device)[None] < lengths[:, None]
+        if mask is not None:
+            live &= mask.bool()
+        self.live = live[:, None, None, :]
+        clean = lambda t: torch.where(live[:, :, None, None], t.double(), 0.0)  # noqa: E731
+        heads = lambda t: t.transpose(1, 2).repeat_interleave(self.G, 1)  # noqa: E731
+        self.q = q.double().transpose(1, 2)
+        self.k, self.v = heads(clean(k)), heads(clean(v))
+        z = bmm(self.q, self.k.transpose(2, 3)) * self.scale
+        self.z = torch.where(self.live, z, -math.inf)
+        self.lse = torch.logsumexp(self.z, -1) if SK else self.z.new_full((B, H, SQ), -math.inf)
+        zmag = bmm(self.q.abs(), self.k.abs().transpose(2, 3)) * self.scale
+        some = self.lse[self.lse > -math.inf].abs()
+        Z = float(zmag.max()) if zmag.numel() else 0.0
+        Z += float(some.max()) if some.numel() else 0.0
+        self.e = 256 * 2.0 ** -24 * (1 + Z)
+
+    def weights(self, lse):
+        return torch.where(lse[..., None] == -math.inf, 0.0, torch.exp(self.z - lse[..., None]))
+
+    def forward(self):
+        p = self.weights(self.lse)
+        out = bmm(p, self.v)
+        u, va = U[self.dt], self.v.abs()
+        tol = (u + self.e) * bmm(p, va) + u * out.abs() + STEP[self.dt]
+        if self.dt == torch.float16:        # the largest unnormalised weight is 1
+            top = torch.exp(self.z.amax(-1, keepdim=True) - self.lse[..., None])
+            top = torch.where(top.isnan(), 0.0, top) if self.z.shape[-1] else 0.0
+            tol = tol + STEP[self.dt] * top * bmm(self.live.double().expand_as(p), va)
+        return out.transpose(1, 2), tol.transpose(1, 2), self.lse
+
+    def backward(self, do, out, lse):
+        do, out = do.double().transpose(1, 2), out.double().transpose(1, 2)
+        p = self.weights(lse.double())
+        dp = bmm(do, self.v.transpose(2, 3))
+        ds = p * (dp - (do * out).sum(-1, keepdim=True))
+        a = p * (bmm(do.abs(), self.v.abs().transpose(2, 3)) +
+                 (do * out).abs().sum(-1, keepdim=True))
+        u, s, e = U[self.dt], self.scale, self.e
+        least = STEP[self.dt] * self.live.double()
+        dst, pt = (u * ds.abs() + 2 * e * a + least) * s, (u + e) * p + least
+
+        def shared(t):                      # [B, H, S, D] -> [B, S, HK, D], heads summed
+            B, H, S, D = t.shape
+            return t.reshape(B, self.HK, self.G, S, D).sum(2).transpose(1, 2)
+        tr = lambda t: t.transpose(2, 3)  # noqa: E731
+        refs = [bmm(ds, self.k).transpose(1, 2) * s, shared(bmm(tr(ds), self.q)) * s,
+                shared(bmm(tr(p), do))]
+        tols = [bmm(dst, self.k.abs()).transpose(1, 2), shared(bmm(tr(dst), self.q.abs())),
+                shared(bmm(tr(pt), do.abs()))]
+        return refs, [t + u * r.abs() + STEP[self.dt] for t, r in zip(tols, refs)]
+
+
+def near(got, ref, tol, what):
+    assert got.shape == ref.shape, what
+    err = (got.double() - ref).abs()
+    assert bool((err <= tol * (1 + 2.0 ** -8)).all()), (what, float((err - tol).max()))
+
+
+def near_lse(got, ref, e):
+    empty = ref == -math.inf
+    assert torch.equal(got == -math.inf, empty)
+    err = torch.where(empty, 0.0, (got.double() - ref).abs())
+    assert err.numel() == 0 or float(err.max()) <= e, float(err.max())
+
+
+def draw(B, SQ, SK, H, HK, D, dtype, seed=0, size=1.0):
+    g = torch.Generator().manual_seed(seed + 1000 * SQ + 10 * SK + D)
+    q = (torch.randn(B, SQ, H, D, generator=g) * size).to(dtype).to(DEV)
+    kv = (torch.randn(B, SK, 2, HK, D, generator=g) * size).to(dtype).to(DEV)
+    do = torch.randn(B, SQ, H, D, generator=g).to(dtype).to(DEV)
+    return q, kv[:, :, 0], kv[:, :, 1], do, g
+
+
+def check(q, k, v, do, lengths=None, mask=None, scale=None, grad=True):
+    ex = Exact(q, k, v, lengths, mask, scale)
+    out, lse = T.attention(q, k, v, kv_lengths=lengths, key_mask=mask, scale=scale, want_lse=True)
+    near(out, *ex.forward()[:2], "out")
+    near_lse(lse, ex.lse, ex.e)
+    if grad:
+        got = T.attention_backward(do, q, k, v, out, lse, kv_lengths=lengths, key_mask=mask,
+                                   scale=scale)
+        for g, r, t, name in zip(got, *ex.backward(do, out, lse), ("dq", "dk", "dv")):
+            near(g, r, t, name)
+    return out, lse
+
+
+SHAPES = [
+    # B, SQ, SK, H, HK, D
+    (1, 1, 1, 1, 1, 8), (1, 1, 64, 2, 2, 64), (2, 3, 65, 4, 2, 72), (1, 31, 33, 2, 1, 32),
+    (1, 33, 63, 3, 3, 40), (2, 128, 128, 2, 2, 128), (1, 129, 127, 2, 2, 112),
+    (2, 200, 77, 4, 4, 64), (1, 257, 300, 16, 16, 72), (2, 65, 1, 2, 2, 96),
+    (1, 1, 1000, 8, 2, 128), (3, 5, 700, 4, 1, 80), (1, 70, 515, 6, 2, 24),
+    (1, 513, 190, 2, 1, 120), (2, 17, 31, 12, 3, 16), (1, 300, 1100, 1, 1, 48),
+]
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_shapes(shape, dtype):
+    q, k, v, do, _ = draw(*shape, dtype)
+    check(q, k, v, do)
+
+
+@pytest.mark.parametrize("D", range(8, 129, 8))
+def test_every_head_dimension(D):
+    q, k, v, do, _ = draw(1, 40, 90, 2, 2, D, torch.bfloat16)
+    check(q, k, v, do, scale=0.3)
+
+
+@pytest.mark.parametrize("shape", [(4, 50, 300, 4, 4, 72), (4, 2, 900, 8, 2, 128),
+                                   (4, 130, 70, 2, 1, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_lengths(shape, dtype):
+    """Lengths of zero, one, a tile's edge, and past either end; what lies
+    beyond them is not used whatever it holds."""
+    q, k, v, do, _ = draw(*shape, dtype)
+    SK = shape[2]
+    for lens in ([0, 1, 64, SK], [SK + 9, -5, 63, 65], [0, 0, 0, 0]):
+        kk, vv = k.clone(), v.clone()
+        for b, n in enumerate(lens):
+            kk[b, max(0, n):] = math.nan
+            vv[b, max(0, n):] = math.inf
+        check(q, kk, vv, do, lengths=torch.tensor(lens, dtype=torch.int32, device=DEV))
+
+
+@pytest.mark.parametrize("shape", [(3, 50, 300, 4, 2, 72), (3, 1, 1100, 4, 1, 64),
+                                   (3, 140, 64, 2, 2, 128)])
+@pytest.mark.parametrize("kind", [torch.bool, torch.uint8])
+def test_masks(shape, kind):
+    """Masks with whole tiles off, one key on, none on; NaN and infinity at
+    keys that are off, and a length on top."""
+    q, k, v, do, g = draw(*shape, torch.bfloat16)
+    B, SK = shape[0], shape[2]
+    mask = torch.rand(B, SK, generator=g) < 0.5
+    mask[0, :] = False
+    mask[1, :SK - 1] = False
+    mask[1, SK - 1] = True
+    mask[2, 64:128] = False
+    mask = mask.to(DEV)
+    kk = torch.where(mask[:, :, None, None], k, math.nan)
+    vv = torch.where(mask[:, :, None, None], v, -math.inf)
+    m = mask if kind == torch.bool else mask.to(torch.uint8) * 128
+    check(q, kk, vv, do, mask=m)
+    check(q, kk, vv, do, mask=m, lengths=torch.tensor([SK, SK, SK // 2], dtype=torch.int32,
+                                                      device=DEV))
+
+
+def test_large_scores():
+    """Scores of hundreds: a weight of one and the rest vanish, and the
+    running maximum rises late in the row."""
+    q, k, v, do, _ = draw(1, 70, 600, 2, 2, 64, torch.bfloat16, size=6.0)
+    k[:, 500:] *= 3
+    check(q, k, v, do)
+    out, _ = T.attention(q, k, v)
+    assert bool(torch.isfinite(out).all())
+
+
+def test_scores_far_below_zero():
+    """All scores near -1e4: the sum must not underflow."""
+    q = torch.full((1, 3, 1, 64), 8.0, dtype=torch.bfloat16, device=DEV)
+    k = torch.full((1, 130, 1, 64), -160.0, dtype=torch.bfloat16, device=DEV)
+    v = torch.randn(1, 130, 1, 64, device=DEV).to(torch.bfloat16)
+    check(q, k, v, torch.randn_like(q))
+
+
+def test_infinite_and_nan_inputs_stay_in_their_rows():
+    q, k, v, do, _ = draw(1, 40, 100, 2, 2, 64, torch.bfloat16)
+    clean, _ = T.attention(q, k, v)
+    q2 = q.clone()
+    q2[0, 7, 1, 3] = math.nan
+    out, _ = T.attention(q2, k, v)
+    assert bool(out[0, 7, 1].isnan().all())
+    keep = torch.ones(40, 2, dtype=torch.bool, device=DEV)
+    keep[7, 1] = False
+    assert torch.equal(out[0][keep], clean[0][keep])
+
+
+def test_strides():
+    """Slices of fused buffers, heads before tokens, broadcast keys."""
+    B, SQ, SK, H, D = 2, 45, 150, 4, 72
+    g = torch.Generator().manual_seed(9)
+    r = lambda *s: torch.randn(*s, generator=g).to(torch.bfloat16).to(DEV)  # noqa: E731
+    qkv = r(B, SK, 3, H, D)
+    q, k, v = qkv[:, :SQ, 0], qkv[:, :, 1], qkv[:, :, 2]
+    do = r(B, H, SQ, D).transpose(1, 2)
+    check(q, k, v, do)
+    k1 = r(B, H, SK, D).transpose(1, 2)
+    check(q, k1, r(1, SK, 1, D).expand(B, SK, H, D), do)
+    check(r(1, 1, 1, D).expand(B, SQ, H, D), k1, v, do)
+    # a single token's strides do not matter
+    lone = torch.as_strided(r(64 * D), (1, 1, 2, D), (3, 5, D, 1))
+    check(lone, k[:1, :, :2], v[:1, :, :2], r(1, 1, 2, D))
+
+
+def test_offsets_past_32_bits():
+    """Keys and values of two batch entries more than 4 GiB apart."""
+    H, D, SK = 2, 64, 130
+    apart = (1 << 31) + 8 * 1000                    # elements: 4 GiB and more
+    buf = torch.empty(apart + SK * H * D, dtype=torch.bfloat16, device=DEV)
+    k = torch.as_strided(buf, (2, SK, H, D), (apart, H * D, D, 1))
+    q, k0, v0, do, _ = draw(2, 20, SK, H, H, D, torch.bfloat16)
+    k.copy_(k0)
+    check(q, k, k, do)
+    # one token row every 2^22 elements: a long stride inside a tile
+    far = torch.as_strided(buf, (1, 130, 1, D), (0, 1 << 22, 0, 1))
+    far.copy_(k0[:1, :, :1])
+    check(q[:1, :, :1], far, v0[:1, :, :1], do[:1, :, :1])
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 9000, 2, 1, 128), (2, 200, 1500, 1, 1, 64),
+                                   (1, 3000, 130, 2, 2, 72)])
+def test_ranges_and_no_workspace_agree(shape):
+    """With ranges side by side and without: both within bounds; the same bits
+    each time."""
+    q, k, v, do, _ = draw(*shape, torch.bfloat16)
+    assert T.attention_workspace_bytes(q, k, backward=True) > 0
+    ex = Exact(q, k, v)
+    ref, tol, _ = ex.forward()
+    none = torch.empty(0, dtype=torch.uint8, device=DEV)
+    out, lse = T.attention(q, k, v, want_lse=True)
+    again, lse2 = T.attention(q, k, v, want_lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    single, lse1 = T.attention(q, k, v, want_lse=True, workspace=none)
+    near(single, ref, tol, "one range")
+    near(out, ref, tol, "ranges")
+    near_lse(lse1, ex.lse, ex.e)
+    rows = torch.empty(4 * shape[0] * shape[1] * shape[3], dtype=torch.uint8, device=DEV)
+    need = (rows.numel() + 255) // 256 * 256
+    rows = torch.empty(need, dtype=torch.uint8, device=DEV)
+    a = T.attention_backward(do, q, k, v, out, lse)
+    b = T.attention_backward(do, q, k, v, out, lse)
+    c = T.attention_backward(do, q, k, v, out, lse, workspace=rows)
+    refs, tols = ex.backward(do, out, lse)
+    for x, y, z, r, t in zip(a, b, c, refs, tols):
+        assert torch.equal(x, y)
+        near(x, r, t, "ranges")
+        near(z, r, t, "one range")
+
+
+def test_gradient_against_differences():
+    """Central differences of the 64-bit forward pass in random directions,
+    truncation of order h^2; the kernels' share is their bound at work: the
+    difference along d is off by at most sum |d| tol, and out's rounding
+    changes delta by U |do||out|, which moves ds by p times that."""
+    shape = (1, 12, 40, 4, 2, 16)
+    q, k, v, do, g = draw(*shape, torch.float16)
+    out, lse = T.attention(q, k, v, want_lse=True)
+    grads = T.attention_backward(do, q, k, v, out, lse)
+    ex = Exact(q, k, v)
+    _, tols = ex.backward(do, out, lse)
+    h = 1e-4
+    moved = U[torch.float16] * float((do.double() * out.double()).abs().sum(-1).max())
+    room = [moved * float(ex.k.abs().sum(2).max()) * ex.scale,
+            moved * float(ex.q.abs().sum(2).max()) * ex.scale * ex.G, 0.0]
+
+    def loss(*t):
+        # the oracle on 64-bit inputs: types only pick its bounds
+        e = Exact.__new__(Exact)
+        x = [s.double().transpose(1, 2) for s in t]
+        kk, vv = (s.repeat_interleave(2, 1) for s in x[1:])
+        z = bmm(x[0], kk.transpose(2, 3)) * ex.scale
+        del e
+        return float((bmm(torch.softmax(z, -1), vv).transpose(1, 2) * do.double()).sum())
+    for i in range(3):
+        for _ in range(4):
+            args = [t.double() for t in (q, k, v)]
+            d = torch.randn(args[i].shape, generator=g).double().to(DEV)
+            up, dn = list(args), list(args)
+            up[i], dn[i] = args[i] + h * d, args[i] - h * d
+            num = (loss(*up) - loss(*dn)) / (2 * h)
+            got = float((grads[i].double() * d).sum())
+            assert abs(num - got) <= float((d.abs() * (tols[i] + room[i])).sum()) + 1e-4
+
+
+def test_empty_sizes():
+    for B, SQ, SK, H in ((0, 3, 4, 2), (1, 0, 4, 2), (1, 3, 0, 2), (2, 0, 0, 1)):
+        q = torch.randn(B, SQ, H, 64, device=DEV).to(torch.bfloat16)
+        k = torch.randn(B, SK, H, 64, device=DEV).to(torch.bfloat16)
+        out, lse = T.attention(q, k, k, want_lse=True)
+        assert float(out.float().abs().sum()) == 0.0 and bool((lse == -math.inf).all())
+        dq, dk, dv = T.attention_backward(q, q, k, k, out, lse)
+        for t, s in ((dq, q), (dk, k), (dv, k)):
+            assert t.shape == s.shape and float(t.float().abs().sum()) == 0.0
+
+
+def test_on_another_stream():
+    q, k, v, do, _ = draw(1, 1, 4000, 4, 1, 64, torch.bfloat16)
+    ref, lse = T.attention(q, k, v, want_lse=True)
+    gref = T.attention_backward(do, q, k, v, ref, lse)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        out, l2 = T.attention(q, k, v, want_lse=True)
+        g2 = T.attention_backward(do, q, k, v, out, l2)
+    s.synchronize()
+    assert torch.equal(out, ref) and torch.equal(l2, lse)
+    assert all(torch.equal(x, y) for x, y in zip(g2, gref))
+
+
+def test_refusals_of_the_wrappers():
+    q, k, v, do, _ = draw(1, 4, 8, 4, 2, 64, torch.bfloat16)
+    with pytest.raises(ValueError):
+        T.attention(q.float(), k, v)
+    with pytest.raises(ValueError):
+        T.attention(q, k.half(), v)
+    with pytest.raises(ValueError):
+        T.attention(q, k, v[:, :4])
+    with pytest.raises(ValueError):
+        T.attention(q, k, v, kv_lengths=torch.zeros(2, dtype=torch.int32, device=DEV))
+    with pytest.raises(ValueError):
+        T.attention(q, k, v, key_mask=torch.zeros(1, 8, device=DEV))
+    with pytest.raises(T.TasqError):        # heads that do not divide
+        T.attention(q[:, :, :3], k, v)
+    with pytest.raises(T.TasqError):        # a head dimension of 60
+        T.attention(q[..., :60], k[..., :60], v[..., :60])
+    with pytest.raises(T.TasqError):        # 8 bytes off
+        T.attention(q[..., 4:12], k[..., 4:12], v[..., 4:12])
+    for bad in (0.0, -1.0, math.nan, math.inf):
+        with pytest.raises(T.TasqError):
+            T.attention(q, k, v, scale=bad)
+    out, lse = T.attention(q, k, v, want_lse=True)
+    with pytest.raises(T.TasqError):        # no room for delta
+        T.attention_backward(do, q, k, v, out, lse,
+                             workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
+    with pytest.raises(ValueError):
+        T.attention_backward(do[:, :2], q, k, v, out, lse)
