@@ -73,24 +73,40 @@ template <int KS> struct Tile {
     }
 };
 
-// A tile on its way from memory to LDS in the registers of NT threads.
+// A tile on its way from memory to LDS in the registers of NT threads: the
+// rows of one operand, `stride` bytes apart, dim elements each.
 template <int KS, int NT> struct Stage {
     static constexpr int kSlots = kAttnTile * KS * 2;       // 16-byte chunks of a tile
     static constexpr int N = (kSlots + NT - 1) / NT;
     u32x4 v[N];
+    uint32_t off[N], bytes;
 
-    // Rows of the tile whose bit in `live` is set, from p on, `stride` bytes
-    // apart, dim elements each; all else is zero and not read.
-    __device__ __forceinline__ void load(const void *p, uint32_t stride, int dim, uint64_t live)
+    __device__ __forceinline__ void init(uint32_t stride, int dim)
     {
-        const rsrc_t r = make_rsrc(p, (kAttnTile - 1) * stride + 2u * (uint32_t)dim);
+        bytes = (kAttnTile - 1) * stride + 2u * (uint32_t)dim;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int id = (int)threadIdx.x + i * NT;
-            const int row = id / (2 * KS), c = id % (2 * KS);
-            const bool ok = id < kSlots && 8 * c < dim && ((live >> (row & 63)) & 1);
-            v[i] = __builtin_bit_cast(
-                u32x4, ld16(r, ok ? (uint32_t)row * stride + 16u * (uint32_t)c : kOOB));
+            const int id = (int)threadIdx.x + i * NT, c = id % (2 * KS);
+            off[i] = id < kSlots && 8 * c < dim
+                         ? (uint32_t)(id / (2 * KS)) * stride + 16u * (uint32_t)c
+                         : kOOB;
+        }
+    }
+    // Rows from p on whose bit in `live` is set; all else is zero and not read.
+    __device__ __forceinline__ void load(const void *p, uint64_t live)
+    {
+        const rsrc_t r = make_rsrc(p, bytes);
+        if (live == ~0ull) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] = __builtin_bit_cast(u32x4, ld16(r, off[i]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int row = ((int)threadIdx.x + i * NT) / (2 * KS);
+                const bool on = (live >> (row & 63)) & 1;
+                v[i] = __builtin_bit_cast(u32x4, ld16(r, on ? off[i] : kOOB));
+            }
         }
     }
     __device__ __forceinline__ void store(char *lds) const
@@ -183,6 +199,17 @@ __device__ __forceinline__ void store_columns_f32(float *p, bool ok, int dim,
                     make_float4(acc[db][4 * j] * f, acc[db][4 * j + 1] * f,
                                 acc[db][4 * j + 2] * f, acc[db][4 * j + 3] * f);
         }
+}
+
+// -inf where the row's bit in `live` is off, else 0, for the 16 rows of block
+// rb that the lane holds.
+__device__ __forceinline__ float dead_row(uint64_t live, int rb, int i)
+{
+    const uint32_t off = ~((uint32_t)(live >> (32 * rb)) >> (4 * ((threadIdx.x & 63) >> 5)));
+    const int bit = 8 * (i / 4) + i % 4;
+    uint32_t u = (uint32_t)((int)(off << (31 - bit)) >> 31) & 0xff800000u;
+    asm("" : "+v"(u));      // or the compiler makes a branch of each row
+    return __uint_as_float(u);
 }
 
 // Keys of a batch entry that count at all.

@@ -88,18 +88,19 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
     const int t1 = min((n + kAttnTile - 1) / kAttnTile, t0 + a.split_tiles);
     const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2];
     const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2];
-    const uint32_t kb = 2u * (uint32_t)a.k_stride[1], vb = 2u * (uint32_t)a.v_stride[1];
 
     v16f_t dq[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
         dq[db] = v16f_t{};
     Stage<KS, NT> kst, vst;
+    kst.init(2u * (uint32_t)a.k_stride[1], a.dim);
+    vst.init(2u * (uint32_t)a.v_stride[1], a.dim);
     uint64_t live = 0, now = 0;
     int next_byte = 0;
     auto fetch = [&](int t) {
-        kst.load(k + (size_t)t * kAttnTile * a.k_stride[1], kb, a.dim, live);
-        vst.load(v + (size_t)t * kAttnTile * a.v_stride[1], vb, a.dim, live);
+        kst.load(k + (size_t)t * kAttnTile * a.k_stride[1], live);
+        vst.load(v + (size_t)t * kAttnTile * a.v_stride[1], live);
     };
     if (t0 < t1) {
         now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
@@ -126,12 +127,14 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
                     pa = mfma(T{}, Tile<KS>::rows(vt, rb, ks), gf[ks], pa);
                 }
                 float x[16];
-                const uint32_t bits = (uint32_t)(now >> (32 * rb)) >> (4 * (lane >> 5));
+                if (now != ~0ull) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        sa[i] += dead_row(now, rb, i);
+                }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    float p = __builtin_amdgcn_exp2f(sa[i] * a.scale_log2 - lse2);
-                    if (now != ~0ull && !((bits >> (8 * (i / 4) + i % 4)) & 1))
-                        p = 0.0f;
+                    const float p = __builtin_amdgcn_exp2f(sa[i] * a.scale_log2 - lse2);
                     x[i] = p * (pa[i] * Range<T>::kScore - delta);
                 }
 #pragma unroll
@@ -196,6 +199,8 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
     const int t0 = sp * a.kv_split_tiles;
     const int t1 = kt_ * 128 < n ? min(group * per_head, t0 + a.kv_split_tiles) : t0;
     Stage<KS, NT> qst, gst;
+    qst.init(2u * (uint32_t)a.q_stride[1], a.dim);
+    gst.init(2u * (uint32_t)a.dout_stride[1], a.dim);
     float st = 0.0f;
     auto fetch = [&](int t) {
         const int g = t / per_head, s0 = (t - g * per_head) * kAttnTile;
@@ -203,10 +208,10 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
         const uint64_t live = left >= kAttnTile ? ~0ull : (1ull << left) - 1;
         qst.load(static_cast<const T *>(a.q) + b * a.q_stride[0] + s0 * a.q_stride[1] +
                      head * a.q_stride[2],
-                 2u * (uint32_t)a.q_stride[1], a.dim, live);
+                 live);
         gst.load(static_cast<const T *>(a.dout) + b * a.dout_stride[0] + s0 * a.dout_stride[1] +
                      head * a.dout_stride[2],
-                 2u * (uint32_t)a.dout_stride[1], a.dim, live);
+                 live);
         if (wave < 2) {         // wave 0 has the rows' lse, wave 1 their delta
             const float *p = wave == 0 ? a.lse : a.delta;
             st = lane < left ? p[((size_t)b * a.heads + head) * a.q_len + s0 + lane]

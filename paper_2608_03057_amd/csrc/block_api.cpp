@@ -121,7 +121,14 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
     const int group = c.kv_heads ? c.heads / c.kv_heads : 0;
     const long long pairs = (long long)c.batch * c.kv_heads;
     const int key_tiles = (c.kv_len + 63) / 64;
-    c.row_tiles = (int)(((long long)group * c.q_len + 127) / 128);
+    const long long pair_rows = (long long)group * c.q_len;
+    // Two blocks of rows to a wave halve what a row reads of LDS; they need
+    // registers (dims up to 96) and two workgroups for every compute unit.
+    c.row_blocks = !backward && (c.dim + 15) / 16 <= tasq::kAttnWideSteps &&
+                           pairs * ((pair_rows + 255) / 256) >= 512
+                       ? 2
+                       : 1;
+    c.row_tiles = (int)((pair_rows + 128 * c.row_blocks - 1) / (128 * c.row_blocks));
     plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, backward ? 2 : 3, &c.splits,
                 &c.split_tiles);
     const size_t rows = (size_t)c.batch * c.heads * c.q_len;

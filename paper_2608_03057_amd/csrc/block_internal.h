@@ -50,8 +50,10 @@ struct HeadCall {
 hipError_t launch_norm_rotate(const HeadCall &call, bool grad, float *part, hipStream_t stream);
 
 // Attention (attn_fwd.h, attn_bwd.h).  Rows are (query head of the group,
-// query) pairs of one key head; a workgroup has 128 rows, or 128 keys in
-// k_attn_dkdv.  plan_attention sets the launch's shape.
+// query) pairs of one key head; a workgroup has 128 rows (256 in the forward
+// pass with row_blocks 2), or 128 keys in k_attn_dkdv.  plan_attention sets
+// the launch's shape.
+constexpr int kAttnWideSteps = 6;   // 16-element steps of a head that row_blocks 2 takes
 struct AttnCall {
     const void *q, *k, *v;
     const int32_t *kv_lengths;  // [batch] or null
@@ -63,6 +65,7 @@ struct AttnCall {
     long long q_stride[3], k_stride[3], v_stride[3], dout_stride[3];    // batch, token, head
     int type, batch, heads, kv_heads, q_len, kv_len, dim;
     float scale, scale_log2;    // scale, and scale * log2(e)
+    int row_blocks;                                 // blocks of 32 rows of a wave
     int row_tiles, splits, split_tiles;             // ranges of the keys, in tiles of 64
     int key_tiles, kv_splits, kv_split_tiles;       // ranges of the rows (k_attn_dkdv)
     float *part, *part_lse;     // [splits][batch][..] parts of out (or dq) and lse
