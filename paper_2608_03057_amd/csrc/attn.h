@@ -42,82 +42,114 @@ __device__ __forceinline__ v16f_t mfma(f16_t, u32x4 a, u32x4 b, v16f_t c)
 constexpr int kAttnTile = 64;           // rows of a streamed tile
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// A tile of KS * 16 columns (the head dimension rounded up) in LDS.  The row
-// pitch is an odd number of 16-byte units, so that the rows of an operand
-// read fall in distinct banks.
+// A tile of KS * 16 columns (the head dimension rounded up) in LDS: rows of
+// 2 KS 16-byte chunks without padding, as the loads to LDS write them, chunk c
+// of row r at place c ^ key(r), so that the rows that an operand read spans
+// fall in distinct banks.
 template <int KS> struct Tile {
-    static constexpr int kPitch = KS * 32 + 16;
-    // The transposing load of an odd KS reads 16 bytes past a row's columns.
-    static constexpr int kBytes = kAttnTile * kPitch + 16;
+    static constexpr int kPitch = KS * 32;
+    // The transposing load of an odd KS reads 32 bytes past a row's columns.
+    static constexpr int kBytes = kAttnTile * kPitch + 32;
     static constexpr int DB = (KS + 1) / 2;     // 32-row blocks of the transposed tile
 
-    // Operand of rows 32 rb .. +31, columns 16 ks .. +15.
-    static __device__ __forceinline__ u32x4 rows(const char *lds, int rb, int ks)
+    static __device__ __forceinline__ int key(int r)
     {
-        const int lane = threadIdx.x & 63;
-        return *reinterpret_cast<const u32x4 *>(lds + (lane & 31) * kPitch + 16 * (lane >> 5) +
-                                                rb * 32 * kPitch + 32 * ks);
+        return KS % 4 == 0 ? r & 7 : KS % 4 == 2 ? (r >> 1) & 3 : (r >> 2) & 1;
     }
-    // Transposed operand: columns 32 db .. +31 as rows, rows r0 .. r0 + 15 in
-    // the order in which an accumulator holds them as k.
-    static __device__ __forceinline__ u32x4 columns(const char *lds, int r0, int db)
+
+    // This lane's part of the addresses.
+    static constexpr int NR = KS % 4 == 0 ? 4 : KS % 4 == 2 ? 2 : 1;
+    static constexpr int NC = KS % 4 == 0 ? 2 : 1;
+    uint32_t row[NR], col[NC];
+
+    __device__ __forceinline__ Tile()
+    {
+        const int lane = threadIdx.x & 63, h = lane >> 5;
+        const int r = lane & 31;
+#pragma unroll
+        for (int i = 0; i < NR; ++i)
+            row[i] = (uint32_t)(r * kPitch + 16 * ((2 * i + h) ^ key(r)));
+        const int c = 4 * h + ((lane & 15) >> 2), x = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+            col[i] = (uint32_t)(c * kPitch + 16 * ((4 * i + x) ^ key(c)) + 8 * (lane & 1));
+    }
+    // Operand of rows 32 rb .. +31, columns 16 ks .. +15.
+    __device__ __forceinline__ u32x4 rows(const char *lds, int rb, int ks) const
+    {
+        return *reinterpret_cast<const u32x4 *>(lds + row[ks % NR] + rb * 32 * kPitch +
+                                                32 * (ks - ks % NR));
+    }
+    // Transposed operand: columns 32 db .. +31 as rows, rows r0 .. r0 + 15 (r0 a
+    // multiple of 16) in the order in which an accumulator holds them as k.
+    __device__ __forceinline__ u32x4 columns(const char *lds, int r0, int db) const
     {
         typedef __attribute__((address_space(3))) v4s_t lds_t;
-        const int lane = threadIdx.x & 63;
-        const char *p = lds + (4 * (lane >> 5) + ((lane & 15) >> 2)) * kPitch +
-                        32 * ((lane >> 4) & 1) + 8 * (lane & 3) + r0 * kPitch + 64 * db;
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)p));
+        const char *p = lds + col[db % NC] + r0 * kPitch + 64 * (db - db % NC);
+        const u32x2 lo =
+            __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)p));
         const u32x2 hi = __builtin_bit_cast(
             u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)(p + 8 * kPitch)));
         return u32x4{lo.x, lo.y, hi.x, hi.y};
     }
 };
 
-// A tile on its way from memory to LDS in the registers of NT threads: the
-// rows of one operand, `stride` bytes apart, dim elements each.
-template <int KS, int NT> struct Stage {
-    static constexpr int kSlots = kAttnTile * KS * 2;       // 16-byte chunks of a tile
-    static constexpr int N = (kSlots + NT - 1) / NT;
-    u32x4 v[N];
-    uint32_t off[N], bytes;
+// Lane l's 16 bytes at `off` of the buffer to lds + 16 l; zeros where the
+// offset is out of bounds.
+__device__ __forceinline__ void load_to_lds(rsrc_t r, char *lds, uint32_t off)
+{
+#ifdef __HIP_DEVICE_COMPILE__       // the host pass knows no 16-byte form
+    typedef __attribute__((address_space(3))) void lds_t;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t *)lds, 16, off, 0, 0, 0);
+#endif
+}
 
-    __device__ __forceinline__ void init(uint32_t stride, int dim)
+// One wave's share of staging two tiles: waves 0 and 1 load the halves of the
+// first operand's, waves 2 and 3 of the second's, straight into LDS (1 KB an
+// instruction, rows `stride` bytes apart, dim elements each).
+template <int KS> struct Stager {
+    uint32_t off[KS], bytes;
+    int half, place;            // of the two tiles of a buffer
+
+    __device__ __forceinline__ void init(int wave, uint32_t stride, int dim)
     {
+        half = wave & 1;
+        place = (wave >> 1) * Tile<KS>::kBytes + half * 32 * Tile<KS>::kPitch;
         bytes = (kAttnTile - 1) * stride + 2u * (uint32_t)dim;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int id = (int)threadIdx.x + i * NT, c = id % (2 * KS);
-            off[i] = id < kSlots && 8 * c < dim
-                         ? (uint32_t)(id / (2 * KS)) * stride + 16u * (uint32_t)c
-                         : kOOB;
+        for (int i = 0; i < KS; ++i) {
+            const int r = row(i), c = slot(i) ^ Tile<KS>::key(r);
+            off[i] = 8 * c < dim ? (uint32_t)r * stride + 16u * (uint32_t)c : kOOB;
         }
     }
-    // Rows from p on whose bit in `live` is set; all else is zero and not read.
-    __device__ __forceinline__ void load(const void *p, uint64_t live)
+    __device__ __forceinline__ int row(int i) const
+    {
+        return 32 * half + (64 * i + (int)(threadIdx.x & 63)) / (2 * KS);
+    }
+    __device__ __forceinline__ int slot(int i) const
+    {
+        return (64 * i + (int)(threadIdx.x & 63)) % (2 * KS);
+    }
+    // Requests the rows from p on whose bit in `live` is set; all else is
+    // written as zero and not read.  wait() before the barrier that hands the
+    // buffer on.
+    __device__ __forceinline__ void request(const void *p, uint64_t live, char *buffer) const
     {
         const rsrc_t r = make_rsrc(p, bytes);
+        char *to = buffer + place;
         if (live == ~0ull) {
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                v[i] = __builtin_bit_cast(u32x4, ld16(r, off[i]));
+            for (int i = 0; i < KS; ++i)
+                load_to_lds(r, to + 1024 * i, off[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int row = ((int)threadIdx.x + i * NT) / (2 * KS);
-                const bool on = (live >> (row & 63)) & 1;
-                v[i] = __builtin_bit_cast(u32x4, ld16(r, on ? off[i] : kOOB));
-            }
+            for (int i = 0; i < KS; ++i)
+                load_to_lds(r, to + 1024 * i, (live >> row(i)) & 1 ? off[i] : kOOB);
         }
     }
-    __device__ __forceinline__ void store(char *lds) const
+    static __device__ __forceinline__ void wait()
     {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int id = (int)threadIdx.x + i * NT;
-            if (kSlots % NT == 0 || id < kSlots)
-                *reinterpret_cast<u32x4 *>(lds + id / (2 * KS) * Tile<KS>::kPitch +
-                                           16 * (id % (2 * KS))) = v[i];
-        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
 };
 

@@ -36,9 +36,10 @@ template <> struct Range<f16_t> {
 
 template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnCall a)
 {
-    constexpr int NT = 256, DB = Tile<KS>::DB;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][Tile<KS>::kBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int DB = Tile<KS>::DB, SIZE = Tile<KS>::kBytes;
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * SIZE];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int u = attn_unit(blockIdx.x, gridDim.x);
     const int mt = u % a.row_tiles;
     u /= a.row_tiles;
@@ -86,35 +87,31 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
     const int n = key_count(a, b);
     const int t0 = sp * a.split_tiles;
     const int t1 = min((n + kAttnTile - 1) / kAttnTile, t0 + a.split_tiles);
-    const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2];
-    const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2];
+    const long long *stride = wave < 2 ? a.k_stride : a.v_stride;
+    const T *kv = static_cast<const T *>(wave < 2 ? a.k : a.v) + b * stride[0] + hk * stride[2];
+    const long long step = kAttnTile * stride[1];
 
     v16f_t dq[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
         dq[db] = v16f_t{};
-    Stage<KS, NT> kst, vst;
-    kst.init(2u * (uint32_t)a.k_stride[1], a.dim);
-    vst.init(2u * (uint32_t)a.v_stride[1], a.dim);
+    const Tile<KS> tile;
+    Stager<KS> stager;
+    stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     uint64_t live = 0, now = 0;
     int next_byte = 0;
-    auto fetch = [&](int t) {
-        kst.load(k + (size_t)t * kAttnTile * a.k_stride[1], live);
-        vst.load(v + (size_t)t * kAttnTile * a.v_stride[1], live);
-    };
     if (t0 < t1) {
         now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
-        fetch(t0);
+        stager.request(kv + t0 * step, live, lds[0]);
         next_byte = mask_byte(a, b, n, t0 + 1);
-        kst.store(lds[0][0]);
-        vst.store(lds[0][1]);
+        stager.wait();
         __syncthreads();
     }
     for (int t = t0; t < t1; ++t) {
-        const char *kt = lds[(t - t0) & 1][0], *vt = lds[(t - t0) & 1][1];
+        const char *kt = lds[(t - t0) & 1], *vt = kt + SIZE;
         if (t + 1 < t1) {
             live = live_keys(a, n, t + 1, next_byte);
-            fetch(t + 1);
+            stager.request(kv + (t + 1) * step, live, lds[(t + 1 - t0) & 1]);
             next_byte = mask_byte(a, b, n, t + 2);
         }
         if (busy && now) {
@@ -123,8 +120,8 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
                 v16f_t sa = {}, pa = {};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    sa = mfma(T{}, Tile<KS>::rows(kt, rb, ks), qf[ks], sa);
-                    pa = mfma(T{}, Tile<KS>::rows(vt, rb, ks), gf[ks], pa);
+                    sa = mfma(T{}, tile.rows(kt, rb, ks), qf[ks], sa);
+                    pa = mfma(T{}, tile.rows(vt, rb, ks), gf[ks], pa);
                 }
                 float x[16];
                 if (now != ~0ull) {
@@ -143,15 +140,12 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
 #pragma unroll
                     for (int db = 0; db < DB; ++db)
                         dq[db] =
-                            mfma(T{}, Tile<KS>::columns(kt, 32 * rb + 16 * s2, db), ds, dq[db]);
+                            mfma(T{}, tile.columns(kt, 32 * rb + 16 * s2, db), ds, dq[db]);
                 }
             }
         }
         now = live;
-        if (t + 1 < t1) {
-            kst.store(lds[(t + 1 - t0) & 1][0]);
-            vst.store(lds[(t + 1 - t0) & 1][1]);
-        }
+        stager.wait();
         __syncthreads();
     }
     if (a.splits > 1)
@@ -164,10 +158,11 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
 
 template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv(AttnCall a)
 {
-    constexpr int NT = 256, DB = Tile<KS>::DB;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][Tile<KS>::kBytes];
+    constexpr int DB = Tile<KS>::DB, SIZE = Tile<KS>::kBytes;
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * SIZE];
     __shared__ __attribute__((aligned(16))) float stat[2][2][kAttnTile];    // lse, delta
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int u = attn_unit(blockIdx.x, gridDim.x);
     const int kt_ = u % a.key_tiles;
     u /= a.key_tiles;
@@ -198,20 +193,17 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
     const int per_head = (a.q_len + kAttnTile - 1) / kAttnTile;
     const int t0 = sp * a.kv_split_tiles;
     const int t1 = kt_ * 128 < n ? min(group * per_head, t0 + a.kv_split_tiles) : t0;
-    Stage<KS, NT> qst, gst;
-    qst.init(2u * (uint32_t)a.q_stride[1], a.dim);
-    gst.init(2u * (uint32_t)a.dout_stride[1], a.dim);
+    const Tile<KS> tile;
+    const long long *stride = wave < 2 ? a.q_stride : a.dout_stride;
+    const T *from = static_cast<const T *>(wave < 2 ? a.q : a.dout) + b * stride[0];
+    Stager<KS> stager;
+    stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     float st = 0.0f;
-    auto fetch = [&](int t) {
+    auto fetch = [&](int t, int i) {
         const int g = t / per_head, s0 = (t - g * per_head) * kAttnTile;
         const int left = a.q_len - s0, head = hk * group + g;
         const uint64_t live = left >= kAttnTile ? ~0ull : (1ull << left) - 1;
-        qst.load(static_cast<const T *>(a.q) + b * a.q_stride[0] + s0 * a.q_stride[1] +
-                     head * a.q_stride[2],
-                 live);
-        gst.load(static_cast<const T *>(a.dout) + b * a.dout_stride[0] + s0 * a.dout_stride[1] +
-                     head * a.dout_stride[2],
-                 live);
+        stager.request(from + s0 * stride[1] + head * stride[2], live, lds[i]);
         if (wave < 2) {         // wave 0 has the rows' lse, wave 1 their delta
             const float *p = wave == 0 ? a.lse : a.delta;
             st = lane < left ? p[((size_t)b * a.heads + head) * a.q_len + s0 + lane]
@@ -226,29 +218,28 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
         }
     };
     auto put = [&](int i) {
-        qst.store(lds[i][0]);
-        gst.store(lds[i][1]);
+        stager.wait();
         if (wave < 2)
             stat[i][wave][lane] = st;
     };
     if (t0 < t1) {
-        fetch(t0);
+        fetch(t0, 0);
         put(0);
         __syncthreads();
     }
     for (int t = t0; t < t1; ++t) {
         const int cur = (t - t0) & 1;
-        const char *qt = lds[cur][0], *gt = lds[cur][1];
+        const char *qt = lds[cur], *gt = qt + SIZE;
         if (t + 1 < t1)
-            fetch(t + 1);
+            fetch(t + 1, cur ^ 1);
         if (busy) {
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb) {
                 v16f_t sa = {}, pa = {};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    sa = mfma(T{}, Tile<KS>::rows(qt, rb, ks), kf[ks], sa);
-                    pa = mfma(T{}, Tile<KS>::rows(gt, rb, ks), vf[ks], pa);
+                    sa = mfma(T{}, tile.rows(qt, rb, ks), kf[ks], sa);
+                    pa = mfma(T{}, tile.rows(gt, rb, ks), vf[ks], pa);
                 }
                 float p[16], x[16];
 #pragma unroll
@@ -271,9 +262,9 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
 #pragma unroll
                     for (int db = 0; db < DB; ++db) {
                         dv[db] =
-                            mfma(T{}, Tile<KS>::columns(gt, 32 * rb + 16 * s2, db), pf, dv[db]);
+                            mfma(T{}, tile.columns(gt, 32 * rb + 16 * s2, db), pf, dv[db]);
                         dk[db] =
-                            mfma(T{}, Tile<KS>::columns(qt, 32 * rb + 16 * s2, db), ds, dk[db]);
+                            mfma(T{}, tile.columns(qt, 32 * rb + 16 * s2, db), ds, dk[db]);
                     }
                 }
             }

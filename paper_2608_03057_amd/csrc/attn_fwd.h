@@ -7,7 +7,7 @@
 // A workgroup of four waves has QB * 128 rows of one key head: (query head of
 // the group, query) pairs, so that query heads which share keys share their
 // loads; a wave has QB blocks of 32.  Tiles of 64 keys and values are staged in
-// two LDS buffers, the next tile in flight in registers.  With few rows the
+// two LDS buffers, the next tile in flight while one is worked on.  With few rows the
 // keys are cut into ranges, one workgroup each, whose partial results
 // k_attn_join brings together.
 #pragma once
@@ -25,9 +25,10 @@ constexpr float kSlack = 8.0f;
 template <class T, int KS, int QB>
 __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forward(AttnCall a)
 {
-    constexpr int NT = 256, DB = Tile<KS>::DB, BM = 128 * QB;
-    __shared__ __attribute__((aligned(16))) char lds[2][2][Tile<KS>::kBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int DB = Tile<KS>::DB, BM = 128 * QB, SIZE = Tile<KS>::kBytes;
+    __shared__ __attribute__((aligned(16))) char lds[2][2 * SIZE];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int u = attn_unit(blockIdx.x, gridDim.x);
     const int mt = u % a.row_tiles;
     u /= a.row_tiles;
@@ -58,8 +59,9 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
     const int n = key_count(a, b);
     const int t0 = sp * a.split_tiles;
     const int t1 = min((n + kAttnTile - 1) / kAttnTile, t0 + a.split_tiles);
-    const T *k = static_cast<const T *>(a.k) + b * a.k_stride[0] + hk * a.k_stride[2];
-    const T *v = static_cast<const T *>(a.v) + b * a.v_stride[0] + hk * a.v_stride[2];
+    const long long *stride = wave < 2 ? a.k_stride : a.v_stride;
+    const T *kv = static_cast<const T *>(wave < 2 ? a.k : a.v) + b * stride[0] + hk * stride[2];
+    const long long step = kAttnTile * stride[1];
 
     v16f_t o[QB][DB];
     float top[QB], sum[QB];
@@ -72,41 +74,33 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
             o[qb][db] = v16f_t{};
     }
 
-    Stage<KS, NT> kst, vst;
-    kst.init(2u * (uint32_t)a.k_stride[1], a.dim);
-    vst.init(2u * (uint32_t)a.v_stride[1], a.dim);
+    const Tile<KS> tile;
+    Stager<KS> stager;
+    stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     uint64_t live = 0, now = 0;
     int next_byte = 0;
-    auto fetch = [&](int t) {
-        kst.load(k + (size_t)t * kAttnTile * a.k_stride[1], live);
-        vst.load(v + (size_t)t * kAttnTile * a.v_stride[1], live);
-    };
     if (t0 < t1) {
         now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
-        fetch(t0);
+        stager.request(kv + t0 * step, live, lds[0]);
         next_byte = mask_byte(a, b, n, t0 + 1);
-        kst.store(lds[0][0]);
-        vst.store(lds[0][1]);
+        stager.wait();
         __syncthreads();
     }
     for (int t = t0; t < t1; ++t) {
-        const int cur = (t - t0) & 1;
-        const char *kt = lds[cur][0], *vt = lds[cur][1];
-        const bool more = t + 1 < t1;
-        if (more) {
+        const char *kt = lds[(t - t0) & 1], *vt = kt + SIZE;
+        if (t + 1 < t1) {
             live = live_keys(a, n, t + 1, next_byte);
-            fetch(t + 1);
+            stager.request(kv + (t + 1) * step, live, lds[(t + 1 - t0) & 1]);
             next_byte = mask_byte(a, b, n, t + 2);
         }
-        u32x4 p[QB][4];
-        const bool work = busy && now;
-        if (work) {
+        if (busy && now) {
+            u32x4 p[QB][4];
             v16f_t x[QB][2];
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
-                    const u32x4 f = Tile<KS>::rows(kt, rb, ks);
+                    const u32x4 f = tile.rows(kt, rb, ks);
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb)
                         x[qb][rb] = mfma(T{}, f, qf[qb][ks], ks ? x[qb][rb] : v16f_t{});
@@ -157,23 +151,18 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
                     p[qb][2 * rb + 1] = pack_rows<T>(e, 1);
                 }
             }
-        }
-        if (more) {
-            kst.store(lds[cur ^ 1][0]);
-            vst.store(lds[cur ^ 1][1]);
-        }
-        if (work) {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
-                    const u32x4 f = Tile<KS>::columns(vt, 16 * r, db);
+                    const u32x4 f = tile.columns(vt, 16 * r, db);
 #pragma unroll
                     for (int qb = 0; qb < QB; ++qb)
                         o[qb][db] = mfma(T{}, f, p[qb][r], o[qb][db]);
                 }
         }
         now = live;
+        stager.wait();
         __syncthreads();
     }
 
@@ -260,13 +249,11 @@ template <class T, int KS> hipError_t attn_forward_ks(const AttnCall &a, hipStre
     const long long grid = (long long)a.batch * a.kv_heads * a.splits * a.row_tiles;
     if (grid == 0)
         return hipSuccess;
-    if constexpr (KS <= kAttnWideSteps) {
-        if (a.row_blocks == 2) {
-            k_attn_forward<T, KS, 2><<<(unsigned)grid, 256, 0, stream>>>(a);
-            return hipGetLastError();
-        }
-    }
-    k_attn_forward<T, KS, 1><<<(unsigned)grid, 256, 0, stream>>>(a);
+    void (*kernel)(AttnCall) = k_attn_forward<T, KS, 1>;
+    if constexpr (KS <= kAttnWideSteps)
+        if (a.row_blocks == 2)
+            kernel = k_attn_forward<T, KS, 2>;
+    kernel<<<(unsigned)grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
