@@ -16,18 +16,216 @@
 
 namespace tasq {
 
-// The running maximum (in units of log2) follows the row's true maximum only
-// when that has risen by more than this: weights are then at most 2^kSlack,
-// far inside the range of either type and of the sums, and most tiles leave
-// the accumulators alone.
-constexpr float kSlack = 8.0f;
+// A row's weights are 2^(z - base), z in units of log2.  Floating-point weights
+// keep their precision whatever the base, which only has to keep them inside
+// the range.  So it starts at 0 and no maximum is computed, unless a lane's sum
+// over a tile reaches kMost, or is below kLeast in the first tile: the tile's
+// weights are then computed again with the base at the row's maximum, and its
+// sums so far are rescaled.
+template <class T> struct Weights;
+template <> struct Weights<bf16_t> {
+    static constexpr float kLeast = 0x1p-60f, kMost = 0x1p60f;
+};
+template <> struct Weights<f16_t> {
+    static constexpr float kLeast = 1.0f, kMost = 0x1p15f;      // the largest half is 65504
+};
+
+// What a wave holds of its QB blocks of 32 rows.
+template <class T, int KS, int QB> struct Rows {
+    static constexpr int DB = Tile<KS>::DB;
+    u32x4 q[QB][KS];
+    v16f_t o[QB][DB];
+    float base[QB], sum[QB];
+
+    // Lane l's row of block qb, l%32 of it: head and query of row m of the
+    // (query head, query) pairs of key head hk.
+    struct Row {
+        bool ok;
+        int head, s;
+        __device__ __forceinline__ Row(const AttnCall &a, int hk, int first, int qb)
+        {
+            const int group = a.heads / a.kv_heads;
+            const int m = first + 32 * qb + (int)(threadIdx.x & 31);
+            ok = m < group * a.q_len;
+            const int g = ok ? m / a.q_len : 0;
+            s = ok ? m - g * a.q_len : 0;
+            head = hk * group + g;
+        }
+    };
+
+    __device__ __forceinline__ void init(const AttnCall &a, int b, int hk, int first)
+    {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const Row r(a, hk, first, qb);
+            load_columns<KS>(static_cast<const T *>(a.q) + b * a.q_stride[0] +
+                                 r.s * a.q_stride[1] + r.head * a.q_stride[2],
+                             r.ok, a.dim, q[qb]);
+            base[qb] = 0.0f;
+            sum[qb] = 0.0f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+                o[qb][db] = v16f_t{};
+        }
+    }
+
+    // 32 NR keys of a tile from row 32 rb on: x = K Q^T, the weights p,
+    // o += V^T P^T.
+    template <int NR>
+    __device__ __forceinline__ void keys(const Tile<KS> &tile, const char *kt, const char *vt,
+                                         int rb, float scale_log2, uint64_t live, bool first)
+    {
+        const uint32_t least = first ? __float_as_uint(Weights<T>::kLeast) : 0;
+        const uint32_t span = __float_as_uint(Weights<T>::kMost) - least;
+        v16f_t x[QB][NR];
+        u32x4 p[QB][NR][2];
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+            scores(tile, kt, rb + r, x, r);
+        if (live != ~0ull) {
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float dead = dead_row(live, rb + r, i);
+#pragma unroll
+                    for (int qb = 0; qb < QB; ++qb)
+                        x[qb][r][i] += dead;
+                }
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            float part = weights(scale_log2, base[qb], x[qb], p[qb]);
+            // As bits, where NaN is above everything and less than least wraps.
+            const bool out = __float_as_uint(part) - least >= span;
+            if (__ballot(out)) {
+                // The other rows keep their base, so that no row's result depends
+                // on those beside it.
+                const bool row_out =
+                    across_halves(out ? 1.0f : 0.0f, [](float u, float v) { return u + v; }) != 0;
+                float to = first ? -__builtin_huge_valf() : base[qb];
+#pragma unroll
+                for (int r = 0; r < NR; ++r)
+                    to = fmaxf(to, maximum(x[qb][r]) * scale_log2);
+                to = row_out ? to : base[qb];
+                // No score above -inf: weights of zero.
+                const float from = to == -__builtin_huge_valf() ? 0.0f : to;
+                const float f = first ? 1.0f : __builtin_amdgcn_exp2f(base[qb] - from);
+                base[qb] = to;
+                sum[qb] *= f;
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        o[qb][db][i] *= f;
+                part = weights(scale_log2, from, x[qb], p[qb]);
+            }
+            sum[qb] += part;
+        }
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+            values(tile, vt, rb + r, p, r);
+    }
+
+    // x[..][at] = K Q^T for 32 keys of a tile, rows rb.
+    template <int NR>
+    __device__ __forceinline__ void scores(const Tile<KS> &tile, const char *kt, int rb,
+                                           v16f_t (&x)[QB][NR], int at) const
+    {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const u32x4 f = tile.rows(kt, rb, ks);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+                x[qb][at] = mfma(T{}, f, q[qb][ks], ks ? x[qb][at] : v16f_t{});
+        }
+    }
+
+    // o += V^T P^T for 32 keys of a tile, rows rb.
+    template <int NR>
+    __device__ __forceinline__ void values(const Tile<KS> &tile, const char *vt, int rb,
+                                           const u32x4 (&p)[QB][NR][2], int at)
+    {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                const u32x4 f = tile.columns(vt, 32 * rb + 16 * r, db);
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb)
+                    o[qb][db] = mfma(T{}, f, p[qb][at][r], o[qb][db]);
+            }
+    }
+
+    // Maximum of 32 scores of this lane's row.  (Four chains, here and below: a
+    // result takes twice an instruction's time to be there for the next.)
+    static __device__ __forceinline__ float maximum(const v16f_t &x)
+    {
+        float m[4];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            m[i % 4] = i < 4 ? x[i] : fmaxf(m[i % 4], x[i]);
+        return across_halves(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])),
+                             [](float u, float v) { return fmaxf(u, v); });
+    }
+
+    // p = 2^(x scale - from), rounded as the next product's operand; returns the
+    // lane's sum.
+    template <int NR>
+    static __device__ __forceinline__ float weights(float scale_log2, float from,
+                                                    const v16f_t (&x)[NR], u32x4 (&p)[NR][2])
+    {
+        float s[4] = {};
+#pragma unroll
+        for (int r = 0; r < NR; ++r) {
+            float e[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                e[i] = __builtin_amdgcn_exp2f(x[r][i] * scale_log2 - from);
+                s[i % 4] += e[i];
+            }
+            p[r][0] = pack_rows<T>(e, 0);
+            p[r][1] = pack_rows<T>(e, 1);
+        }
+        return (s[0] + s[1]) + (s[2] + s[3]);
+    }
+
+    // Writes the rows' results, or those of range sp of the keys.
+    __device__ __forceinline__ void store(const AttnCall &a, int b, int hk, int first,
+                                          int sp) const
+    {
+        const bool first_half = (threadIdx.x & 63) < 32;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const Row r(a, hk, first, qb);
+            const float l = across_halves(sum[qb], [](float u, float v) { return u + v; });
+            const bool none = __float_as_uint(l) == 0;
+            const float inv = none ? 0.0f : 1.0f / l;
+            const float lse = none ? -__builtin_huge_valf() : (base[qb] + __log2f(l)) * kLn2;
+            const size_t row = ((size_t)b * a.heads + r.head) * a.q_len + r.s;
+            if (a.splits > 1) {
+                const size_t all = (size_t)a.batch * a.heads * a.q_len;
+                store_columns_f32<DB>(a.part + (sp * all + row) * a.dim, r.ok, a.dim, o[qb],
+                                      inv);
+                if (r.ok && first_half)
+                    a.part_lse[sp * all + row] = lse;
+            } else {
+                store_columns<T, DB>(static_cast<T *>(a.out) +
+                                         (((size_t)b * a.q_len + r.s) * a.heads + r.head) *
+                                             a.dim,
+                                     r.ok, a.dim, o[qb], inv);
+                if (a.lse && r.ok && first_half)
+                    a.lse[row] = lse;
+            }
+        }
+    }
+};
 
 template <class T, int KS, int QB>
 __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forward(AttnCall a)
 {
-    constexpr int DB = Tile<KS>::DB, BM = 128 * QB, SIZE = Tile<KS>::kBytes;
+    constexpr int BM = 128 * QB, SIZE = Tile<KS>::kBytes;
     __shared__ __attribute__((aligned(16))) char lds[2][2 * SIZE];
-    const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int u = attn_unit(blockIdx.x, gridDim.x);
     const int mt = u % a.row_tiles;
@@ -35,26 +233,10 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
     const int sp = u % a.splits;
     u /= a.splits;
     const int hk = u % a.kv_heads, b = u / a.kv_heads;
-    const int group = a.heads / a.kv_heads;
-
-    // This lane's rows.
-    const int rows = group * a.q_len;
     const int first = mt * BM + wave * 32 * QB;
-    const bool busy = first < rows;             // the wave has rows
-    bool ok[QB];
-    int head[QB], s[QB];
-    u32x4 qf[QB][KS];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int m = first + 32 * qb + (lane & 31);
-        ok[qb] = m < rows;
-        const int g = ok[qb] ? m / a.q_len : 0;
-        s[qb] = ok[qb] ? m - g * a.q_len : 0;
-        head[qb] = hk * group + g;
-        load_columns<KS>(static_cast<const T *>(a.q) + b * a.q_stride[0] +
-                             s[qb] * a.q_stride[1] + head[qb] * a.q_stride[2],
-                         ok[qb], a.dim, qf[qb]);
-    }
+    const bool busy = first < a.heads / a.kv_heads * a.q_len;   // the wave has rows
+    Rows<T, KS, QB> rows;
+    rows.init(a, b, hk, first);
 
     const int n = key_count(a, b);
     const int t0 = sp * a.split_tiles;
@@ -62,23 +244,12 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
     const long long *stride = wave < 2 ? a.k_stride : a.v_stride;
     const T *kv = static_cast<const T *>(wave < 2 ? a.k : a.v) + b * stride[0] + hk * stride[2];
     const long long step = kAttnTile * stride[1];
-
-    v16f_t o[QB][DB];
-    float top[QB], sum[QB];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        top[qb] = -__builtin_huge_valf();
-        sum[qb] = 0.0f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-            o[qb][db] = v16f_t{};
-    }
-
     const Tile<KS> tile;
     Stager<KS> stager;
     stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     uint64_t live = 0, now = 0;
     int next_byte = 0;
+    bool fresh = true;
     if (t0 < t1) {
         now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
         stager.request(kv + t0 * step, live, lds[0]);
@@ -94,153 +265,76 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
             next_byte = mask_byte(a, b, n, t + 2);
         }
         if (busy && now) {
-            u32x4 p[QB][4];
-            v16f_t x[QB][2];
-#pragma unroll
-            for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const u32x4 f = tile.rows(kt, rb, ks);
-#pragma unroll
-                    for (int qb = 0; qb < QB; ++qb)
-                        x[qb][rb] = mfma(T{}, f, qf[qb][ks], ks ? x[qb][rb] : v16f_t{});
-                }
-            if (now != ~0ull) {
-#pragma unroll
-                for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float dead = dead_row(now, rb, i);
-#pragma unroll
-                        for (int qb = 0; qb < QB; ++qb)
-                            x[qb][rb][i] += dead;
-                    }
-            }
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                float mx = fmaxf(x[qb][0][0], x[qb][1][0]);
-#pragma unroll
-                for (int i = 1; i < 16; ++i)
-                    mx = fmaxf(mx, fmaxf(x[qb][0][i], x[qb][1][i]));
-                mx = across_halves(mx, [](float p, float q) { return fmaxf(p, q); });
-                mx *= a.scale_log2;
-                if (__ballot(mx > top[qb] + kSlack)) {
-                    const float newtop = fmaxf(top[qb], mx);
-                    // A row without a key so far has nothing to rescale.
-                    const float f = newtop == -__builtin_huge_valf()
-                                        ? 0.0f
-                                        : __builtin_amdgcn_exp2f(top[qb] - newtop);
-                    top[qb] = newtop;
-                    sum[qb] *= f;
-#pragma unroll
-                    for (int db = 0; db < DB; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            o[qb][db][i] *= f;
-                }
-                const float base = top[qb] == -__builtin_huge_valf() ? 0.0f : top[qb];
-#pragma unroll
-                for (int rb = 0; rb < 2; ++rb) {
-                    float e[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        e[i] = __builtin_amdgcn_exp2f(x[qb][rb][i] * a.scale_log2 - base);
-                        sum[qb] += e[i];
-                    }
-                    p[qb][2 * rb] = pack_rows<T>(e, 0);
-                    p[qb][2 * rb + 1] = pack_rows<T>(e, 1);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    const u32x4 f = tile.columns(vt, 16 * r, db);
-#pragma unroll
-                    for (int qb = 0; qb < QB; ++qb)
-                        o[qb][db] = mfma(T{}, f, p[qb][r], o[qb][db]);
-                }
+            rows.template keys<2>(tile, kt, vt, 0, a.scale_log2, now, fresh);
+            fresh = false;
         }
         now = live;
         stager.wait();
         __syncthreads();
     }
-
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const float l = across_halves(sum[qb], [](float p, float q) { return p + q; });
-        const bool none = __float_as_uint(l) == 0;
-        const float inv = none ? 0.0f : 1.0f / l;
-        const float lse = none ? -__builtin_huge_valf() : (top[qb] + __log2f(l)) * kLn2;
-        const size_t row = ((size_t)b * a.heads + head[qb]) * a.q_len + s[qb];
-        if (a.splits > 1) {
-            const size_t all = (size_t)a.batch * a.heads * a.q_len;
-            store_columns_f32<DB>(a.part + (sp * all + row) * a.dim, ok[qb], a.dim, o[qb], inv);
-            if (ok[qb] && lane < 32)
-                a.part_lse[sp * all + row] = lse;
-        } else {
-            store_columns<T, DB>(static_cast<T *>(a.out) +
-                                     (((size_t)b * a.q_len + s[qb]) * a.heads + head[qb]) *
-                                         a.dim,
-                                 ok[qb], a.dim, o[qb], inv);
-            if (a.lse && ok[qb] && lane < 32)
-                a.lse[row] = lse;
-        }
-    }
+    rows.store(a, b, hk, first, sp);
 }
 
-// Brings the ranges of keys together.  A workgroup has one row; its four waves
-// take every fourth range, two elements to a lane, and meet in LDS.
-template <class T> __global__ void __launch_bounds__(256) k_attn_join(AttnCall a)
+// Brings the ranges of keys together: 32 lanes with four elements each have
+// every SLICES-th range of a row, whose parts meet in LDS.
+template <class T, int SLICES> __global__ void __launch_bounds__(256) k_attn_join(AttnCall a)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const size_t all = (size_t)a.batch * a.heads * a.q_len, row = blockIdx.x;
-    __shared__ float sums[4], vals[4][TASQ_MAX_ATTENTION_DIM];
-    float top = -__builtin_huge_valf();
-    for (int sp = lane; sp < a.splits; sp += 64)
-        top = fmaxf(top, a.part_lse[sp * all + row]);
+    constexpr int ROWS = 8 / SLICES;
+    const int l = threadIdx.x & 31, slice = (threadIdx.x >> 5) % SLICES;
+    const size_t all = (size_t)a.batch * a.heads * a.q_len;
+    const size_t row = (size_t)blockIdx.x * ROWS + (threadIdx.x >> 5) / SLICES;
+    const bool ok = row < all, has = ok && 4 * l < a.dim;
+    float top = -__builtin_huge_valf(), sum = 0.0f, v[4] = {};
+    if (ok)
+        for (int sp = l; sp < a.splits; sp += 32)
+            top = fmaxf(top, a.part_lse[sp * all + row]);
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
+    for (int off = 16; off > 0; off >>= 1)
         top = fmaxf(top, __shfl_xor(top, off));
     const float base = top == -__builtin_huge_valf() ? 0.0f : top;
-    float sum = 0.0f, v0 = 0.0f, v1 = 0.0f;
-    const bool ok = 2 * lane < a.dim;
-#pragma unroll 4
-    for (int sp = wave; sp < a.splits; sp += 4) {
-        const float w = __builtin_amdgcn_exp2f((a.part_lse[sp * all + row] - base) * kLog2e);
-        const float2 p = ok ? *reinterpret_cast<const float2 *>(
-                                  a.part + (sp * all + row) * a.dim + 2 * lane)
-                            : make_float2(0.0f, 0.0f);
-        sum += w;
-        v0 += w * p.x;
-        v1 += w * p.y;
-    }
     if (ok) {
-        vals[wave][2 * lane] = v0;
-        vals[wave][2 * lane + 1] = v1;
+#pragma unroll 4
+        for (int sp = slice; sp < a.splits; sp += SLICES) {
+            const float w = __builtin_amdgcn_exp2f((a.part_lse[sp * all + row] - base) * kLog2e);
+            float p[4] = {};
+            if (has)
+                load_vec(a.part + (sp * all + row) * a.dim + 4 * l, p);
+            sum += w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] += w * p[i];
+        }
     }
-    if (lane == 0)
-        sums[wave] = sum;
-    __syncthreads();
-    if (wave != 0)
-        return;
-    sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    if constexpr (SLICES > 1) {
+        __shared__ float sums[SLICES], vals[SLICES][TASQ_MAX_ATTENTION_DIM];
+        store_vec(&vals[slice][4 * l], v);
+        if (l == 0)
+            sums[slice] = sum;
+        __syncthreads();
+        if (slice != 0)
+            return;
+#pragma unroll
+        for (int i = 1; i < SLICES; ++i) {
+            float p[4];
+            load_vec(&vals[i][4 * l], p);
+            sum += sums[i];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] += p[e];
+        }
+    }
     const bool none = __float_as_uint(sum) == 0;
     const float inv = none ? 0.0f : 1.0f / sum;
-    const int s = (int)(row % a.q_len), bh = (int)(row / a.q_len);
-    const int head = bh % a.heads, b = bh / a.heads;
-    if (ok) {
-        float y[2];
+    const int s = (int)(row % a.q_len);
+    const size_t bh = row / a.q_len;
+    const size_t head = bh % a.heads, b = bh / a.heads;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            y[i] = ((vals[0][2 * lane + i] + vals[1][2 * lane + i]) +
-                    (vals[2][2 * lane + i] + vals[3][2 * lane + i])) *
-                   inv;
-        *reinterpret_cast<uint32_t *>(static_cast<T *>(a.out) +
-                                      (((size_t)b * a.q_len + s) * a.heads + head) * a.dim +
-                                      2 * lane) = pack2<T>(y[0], y[1]);
-    }
-    if (a.lse && lane == 0)
+    for (int i = 0; i < 4; ++i)
+        v[i] *= inv;
+    if (has)
+        store_vec(static_cast<T *>(a.out) + ((b * a.q_len + s) * a.heads + head) * a.dim + 4 * l,
+                  v);
+    if (a.lse && ok && l == 0)
         a.lse[row] = none ? -__builtin_huge_valf() : base + __log2f(sum) * kLn2;
 }
 
@@ -272,8 +366,11 @@ template <class T> hipError_t attn_forward_typed(const AttnCall &a, hipStream_t 
     }
     if (e != hipSuccess || a.splits == 1)
         return e;
-    const long long rows = (long long)a.batch * a.heads * a.q_len;
-    k_attn_join<T><<<(unsigned)rows, 256, 0, stream>>>(a);
+    const size_t rows = (size_t)a.batch * a.heads * a.q_len;
+    if (a.splits < 16)
+        k_attn_join<T, 1><<<(unsigned)((rows + 7) / 8), 256, 0, stream>>>(a);
+    else
+        k_attn_join<T, 8><<<(unsigned)rows, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -98,17 +98,21 @@ int norm_rotate(const tasq_heads *jobs, int n, int type, int dim, float eps, int
 }
 
 // Ranges that `tiles` streamed tiles are cut into when `base` workgroups would
-// run uncut: enough to give each compute unit `per_cu` workgroups, at least
-// four tiles each.
-void plan_ranges(long long base, int tiles, int per_cu, int *ranges, int *range_tiles)
+// run uncut: two workgroups to each compute unit, or one where that already
+// takes many ranges, at least four tiles each.  Forward, 16 heads of 72 and
+// fewer over 4096 keys, microseconds uncut and cut: base 32 64.8 and 20.4 (8
+// ranges), 64 65.3 and 27.7, 128 65.7 and 38.0, 192 66.4 and 53.0 (2); one query
+// over 8191 keys of 128, base 8, 162 and 16 (32).  From 320 on uncut is faster
+// (76 and 97), as parts are written in fp32 and read again.
+void plan_ranges(long long base, int tiles, int *ranges, int *range_tiles)
 {
     *ranges = 1;
     *range_tiles = tiles > 0 ? tiles : 1;
-    if (base <= 0 || tiles < 8)
+    if (base <= 0 || base > 256 || tiles < 8)
         return;
-    const long long want = 256LL * per_cu / base;
+    const long long want = (base < 48 ? 256 : 512) / base;
     const int most = tiles / 4;
-    const int r = want < 2 ? 1 : want < most ? (int)want : most;
+    const int r = want < most ? (int)want : most;
     *range_tiles = (tiles + r - 1) / r;
     *ranges = (tiles + *range_tiles - 1) / *range_tiles;
 }
@@ -123,14 +127,15 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
     const int key_tiles = (c.kv_len + 63) / 64;
     const long long pair_rows = (long long)group * c.q_len;
     // Two blocks of rows to a wave halve what a row reads of LDS; they need
-    // registers (dims up to 96) and two workgroups for every compute unit.
+    // registers (dims up to 80) and two workgroups for every compute unit.  4096
+    // tokens among themselves, us with one block and two: 32 heads of 64 156 and
+    // 137, of 72 192 and 184; 10 heads of 64 (160 workgroups) 76 and 87.
     c.row_blocks = !backward && (c.dim + 15) / 16 <= tasq::kAttnWideSteps &&
                            pairs * ((pair_rows + 255) / 256) >= 512
                        ? 2
                        : 1;
     c.row_tiles = (int)((pair_rows + 128 * c.row_blocks - 1) / (128 * c.row_blocks));
-    plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, backward ? 2 : 3, &c.splits,
-                &c.split_tiles);
+    plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, &c.splits, &c.split_tiles);
     const size_t rows = (size_t)c.batch * c.heads * c.q_len;
     size_t bytes = 0;
     if (c.splits > 1) {
@@ -139,8 +144,8 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
     }
     if (backward) {
         c.key_tiles = (c.kv_len + 127) / 128;
-        plan_ranges(cut ? pairs * c.key_tiles : 0, group * ((c.q_len + 63) / 64), 2,
-                    &c.kv_splits, &c.kv_split_tiles);
+        plan_ranges(cut ? pairs * c.key_tiles : 0, group * ((c.q_len + 63) / 64), &c.kv_splits,
+                    &c.kv_split_tiles);
         bytes += round256(rows * sizeof(float));
         if (c.kv_splits > 1)
             bytes += round256((size_t)c.kv_splits * 2 * c.batch * c.kv_len * c.kv_heads * c.dim *
