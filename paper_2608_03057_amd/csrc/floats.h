@@ -104,6 +104,38 @@ template <class T, int N> __device__ __forceinline__ void store_vec(T *p, const 
     }
 }
 
+// v of all N lanes of a group (N a power of two, groups aligned) combined by f,
+// in every lane: exchanges within the vector unit, which take a few
+// instructions' time where one through LDS takes a hundred cycles.
+template <int CTRL> __device__ __forceinline__ float dpp_move(float v)
+{
+    const int i = (int)__float_as_uint(v);
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(i, i, CTRL, 0xf, 0xf, false));
+}
+
+template <int N, class F> __device__ __forceinline__ float group_reduce(float v, F f)
+{
+    if constexpr (N >= 2)
+        v = f(v, dpp_move<0xB1>(v));        // lane ^ 1
+    if constexpr (N >= 4)
+        v = f(v, dpp_move<0x4E>(v));        // lane ^ 2
+    if constexpr (N >= 8)
+        v = f(v, dpp_move<0x141>(v));       // mirrored within eight
+    if constexpr (N >= 16)
+        v = f(v, dpp_move<0x140>(v));       // mirrored within sixteen
+    if constexpr (N >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v),
+                                                        false, false);
+        v = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    if constexpr (N >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v),
+                                                        false, false);
+        v = f(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    }
+    return v;
+}
+
 inline int type_bytes(int type) { return type == TASQ_TYPE_F32 ? 4 : 2; }
 
 // f with a value of the type that `type` names.

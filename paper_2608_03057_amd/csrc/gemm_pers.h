@@ -165,13 +165,14 @@ struct StepLayers {
     }
 };
 
-struct OneLayer {
-    const LayerDesc &d;
+template <class D> struct OneLayerOf {
+    const D &d;
 
     __device__ __forceinline__ int find(int) const { return 0; }
-    __device__ __forceinline__ const LayerDesc &desc(int) const { return d; }
+    __device__ __forceinline__ const D &desc(int) const { return d; }
     __device__ __forceinline__ int bits(int) const { return d.bits; }
 };
+using OneLayer = OneLayerOf<LayerDesc>;
 
 // The work units that a workgroup walks: every wgs-th of its part of its XCD's
 // run (as in k_masked_gemm_persistent), ...
@@ -217,12 +218,55 @@ struct ListWalk {
     }
 };
 
+// What a tile ends with.  request() asks for what the epilogue reads, before the
+// last K tile's matrix work; write() stores the tile.  The weight stages
+// (smB) are idle from the last K tile's final LDS reads (every wave's, after a
+// barrier) until the next tile's prologue stores its weight K tile 0, and may
+// be used in between.
+template <class C, bool EXTRAS> struct LayerEpilogue {
+    ColLoads<C> cl;
+
+    __device__ __forceinline__ void request(const LayerDesc &d, int, int n0, int bits)
+    {
+        cols_request<C, EXTRAS>(d, n0, bits, cl);
+    }
+    __device__ __forceinline__ void write(const LayerDesc &dc, int mc, int nc,
+                                          const v16i (&acc)[C::FM][C::FN], char *smB) const
+    {
+        EpiCols<C> ec;
+        cols_finish<C, EXTRAS>(dc, mc, nc, cl, ec);
+        // The low-rank and weight-zero-point operands of the tile are staged
+        // in the weight stages.
+        bool staged = false;
+        if constexpr (EXTRAS) {
+            const bool lowrank = dc.lr_T != nullptr && dc.y != nullptr;
+            const bool wzero = dc.wz != nullptr && dc.y != nullptr;
+            staged = lowrank || wzero;
+            if (staged) {
+                pers::wait_lgkm0();
+                pers::barrier();
+                if (lowrank)
+                    stage_lowrank<C>(dc, mc, nc, smB);
+                if (wzero)
+                    stage_rowsums<C>(dc, mc, smB);
+                pers::wait_lgkm0();
+                pers::barrier();
+            }
+        }
+        epilogue_write<C, true, EXTRAS>(dc, acc, ec, smB);
+        if (staged) {
+            pers::wait_lgkm0();
+            pers::barrier();
+        }
+    }
+};
+
 // One workgroup per compute unit walks its work units.  g counts K tiles across the walk: K tile t of
 // the current tile is global K tile g0 + t, in activation stage (g0+t) % 3
 // and weight stage (g0+t) % 2; weight K tile t sits in register slot t % 2
 // from its load until its LDS store (both slots are empty at a tile
 // boundary, so the slots need not rotate across tiles).
-template <class C, bool EXTRAS, class Layers, class Walk>
+template <class C, class Epilogue, class Layers, class Walk>
 __device__ __forceinline__ void persistent_ds(const Layers &layers, Walk walk, char *sm)
 {
     using Ops = PersOperands<C>;
@@ -263,12 +307,12 @@ __device__ __forceinline__ void persistent_ds(const Layers &layers, Walk walk, c
     int g0 = 0;                       // global K tile of the current tile's K tile 0
     bool first = true;
     {
-        const LayerDesc &d0 = layers.desc(seg);
+        const auto &d0 = layers.desc(seg);
         ops.init(d0, m0, n0, tid);
         issue_first(0, 0);
     }
     for (;;) {
-        const LayerDesc &d = layers.desc(seg);
+        const auto &d = layers.desc(seg);
         const int nk = (d.K + C::BK - 1) / C::BK;
         const uint32_t wmask = keep_mask_dword(bits);
 
@@ -345,8 +389,8 @@ __device__ __forceinline__ void persistent_ds(const Layers &layers, Walk walk, c
             // tile t+2, activation K tile t+2 and weight K tile t+3, 12
             // requests.
             // Right after a tile boundary the previous tile's output stores
-            // sit between them, well over the 63 requests a wave can have in
-            // flight, so the hardware's own limit has already retired it.
+            // sit between them; there the store of weight K tile 1 above, whose
+            // request is younger, has waited for it.
             if (t == 0 && !first)
                 pers::wait_vm_lgkm0<63>();
             else
@@ -386,9 +430,9 @@ __device__ __forceinline__ void persistent_ds(const Layers &layers, Walk walk, c
         // nk-2 (or the previous tile's), whose reads every wave finished
         // before the last barrier; the register slots hold only the requests
         // past K.
-        ColLoads<C> cl;
-        cols_request<C, EXTRAS>(d, n0, bits, cl);
-        const LayerDesc &dc = d;
+        Epilogue epi;
+        epi.request(d, m0, n0, bits);
+        const auto &dc = d;
         const int mc = m0, nc = n0;
         const int g1 = g0 + nk;
         walk.next();
@@ -417,33 +461,7 @@ __device__ __forceinline__ void persistent_ds(const Layers &layers, Walk walk, c
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        EpiCols<C> ec;
-        cols_finish<C, EXTRAS>(dc, mc, nc, cl, ec);
-        // The low-rank and weight-zero-point operands of the tile are staged
-        // in the weight stages, idle from the last K tile's final LDS reads
-        // (every wave's, after the first barrier) until the next tile's
-        // prologue stores its weight K tile 0 (after the last barrier).
-        bool staged = false;
-        if constexpr (EXTRAS) {
-            const bool lowrank = dc.lr_T != nullptr && dc.y != nullptr;
-            const bool wzero = dc.wz != nullptr && dc.y != nullptr;
-            staged = lowrank || wzero;
-            if (staged) {
-                pers::wait_lgkm0();
-                pers::barrier();
-                if (lowrank)
-                    stage_lowrank<C>(dc, mc, nc, smB);
-                if (wzero)
-                    stage_rowsums<C>(dc, mc, smB);
-                pers::wait_lgkm0();
-                pers::barrier();
-            }
-        }
-        epilogue_write<C, true, EXTRAS>(dc, acc, ec, smB);
-        if (staged) {
-            pers::wait_lgkm0();
-            pers::barrier();
-        }
+        epi.write(dc, mc, nc, acc, smB);
         __builtin_amdgcn_sched_barrier(0);
         if (!more)
             break;
@@ -458,7 +476,7 @@ k_masked_gemm_persistent_ds(const LayerDesc *__restrict__ descs, int L, int tota
                             const uint8_t *__restrict__ table, int S, int stage, int parties)
 {
     __shared__ __attribute__((aligned(1024))) char sm[PersOperands<C>::LDS];
-    persistent_ds<C, EXTRAS>(StepLayers{descs, table, L, S, stage}, RunWalk(runs, parties), sm);
+    persistent_ds<C, LayerEpilogue<C, EXTRAS>>(StepLayers{descs, table, L, S, stage}, RunWalk(runs, parties), sm);
 }
 
 // The step as lists of units (unit_lists in tasq_api.cpp).
@@ -469,7 +487,7 @@ k_masked_gemm_lists_ds(const LayerDesc *__restrict__ descs, int L,
                        int S, int stage)
 {
     __shared__ __attribute__((aligned(1024))) char sm[PersOperands<C>::LDS];
-    persistent_ds<C, EXTRAS>(StepLayers{descs, table, L, S, stage}, ListWalk(order), sm);
+    persistent_ds<C, LayerEpilogue<C, EXTRAS>>(StepLayers{descs, table, L, S, stage}, ListWalk(order), sm);
 }
 
 // A single layer of at least about half a tile per compute unit, whose K loop
@@ -483,7 +501,7 @@ __global__ void __launch_bounds__(C::NT, C::OCC) k_masked_gemm_ds(LayerDesc d, X
     __shared__ __attribute__((aligned(1024))) char sm[PersOperands<C>::LDS];
     if constexpr (!EXTRAS)          // with them the scalar registers would not hold it all
         pin(d);
-    persistent_ds<C, EXTRAS>(OneLayer{d}, RunWalk(runs, 1), sm);
+    persistent_ds<C, LayerEpilogue<C, EXTRAS>>(OneLayer{d}, RunWalk(runs, 1), sm);
 }
 
 template <class C, bool EXTRAS>

@@ -103,10 +103,7 @@ template <class T, bool INTERLEAVED> struct Pairs {
 // Sum over the LPR lanes of a group.
 template <int LPR> __device__ __forceinline__ float group_sum(float v)
 {
-#pragma unroll
-    for (int off = LPR / 2; off > 0; off >>= 1)
-        v += __shfl_xor(v, off);
-    return v;
+    return group_reduce<LPR>(v, [](float a, float b) { return a + b; });
 }
 
 __device__ __forceinline__ void cos_sin(const HeadJob &j, int p, int l, float (&c)[4],
@@ -370,21 +367,26 @@ __global__ void __launch_bounds__(256) k_norm_rotate_backward(HeadCall call, flo
     }
 }
 
-// dw[d] = sum of `groups` workgroups' parts, 16 slices of them side by side.
+// dw[d] = sum of `groups` workgroups' parts: 8 columns to a workgroup, 32 slices
+// of the parts side by side.
 __global__ void __launch_bounds__(256) k_sum_dweight(HeadCall call, const float *part, int groups)
 {
-    const int job = blockIdx.y, d = blockIdx.x * 16 + (threadIdx.x & 15);
-    const int slice = threadIdx.x >> 4;
-    __shared__ float sum[16][17];
+    const int job = blockIdx.y, d = blockIdx.x * 8 + (threadIdx.x & 7);
+    const int slice = threadIdx.x >> 3;
+    __shared__ float sum[32][9];
     float v = 0.0f;
-    if (d < call.dim)
-        for (int g = slice; g < groups; g += 16)
-            v += part[((size_t)job * groups + g) * call.dim + d];
-    sum[slice][threadIdx.x & 15] = v;
+    if (d < call.dim) {
+        const float *p = part + (size_t)job * groups * call.dim + d;
+#pragma unroll 8
+        for (int g = slice; g < groups; g += 32)
+            v += p[(size_t)g * call.dim];
+    }
+    sum[slice][threadIdx.x & 7] = v;
     __syncthreads();
-    if (threadIdx.x < 16 && d < call.dim && call.job[job].dweight) {
+    if (threadIdx.x < 8 && d < call.dim && call.job[job].dweight) {
         v = 0.0f;
-        for (int g = 0; g < 16; ++g)
+#pragma unroll
+        for (int g = 0; g < 32; ++g)
             v += sum[g][threadIdx.x];
         call.job[job].dweight[d] = v;
     }
@@ -484,7 +486,7 @@ hipError_t launch_norm_rotate(const HeadCall &in, bool grad, float *part, hipStr
     });
     if (e != hipSuccess || !grad || c.n == 0)
         return e;
-    k_sum_dweight<<<dim3((c.dim + 15) / 16, c.n), 256, 0, stream>>>(c, part, groups);
+    k_sum_dweight<<<dim3((c.dim + 7) / 8, c.n), 256, 0, stream>>>(c, part, groups);
     return hipGetLastError();
 }
 

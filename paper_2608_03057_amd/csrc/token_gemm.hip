@@ -4,12 +4,12 @@
 //   y[m][n] = (sum_k X[m][k] W_b[n][k]) * sx[m] * sw[n] (+ bias[n]),
 //
 // W_b = W & keep_mask(b), the sum exact in int32, y fp32, bfloat16 or half,
-// rounded once.  The K loop is that of gemm_core.h; the epilogue is its own:
-// a factor per row, and 16-bit outputs that cross LDS so that a lane stores 16
-// bytes of a row.
+// rounded once.  The K loops are those of gemm_core.h and gemm_pers.h; the
+// epilogue is their own: a factor per row, and 16-bit outputs that cross LDS so
+// that a lane stores 16 bytes of a row.
 #include "block_internal.h"
 #include "floats.h"
-#include "gemm_core.h"
+#include "gemm_pers.h"
 
 namespace tasq {
 
@@ -115,15 +115,131 @@ __global__ void __launch_bounds__(C::NT, C::OCC) k_token_gemm(TokenLinear t, int
     token_epilogue<C, T>(t, m0, n0, acc, reinterpret_cast<char *>(sm), rows);
 }
 
-template <class C, class T> hipError_t launch_cfg(const TokenLinear &t, hipStream_t stream)
+// The persistent walk of gemm_pers.h with a token epilogue.
+struct TokenLayer : LayerDesc {
+    const float *rows;          // [M] token scales
+    void *out;                  // [M][N] of T, below 2 GiB; 16-bit rows 16-byte aligned
+};
+
+template <class C, class T> struct TokenEpilogue {
+    float scale[C::FN], bias[C::FN], row;
+
+    __device__ __forceinline__ void request(const TokenLayer &d, int m0, int n0, int)
+    {
+        const int lane = threadIdx.x & 63, wn = (threadIdx.x >> 6) % C::WAVES_N;
+        const rsrc_t rsw = make_rsrc(d.sw, (uint32_t)d.N * 4u);
+        const rsrc_t rb = make_rsrc(d.bias, d.bias ? (uint32_t)d.N * 4u : 0u);
+        const rsrc_t rr = make_rsrc(d.rows, (uint32_t)d.M * 4u);
+#pragma unroll
+        for (int j = 0; j < C::FN; ++j) {
+            const uint32_t on = 4u * (uint32_t)(n0 + wn * C::WTN + j * 32 + (lane & 31));
+            scale[j] =
+                __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rsw, on, 0, 0));
+            bias[j] =
+                __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, on, 0, 0));
+        }
+        const uint32_t om = threadIdx.x < C::BM ? 4u * (uint32_t)(m0 + (int)threadIdx.x) : kOOB;
+        row = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rr, om, 0, 0));
+    }
+
+    __device__ __forceinline__ void write(const TokenLayer &d, int m0, int n0,
+                                          const v16i (&acc)[C::FM][C::FN], char *smB) const
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int wm = wave / C::WAVES_N, wn = wave % C::WAVES_N;
+        float *rows = reinterpret_cast<float *>(smB);
+        char *out = smB + 4 * C::BM + wave * 32 * kOutPitch<C>;
+        pers::wait_lgkm0();
+        pers::barrier();
+        if (threadIdx.x < C::BM)
+            rows[threadIdx.x] = row;
+        pers::wait_lgkm0();
+        pers::barrier();
+        constexpr uint32_t ES = sizeof(T);
+        const rsrc_t ry = make_rsrc(d.out, (uint32_t)d.M * (uint32_t)d.N * ES);
+        const int mw = m0 + wm * C::WTM, nw = n0 + wn * C::WTN;
+#pragma unroll
+        for (int i = 0; i < C::FM; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r0 = 8 * q + 4 * (lane >> 5);
+                const float4 f =
+                    *reinterpret_cast<const float4 *>(rows + wm * C::WTM + 32 * i + r0);
+                const float rs[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                for (int j = 0; j < C::FN; ++j) {
+                    const int n = nw + 32 * j + (lane & 31);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const float val =
+                            (float)acc[i][j][4 * q + v] * (rs[v] * scale[j]) + bias[j];
+                        if constexpr (ES == 4) {
+                            // Rows past M fall past the buffer's end.
+                            const int m = mw + 32 * i + r0 + v;
+                            st32(ry,
+                                 n < d.N ? ((uint32_t)m * (uint32_t)d.N + (uint32_t)n) * 4u : kOOB,
+                                 __float_as_uint(val));
+                        } else {
+                            *reinterpret_cast<T *>(out + (r0 + v) * kOutPitch<C> +
+                                                   2 * (32 * j + (lane & 31))) = (T)val;
+                        }
+                    }
+                }
+            }
+            if constexpr (ES == 2) {
+                constexpr int CH = C::WTN / 8;
+#pragma unroll
+                for (int e = 0; e < CH / 2; ++e) {
+                    const int r = (64 * e + lane) / CH, c = lane % CH;
+                    const int m = mw + 32 * i + r, n = nw + 8 * c;
+                    const u32x4 u = *reinterpret_cast<const u32x4 *>(out + r * kOutPitch<C> + 16 * c);
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        u, ry, n < d.N ? ((uint32_t)m * (uint32_t)d.N + (uint32_t)n) * 2u : kOOB,
+                        0, 0);
+                }
+            }
+        }
+        pers::wait_lgkm0();
+        pers::barrier();
+    }
+};
+
+template <class C, class T>
+__global__ void __launch_bounds__(C::NT, C::OCC) k_token_gemm_walk(TokenLayer d, XcdRuns runs)
+{
+    __shared__ __attribute__((aligned(1024))) char sm[PersOperands<C>::LDS];
+    persistent_ds<C, TokenEpilogue<C, T>>(OneLayerOf<TokenLayer>{d}, RunWalk(runs, 1), sm);
+}
+
+template <class C, class T> hipError_t launch_walk(const TokenLinear &t, hipStream_t stream)
+{
+    TokenLayer d{};
+    d.X = t.X;
+    d.W = t.W;
+    d.sw = t.sw;
+    d.bias = t.bias;
+    d.rows = t.sx;
+    d.out = t.y;
+    d.M = t.M;
+    d.N = t.N;
+    d.K = t.K;
+    d.bits = t.bits;
+    fill_tiles<C>(d);
+    const long long tiles = (long long)d.tiles_m * d.tiles_n;
+    XcdRuns runs;
+    for (int x = 0; x <= 8; ++x)
+        runs.begin[x] = (int)(tiles * x / 8);
+    k_token_gemm_walk<C, T><<<256, C::NT, 0, stream>>>(d, runs);
+    return hipGetLastError();
+}
+
+template <class C, class T>
+hipError_t launch_cfg(const TokenLinear &t, bool aligned, hipStream_t stream)
 {
     const int tm = (t.M + C::BM - 1) / C::BM, tn = (t.N + C::BN - 1) / C::BN;
     const long long grid = (long long)tm * tn;
     if (grid > 0x7fffffffLL)
         return hipErrorInvalidValue;
-    const bool aligned = t.K % 16 == 0 && reinterpret_cast<uintptr_t>(t.X) % 16 == 0 &&
-                         reinterpret_cast<uintptr_t>(t.W) % 16 == 0 &&
-                         (long long)t.M * t.K < (1LL << 31) && (long long)t.N * t.K < (1LL << 31);
     if (aligned)
         k_token_gemm<C, true, T><<<(unsigned)grid, C::NT, 0, stream>>>(t, tm, tn);
     else
@@ -131,16 +247,115 @@ template <class C, class T> hipError_t launch_cfg(const TokenLinear &t, hipStrea
     return hipGetLastError();
 }
 
+// Few tokens: the weight is read once, by workgroups of 16 channels whose four
+// waves have every fourth 64 bytes of K each, straight from memory as matrix
+// operands (lane l: channel l%16, bytes 16 (l/16) .. of the 64), against the
+// tokens' codes read alike; the waves' int32 sums meet in LDS.  Bound by the
+// latency of one round of loads and the launch: 1x1152 -> 3456 (4 MB) 3.9 us,
+// 16x4608 -> 1152 7.1 (13.0 with 64x64 tiles).
+constexpr int kFewTokens = 64;
+
+template <class T, int MB>
+__global__ void __launch_bounds__(256) k_token_few(TokenLinear t)
+{
+    constexpr int UNROLL = MB <= 2 ? 8 : 4;
+    typedef int v4 __attribute__((ext_vector_type(4)));
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n0 = blockIdx.x * 16, r = lane & 15, kb = 16 * (lane >> 4);
+    const rsrc_t rw = make_rsrc(t.W, (uint32_t)t.N * (uint32_t)t.K);
+    const rsrc_t rx = make_rsrc(t.X, (uint32_t)t.M * (uint32_t)t.K);
+    const uint32_t ow = n0 + r < t.N ? (uint32_t)(n0 + r) * (uint32_t)t.K : kOOB;
+    uint32_t ox[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+        ox[mb] = 16 * mb + r < t.M ? (uint32_t)(16 * mb + r) * (uint32_t)t.K : kOOB;
+    const int mask = (int)keep_mask_dword(t.bits);
+    v4 acc[MB] = {};
+    for (int k0 = 64 * wave; k0 < t.K; k0 += 256 * UNROLL) {
+        v4i w[UNROLL], x[UNROLL][MB];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int k = k0 + 256 * u + kb;
+            const bool in = k < t.K;            // K % 16 == 0: whole chunks
+            w[u] = ld16(rw, in ? ow + (uint32_t)k : kOOB);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+                x[u][mb] = ld16(rx, in ? ox[mb] + (uint32_t)k : kOOB);
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const v4i wm = {w[u].x & mask, w[u].y & mask, w[u].z & mask, w[u].w & mask};
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+                acc[mb] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wm, x[u][mb], acc[mb], 0, 0, 0);
+        }
+    }
+    // Register v of lane l: channel 4 (l/16) + v, token l%16.
+    __shared__ v4 part[4][MB][64];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+        part[wave][mb][lane] = acc[mb];
+    __syncthreads();
+    for (int mb = wave; mb < MB; mb += 4) {
+        const int m = 16 * mb + r;
+        if (m >= t.M)
+            continue;
+        const v4 s = part[0][mb][lane] + part[1][mb][lane] + part[2][mb][lane] + part[3][mb][lane];
+        const float sx = t.sx[m];
+        T *y = static_cast<T *>(t.y) + (size_t)m * t.N;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int n = n0 + 4 * (lane >> 4) + v;
+            if (n < t.N)
+                y[n] = (T)((float)s[v] * (sx * t.sw[n]) + (t.bias ? t.bias[n] : 0.0f));
+        }
+    }
+}
+
+template <class T> hipError_t launch_few(const TokenLinear &t, hipStream_t stream)
+{
+    const unsigned grid = (unsigned)((t.N + 15) / 16);
+    if (t.M <= 16)
+        k_token_few<T, 1><<<grid, 256, 0, stream>>>(t);
+    else if (t.M <= 32)
+        k_token_few<T, 2><<<grid, 256, 0, stream>>>(t);
+    else
+        k_token_few<T, 4><<<grid, 256, 0, stream>>>(t);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_linear_tokens(const TokenLinear &t, hipStream_t stream)
 {
+    const bool aligned = t.K % 16 == 0 && reinterpret_cast<uintptr_t>(t.X) % 16 == 0 &&
+                         reinterpret_cast<uintptr_t>(t.W) % 16 == 0 &&
+                         (long long)t.M * t.K < (1LL << 31) && (long long)t.N * t.K < (1LL << 31);
     return with_type(t.type, [&](auto zero) {
         using T = decltype(zero);
-        const long long big = ((t.M + 127LL) / 128) * ((t.N + 127LL) / 128);
-        if (big >= 256)
-            return launch_cfg<Cfg<128, 128, 128, 2, 2, 2>, T>(t, stream);
-        return launch_cfg<Cfg<64, 64, 128, 2, 2, 2>, T>(t, stream);
+        if (aligned && t.M <= kFewTokens)
+            return launch_few<T>(t, stream);
+        // Tiles of 64x64 where larger ones would leave compute units idle, else
+        // 128x128, and from about half a tile per compute unit on 256x256, as a
+        // persistent walk where the operands allow it.  us, 64x64 / 128x128 /
+        // walk, bfloat16 out: 300x1152 -> 3456 7.0 / 9.3 / 16.7, 1024x1280 -> 3840
+        // 13.5 / 11.9 / 19.1, 8192x1152 -> 1152 (160 tiles of 256x256) 23.9 / 22.9 /
+        // 19.6, 4096x640 -> 5120 (320) 33.2 / 26.1 / 26.1, 8192x1152 -> 3456 (448)
+        // 64.8 / 49.8 / 40.2; 4096x2240 -> 6720 fp32 147 / 125 / 76.
+        const long long t128 = ((t.M + 127LL) / 128) * ((t.N + 127LL) / 128);
+        const long long t256 = ((t.M + 255LL) / 256) * ((t.N + 255LL) / 256);
+        if (t256 >= 140) {
+            const bool rows = sizeof(T) == 4 ||
+                              (t.N % 8 == 0 && reinterpret_cast<uintptr_t>(t.y) % 16 == 0);
+            const bool fits = (long long)t.M * t.N * (int)sizeof(T) < (1LL << 31);
+            if (aligned && rows && fits && t.K > 0)
+                return launch_walk<Cfg<256, 256, 128, 2, 4, 1>, T>(t, stream);
+            // (8192x1151 -> 3456 56 us, 69 with 128x128.)
+            return launch_cfg<Cfg<256, 256, 128, 2, 4, 1>, T>(t, aligned, stream);
+        }
+        if (t128 >= 200)
+            return launch_cfg<Cfg<128, 128, 128, 2, 2, 2>, T>(t, aligned, stream);
+        return launch_cfg<Cfg<64, 64, 128, 2, 2, 2, 4>, T>(t, aligned, stream);
     });
 }
 

@@ -23,21 +23,34 @@ struct TokenScale {
         : s(__fmul_rn(top, 1.0f / 127.0f)), div(s)
     {
     }
-    __device__ __forceinline__ int code(float x) const
+    // The code as a whole number.  (EXACT: the common case of Divider, decided
+    // once for a row.)
+    template <bool EXACT> __device__ __forceinline__ float code(float x) const
     {
-        if (s == 0.0f)
-            return 0;
-        const float q = div.exact ? div(x) : __fdiv_rn(x, s);
-        return (int)fminf(fmaxf(__builtin_rintf(q), -127.0f), 127.0f);
+        const float q = EXACT ? div(x) : s == 0.0f ? 0.0f : __fdiv_rn(x, s);
+        return __builtin_amdgcn_fmed3f(__builtin_rintf(q), -127.0f, 127.0f);
+    }
+    // Eight codes.
+    __device__ __forceinline__ uint2 codes(const float (&v)[8]) const
+    {
+        float q[8];
+        if (div.exact) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                q[e] = code<true>(v[e]) + 128.0f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                q[e] = code<false>(v[e]) + 128.0f;
+        }
+        return make_uint2(pack_codes(q[0], q[1], q[2], q[3]), pack_codes(q[4], q[5], q[6], q[7]));
     }
 };
 
 // Maximum over the TPR threads of a row (TPR 64: a wave; 256: a workgroup).
 template <int TPR> __device__ __forceinline__ float row_max(float v)
 {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1)
-        v = fmaxf(v, __shfl_xor(v, off));
+    v = group_reduce<64>(v, [](float a, float b) { return fmaxf(a, b); });
     if constexpr (TPR > 64) {
         __shared__ float part[TPR / 64];
         if ((threadIdx.x & 63) == 0)
@@ -84,12 +97,8 @@ __global__ void __launch_bounds__(256) k_quantize_tokens(const T *__restrict__ x
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         if (t + i * TPR < chunks) {
-            uint32_t w[2] = {0, 0};
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                w[e >> 2] |= (uint32_t)(uint8_t)ts.code(v[i][e]) << (8 * (e & 3));
             *reinterpret_cast<uint2 *>(q + (size_t)m * K + 8 * (size_t)(t + i * TPR)) =
-                make_uint2(w[0], w[1]);
+                ts.codes(v[i]);
         }
     }
     if (t == 0)
@@ -110,7 +119,7 @@ __global__ void __launch_bounds__(256) k_quantize_tokens_any(const T *__restrict
         top = fmaxf(top, fabsf((float)row[k]));
     const TokenScale ts(row_max<256>(top));
     for (int k = threadIdx.x; k < K; k += 256)
-        q[(size_t)m * K + k] = (int8_t)ts.code((float)row[k]);
+        q[(size_t)m * K + k] = (int8_t)(int)ts.code<false>((float)row[k]);
     if (threadIdx.x == 0)
         sx[m] = ts.s;
 }
@@ -140,6 +149,8 @@ hipError_t launch_typed(const T *x, int M, int K, long long stride, int8_t *q, f
         return launch_rows<T, 64, 1>(x, M, K, stride, q, sx, stream);
     if (K <= 64 * 8 * 2)
         return launch_rows<T, 64, 2>(x, M, K, stride, q, sx, stream);
+    if (K <= 64 * 8 * 3)
+        return launch_rows<T, 64, 3>(x, M, K, stride, q, sx, stream);
     if (K <= 64 * 8 * 4)
         return launch_rows<T, 64, 4>(x, M, K, stride, q, sx, stream);
     if (K <= 256 * 8 * 2)
