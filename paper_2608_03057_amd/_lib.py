@@ -197,18 +197,19 @@ def lib() -> ctypes.CDLL:
         L.tasq_masked_linear_tokens.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, i32,
                                                 vp]
         L.tasq_masked_linear_tokens.restype = i32
-        L.tasq_norm_rotate.argtypes = [ctypes.POINTER(Heads), i32, i32, i32, f32, i32, vp]
+        # (Descriptors as addresses: a Structure by reference, or packed bytes.)
+        L.tasq_norm_rotate.argtypes = [vp, i32, i32, i32, f32, i32, vp]
         L.tasq_norm_rotate.restype = i32
-        L.tasq_norm_rotate_backward.argtypes = [ctypes.POINTER(Heads), i32, i32, i32, f32, i32,
+        L.tasq_norm_rotate_backward.argtypes = [vp, i32, i32, i32, f32, i32,
                                                 vp, size, vp]
         L.tasq_norm_rotate_backward.restype = i32
         L.tasq_norm_rotate_workspace_bytes.argtypes = [i32, i32]
         L.tasq_norm_rotate_workspace_bytes.restype = size
         for name in ("tasq_attention_forward", "tasq_attention_backward"):
             f = getattr(L, name)
-            f.argtypes = [ctypes.POINTER(Attention), vp]
+            f.argtypes = [vp, vp]
             f.restype = i32
-        L.tasq_attention_workspace_bytes.argtypes = [ctypes.POINTER(Attention), i32]
+        L.tasq_attention_workspace_bytes.argtypes = [vp, i32]
         L.tasq_attention_workspace_bytes.restype = size
         L.tasq_status_string.argtypes = [i32]
         L.tasq_status_string.restype = ctypes.c_char_p

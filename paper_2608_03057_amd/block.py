@@ -5,17 +5,21 @@ As in ``api``: tensors are checked, pointers and the current stream go to the
 C ABI of ``include/tasq.h``, an error raises ``TasqError``, and the work is
 asynchronous on the current stream.  Outputs and workspaces are allocated
 when they are not given.
+
+Descriptor structs are packed with ``struct`` (0.3 us; filling a ctypes
+Structure field by field takes 5): a call on one token is as long as its host
+side.  The formats are those of ``_lib.Heads`` and ``_lib.Attention``.
 """
 from __future__ import annotations
 
-import ctypes
+import struct
 from typing import Optional, Tuple
 
 import torch
 
 from . import _lib
-from ._lib import Attention, Heads, check
-from .api import _need, _ptr, _stream
+from ._lib import check
+from .api import _need, _stream
 
 _TYPES = {torch.float32: _lib.TYPE_F32, torch.bfloat16: _lib.TYPE_BF16,
           torch.float16: _lib.TYPE_F16}
@@ -24,23 +28,53 @@ _TYPES = {torch.float32: _lib.TYPE_F32, torch.bfloat16: _lib.TYPE_BF16,
 # tokens' rows of them, int32 [batch, tokens].
 Rope = Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]
 
+_HEADS = struct.Struct("8P6q5i4x")          # tasq_heads
+_ATTENTION = struct.Struct("7if3P9q5P3q4PN")    # tasq_attention
+
 
 def _type(t: torch.Tensor, name: str) -> int:
-    if t.dtype not in _TYPES:
+    code = _TYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    return _TYPES[t.dtype]
+    return code
 
 
 def _strided(t: torch.Tensor, dtype, shape, name):
-    """A GPU tensor with a contiguous innermost dimension and any other strides."""
+    """Strides of a GPU tensor with a contiguous innermost dimension."""
+    st = t.stride()
+    if t.is_cuda and t.dtype == dtype and t.shape == shape and st[-1] == 1:
+        return st
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    if st[-1] != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
+    return st
+
+
+def _at(t: Optional[torch.Tensor], dtype, shape, name) -> int:
+    """Address of a contiguous GPU tensor, 0 for None."""
+    if t is None:
+        return 0
+    _need(t, dtype, shape, name)
+    return t.data_ptr()
+
+
+def _like(t: torch.Tensor, dtype=None) -> torch.Tensor:
+    """A contiguous tensor of t's shape, uninitialised.  (1.3 us against 2.2 of
+    torch.empty with a shape, of which a call makes several.)"""
+    return torch.empty_like(t, dtype=dtype, memory_format=torch.contiguous_format)
+
+
+def _workspace(workspace, nbytes, device, name):
+    if workspace is None:
+        return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError(f"workspace of {name} must be a contiguous GPU tensor")
+    return workspace
 
 
 def quantize_tokens(x: torch.Tensor, out: Optional[torch.Tensor] = None,
@@ -48,15 +82,17 @@ def quantize_tokens(x: torch.Tensor, out: Optional[torch.Tensor] = None,
     """(int8 codes [M, K], fp32 scales [M]) of activations x [M, K] of any
     floating type, rows at any stride: scale max|x| * fl(1/127) per token,
     codes round(x / scale)."""
-    M, K = x.shape
-    _strided(x, x.dtype, x.shape, "x")
+    M, K = shape = x.shape
+    st = _strided(x, x.dtype, shape, "x")
     if out is None:
-        out = torch.empty((M, K), dtype=torch.int8, device=x.device)
+        out = _like(x, torch.int8)
+    else:
+        _need(out, torch.int8, shape, "out")
     if scales is None:
         scales = torch.empty(M, dtype=torch.float32, device=x.device)
-    _need(out, torch.int8, (M, K), "out")
-    _need(scales, torch.float32, (M,), "scales")
-    rc = _lib.lib().tasq_quantize_tokens(x.data_ptr(), _type(x, "x"), M, K, x.stride(0),
+    else:
+        _need(scales, torch.float32, (M,), "scales")
+    rc = _lib.lib().tasq_quantize_tokens(x.data_ptr(), _type(x, "x"), M, K, st[0],
                                          out.data_ptr(), scales.data_ptr(), _stream())
     if rc:
         check(rc, "tasq_quantize_tokens")
@@ -76,45 +112,51 @@ def masked_linear_tokens(X: torch.Tensor, W: torch.Tensor, sx: torch.Tensor, sw:
     _need(W, torch.int8, (N, K), "W")
     _need(sx, torch.float32, (M,), "sx")
     _need(sw, torch.float32, (N,), "sw")
-    _need(bias, torch.float32, (N,), "bias")
     if y is None:
-        y = torch.empty((M, N), dtype=out_dtype, device=X.device)
-    _need(y, y.dtype, (M, N), "y")
-    rc = _lib.lib().tasq_masked_linear_tokens(X.data_ptr(), sx.data_ptr(), W.data_ptr(),
-                                              sw.data_ptr(), _ptr(bias), M, N, K, int(b),
-                                              y.data_ptr(), _type(y, "y"), _stream())
+        y = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=X.device)
+    else:
+        _need(y, y.dtype, (M, N), "y")
+    rc = _lib.lib().tasq_masked_linear_tokens(
+        X.data_ptr(), sx.data_ptr(), W.data_ptr(), sw.data_ptr(),
+        _at(bias, torch.float32, (N,), "bias"), M, N, K, int(b), y.data_ptr(), _type(y, "y"),
+        _stream())
     if rc:
         check(rc, "tasq_masked_linear_tokens")
     return y
 
 
-def _heads(j: Heads, x, weight, rope: Optional[Rope], out, name, dy=None, dweight=None):
-    """Fills one tasq_heads; returns out (allocated when None)."""
-    if x.dim() != 4:
+def _heads(x, weight, rope: Optional[Rope], out, name, dy=None, dweight=None):
+    """(a packed tasq_heads, out): out is allocated when None."""
+    shape = x.shape
+    if len(shape) != 4:
         raise ValueError(f"{name} must be [batch, tokens, heads, dim]")
-    _strided(x, x.dtype, x.shape, name)
-    B, S, H, D = x.shape
+    B, S, H, D = shape
+    st = _strided(x, x.dtype, shape, name)
     if out is None:
-        out = torch.empty((B, S, H, D), dtype=x.dtype, device=x.device)
-    _need(out, x.dtype, (B, S, H, D), f"output of {name}")
-    _need(weight, torch.float32, (D,), f"weight of {name}")
-    j.x, j.out, j.weight = x.data_ptr(), out.data_ptr(), _ptr(weight)
-    j.x_stride[:] = x.stride()[:3]
-    j.batch, j.tokens, j.heads = B, S, H
+        out = _like(x)
+    else:
+        _need(out, x.dtype, shape, f"output of {name}")
+    cos_at = sin_at = position_at = positions = rot = 0
     if rope is not None:
         cos, sin, position = rope
-        P, half = cos.shape
-        _need(cos, torch.float32, (P, half), "cos")
-        _need(sin, torch.float32, (P, half), "sin")
-        _need(position, torch.int32, (B, S), "positions")
-        j.cos, j.sin, j.position = cos.data_ptr(), sin.data_ptr(), _ptr(position)
-        j.positions, j.rot = P, 2 * half
+        positions, half = cos.shape
+        cos_at = _at(cos, torch.float32, (positions, half), "cos")
+        sin_at = _at(sin, torch.float32, (positions, half), "sin")
+        position_at = _at(position, torch.int32, (B, S), "positions")
+        rot = 2 * half
+    gat, gst, dwat = 0, (0, 0, 0, 0), 0
     if dy is not None:
-        _strided(dy, x.dtype, x.shape, f"gradient of {name}")
-        j.dy = dy.data_ptr()
-        j.dy_stride[:] = dy.stride()[:3]
-        j.dweight = _ptr(dweight)
-    return out
+        gst = _strided(dy, x.dtype, shape, f"gradient of {name}")
+        gat, dwat = dy.data_ptr(), 0 if dweight is None else dweight.data_ptr()
+    return _HEADS.pack(x.data_ptr(), gat, out.data_ptr(),
+                       _at(weight, torch.float32, (D,), f"weight of {name}"), dwat, cos_at,
+                       sin_at, position_at, st[0], st[1], st[2], gst[0], gst[1], gst[2], B, S, H,
+                       positions, rot), out
+
+
+def _same_heads(q, k):
+    if k.dtype != q.dtype or k.shape[-1] != q.shape[-1]:
+        raise ValueError("q and k differ in type or head dimension")
 
 
 def qk_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torch.Tensor] = None,
@@ -126,13 +168,12 @@ def qk_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torc
     one type, any strides: root-mean-square norm of every head with weight
     [D], then the rotation of its first elements by rope = (cos, sin,
     positions).  Pairs lie rot/2 apart, or side by side with interleaved."""
-    n = 1 if k is None else 2
-    if k is not None and (k.dtype != q.dtype or k.shape[-1] != q.shape[-1]):
-        raise ValueError("q and k differ in type or head dimension")
-    jobs = (Heads * 2)()
-    out_q = _heads(jobs[0], q, wq, rope_q, out_q, "q")
+    jobs, out_q = _heads(q, wq, rope_q, out_q, "q")
+    n = 1
     if k is not None:
-        out_k = _heads(jobs[1], k, wk, rope_k, out_k, "k")
+        _same_heads(q, k)
+        more, out_k = _heads(k, wk, rope_k, out_k, "k")
+        jobs, n = jobs + more, 2
     rc = _lib.lib().tasq_norm_rotate(jobs, n, _type(q, "q"), q.shape[3], eps, interleaved,
                                      _stream())
     if rc:
@@ -145,14 +186,6 @@ def qk_norm_rotate_workspace_bytes(dim: int, n: int = 2) -> int:
     return _lib.lib().tasq_norm_rotate_workspace_bytes(n, dim)
 
 
-def _workspace(workspace, nbytes, device, name):
-    if workspace is None:
-        return torch.empty(max(nbytes, 1), dtype=torch.uint8, device=device)
-    if not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError(f"workspace of {name} must be a contiguous GPU tensor")
-    return workspace
-
-
 def qk_norm_rotate_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: torch.Tensor,
                             k: Optional[torch.Tensor], wq: Optional[torch.Tensor] = None,
                             wk: Optional[torch.Tensor] = None, rope_q: Optional[Rope] = None,
@@ -162,73 +195,72 @@ def qk_norm_rotate_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: tor
     """Gradients (dq, dk, dwq, dwk) of qk_norm_rotate from the gradients dq,
     dk of its outputs: of its inputs, in their type, and of its weights, fp32
     [D] (None where there is no weight, or no k)."""
-    n = 1 if k is None else 2
-    if k is not None and (k.dtype != q.dtype or k.shape[-1] != q.shape[-1]):
-        raise ValueError("q and k differ in type or head dimension")
     D = q.shape[-1]
     dwq, dwk = (None if w is None else torch.empty(D, dtype=torch.float32, device=q.device)
                 for w in (wq, wk))
-    jobs = (Heads * 2)()
-    gq = _heads(jobs[0], q, wq, rope_q, None, "q", dq, dwq)
-    gk = None
+    jobs, gq = _heads(q, wq, rope_q, None, "q", dq, dwq)
+    n, gk = 1, None
     if k is not None:
-        gk = _heads(jobs[1], k, wk, rope_k, None, "k", dk, dwk)
-    ws = _workspace(workspace, qk_norm_rotate_workspace_bytes(D, n), q.device,
+        _same_heads(q, k)
+        more, gk = _heads(k, wk, rope_k, None, "k", dk, dwk)
+        jobs, n = jobs + more, 2
+    L = _lib.lib()
+    ws = _workspace(workspace, L.tasq_norm_rotate_workspace_bytes(n, D), q.device,
                     "qk_norm_rotate_backward")
-    rc = _lib.lib().tasq_norm_rotate_backward(jobs, n, _type(q, "q"), D, eps, interleaved,
-                                              ws.data_ptr(), ws.numel() * ws.element_size(),
-                                              _stream())
+    rc = L.tasq_norm_rotate_backward(jobs, n, _type(q, "q"), D, eps, interleaved, ws.data_ptr(),
+                                     ws.numel() * ws.element_size(), _stream())
     if rc:
         check(rc, "tasq_norm_rotate_backward")
     return gq, gk, dwq, dwk
 
 
-def _attention(q, k, v, kv_lengths, key_mask, scale) -> Attention:
-    if q.dim() != 4 or k.dim() != 4:
+def _attention_head(q, k, v, kv_lengths, key_mask, scale):
+    """The fields of a tasq_attention that both directions share."""
+    qs, ks = q.shape, k.shape
+    if len(qs) != 4 or len(ks) != 4:
         raise ValueError("q, k and v must be [batch, tokens, heads, dim]")
-    B, SQ, H, D = q.shape
-    SK, HK = k.shape[1:3]
-    if q.dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError(f"q must be bfloat16 or float16, got {q.dtype}")
-    _strided(q, q.dtype, q.shape, "q")
-    _strided(k, q.dtype, (B, SK, HK, D), "k")
-    _strided(v, q.dtype, (B, SK, HK, D), "v")
-    _need(kv_lengths, torch.int32, (B,), "kv_lengths")
+    B, SQ, H, D = qs
+    SK, HK = ks[1], ks[2]
+    dtype = q.dtype
+    if dtype != torch.bfloat16 and dtype != torch.float16:
+        raise ValueError(f"q must be bfloat16 or float16, got {dtype}")
+    sq = _strided(q, dtype, qs, "q")
+    sk = _strided(k, dtype, (B, SK, HK, D), "k")
+    sv = _strided(v, dtype, ks, "v")
+    mask_at = 0
     if key_mask is not None:
         if key_mask.dtype not in (torch.bool, torch.uint8):
             raise ValueError("key_mask must be bool or uint8")
-        _need(key_mask, key_mask.dtype, (B, SK), "key_mask")
-    a = Attention()
-    a.type = _TYPES[q.dtype]
-    a.batch, a.heads, a.kv_heads, a.q_len, a.kv_len, a.dim = B, H, HK, SQ, SK, D
-    a.scale = D ** -0.5 if scale is None else scale
-    a.q, a.k, a.v = q.data_ptr(), k.data_ptr(), v.data_ptr()
-    a.q_stride[:] = q.stride()[:3]
-    a.k_stride[:] = k.stride()[:3]
-    a.v_stride[:] = v.stride()[:3]
-    a.kv_lengths, a.key_mask = _ptr(kv_lengths), _ptr(key_mask)
-    return a
+        mask_at = _at(key_mask, key_mask.dtype, (B, SK), "key_mask")
+    return (_TYPES[dtype], B, H, HK, SQ, SK, D, D ** -0.5 if scale is None else scale,
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), sq[0], sq[1], sq[2], sk[0], sk[1], sk[2],
+            sv[0], sv[1], sv[2], _at(kv_lengths, torch.int32, (B,), "kv_lengths"), mask_at)
+
+
+_NO_GRADS = (0, 0, 0, 0, 0, 0, 0)           # dout, its strides, dq, dk, dv
 
 
 def attention_workspace_bytes(q: torch.Tensor, k: torch.Tensor, *, backward: bool = False) -> int:
     """Workspace with which attention (or its backward pass) of these shapes
     runs ranges of a long axis side by side."""
-    a = _attention(q, k, k, None, None, None)
-    return _lib.lib().tasq_attention_workspace_bytes(ctypes.byref(a), backward)
+    a = _ATTENTION.pack(*_attention_head(q, k, k, None, None, None), 0, 0, *_NO_GRADS, 0, 0)
+    return _lib.lib().tasq_attention_workspace_bytes(a, backward)
 
 
-def _take_workspace(a: Attention, workspace, device, backward):
-    """Sets the workspace, allocated when None and of any use; returns what
-    has to live until the call has been made."""
+def _run_attention(fields, backward: bool, workspace, device, f, name):
+    """Calls f with the workspace that the caller gave, or with one of the size
+    that the library asks for."""
+    a = _ATTENTION.pack(*fields, 0, 0)
     if workspace is None:
-        nbytes = _lib.lib().tasq_attention_workspace_bytes(ctypes.byref(a), backward)
-        if not nbytes:
-            return None
+        nbytes = _lib.lib().tasq_attention_workspace_bytes(a, backward)
     else:
         nbytes = workspace.numel() * workspace.element_size()
-    ws = _workspace(workspace, nbytes, device, "attention")
-    a.workspace, a.workspace_bytes = ws.data_ptr(), nbytes
-    return ws
+    if nbytes:
+        ws = _workspace(workspace, nbytes, device, "attention")
+        a = _ATTENTION.pack(*fields, ws.data_ptr(), nbytes)
+    rc = f(a, _stream())
+    if rc:
+        check(rc, name)
 
 
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
@@ -242,18 +274,21 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
     multiple of HK, whose heads are shared.  Keys count where they are below
     kv_lengths (int32 [B]) and nonzero in key_mask (bool or uint8 [B, SK]); a
     query without keys gives zeros.  scale defaults to D ** -0.5."""
-    a = _attention(q, k, v, kv_lengths, key_mask, scale)
+    head = _attention_head(q, k, v, kv_lengths, key_mask, scale)
+    shape = q.shape
+    stats = (head[1], head[2], head[4])     # batch, heads, queries
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if lse is None and want_lse:
-        lse = torch.empty((a.batch, a.heads, a.q_len), dtype=torch.float32, device=q.device)
-    _need(out, q.dtype, q.shape, "out")
-    _need(lse, torch.float32, (a.batch, a.heads, a.q_len), "lse")
-    a.out, a.lse = out.data_ptr(), _ptr(lse)
-    ws = _take_workspace(a, workspace, q.device, 0)  # noqa: F841
-    rc = _lib.lib().tasq_attention_forward(ctypes.byref(a), _stream())
-    if rc:
-        check(rc, "tasq_attention_forward")
+        out = _like(q)
+    else:
+        _need(out, q.dtype, shape, "out")
+    if lse is not None:
+        _need(lse, torch.float32, stats, "lse")
+    elif want_lse:
+        lse = torch.empty_strided(stats, (stats[1] * stats[2], stats[2], 1), dtype=torch.float32,
+                                  device=q.device)
+    _run_attention((*head, out.data_ptr(), 0 if lse is None else lse.data_ptr(), *_NO_GRADS),
+                   False, workspace, q.device, _lib.lib().tasq_attention_forward,
+                   "tasq_attention_forward")
     return out, lse
 
 
@@ -267,24 +302,20 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     """Gradients (dq, dk, dv) of attention from the gradient dout of its
     output, with the out and lse that the forward call gave for the same
     arguments."""
-    a = _attention(q, k, v, kv_lengths, key_mask, scale)
-    _strided(dout, q.dtype, q.shape, "dout")
-    _need(out, q.dtype, q.shape, "out")
-    _need(lse, torch.float32, (a.batch, a.heads, a.q_len), "lse")
-    if dq is None:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if dk is None:
-        dk = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-    if dv is None:
-        dv = torch.empty(k.shape, dtype=q.dtype, device=q.device)
-    _need(dq, q.dtype, q.shape, "dq")
-    _need(dk, q.dtype, k.shape, "dk")
-    _need(dv, q.dtype, k.shape, "dv")
-    a.out, a.lse, a.dout = out.data_ptr(), lse.data_ptr(), dout.data_ptr()
-    a.dout_stride[:] = dout.stride()[:3]
-    a.dq, a.dk, a.dv = dq.data_ptr(), dk.data_ptr(), dv.data_ptr()
-    ws = _take_workspace(a, workspace, q.device, 1)  # noqa: F841
-    rc = _lib.lib().tasq_attention_backward(ctypes.byref(a), _stream())
-    if rc:
-        check(rc, "tasq_attention_backward")
+    head = _attention_head(q, k, v, kv_lengths, key_mask, scale)
+    shape, dtype = q.shape, q.dtype
+    gs = _strided(dout, dtype, shape, "dout")
+    _need(out, dtype, shape, "out")
+    _need(lse, torch.float32, (head[1], head[2], head[4]), "lse")
+
+    def grad(t, like, name):
+        if t is None:
+            return _like(like)
+        _need(t, dtype, like.shape, name)
+        return t
+    dq, dk, dv = grad(dq, q, "dq"), grad(dk, k, "dk"), grad(dv, v, "dv")
+    _run_attention((*head, out.data_ptr(), lse.data_ptr(), dout.data_ptr(), gs[0], gs[1], gs[2],
+                    dq.data_ptr(), dk.data_ptr(), dv.data_ptr()),
+                   True, workspace, q.device, _lib.lib().tasq_attention_backward,
+                   "tasq_attention_backward")
     return dq, dk, dv
