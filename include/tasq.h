@@ -608,8 +608,8 @@ enum { TASQ_TYPE_F32 = 0, TASQ_TYPE_BF16 = 1, TASQ_TYPE_F16 = 2 };
  *             takes vector loads, any other layout element loads.
  *   X_out     int8 [M][K]; sx_out fp32 [M] (4-byte aligned).
  * M == 0 enqueues nothing; K == 0 writes sx = 0.  Errors: TASQ_ERR_NULL,
- * _DIM (negative sizes, x_stride < K), _OVERFLOW (K > TASQ_MAX_K), _KIND,
- * _ALIGN (x not aligned to its elements), _HIP.
+ * _DIM (a negative size, M > 2^30, x_stride < K), _OVERFLOW (K >
+ * TASQ_MAX_K), _KIND, _ALIGN (x not aligned to its elements), _HIP.
  */
 int tasq_quantize_tokens(const void *x, int x_type, int M, int K, long long x_stride,
                          int8_t *X_out, float *sx_out, void *stream);
@@ -622,8 +622,9 @@ int tasq_quantize_tokens(const void *x, int x_type, int M, int K, long long x_st
  * [M], sw fp32 [N], bias fp32 [N] or NULL, y_out [M][N] of y_type, all
  * contiguous; b as in tasq_masked_linear.  K a multiple of 16 with X and W
  * 16-byte aligned takes whole vector loads.  M == 0 or N == 0 enqueues
- * nothing.  Errors: TASQ_ERR_NULL, _DIM, _BITS, _OVERFLOW, _KIND, _ALIGN (a
- * floating array not aligned to its elements), _HIP.
+ * nothing.  Errors: TASQ_ERR_NULL, _DIM (a negative size, M or N > 2^30),
+ * _BITS, _OVERFLOW, _KIND, _ALIGN (a floating array not aligned to its
+ * elements), _HIP.
  */
 int tasq_masked_linear_tokens(const int8_t *X, const float *sx, const int8_t *W, const float *sw,
                               const float *bias, int M, int N, int K, int b, void *y_out,

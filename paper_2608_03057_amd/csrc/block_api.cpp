@@ -7,6 +7,8 @@
 
 namespace {
 
+constexpr int kMostRows = 1 << 30;  // rounded up to tiles in 32 bits
+
 bool type_known(int t)
 {
     return t == TASQ_TYPE_F32 || t == TASQ_TYPE_BF16 || t == TASQ_TYPE_F16;
@@ -284,7 +286,7 @@ int tasq_quantize_tokens(const void *x, int x_type, int M, int K, long long x_st
 {
     if (!type_known(x_type))
         return TASQ_ERR_KIND;
-    if (M < 0 || K < 0 || (M > 1 && x_stride < K))
+    if (M < 0 || M > kMostRows || K < 0 || (M > 1 && x_stride < K))
         return TASQ_ERR_DIM;
     if (K > TASQ_MAX_K)
         return TASQ_ERR_OVERFLOW;
@@ -304,7 +306,7 @@ int tasq_masked_linear_tokens(const int8_t *X, const float *sx, const int8_t *W,
 {
     if (!type_known(y_type))
         return TASQ_ERR_KIND;
-    if (M < 0 || N < 0 || K < 0)
+    if (M < 0 || M > kMostRows || N < 0 || N > kMostRows || K < 0)
         return TASQ_ERR_DIM;
     if (K > TASQ_MAX_K)
         return TASQ_ERR_OVERFLOW;

