@@ -125,33 +125,42 @@ def masked_linear_tokens(X: torch.Tensor, W: torch.Tensor, sx: torch.Tensor, sw:
     return y
 
 
-def _heads(x, weight, rope: Optional[Rope], out, name, dy=None, dweight=None):
-    """(a packed tasq_heads, out): out is allocated when None."""
-    shape = x.shape
+def _rope(rope: Optional[Rope], B: int, S: int):
+    """(addresses of cos, sin and positions, rows of the tables, rotated elements)"""
+    if rope is None:
+        return 0, 0, 0, 0, 0
+    cos, sin, position = rope
+    shape = cos.shape
+    positions, half = shape
+    return (_at(cos, torch.float32, shape, "cos"), _at(sin, torch.float32, shape, "sin"),
+            _at(position, torch.int32, (B, S), "positions"), positions, 2 * half)
+
+
+def _heads(x, weight, rope: Optional[Rope], out, name, dy=None, dweight=None, like=None):
+    """(a packed tasq_heads, out, what `rope` gave): out is allocated when None.
+    like: (rope, its batch and tokens, what it gave) of the tensor before, which
+    mostly shares them."""
+    dtype, shape = x.dtype, x.shape
     if len(shape) != 4:
         raise ValueError(f"{name} must be [batch, tokens, heads, dim]")
     B, S, H, D = shape
-    st = _strided(x, x.dtype, shape, name)
+    st = _strided(x, dtype, shape, name)
     if out is None:
         out = _like(x)
     else:
-        _need(out, x.dtype, shape, f"output of {name}")
-    cos_at = sin_at = position_at = positions = rot = 0
-    if rope is not None:
-        cos, sin, position = rope
-        positions, half = cos.shape
-        cos_at = _at(cos, torch.float32, (positions, half), "cos")
-        sin_at = _at(sin, torch.float32, (positions, half), "sin")
-        position_at = _at(position, torch.int32, (B, S), "positions")
-        rot = 2 * half
+        _need(out, dtype, shape, f"output of {name}")
+    if like is not None and like[0] is rope and like[1] == (B, S):
+        turn = like[2]
+    else:
+        turn = _rope(rope, B, S)
     gat, gst, dwat = 0, (0, 0, 0, 0), 0
     if dy is not None:
-        gst = _strided(dy, x.dtype, shape, f"gradient of {name}")
+        gst = _strided(dy, dtype, shape, f"gradient of {name}")
         gat, dwat = dy.data_ptr(), 0 if dweight is None else dweight.data_ptr()
     return _HEADS.pack(x.data_ptr(), gat, out.data_ptr(),
-                       _at(weight, torch.float32, (D,), f"weight of {name}"), dwat, cos_at,
-                       sin_at, position_at, st[0], st[1], st[2], gst[0], gst[1], gst[2], B, S, H,
-                       positions, rot), out
+                       _at(weight, torch.float32, (D,), f"weight of {name}"), dwat, turn[0],
+                       turn[1], turn[2], st[0], st[1], st[2], gst[0], gst[1], gst[2], B, S, H,
+                       turn[3], turn[4]), out, (rope, (B, S), turn)
 
 
 def _same_heads(q, k):
@@ -168,11 +177,11 @@ def qk_norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torc
     one type, any strides: root-mean-square norm of every head with weight
     [D], then the rotation of its first elements by rope = (cos, sin,
     positions).  Pairs lie rot/2 apart, or side by side with interleaved."""
-    jobs, out_q = _heads(q, wq, rope_q, out_q, "q")
+    jobs, out_q, turn = _heads(q, wq, rope_q, out_q, "q")
     n = 1
     if k is not None:
         _same_heads(q, k)
-        more, out_k = _heads(k, wk, rope_k, out_k, "k")
+        more, out_k, _ = _heads(k, wk, rope_k, out_k, "k", like=turn)
         jobs, n = jobs + more, 2
     rc = _lib.lib().tasq_norm_rotate(jobs, n, _type(q, "q"), q.shape[3], eps, interleaved,
                                      _stream())
@@ -198,11 +207,11 @@ def qk_norm_rotate_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: tor
     D = q.shape[-1]
     dwq, dwk = (None if w is None else torch.empty(D, dtype=torch.float32, device=q.device)
                 for w in (wq, wk))
-    jobs, gq = _heads(q, wq, rope_q, None, "q", dq, dwq)
+    jobs, gq, turn = _heads(q, wq, rope_q, None, "q", dq, dwq)
     n, gk = 1, None
     if k is not None:
         _same_heads(q, k)
-        more, gk = _heads(k, wk, rope_k, None, "k", dk, dwk)
+        more, gk, _ = _heads(k, wk, rope_k, None, "k", dk, dwk, turn)
         jobs, n = jobs + more, 2
     L = _lib.lib()
     ws = _workspace(workspace, L.tasq_norm_rotate_workspace_bytes(n, D), q.device,
