@@ -200,31 +200,38 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
     Stager<KS> stager;
     stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     float st = 0.0f;
-    auto fetch = [&](int t, int i) {
-        const int g = t / per_head, s0 = (t - g * per_head) * kAttnTile;
+    int g = per_head ? t0 / per_head : 0;       // head and first row of the next tile
+    int s0 = (t0 - g * per_head) * kAttnTile;
+    auto fetch = [&](int i) {
         const int left = a.q_len - s0, head = hk * group + g;
         const uint64_t live = left >= kAttnTile ? ~0ull : (1ull << left) - 1;
         stager.request(from + s0 * stride[1] + head * stride[2], live, lds[i]);
         if (wave < 2) {         // wave 0 has the rows' lse, wave 1 their delta
             const float *p = wave == 0 ? a.lse : a.delta;
-            st = lane < left ? p[((size_t)b * a.heads + head) * a.q_len + s0 + lane]
-                             : -__builtin_huge_valf();
-            if (wave == 0) {    // rows past the end and rows without keys have P = 0
-                st = st * kLog2e - Range<T>::kShift;
-                if (st == -__builtin_huge_valf())
-                    st = __builtin_huge_valf();
-            } else {
-                st = lane < left ? st * Range<T>::kScore : 0.0f;
-            }
+            st = wave == 0 ? -__builtin_huge_valf() : 0.0f;
+            if (lane < left)
+                st = p[((size_t)b * a.heads + head) * a.q_len + s0 + lane];
+        }
+        s0 += kAttnTile;
+        if (s0 >= a.q_len) {
+            s0 = 0;
+            ++g;
         }
     };
+    // The rows' statistics are looked at here, when they have arrived, and not
+    // where they are requested (4096 tokens among themselves, 16 heads of 64: two of
+    // four waves waited 800 of 4100 cycles a tile there).
     auto put = [&](int i) {
         stager.wait();
-        if (wave < 2)
-            stat[i][wave][lane] = st;
+        if (wave == 0) {        // rows past the end and rows without keys have P = 0
+            const float l = st * kLog2e - Range<T>::kShift;
+            stat[i][0][lane] = l == -__builtin_huge_valf() ? __builtin_huge_valf() : l;
+        } else if (wave == 1) {
+            stat[i][1][lane] = st * Range<T>::kScore;
+        }
     };
     if (t0 < t1) {
-        fetch(t0, 0);
+        fetch(0);
         put(0);
         __syncthreads();
     }
@@ -232,7 +239,7 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
         const int cur = (t - t0) & 1;
         const char *qt = lds[cur], *gt = qt + SIZE;
         if (t + 1 < t1)
-            fetch(t + 1, cur ^ 1);
+            fetch(cur ^ 1);
         if (busy) {
 #pragma unroll
             for (int rb = 0; rb < 2; ++rb) {
