@@ -1,8 +1,7 @@
 // Attention, forward: O = softmax(scale Q K^T) V and its log-sum-exp, one pass
-// over the keys with a running maximum and sum (the statistics, S and O in
-// fp32; P is rounded to the inputs' type for the second product, as V is of
-// that type, after the running maximum has been taken off, so that its
-// largest value is 1).
+// over the keys with a running base and sum (the statistics, S and O in fp32; P
+// is rounded to the inputs' type for the second product, as V is of that type;
+// the sum takes the weights before that rounding).
 //
 // A workgroup of four waves has QB * 128 rows of one key head: (query head of
 // the group, query) pairs, so that query heads which share keys share their
@@ -10,6 +9,15 @@
 // two LDS buffers, the next tile in flight while one is worked on.  With few rows the
 // keys are cut into ranges, one workgroup each, whose partial results
 // k_attn_join brings together.
+//
+// Bound by the products and the weights' vector instructions (a fused
+// multiply-add, an exponential, an addition and half a conversion each), which
+// take about as long, hardly overlap between the waves of a SIMD, and together
+// leave it idle for 7% of the time at the 2.1 GHz that the power allows: 4096
+// tokens among themselves, batch 2, 16 heads of 72 in bfloat16 (155 GFLOP) 182 us,
+// 0.85 PFLOP/s, 8 heads of 128 137 us, 1.0; over texts of up to 300 words 21.6.
+// One query over 8191 keys, 4 key heads of 128, batch 2 (a stream of 34 MB): 10.5
+// and 3.6 for the join.
 #pragma once
 
 #include "attn.h"

