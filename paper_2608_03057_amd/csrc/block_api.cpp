@@ -99,22 +99,29 @@ int norm_rotate(const tasq_heads *jobs, int n, int type, int dim, float eps, int
                                            static_cast<hipStream_t>(stream)));
 }
 
-// Ranges that `tiles` streamed tiles are cut into when `base` workgroups would
-// run uncut: two workgroups to each compute unit (one in a forward pass that
-// already takes many ranges), at least four tiles each, and none where there
-// are enough workgroups for the parts, written in fp32 and read again, to cost
-// more.  Microseconds uncut and cut: forward, heads of 72 over 4096 keys, base
-// 32 64.8 and 20.4 (8 ranges), 64 65.3 and 27.7, 128 65.7 and 38.0, 192 66.4 and
-// 53.0 (2), 320 76 and 97; one query over 8191 keys of 128, base 8, 162 and 16
-// (32).  dK and dV, base 20 112 and 40 (8), 32 599 and 96 (16), 96 160 and 82
-// (5), 160 48.5 and 56 (2).
-void plan_ranges(long long base, int tiles, bool backward, int *ranges, int *range_tiles)
+enum Pass { kForward, kQueryGrad, kKeyGrad };
+
+// Ranges that `tiles` streamed tiles of a pass are cut into when `base` workgroups
+// would run uncut: two workgroups to each compute unit (one in a forward pass
+// that already takes many ranges), at least four tiles each, and none where
+// there are enough workgroups for the parts, written in fp32 and read again, to
+// cost more: above 256, and for a gradient above 128 unless the tiles are many.
+// Microseconds uncut and cut: forward, heads of 72 over 4096 keys, base 32 64.8
+// and 20.4 (8 ranges), 64 65.3 and 27.7, 128 65.7 and 38.0, 192 66.4 and 53.0 (2),
+// 320 76 and 97; one query over 8191 keys of 128, base 8, 162 and 16 (32).  Both
+// gradients with dK and dV cut, 4096 queries, heads of 72: base 96 156 and 80 (5),
+// 128 166 and 105 (4), 160 174 and 125 (3), 256 199 and 177 (2), 320 230 and 246
+// (2); 1024 queries, base 192 55.7 and 58.3, of 128 107 and 92; 2048, of 64 77.4
+// and 70.9.  With dQ cut: base 160, heads of 72 over 4096 keys 151 and 122, over
+// 2048 79.9 and 70.7, over 1024 49.3 and 52.4, of 128 over 1024 86.9 and 88.7.
+void plan_ranges(long long base, int tiles, int dim, Pass pass, int *ranges, int *range_tiles)
 {
     *ranges = 1;
     *range_tiles = tiles > 0 ? tiles : 1;
-    if (base <= 0 || base > (backward ? 128 : 256) || tiles < 8)
+    const long long many = pass == kQueryGrad ? 2304 : pass == kKeyGrad ? 2048 : 0;
+    if (base <= 0 || tiles < 8 || base > ((long long)tiles * dim >= many ? 256 : 128))
         return;
-    const long long want = (base < 48 && !backward ? 256 : 512) / base;
+    const long long want = (base < 48 && pass == kForward ? 256 : 512) / base;
     const int most = tiles / 4;
     const int r = want < most ? (int)want : most;
     *range_tiles = (tiles + r - 1) / r;
@@ -139,7 +146,8 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
                        ? 2
                        : 1;
     c.row_tiles = (int)((pair_rows + 128 * c.row_blocks - 1) / (128 * c.row_blocks));
-    plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, backward, &c.splits, &c.split_tiles);
+    plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, c.dim,
+                backward ? kQueryGrad : kForward, &c.splits, &c.split_tiles);
     const size_t rows = (size_t)c.batch * c.heads * c.q_len;
     size_t bytes = 0;
     if (c.splits > 1) {
@@ -148,7 +156,7 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
     }
     if (backward) {
         c.key_tiles = (c.kv_len + 127) / 128;
-        plan_ranges(cut ? pairs * c.key_tiles : 0, group * ((c.q_len + 63) / 64), true,
+        plan_ranges(cut ? pairs * c.key_tiles : 0, group * ((c.q_len + 63) / 64), c.dim, kKeyGrad,
                     &c.kv_splits, &c.kv_split_tiles);
         bytes += round256(rows * sizeof(float));
         if (c.kv_splits > 1)
