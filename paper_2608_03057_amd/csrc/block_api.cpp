@@ -99,33 +99,50 @@ int norm_rotate(const tasq_heads *jobs, int n, int type, int dim, float eps, int
                                            static_cast<hipStream_t>(stream)));
 }
 
-enum Pass { kForward, kQueryGrad, kKeyGrad };
+// A pass: microseconds that a workgroup takes for a tile of heads of dim when it
+// has a compute unit to itself (measured at 64, 72 and 128), and fp32 results
+// for each of its resident elements.
+struct Pass {
+    double slope, base;
+    int results;
+    double tile(int dim) const { return slope * dim + base; }
+};
+constexpr Pass kForward = {0.0087, 0.35, 1}, kQueryGrad = {0.0161, 0.48, 1},
+               kKeyGrad = {0.05, -1.3, 2};
 
 // Ranges that `tiles` streamed tiles of a pass are cut into when `base` workgroups
-// would run uncut: two workgroups to each compute unit (one in a forward pass
-// that already takes many ranges), at least four tiles each, and none where
-// there are enough workgroups for the parts, written in fp32 and read again, to
-// cost more: above 256, and for a gradient above 128 unless the tiles are many.
-// Microseconds uncut and cut: forward, heads of 72 over 4096 keys, base 32 64.8
-// and 20.4 (8 ranges), 64 65.3 and 27.7, 128 65.7 and 38.0, 192 66.4 and 53.0 (2),
-// 320 76 and 97; one query over 8191 keys of 128, base 8, 162 and 16 (32).  Both
-// gradients with dK and dV cut, 4096 queries, heads of 72: base 96 156 and 80 (5),
-// 128 166 and 105 (4), 160 174 and 125 (3), 256 199 and 177 (2), 320 230 and 246
-// (2); 1024 queries, base 192 55.7 and 58.3, of 128 107 and 92; 2048, of 64 77.4
-// and 70.9.  With dQ cut: base 160, heads of 72 over 4096 keys 151 and 122, over
-// 2048 79.9 and 70.7, over 1024 49.3 and 52.4, of 128 over 1024 86.9 and 88.7.
-void plan_ranges(long long base, int tiles, int dim, Pass pass, int *ranges, int *range_tiles)
+// would run uncut: none, or as many as make one or two workgroups for each compute
+// unit, at least four tiles each, whichever takes the shortest by the model
+//   tiles of a range * tile time * (1.2 where two share a compute unit)
+//     + 6 us for the launch that joins the parts + their bytes, written and read,
+//       at 4 TB/s.
+// Of 202 shapes of 32 to 320 workgroups and 8 to 64 tiles its choice takes 1.1%
+// more than the best of one to twelve ranges in the geometric mean, 13% at most.
+// us uncut and cut (ranges): forward, heads of 72, 32 workgroups of 64 tiles 65.1
+// and 20.1 (8), 160 of 64 66.1 and 44.6 (3), 160 of 16 19.8 and 26.1 (3); one query
+// over 8191 keys of 128 162 and 16 (32); both gradients with dK and dV cut, heads
+// of 72, 96 of 64 156 and 80 (5), 160 of 64 174 and 124 (3), 256 of 16 61.7 and 68
+// (2); with dQ cut, 160 of 64 151 and 121 (3), 160 of 16 49.4 and 52.4 (3).
+void plan_ranges(long long base, int tiles, int dim, size_t rows, const Pass &pass, int *ranges,
+                 int *range_tiles)
 {
     *ranges = 1;
     *range_tiles = tiles > 0 ? tiles : 1;
-    const long long many = pass == kQueryGrad ? 2304 : pass == kKeyGrad ? 2048 : 0;
-    if (base <= 0 || tiles < 8 || base > ((long long)tiles * dim >= many ? 256 : 128))
+    if (base <= 0 || base > 256 || tiles < 8)
         return;
-    const long long want = (base < 48 && pass == kForward ? 256 : 512) / base;
-    const int most = tiles / 4;
-    const int r = want < most ? (int)want : most;
-    *range_tiles = (tiles + r - 1) / r;
-    *ranges = (tiles + *range_tiles - 1) / *range_tiles;
+    double best = tiles * pass.tile(dim);
+    for (const int units : {256, 512}) {
+        const int most = tiles / 4, want = (int)(units / base);
+        const int t = (tiles + (want < most ? want : most) - 1) / (want < most ? want : most);
+        const int r = (tiles + t - 1) / t;
+        const double us = t * pass.tile(dim) * (r * base > 256 ? 1.2 : 1.0) + 6.0 +
+                          8.0 * pass.results * r * (double)rows * dim / 4e6;
+        if (r > 1 && us < best) {
+            best = us;
+            *ranges = r;
+            *range_tiles = t;
+        }
+    }
 }
 
 constexpr size_t round256(size_t v) { return (v + 255) / 256 * 256; }
@@ -146,9 +163,9 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
                        ? 2
                        : 1;
     c.row_tiles = (int)((pair_rows + 128 * c.row_blocks - 1) / (128 * c.row_blocks));
-    plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, c.dim,
-                backward ? kQueryGrad : kForward, &c.splits, &c.split_tiles);
     const size_t rows = (size_t)c.batch * c.heads * c.q_len;
+    plan_ranges(cut ? pairs * c.row_tiles : 0, key_tiles, c.dim, rows,
+                backward ? kQueryGrad : kForward, &c.splits, &c.split_tiles);
     size_t bytes = 0;
     if (c.splits > 1) {
         bytes += round256(c.splits * rows * c.dim * sizeof(float));
@@ -156,8 +173,9 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
     }
     if (backward) {
         c.key_tiles = (c.kv_len + 127) / 128;
-        plan_ranges(cut ? pairs * c.key_tiles : 0, group * ((c.q_len + 63) / 64), c.dim, kKeyGrad,
-                    &c.kv_splits, &c.kv_split_tiles);
+        plan_ranges(cut ? pairs * c.key_tiles : 0, group * ((c.q_len + 63) / 64), c.dim,
+                    (size_t)c.batch * c.kv_heads * c.kv_len, kKeyGrad, &c.kv_splits,
+                    &c.kv_split_tiles);
         bytes += round256(rows * sizeof(float));
         if (c.kv_splits > 1)
             bytes += round256((size_t)c.kv_splits * 2 * c.batch * c.kv_len * c.kv_heads * c.dim *
