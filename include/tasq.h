@@ -604,8 +604,6 @@ enum { TASQ_TYPE_F32 = 0, TASQ_TYPE_BF16 = 1, TASQ_TYPE_F16 = 2 };
  * 1/127; a correctly rounded division, then ties to even), codes in
  * [-127, 127]; a token whose scale is zero has codes 0.
  *   x         [M][K] of x_type, row m at x + m * x_stride; finite values.
- *             K % 8 == 0 with rows and X_out aligned to 16 and 8 bytes
- *             takes vector loads, any other layout element loads.
  *   X_out     int8 [M][K]; sx_out fp32 [M] (4-byte aligned).
  * M == 0 enqueues nothing; K == 0 writes sx = 0.  Errors: TASQ_ERR_NULL,
  * _DIM (a negative size, M > 2^30, x_stride < K), _OVERFLOW (K >
