@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(256) k_norm_rotate_any(HeadCall call, float *p
 // its sum goes to part[job][workgroup][dim], which k_sum_dweight adds up in
 // order.  (No atomics: their order would change dw from run to run.)
 template <class T, bool INTERLEAVED, int LPR>
-__global__ void __launch_bounds__(256) k_norm_rotate_backward(HeadCall call, float *part)
+__global__ void __launch_bounds__(256, 4) k_norm_rotate_backward(HeadCall call, float *part)
 {
     constexpr int GROUPS = 256 / LPR;
     const int l = threadIdx.x % LPR, group = threadIdx.x / LPR;
