@@ -660,8 +660,7 @@ typedef struct tasq_heads {
  *   jobs  host array of n tensors (0..TASQ_MAX_NORM_JOBS), queries and keys,
  *         in one launch; read during the call only.
  *   type  of x, dy and out; dim even, 2..TASQ_MAX_NORM_DIM; eps >= 0.
- * dim and rot multiples of 8 with 16-byte aligned tensors and strides (8-byte
- * where pairs are rot/2 apart and the type has 16 bits) take vector loads.
+ * dim a multiple of 8 takes vector loads, at any alignment.
  * A tensor without elements enqueues nothing.  Errors: TASQ_ERR_NULL (x, out,
  * or cos and sin with rot > 0), _DIM (a size, a stride, rot), _RANGE (n, eps),
  * _KIND, _ALIGN (a pointer not aligned to its elements), _HIP.

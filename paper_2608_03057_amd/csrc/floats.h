@@ -30,6 +30,37 @@ template <class T> __device__ __forceinline__ f32x2 unpack2(uint32_t u)
     return __builtin_convertvector(__builtin_bit_cast(typename Pair<T>::type, u), f32x2);
 }
 
+// N consecutive elements as they lie in memory, at the alignment of one: a load
+// or store takes the same instructions as an aligned one.
+template <class T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Packed {
+    static constexpr int kWords = N * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+
+    __device__ __forceinline__ void floats(float (&v)[N]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                v[i] = __uint_as_float(w[i]);
+            } else {
+                const f32x2 f = unpack2<T>(w[i]);
+                v[2 * i] = f.x;
+                v[2 * i + 1] = f.y;
+            }
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[N])
+    {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            if constexpr (sizeof(T) == 4)
+                w[i] = __float_as_uint(v[i]);
+            else
+                w[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+        }
+    }
+};
+
 // N consecutive elements as floats: N * sizeof(T) bytes in loads of up to 16
 // bytes, p aligned to the smaller of 16 and that size.
 template <class T, int N> __device__ __forceinline__ void load_vec(const T *p, float (&v)[N])

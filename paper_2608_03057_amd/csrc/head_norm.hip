@@ -51,37 +51,81 @@ __device__ __forceinline__ int position_of(const HeadJob &j, const Unit &u)
     return j.rot && (unsigned)p < (unsigned)j.positions ? p : -1;
 }
 
-// Lane l's eight elements of a head as pairs (x1[i], x2[i]), i < 4.
-template <class T, bool INTERLEAVED> struct Pairs {
-    int o1, o2;                 // interleaved: o1 alone, eight elements from it
+// Lane l's eight elements of a head as pairs (x1[i], x2[i]), i < 4: pairs 4 l .. of
+// the rotated ones and, behind them, of neighbours that nothing turns.
+// (kSplit: as kHalves, where a lane has pairs of both kinds, R / 2 not a multiple of
+// four; the lanes that do take their elements one by one.  8192 tokens, 32 heads of
+// 72 of which 36 rotate, in bfloat16 29 us a call and 48 backward, against 60 and
+// 104 of a wave to each head; 17.4 and 30.7 where all 72 rotate.)
+enum Form { kHalves, kInterleaved, kSplit };
 
-    __device__ __forceinline__ void init(int l, int rot, int dim)
+template <Form FORM> struct Pairs {
+    static constexpr bool INTERLEAVED = FORM == kInterleaved;
+    int o1, o2;                 // first elements of x1 and x2 (interleaved: o1 alone)
+    int turned;                 // of the four pairs, those that rotate
+    int rot;
+    bool mixed;                 // some of the four rotate and some do not
+
+    template <class P> struct Raw {
+        Packed<P, 4> a, b;
+    };
+
+    __device__ __forceinline__ void init(int l, int rot_)
     {
-        if constexpr (INTERLEAVED) {
-            o1 = 8 * l;
-            o2 = o1 + 4;
-        } else if (8 * l < rot) {
-            o1 = 4 * l;
-            o2 = rot / 2 + 4 * l;
-        } else {
-            o1 = rot + 4 * l - rot / 2;
-            o2 = o1 + (dim - rot) / 2;
+        rot = rot_;
+        turned = min(max(rot / 2 - 4 * l, 0), 4);
+        mixed = FORM == kSplit && (turned & 3) != 0;
+        o1 = INTERLEAVED || turned == 0 ? 8 * l : 4 * l;
+        o2 = INTERLEAVED || turned == 0 ? o1 + 4 : o1 + rot / 2;
+    }
+    // Element of x1[i] (second: of x2[i]).
+    __device__ __forceinline__ int element(int i, bool second) const
+    {
+        if (INTERLEAVED)
+            return o1 + 2 * i + second;
+        if (mixed && i >= turned)
+            return rot + 2 * (i - turned) + second;
+        return (second ? o2 : o1) + i;
+    }
+    template <class P> __device__ __forceinline__ Raw<P> fetch(const P *p) const
+    {
+        if (!mixed) {
+            if constexpr (INTERLEAVED)
+                return *reinterpret_cast<const Raw<P> *>(p + o1);
+            else
+                return {*reinterpret_cast<const Packed<P, 4> *>(p + o1),
+                        *reinterpret_cast<const Packed<P, 4> *>(p + o2)};
         }
+        P e[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e[i] = p[element(i, false)];
+            e[4 + i] = p[element(i, true)];
+        }
+        return __builtin_bit_cast(Raw<P>, e);
     }
     template <class P>
-    __device__ __forceinline__ void load(const P *p, float (&x1)[4], float (&x2)[4]) const
+    static __device__ __forceinline__ void pairs(Raw<P> r, float (&x1)[4], float (&x2)[4])
     {
+        // Here, and not for all heads at once, which takes twice the registers.
+#pragma unroll
+        for (int i = 0; i < Packed<P, 4>::kWords; ++i) {
+            uint32_t u = r.a.w[i], v = r.b.w[i];
+            asm volatile("" : "+v"(u), "+v"(v));
+            r.a.w[i] = u;
+            r.b.w[i] = v;
+        }
         if constexpr (INTERLEAVED) {
             float e[8];
-            load_vec(p + o1, e);
+            __builtin_bit_cast(Packed<P, 8>, r).floats(e);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 x1[i] = e[2 * i];
                 x2[i] = e[2 * i + 1];
             }
         } else {
-            load_vec(p + o1, x1);
-            load_vec(p + o2, x2);
+            r.a.floats(x1);
+            r.b.floats(x2);
         }
     }
     template <class P>
@@ -94,11 +138,25 @@ template <class T, bool INTERLEAVED> struct Pairs {
                 e[2 * i] = x1[i];
                 e[2 * i + 1] = x2[i];
             }
-            store_vec(p + o1, e);
+            reinterpret_cast<Packed<P, 8> *>(p + o1)->set(e);
+        } else if (!mixed) {
+            reinterpret_cast<Packed<P, 4> *>(p + o1)->set(x1);
+            reinterpret_cast<Packed<P, 4> *>(p + o2)->set(x2);
         } else {
-            store_vec(p + o1, x1);
-            store_vec(p + o2, x2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[element(i, false)] = (P)x1[i];
+                p[element(i, true)] = (P)x2[i];
+            }
         }
+    }
+    __device__ __forceinline__ void weights(const float *w, float (&w1)[4], float (&w2)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w1[i] = w2[i] = 1.0f;
+        if (w)
+            pairs(fetch(w), w1, w2);
     }
 };
 
@@ -108,23 +166,26 @@ template <int LPR> __device__ __forceinline__ float group_sum(float v)
     return group_reduce<LPR>(v, [](float a, float b) { return a + b; });
 }
 
-__device__ __forceinline__ void cos_sin(const HeadJob &j, int p, int l, float (&c)[4],
+// Cosines and sines of lane l's pairs at row p of the tables, of which `turned`
+// rotate.
+__device__ __forceinline__ void cos_sin(const HeadJob &j, int p, int l, int turned, float (&c)[4],
                                         float (&s)[4])
 {
-    if (p >= 0 && 8 * l < j.rot) {
-        const size_t at = (size_t)p * (j.rot / 2) + 4 * l;
-        load_vec(j.cos + at, c);
-        load_vec(j.sin + at, s);
+    const size_t at = (size_t)p * (j.rot / 2) + 4 * l;
+    if (p >= 0 && turned == 4) {
+        reinterpret_cast<const Packed<float, 4> *>(j.cos + at)->floats(c);
+        reinterpret_cast<const Packed<float, 4> *>(j.sin + at)->floats(s);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            c[i] = 1.0f;
-            s[i] = 0.0f;
+            const bool turn = p >= 0 && i < turned;
+            c[i] = turn ? j.cos[at + i] : 1.0f;
+            s[i] = turn ? j.sin[at + i] : 0.0f;
         }
     }
 }
 
-template <class T, bool INTERLEAVED, int LPR>
+template <class T, Form FORM, int LPR>
 __global__ void __launch_bounds__(256) k_norm_rotate(HeadCall call)
 {
     constexpr int GROUPS = 256 / LPR;
@@ -138,41 +199,32 @@ __global__ void __launch_bounds__(256) k_norm_rotate(HeadCall call)
     const int l = threadIdx.x % LPR;
     const Unit un = unit_of(j, (unsigned)u);
     const bool live = 8 * l < call.dim;
-    Pairs<T, INTERLEAVED> at;
-    at.init(live ? l : 0, j.rot, call.dim);
+    Pairs<FORM> at;
+    at.init(live ? l : 0, j.rot);
     const T *x = static_cast<const T *>(j.x) + un.b * j.x_stride[0] + un.s * j.x_stride[1];
-    float x1[kHeads][4], x2[kHeads][4];
+    typename Pairs<FORM>::template Raw<T> raw[kHeads];
 #pragma unroll
     for (int k = 0; k < kHeads; ++k) {
-        if (live && un.h + k < j.heads) {
-            at.load(x + (un.h + k) * j.x_stride[2], x1[k], x2[k]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                x1[k][i] = x2[k][i] = 0.0f;
-        }
+        raw[k] = {};
+        if (live && un.h + k < j.heads)
+            raw[k] = at.fetch(x + (un.h + k) * j.x_stride[2]);
     }
     float c[4], s[4], w1[4], w2[4];
-    cos_sin(j, position_of(j, un), live ? l : 0, c, s);
-    if (j.weight) {
-        at.load(j.weight, w1, w2);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w1[i] = w2[i] = 1.0f;
-    }
+    cos_sin(j, position_of(j, un), live ? l : 0, at.turned, c, s);
+    at.weights(j.weight, w1, w2);
     T *y = static_cast<T *>(j.out) + (size_t)un.token * j.heads * call.dim;
 #pragma unroll
     for (int k = 0; k < kHeads; ++k) {
-        float sum = 0.0f;
+        float sum = 0.0f, x1[4], x2[4];
+        at.pairs(raw[k], x1, x2);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            sum += x1[k][i] * x1[k][i] + x2[k][i] * x2[k][i];
+            sum += x1[i] * x1[i] + x2[i] * x2[i];
         const float r = rsqrtf(group_sum<LPR>(sum) * call.inv_dim + call.eps);
         float y1[4], y2[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float n1 = x1[k][i] * r * w1[i], n2 = x2[k][i] * r * w2[i];
+            const float n1 = x1[i] * r * w1[i], n2 = x2[i] * r * w2[i];
             y1[i] = n1 * c[i] - n2 * s[i];
             y2[i] = n1 * s[i] + n2 * c[i];
         }
@@ -181,8 +233,8 @@ __global__ void __launch_bounds__(256) k_norm_rotate(HeadCall call)
     }
 }
 
-// Any even head dimension, rotation, alignment and stride: one wave per head,
-// pairs p, p + 64, .. of lane p.  The gradient's dw meets in `part` as below.
+// Head dimensions that are not a multiple of eight: one wave per head, pairs p,
+// p + 64, .. of lane p.  The gradient's dw meets in `part` as below.
 template <class T, bool GRAD>
 __global__ void __launch_bounds__(256) k_norm_rotate_any(HeadCall call, float *part)
 {
@@ -288,8 +340,9 @@ __global__ void __launch_bounds__(256) k_norm_rotate_any(HeadCall call, float *p
 // keeps its part of dw in registers, the workgroup's parts meet in LDS and
 // its sum goes to part[job][workgroup][dim], which k_sum_dweight adds up in
 // order.  (No atomics: their order would change dw from run to run.)
-template <class T, bool INTERLEAVED, int LPR>
-__global__ void __launch_bounds__(256, 4) k_norm_rotate_backward(HeadCall call, float *part)
+template <class T, Form FORM, int LPR>
+__global__ void __launch_bounds__(256, FORM == kSplit && sizeof(T) == 4 ? 3 : 4)
+    k_norm_rotate_backward(HeadCall call, float *part)
 {
     constexpr int GROUPS = 256 / LPR;
     const int l = threadIdx.x % LPR, group = threadIdx.x / LPR;
@@ -297,55 +350,48 @@ __global__ void __launch_bounds__(256, 4) k_norm_rotate_backward(HeadCall call, 
     __shared__ float sum[GROUPS][8 * LPR + 1];
     for (int job = 0; job < call.n; ++job) {
         const HeadJob &j = call.job[job];
-        Pairs<T, INTERLEAVED> at;
-        at.init(live ? l : 0, j.rot, call.dim);
+        Pairs<FORM> at;
+        at.init(live ? l : 0, j.rot);
         float w1[4], w2[4], dw1[4] = {}, dw2[4] = {};
-        if (j.weight) {
-            at.load(j.weight, w1, w2);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                w1[i] = w2[i] = 1.0f;
-        }
+        at.weights(j.weight, w1, w2);
         for (int u = blockIdx.x * GROUPS + group; u < j.units; u += gridDim.x * GROUPS) {
             const Unit un = unit_of(j, (unsigned)u);
             const T *x =
                 static_cast<const T *>(j.x) + un.b * j.x_stride[0] + un.s * j.x_stride[1];
             const T *dy =
                 static_cast<const T *>(j.dy) + un.b * j.dy_stride[0] + un.s * j.dy_stride[1];
-            float x1[kHeads][4], x2[kHeads][4], d1[kHeads][4], d2[kHeads][4];
+            typename Pairs<FORM>::template Raw<T> xs[kHeads], ds[kHeads];
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
+                xs[k] = ds[k] = {};
                 if (live && un.h + k < j.heads) {
-                    at.load(x + (un.h + k) * j.x_stride[2], x1[k], x2[k]);
-                    at.load(dy + (un.h + k) * j.dy_stride[2], d1[k], d2[k]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        x1[k][i] = x2[k][i] = d1[k][i] = d2[k][i] = 0.0f;
+                    xs[k] = at.fetch(x + (un.h + k) * j.x_stride[2]);
+                    ds[k] = at.fetch(dy + (un.h + k) * j.dy_stride[2]);
                 }
             }
             float c[4], s[4];
-            cos_sin(j, position_of(j, un), live ? l : 0, c, s);
+            cos_sin(j, position_of(j, un), live ? l : 0, at.turned, c, s);
             T *dx = static_cast<T *>(j.out) + (size_t)un.token * j.heads * call.dim;
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
-                float sq = 0.0f, inner = 0.0f, g1[4], g2[4];
+                float sq = 0.0f, inner = 0.0f, g1[4], g2[4], x1[4], x2[4], d1[4], d2[4];
+                at.pairs(xs[k], x1, x2);
+                at.pairs(ds[k], d1, d2);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    g1[i] = d1[k][i] * c[i] + d2[k][i] * s[i];
-                    g2[i] = d2[k][i] * c[i] - d1[k][i] * s[i];
-                    sq += x1[k][i] * x1[k][i] + x2[k][i] * x2[k][i];
-                    inner += g1[i] * w1[i] * x1[k][i] + g2[i] * w2[i] * x2[k][i];
+                    g1[i] = d1[i] * c[i] + d2[i] * s[i];
+                    g2[i] = d2[i] * c[i] - d1[i] * s[i];
+                    sq += x1[i] * x1[i] + x2[i] * x2[i];
+                    inner += g1[i] * w1[i] * x1[i] + g2[i] * w2[i] * x2[i];
                 }
                 const float r = rsqrtf(group_sum<LPR>(sq) * call.inv_dim + call.eps);
                 const float t = group_sum<LPR>(inner) * call.inv_dim * r * r;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    dw1[i] += g1[i] * x1[k][i] * r;
-                    dw2[i] += g2[i] * x2[k][i] * r;
-                    g1[i] = r * (g1[i] * w1[i] - x1[k][i] * t);
-                    g2[i] = r * (g2[i] * w2[i] - x2[k][i] * t);
+                    dw1[i] += g1[i] * x1[i] * r;
+                    dw2[i] += g2[i] * x2[i] * r;
+                    g1[i] = r * (g1[i] * w1[i] - x1[i] * t);
+                    g2[i] = r * (g2[i] * w2[i] - x2[i] * t);
                 }
                 if (live && un.h + k < j.heads)
                     at.store(dx + (size_t)(un.h + k) * call.dim, g1, g2);
@@ -355,8 +401,8 @@ __global__ void __launch_bounds__(256, 4) k_norm_rotate_backward(HeadCall call, 
         if (live) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                sum[group][INTERLEAVED ? at.o1 + 2 * i : at.o1 + i] = dw1[i];
-                sum[group][INTERLEAVED ? at.o1 + 2 * i + 1 : at.o2 + i] = dw2[i];
+                sum[group][at.element(i, false)] = dw1[i];
+                sum[group][at.element(i, true)] = dw2[i];
             }
         }
         __syncthreads();
@@ -394,29 +440,6 @@ __global__ void __launch_bounds__(256) k_sum_dweight(HeadCall call, const float 
     }
 }
 
-bool fits(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
-
-// Whether the kernels with eight elements to a lane take the call: whole
-// lanes of pairs, and every load of a head aligned to its own size.
-bool vectors(const HeadCall &c, bool grad)
-{
-    const int es = c.type == TASQ_TYPE_F32 ? 4 : 2;
-    for (int i = 0; i < c.n; ++i) {
-        const HeadJob &j = c.job[i];
-        const size_t load = es == 4 || c.interleaved ? 16 : 8;
-        const int step = (int)load / es;
-        if (c.dim % 8 || j.rot % 8 || !fits(j.x, load) || !fits(j.out, load) ||
-            !fits(j.weight, 16) || (j.rot && (!fits(j.cos, 16) || !fits(j.sin, 16))))
-            return false;
-        for (int k = 0; k < 3; ++k)
-            if (j.x_stride[k] % step || (grad && j.dy_stride[k] % step))
-                return false;
-        if (grad && !fits(j.dy, load))
-            return false;
-    }
-    return true;
-}
-
 // Workgroups of the gradient: enough to fill the GPU, few enough that their
 // partial sums stay small.
 int grad_groups(const HeadCall &c, int units_per_group)
@@ -426,31 +449,31 @@ int grad_groups(const HeadCall &c, int units_per_group)
     return all < kHeadGroups ? all : kHeadGroups;
 }
 
-template <class T, bool INTERLEAVED, int LPR>
+template <class T, Form FORM, int LPR>
 void launch_vectors(const HeadCall &c, bool grad, float *part, int *groups, hipStream_t stream)
 {
     constexpr int GROUPS = 256 / LPR;
     if (grad) {
         *groups = grad_groups(c, GROUPS);
-        k_norm_rotate_backward<T, INTERLEAVED, LPR><<<*groups, 256, 0, stream>>>(c, part);
+        k_norm_rotate_backward<T, FORM, LPR><<<*groups, 256, 0, stream>>>(c, part);
     } else {
         const int blocks = (c.job[0].units + GROUPS - 1) / GROUPS +
                            (c.job[1].units + GROUPS - 1) / GROUPS;
-        k_norm_rotate<T, INTERLEAVED, LPR><<<blocks, 256, 0, stream>>>(c);
+        k_norm_rotate<T, FORM, LPR><<<blocks, 256, 0, stream>>>(c);
     }
 }
 
-template <class T, bool INTERLEAVED>
+template <class T, Form FORM>
 void launch_lanes(const HeadCall &c, bool grad, float *part, int *groups, hipStream_t stream)
 {
     if (c.dim <= 32)
-        launch_vectors<T, INTERLEAVED, 4>(c, grad, part, groups, stream);
+        launch_vectors<T, FORM, 4>(c, grad, part, groups, stream);
     else if (c.dim <= 64)
-        launch_vectors<T, INTERLEAVED, 8>(c, grad, part, groups, stream);
+        launch_vectors<T, FORM, 8>(c, grad, part, groups, stream);
     else if (c.dim <= 128)
-        launch_vectors<T, INTERLEAVED, 16>(c, grad, part, groups, stream);
+        launch_vectors<T, FORM, 16>(c, grad, part, groups, stream);
     else
-        launch_vectors<T, INTERLEAVED, 32>(c, grad, part, groups, stream);
+        launch_vectors<T, FORM, 32>(c, grad, part, groups, stream);
 }
 
 }  // namespace
@@ -473,10 +496,12 @@ hipError_t launch_norm_rotate(const HeadCall &in, bool grad, float *part, hipStr
     int groups = 0;
     hipError_t e = units == 0 ? hipSuccess : with_type(c.type, [&](auto zero) {
         using T = decltype(zero);
-        if (vectors(c, grad) && c.interleaved) {
-            launch_lanes<T, true>(c, grad, part, &groups, stream);
-        } else if (vectors(c, grad)) {
-            launch_lanes<T, false>(c, grad, part, &groups, stream);
+        if (c.dim % 8 == 0 && c.interleaved) {
+            launch_lanes<T, kInterleaved>(c, grad, part, &groups, stream);
+        } else if (c.dim % 8 == 0 && c.job[0].rot % 8 == 0 && c.job[1].rot % 8 == 0) {
+            launch_lanes<T, kHalves>(c, grad, part, &groups, stream);
+        } else if (c.dim % 8 == 0) {
+            launch_lanes<T, kSplit>(c, grad, part, &groups, stream);
         } else {
             groups = grad_groups(c, 4);
             if (grad)

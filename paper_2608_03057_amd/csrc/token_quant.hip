@@ -66,25 +66,6 @@ template <int TPR> __device__ __forceinline__ float row_max(float v)
     return v;
 }
 
-// Eight elements, or eight codes, at the alignment of one: the same single
-// instruction as aligned ones.
-template <class T> struct __attribute__((packed, aligned(sizeof(T)))) Eight {
-    uint32_t w[2 * sizeof(T)];
-    __device__ __forceinline__ void floats(float (&v)[8]) const
-    {
-#pragma unroll
-        for (int i = 0; i < 2 * (int)sizeof(T); ++i) {
-            if constexpr (sizeof(T) == 4) {
-                v[i] = __uint_as_float(w[i]);
-            } else {
-                const f32x2 f = unpack2<T>(w[i]);
-                v[2 * i] = f.x;
-                v[2 * i + 1] = f.y;
-            }
-        }
-    }
-};
-
 // Rows of up to 8 * NV * TPR elements at any alignment and stride; the last K % 8
 // elements of a row are one thread's, one by one.  (8192x1151 bfloat16 8.8 us a
 // call; 15.8 with a read for the maximum and one for the codes, element by element.)
@@ -106,7 +87,7 @@ __global__ void __launch_bounds__(256) k_quantize_tokens(const T *__restrict__ x
     for (int i = 0; i < NV; ++i) {
         const int k = 8 * (t + i * TPR);
         if (k + 8 <= K) {
-            reinterpret_cast<const Eight<T> *>(row + k)->floats(v[i]);
+            reinterpret_cast<const Packed<T, 8> *>(row + k)->floats(v[i]);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -126,7 +107,7 @@ __global__ void __launch_bounds__(256) k_quantize_tokens(const T *__restrict__ x
             continue;
         const uint2 c = ts.codes(v[i]);
         if (k + 8 <= K) {
-            *reinterpret_cast<Eight<int8_t> *>(out + k) = {c.x, c.y};
+            *reinterpret_cast<Packed<int8_t, 8> *>(out + k) = {c.x, c.y};
         } else {
             for (int e = 0; e < K - k; ++e)
                 out[k + e] = (int8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3)));

@@ -235,3 +235,52 @@ def test_refusals_of_the_wrappers():
     with pytest.raises(T.TasqError):
         T.qk_norm_rotate_backward(q, None, q, None,
                                   workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+
+
+# Whole groups of eight elements whose rotated part ends inside a group.
+PART_GROUPS = [
+    (1, 37, 6, 3, 72, 36, False, True), (2, 9, 5, 1, 40, 20, False, False),
+    (2, 9, 5, 1, 40, 20, True, False), (1, 5, 3, 1, 64, 2, False, True),
+    (1, 5, 3, 1, 128, 126, False, True), (1, 3, 2, 2, 256, 250, False, True),
+    (1, 3, 2, 2, 256, 250, True, True), (2, 3, 2, 1, 24, 12, False, False),
+    (3, 70, 9, 4, 104, 52, False, True),
+]
+
+
+@pytest.mark.parametrize("case", PART_GROUPS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_rotation_that_ends_inside_a_group(case, dtype):
+    test_forward(case, dtype)
+    test_backward(case, dtype)
+
+
+def test_one_rotation_ends_inside_a_group_and_one_does_not():
+    g = torch.Generator().manual_seed(8)
+    q = torch.randn(2, 21, 5, 72, generator=g).to(torch.bfloat16).to(DEV)
+    k = torch.randn(2, 21, 3, 72, generator=g).to(torch.bfloat16).to(DEV)
+    ropes = (*tables(21, 72), None), (*tables(21, 36, 1), None)
+    y = T.qk_norm_rotate(q, k, None, None, *ropes)
+    d = T.qk_norm_rotate_backward(q, k, q, k, None, None, *ropes)
+    for i, (x, rope) in enumerate(zip((q, k), ropes)):
+        near(y[i], *forward(x, None, rope, False), 24)
+        near(d[i], *backward(x, x, None, rope, False)[:2], 48)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("inter", [False, True])
+def test_tables_weights_and_outputs_at_any_element(dtype, inter):
+    g = torch.Generator().manual_seed(9)
+
+    def off(t):         # the same values, one element after an aligned base
+        b = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+        b[1:] = t.reshape(-1)
+        return b[1:].view(t.shape)
+    x = torch.randn(2, 11, 3, 64, generator=g).to(dtype).to(DEV)
+    w = torch.randn(64, generator=g).to(DEV)
+    cos, sin = tables(11, 64)
+    rope = (cos, sin, None)
+    want, _ = T.qk_norm_rotate(x, None, w, None, rope, interleaved=inter)
+    out = off(torch.zeros_like(x))
+    got, _ = T.qk_norm_rotate(off(x), None, off(w), None, (off(cos), off(sin), None),
+                              interleaved=inter, out_q=out)
+    assert got.data_ptr() == out.data_ptr() and torch.equal(got, want)
