@@ -14,10 +14,10 @@
 // multiply-add, an exponential, an addition and half a conversion each), which
 // take about as long, hardly overlap between the waves of a SIMD, and together
 // leave it idle for 7% of the time at the 2.1 GHz that the power allows: 4096
-// tokens among themselves, batch 2, 16 heads of 72 in bfloat16 (155 GFLOP) 182 us,
-// 0.85 PFLOP/s, 8 heads of 128 137 us, 1.0; over texts of up to 300 words 21.6.
+// tokens among themselves, batch 2, 16 heads of 72 in bfloat16 (155 GFLOP) 186 us,
+// 0.83 PFLOP/s, 8 heads of 128 137 us, 1.0; over texts of up to 300 words 21.
 // One query over 8191 keys, 4 key heads of 128, batch 2 (a stream of 34 MB): 10.5
-// and 3.6 for the join.
+// and 3.7 for the join.
 #pragma once
 
 #include "attn.h"

@@ -12,8 +12,8 @@
 // is fp32.
 //
 // Bound by memory: x (and dy) are read once, y (dx) is written once.  q and k of
-// 8192 tokens, 16 heads of 72 each in bfloat16: 19.3 us, 3.9 TB/s; the gradient of
-// 4096 tokens, 20 heads of 112 each in half: 27.4 us, 4.0 TB/s, and 3.9 us for the
+// 8192 tokens, 16 heads of 72 each in bfloat16: 16.1 us, 4.7 TB/s; the gradient of
+// 4096 tokens, 20 heads of 112 each in half: 27.1 us, 4.1 TB/s, and 3.9 us for the
 // weights' sums.  A head belongs to a group of lanes of a wave with eight elements
 // each, four pairs that meet the same four frequencies, so the norm's sum is a
 // few lane exchanges and the rotation needs none; a group takes kHeads heads of

@@ -8,7 +8,7 @@
 // One read of x: a row stays in the registers of the threads that loaded it
 // between its maximum and its codes, a wave to a row up to 2048 elements, which
 // needs no barrier, and a workgroup above.  Bound by memory: 8192x1152 bfloat16
-// 9.7 to 11.2 us, 2.5 to 2.9 TB/s of activations and codes.
+// 10.3 to 11.6 us, 2.4 to 2.7 TB/s of activations and codes.
 #include "block_internal.h"
 #include "floats.h"
 #include "quant.h"
