@@ -100,24 +100,24 @@ int norm_rotate(const tasq_heads *jobs, int n, int type, int dim, float eps, int
 }
 
 // A pass: microseconds that a workgroup takes for a tile of heads of dim when it
-// has a compute unit to itself (measured at 64, 72 and 128), and fp32 results
-// for each of its resident elements.
+// has a compute unit to itself (measured at 16 to 128; from 64 on registers run
+// short in dK and dV), and fp32 results for each of its resident elements.
 struct Pass {
-    double slope, base;
+    double slope, base, wide_slope, wide_base;
     int results;
-    double tile(int dim) const { return slope * dim + base; }
+    double tile(int dim) const { return fmax(slope * dim + base, wide_slope * dim + wide_base); }
 };
-constexpr Pass kForward = {0.0087, 0.35, 1}, kQueryGrad = {0.0161, 0.48, 1},
-               kKeyGrad = {0.05, -1.3, 2};
+constexpr Pass kForward = {0.0087, 0.35, 0, 0, 1}, kQueryGrad = {0.0161, 0.48, 0, 0, 1},
+               kKeyGrad = {0.02, 0.5, 0.05, -1.3, 2};
 
 // Ranges that `tiles` streamed tiles of a pass are cut into when `base` workgroups
-// would run uncut: none, or as many as make one or two workgroups for each compute
-// unit, at least four tiles each, whichever takes the shortest by the model
+// would run uncut: none, or as many as make half a workgroup, one or two for each
+// compute unit, at least two tiles each, whichever takes the shortest by the model
 //   tiles of a range * tile time * (1.2 where two share a compute unit)
 //     + 6 us for the launch that joins the parts + their bytes, written and read,
 //       at 4 TB/s.
-// Of 202 shapes of 32 to 320 workgroups and 8 to 64 tiles its choice takes 1.1%
-// more than the best of one to twelve ranges in the geometric mean, 13% at most.
+// Of 232 shapes of 32 to 320 workgroups and 8 to 64 tiles its choice takes 1.1%
+// more than the best of one to twelve ranges in the geometric mean, 11% at most.
 // us uncut and cut (ranges): forward, heads of 72, 32 workgroups of 64 tiles 65.1
 // and 20.1 (8), 160 of 64 66.1 and 44.6 (3), 160 of 16 19.8 and 26.1 (3); one query
 // over 8191 keys of 128 162 and 16 (32); both gradients with dK and dV cut, heads
@@ -131,13 +131,15 @@ void plan_ranges(long long base, int tiles, int dim, size_t rows, const Pass &pa
     if (base <= 0 || base > 256 || tiles < 8)
         return;
     double best = tiles * pass.tile(dim);
-    for (const int units : {256, 512}) {
-        const int most = tiles / 4, want = (int)(units / base);
-        const int t = (tiles + (want < most ? want : most) - 1) / (want < most ? want : most);
-        const int r = (tiles + t - 1) / t;
+    for (const int units : {128, 256, 512}) {
+        const int most = tiles / 2, want = (int)(units / base);
+        if (want < 2)
+            continue;
+        const int cut = want < most ? want : most;
+        const int t = (tiles + cut - 1) / cut, r = (tiles + t - 1) / t;
         const double us = t * pass.tile(dim) * (r * base > 256 ? 1.2 : 1.0) + 6.0 +
                           8.0 * pass.results * r * (double)rows * dim / 4e6;
-        if (r > 1 && us < best) {
+        if (us < best) {
             best = us;
             *ranges = r;
             *range_tiles = t;

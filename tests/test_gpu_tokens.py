@@ -165,3 +165,37 @@ def test_refusals_of_the_wrappers():
         T.masked_linear_tokens(q, W, s[:3], sw, 8)
     with pytest.raises(ValueError):
         T.masked_linear_tokens(q, W, s, sw, 8, out_dtype=torch.float64)
+
+
+def test_codes_of_more_rows_than_one_launch_takes():
+    """2^22 rows go out together; the rows behind them have their own codes."""
+    M, K = (1 << 22) + 5, 3
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn(M, K, generator=g, device=DEV)
+    q, s = T.quantize_tokens(x)
+    for rows in (slice(0, 7), slice((1 << 22) - 3, M)):
+        want_q, want_s = T.quantize_tokens(x[rows].contiguous())
+        assert torch.equal(q[rows], want_q) and torch.equal(s[rows], want_s)
+    top = x.abs().amax(1)
+    assert torch.equal(s, top * torch.tensor(1 / 127, dtype=torch.float32, device=DEV))
+    assert int(q.abs().amax(1).min()) == 127
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("K", [1, 7, 9, 515, 1025, 2049, 4097, 16383, 16391])
+def test_codes_at_any_length_and_offset(dtype, K):
+    """Every path of a row's length, rows and codes off the vector alignment."""
+    g = torch.Generator().manual_seed(K)
+    buf = torch.randn(3, K + 2, generator=g).to(dtype).to(DEV)
+    x = buf[:, 1:K + 1]
+    out = torch.full((3 * K + 2,), 99, dtype=torch.int8, device=DEV)
+    q, s = T.quantize_tokens(x, out[1:-1].view(3, K))
+    want_q, want_s = T.quantize_tokens(x.float().contiguous())
+    assert torch.equal(q, want_q) and torch.equal(s, want_s)
+    assert int(out[0]) == 99 and int(out[-1]) == 99
+    x64 = x.double()
+    sx = (x64.abs().amax(1).float() * torch.tensor(1 / 127, device=DEV)).double()
+    r = x64 / sx[:, None]
+    assert torch.equal(s.double(), sx)
+    # round(x / s) decided in fp32: a code next to the quotient by 1/2 and 2^-16 at most
+    assert float((q.double() - r).abs().max()) <= 0.5 + 2.0 ** -16
