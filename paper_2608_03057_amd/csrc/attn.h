@@ -252,6 +252,17 @@ __device__ __forceinline__ int key_count(const AttnCall &a, int b)
     return min(max(a.kv_lengths[b], 0), a.kv_len);
 }
 
+// Tiles t0 .. t1 - 1 of range sp of the n keys that count in length: where the
+// entries have lengths, as many ranges of the tiles that each has, so that short
+// ones do not leave workgroups idle.
+__device__ __forceinline__ void key_range(const AttnCall &a, int n, int sp, int &t0, int &t1)
+{
+    const int tiles = (n + kAttnTile - 1) / kAttnTile;
+    const int each = a.kv_lengths ? (tiles + a.splits - 1) / a.splits : a.split_tiles;
+    t0 = sp * each;
+    t1 = min(tiles, t0 + each);
+}
+
 // Bits of the keys of tile t that count, the keys below n and with a nonzero
 // byte in the mask (`byte`: that of key 64 t + lane).
 __device__ __forceinline__ uint64_t live_keys(const AttnCall &a, int n, int t, int byte)

@@ -247,8 +247,8 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
     rows.init(a, b, hk, first);
 
     const int n = key_count(a, b);
-    const int t0 = sp * a.split_tiles;
-    const int t1 = min((n + kAttnTile - 1) / kAttnTile, t0 + a.split_tiles);
+    int t0, t1;
+    key_range(a, n, sp, t0, t1);
     const long long *stride = wave < 2 ? a.k_stride : a.v_stride;
     const T *kv = static_cast<const T *>(wave < 2 ? a.k : a.v) + b * stride[0] + hk * stride[2];
     const long long step = kAttnTile * stride[1];
