@@ -53,7 +53,8 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
     u /= a.row_tiles;
     const int sp = u % a.splits;
     u /= a.splits;
-    const int hk = u % a.kv_heads, b = u / a.kv_heads;
+    int hk, b;
+    head_and_entry(a, u, hk, b);
     const int group = a.heads / a.kv_heads;
 
     const int rows = group * a.q_len;
@@ -177,7 +178,8 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
     u /= a.key_tiles;
     const int sp = u % a.kv_splits;
     u /= a.kv_splits;
-    const int hk = u % a.kv_heads, b = u / a.kv_heads;
+    int hk, b;
+    head_and_entry(a, u, hk, b);
     const int group = a.heads / a.kv_heads;
 
     const int n = key_count(a, b);

@@ -240,7 +240,8 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
     u /= a.row_tiles;
     const int sp = u % a.splits;
     u /= a.splits;
-    const int hk = u % a.kv_heads, b = u / a.kv_heads;
+    int hk, b;
+    head_and_entry(a, u, hk, b);
     const int first = mt * BM + wave * 32 * QB;
     const bool busy = first < a.heads / a.kv_heads * a.q_len;   // the wave has rows
     Rows<T, KS, QB> rows;
