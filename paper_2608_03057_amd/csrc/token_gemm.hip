@@ -255,41 +255,97 @@ hipError_t launch_cfg(const TokenLinear &t, bool aligned, hipStream_t stream)
 // tokens' codes read alike; the waves' int32 sums meet in LDS.  Bound by the
 // latency of one round of loads and the launch: 1x1152 -> 3456 (4 MB) 3.9 us,
 // 16x4608 -> 1152 7.1 (13.0 with 64x64 tiles).
-constexpr int kFewTokens = 64;
+// Off the alignment of 16 bytes (a row's length is enough for that) each load is
+// several, and the tokens' are repeated by every workgroup: up to eight tokens,
+// 1x5538 -> 4090 12.6 a call and 24.1 with 64x64 tiles, 8x2315 -> 4436 10.8 and 12.1,
+// 16x1151 -> 3456 8.3 and 7.2.
+constexpr int kFewTokens = 64, kFewTokensAnywhere = 8;
 
-template <class T, int MB>
+// Sixteen codes of a row of K >= 16 from byte k on, zeros past its end, at any
+// alignment.
+__device__ __forceinline__ v4i row_chunk(const int8_t *row, int k, int K, bool live)
+{
+    const int at = k + 16 <= K ? k : K - 16, s = 8 * (k - at);
+    const Packed<int8_t, 16> c = *reinterpret_cast<const Packed<int8_t, 16> *>(row + at);
+    uint64_t lo = c.w[0] | (uint64_t)c.w[1] << 32, hi = c.w[2] | (uint64_t)c.w[3] << 32;
+    if (s) {
+        lo = s >= 128 ? 0 : s >= 64 ? hi >> (s - 64) : lo >> s | hi << (64 - s);
+        hi = s >= 64 ? 0 : hi >> s;
+    }
+    lo = live ? lo : 0;
+    hi = live ? hi : 0;
+    return {(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
+}
+
+template <class T, int MB, bool ALIGNED>
 __global__ void __launch_bounds__(256) k_token_few(TokenLinear t)
 {
     constexpr int UNROLL = MB <= 2 ? 8 : 4;
     typedef int v4 __attribute__((ext_vector_type(4)));
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int n0 = blockIdx.x * 16, r = lane & 15, kb = 16 * (lane >> 4);
-    const rsrc_t rw = make_rsrc(t.W, (uint32_t)t.N * (uint32_t)t.K);
-    const rsrc_t rx = make_rsrc(t.X, (uint32_t)t.M * (uint32_t)t.K);
-    const uint32_t ow = n0 + r < t.N ? (uint32_t)(n0 + r) * (uint32_t)t.K : kOOB;
-    uint32_t ox[MB];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-        ox[mb] = 16 * mb + r < t.M ? (uint32_t)(16 * mb + r) * (uint32_t)t.K : kOOB;
     const int mask = (int)keep_mask_dword(t.bits);
     v4 acc[MB] = {};
-    for (int k0 = 64 * wave; k0 < t.K; k0 += 256 * UNROLL) {
-        v4i w[UNROLL], x[UNROLL][MB];
+    auto multiply = [&](v4i w, const v4i (&x)[MB]) {
+        const v4i wm = {w.x & mask, w.y & mask, w.z & mask, w.w & mask};
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const int k = k0 + 256 * u + kb;
-            const bool in = k < t.K;            // K % 16 == 0: whole chunks
-            w[u] = ld16(rw, in ? ow + (uint32_t)k : kOOB);
+        for (int mb = 0; mb < MB; ++mb)
+            acc[mb] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wm, x[mb], acc[mb], 0, 0, 0);
+    };
+    if constexpr (ALIGNED) {
+        const rsrc_t rw = make_rsrc(t.W, (uint32_t)t.N * (uint32_t)t.K);
+        const rsrc_t rx = make_rsrc(t.X, (uint32_t)t.M * (uint32_t)t.K);
+        const uint32_t ow = n0 + r < t.N ? (uint32_t)(n0 + r) * (uint32_t)t.K : kOOB;
+        uint32_t ox[MB];
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
-                x[u][mb] = ld16(rx, in ? ox[mb] + (uint32_t)k : kOOB);
+        for (int mb = 0; mb < MB; ++mb)
+            ox[mb] = 16 * mb + r < t.M ? (uint32_t)(16 * mb + r) * (uint32_t)t.K : kOOB;
+        for (int k0 = 64 * wave; k0 < t.K; k0 += 256 * UNROLL) {
+            v4i w[UNROLL], x[UNROLL][MB];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const int k = k0 + 256 * u + kb;
+                const bool in = k < t.K;            // K % 16 == 0: whole chunks
+                w[u] = ld16(rw, in ? ow + (uint32_t)k : kOOB);
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+                    x[u][mb] = ld16(rx, in ? ox[mb] + (uint32_t)k : kOOB);
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+                multiply(w[u], x[u]);
         }
+    } else {
+        // Rows past the end are read as the last ones and not used.
+        const int8_t *pw = t.W + (size_t)min(n0 + r, t.N - 1) * t.K;
+        const int8_t *px[MB];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
-            const v4i wm = {w[u].x & mask, w[u].y & mask, w[u].z & mask, w[u].w & mask};
+        for (int mb = 0; mb < MB; ++mb)
+            px[mb] = t.X + (size_t)min(16 * mb + r, t.M - 1) * t.K;
+        const int whole = t.K / 64;                 // steps of 64
+        int step = wave;
+        for (; step + 4 * (UNROLL - 1) < whole; step += 4 * UNROLL) {
+            v4i w[UNROLL], x[UNROLL][MB];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const int k = 64 * (step + 4 * u) + kb;
+                w[u] = row_chunk(pw, k, 0x7fffffff, true);
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+                    x[u][mb] = row_chunk(px[mb], k, 0x7fffffff, true);
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+                multiply(w[u], x[u]);
+        }
+        for (; 64 * step < t.K; step += 4) {
+            const int k = 64 * step + kb;
+            v4i x[MB];
+            const v4i w = row_chunk(pw, k, t.K, k < t.K);
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
-                acc[mb] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wm, x[u][mb], acc[mb], 0, 0, 0);
+                x[mb] = row_chunk(px[mb], k, t.K, k < t.K);
+            multiply(w, x);
         }
     }
     // Register v of lane l: channel 4 (l/16) + v, token l%16.
@@ -314,15 +370,17 @@ __global__ void __launch_bounds__(256) k_token_few(TokenLinear t)
     }
 }
 
-template <class T> hipError_t launch_few(const TokenLinear &t, hipStream_t stream)
+template <class T> hipError_t launch_few(const TokenLinear &t, bool aligned, hipStream_t stream)
 {
     const unsigned grid = (unsigned)((t.N + 15) / 16);
-    if (t.M <= 16)
-        k_token_few<T, 1><<<grid, 256, 0, stream>>>(t);
+    if (!aligned)
+        k_token_few<T, 1, false><<<grid, 256, 0, stream>>>(t);
+    else if (t.M <= 16)
+        k_token_few<T, 1, true><<<grid, 256, 0, stream>>>(t);
     else if (t.M <= 32)
-        k_token_few<T, 2><<<grid, 256, 0, stream>>>(t);
+        k_token_few<T, 2, true><<<grid, 256, 0, stream>>>(t);
     else
-        k_token_few<T, 4><<<grid, 256, 0, stream>>>(t);
+        k_token_few<T, 4, true><<<grid, 256, 0, stream>>>(t);
     return hipGetLastError();
 }
 
@@ -335,8 +393,8 @@ hipError_t launch_linear_tokens(const TokenLinear &t, hipStream_t stream)
                          (long long)t.M * t.K < (1LL << 31) && (long long)t.N * t.K < (1LL << 31);
     return with_type(t.type, [&](auto zero) {
         using T = decltype(zero);
-        if (aligned && t.M <= kFewTokens)
-            return launch_few<T>(t, stream);
+        if (t.M <= (aligned ? kFewTokens : kFewTokensAnywhere) && (aligned || t.K >= 16))
+            return launch_few<T>(t, aligned, stream);
         // Tiles of 64x64 where larger ones would leave compute units idle, else
         // 128x128, and from about half a tile per compute unit on 256x256, as a
         // persistent walk where the operands allow it.  us, 64x64 / 128x128 /

@@ -199,3 +199,24 @@ def test_codes_at_any_length_and_offset(dtype, K):
     assert torch.equal(s.double(), sx)
     # round(x / s) decided in fp32: a code next to the quotient by 1/2 and 2^-16 at most
     assert float((q.double() - r).abs().max()) <= 0.5 + 2.0 ** -16
+
+
+@pytest.mark.parametrize("M", [1, 3, 8])
+@pytest.mark.parametrize("K", [16, 17, 31, 63, 64, 65, 127, 255, 257, 1151, 2063, 4607])
+def test_linear_of_few_tokens_at_any_length(M, K):
+    check_linear(M, 71, K, 7, torch.float32, offset=K % 4)
+
+
+def test_linear_reads_no_byte_past_its_operands():
+    """Rows end where the allocation does, codes behind them change nothing."""
+    K, N, M = 1151, 33, 5
+    g = torch.Generator().manual_seed(12)
+    buf = torch.randint(-128, 128, (2, M * K + N * K + 64), generator=g,
+                        dtype=torch.int64).to(torch.int8).to(DEV)
+    buf[1] = buf[0]
+    buf[1, M * K:M * K + 32] = 77               # behind X
+    buf[1, M * K + 32 + N * K:] = -55           # behind W
+    y = [T.masked_linear_tokens(r[:M * K].view(M, K), r[M * K + 32:M * K + 32 + N * K].view(N, K),
+                                torch.ones(M, device=DEV), torch.ones(N, device=DEV), 8,
+                                out_dtype=torch.float32) for r in buf]
+    assert torch.equal(y[0], y[1])
