@@ -353,7 +353,7 @@ template <class T, int KS> hipError_t attn_forward_ks(const AttnCall &a, hipStre
     if (grid == 0)
         return hipSuccess;
     void (*kernel)(AttnCall) = k_attn_forward<T, KS, 1>;
-    if constexpr (KS <= kAttnWideSteps)
+    if constexpr (KS >= kAttnWideFrom && KS <= kAttnWideSteps)
         if (a.row_blocks == 2)
             kernel = k_attn_forward<T, KS, 2>;
     kernel<<<(unsigned)grid, 256, 0, stream>>>(a);

@@ -156,12 +156,20 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
     const long long pairs = (long long)c.batch * c.kv_heads;
     const int key_tiles = (c.kv_len + 63) / 64;
     const long long pair_rows = (long long)group * c.q_len;
-    // Two blocks of rows to a wave halve what a row reads of LDS; they need
-    // registers (dims up to 80) and two workgroups for every compute unit.  4096
-    // tokens among themselves, us with one block and two: 32 heads of 64 156 and
-    // 137, of 72 192 and 184; 10 heads of 64 (160 workgroups) 76 and 87.
-    c.row_blocks = !backward && (c.dim + 15) / 16 <= tasq::kAttnWideSteps &&
-                           pairs * ((pair_rows + 255) / 256) >= 512
+    // Two blocks of rows to a wave halve what a row reads of LDS, but take registers:
+    // two workgroups of 256 rows to a compute unit where three of 128 fit.  So they
+    // run where one round of them replaces two of the smaller, and where rounds
+    // are many for dims up to 64.  us with one block and two over 1024 keys, by
+    // workgroups of 256 rows: heads of 72 256 30.3 and 39.9, 352 40.7 and 50.4, 392
+    // 52.3 and 50.1, 512 over 4096 198 and 190, 544 over 2048 115 and 152, 2048 387
+    // and 400; of 64 352 34.4 and 38.3, 416 46.0 and 39.6, 544 100 and 111, 704 63.6
+    // and 61.6, 2048 321 and 305.  (Heads up to 32: 392 29.0 and 29.8, 704 43.0 and
+    // 44.8.)
+    const int steps = (c.dim + 15) / 16;
+    const long long wide = pairs * ((pair_rows + 255) / 256);
+    const bool fits = steps >= tasq::kAttnWideFrom && steps <= tasq::kAttnWideSteps;
+    c.row_blocks = !backward && fits &&
+                           ((wide > 384 && wide <= 512) || (steps <= 4 && wide >= 704))
                        ? 2
                        : 1;
     c.row_tiles = (int)((pair_rows + 128 * c.row_blocks - 1) / (128 * c.row_blocks));

@@ -53,7 +53,8 @@ hipError_t launch_norm_rotate(const HeadCall &call, bool grad, float *part, hipS
 // query) pairs of one key head; a workgroup has 128 rows (256 in the forward
 // pass with row_blocks 2), or 128 keys in k_attn_dkdv.  plan_attention sets
 // the launch's shape.
-constexpr int kAttnWideSteps = 5;   // 16-element steps of a head that row_blocks 2 takes
+// 16-element steps of a head that row_blocks 2 takes.
+constexpr int kAttnWideFrom = 3, kAttnWideSteps = 5;
 struct AttnCall {
     const void *q, *k, *v;
     const int32_t *kv_lengths;  // [batch] or null
