@@ -368,3 +368,49 @@ def test_refusals_of_the_wrappers():
                              workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
     with pytest.raises(ValueError):
         T.attention_backward(do[:, :2], q, k, v, out, lse)
+
+
+@pytest.mark.parametrize("shape", [(8, 3, 70, 64, 64, 72), (8, 300, 130, 25, 25, 40),
+                                   (9, 130, 65, 80, 80, 64), (4, 70, 33, 112, 28, 80),
+                                   (8, 3, 70, 64, 64, 32), (8, 300, 130, 25, 25, 88)])
+def test_many_workgroups(shape):
+    """Where a wave has two blocks of rows, and sizes beside it where it has one."""
+    q, k, v, do, _ = draw(*shape, torch.bfloat16)
+    check(q, k, v, do)
+
+
+@pytest.mark.parametrize("shape", [(4, 200, 900, 3, 3, 72), (3, 700, 640, 2, 1, 64)])
+def test_entries_of_different_lengths_in_turn(shape):
+    """Long keys with lengths: entries take turns, each entry's keys in ranges."""
+    q, k, v, do, g = draw(*shape, torch.bfloat16)
+    B, SK = shape[0], shape[2]
+    for few in (0, 1, 63, SK):
+        lengths = torch.tensor([SK, few, SK // 2 + 1, 130][:B], dtype=torch.int32, device=DEV)
+        check(q, k, v, do, lengths=lengths)
+
+
+@pytest.mark.parametrize("D", [40, 64, 72])
+def test_two_row_blocks_with_masks_and_wide_scores(D):
+    """400 workgroups of 256 rows: whole tiles off, nothing on, NaN and infinity at
+    keys that are off, scores of hundreds late in the row, a NaN in one query."""
+    B, SQ, SK, H = 4, 200, 300, 100
+    q, k, v, do, g = draw(B, SQ, SK, H, H, D, torch.float16)
+    mask = torch.rand(B, SK, generator=g) < 0.5
+    mask[0, :] = False
+    mask[1, :SK - 1] = False
+    mask[1, SK - 1] = True
+    mask[2, 64:192] = False
+    mask = mask.to(DEV)
+    kk = torch.where(mask[:, :, None, None], k, math.nan)
+    vv = torch.where(mask[:, :, None, None], v, -math.inf)
+    check(q, kk, vv, do, mask=mask)
+    q2, k2 = q * 4, k.clone()
+    k2[:, 250:] *= 8
+    check(q2, k2, v, do, grad=False)
+    clean, _ = T.attention(q2, k2, v)
+    q2[2, 77, 5, 3] = math.nan
+    out, _ = T.attention(q2, k2, v)
+    assert bool(out[2, 77, 5].isnan().all())
+    keep = torch.ones(B, SQ, H, dtype=torch.bool, device=DEV)
+    keep[2, 77, 5] = False
+    assert torch.equal(out[keep], clean[keep])
