@@ -407,7 +407,12 @@ hipError_t launch_linear_tokens(const TokenLinear &t, hipStream_t stream)
         if (t256 >= 140) {
             const bool rows = sizeof(T) == 4 ||
                               (t.N % 8 == 0 && reinterpret_cast<uintptr_t>(t.y) % 16 == 0);
-            const bool fits = (long long)t.M * t.N * (int)sizeof(T) < (1LL << 31);
+            // The walk's stores take 32-bit byte offsets: those of the last tile's
+            // rows past M have to fall past the output's end as well and not come
+            // round to its start, as those of 66 rows of 4,300,000 in fp32 would.
+            const long long row = (long long)t.N * (int)sizeof(T);
+            const bool fits = t.M * row < (1LL << 31) &&
+                              (t.M + 255LL) / 256 * 256 * row <= (1LL << 32);
             if (aligned && rows && fits && t.K > 0)
                 return launch_walk<Cfg<256, 256, 128, 2, 4, 1>, T>(t, stream);
             // (8192x1151 -> 3456 56 us, 69 with 128x128.)

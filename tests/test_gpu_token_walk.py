@@ -86,3 +86,15 @@ def test_walk_repeats_its_bits():
     X, W, sx, sw, bias = problem(4100, 4104, 640, True)
     y = [T.masked_linear_tokens(X, W, sx, sw, 5, bias) for _ in range(4)]
     assert all(torch.equal(y[0], t) for t in y[1:])
+
+
+@pytest.mark.parametrize("N,dtype", [(4_300_000, torch.float32), (8_600_000, torch.bfloat16),
+                                     (8_600_000, torch.float16)])
+def test_rows_past_the_end_of_a_very_wide_output(N, dtype):
+    """66 rows of a 256-row tile: 250 rows on, an offset of 32 bits in bytes would be
+    back inside the output."""
+    M, K = 66, 16
+    assert M * N * dtype.itemsize < 2 ** 31 and 255 * N * dtype.itemsize > 2 ** 32
+    X, W, sx, sw, bias = problem(M, N, K, True)
+    y = T.masked_linear_tokens(X, W, sx, sw, 8, bias, out_dtype=dtype)
+    compare(y, X, W, sx, sw, 8, bias)
