@@ -384,7 +384,10 @@ __global__ void __launch_bounds__(256, FORM == kSplit && sizeof(T) == 4 ? 3 : 4)
                     sq += x1[i] * x1[i] + x2[i] * x2[i];
                     inner += g1[i] * w1[i] * x1[i] + g2[i] * w2[i] * x2[i];
                 }
-                const float r = rsqrtf(group_sum<LPR>(sq) * call.inv_dim + call.eps);
+                // (A head past the last one is zeros, whose r without eps is infinite:
+                // none of it may reach dw.)
+                const float norm = rsqrtf(group_sum<LPR>(sq) * call.inv_dim + call.eps);
+                const float r = un.h + k < j.heads ? norm : 0.0f;
                 const float t = group_sum<LPR>(inner) * call.inv_dim * r * r;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
