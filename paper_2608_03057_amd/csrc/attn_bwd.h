@@ -10,11 +10,11 @@
 // operands of the products.
 //
 // A weight of a long row is small, and as fp32 or half it would lose bits or
-// vanish: the kernels hold P' = 2^kShift P (kShift is taken off the exponent's
-// lse) and dS' = P' (kScore dO V^T - kScore delta), and take the factors out of
-// the sums at the end.  bfloat16 has fp32's range, so both carry 2^32 and
-// weights down to 2^-158 count; half ends at 65504, so P carries 2^14 and dS,
-// which is as large as the gradients are, nothing.
+// vanish, so the kernels hold P' = 2^kShift P (kShift is taken off the exponent's
+// lse) and dS' = 2^at P (dO V^T - delta), and take the factors out of the sums at
+// the end.  bfloat16 has fp32's range: both carry 2^32, and weights down to 2^-158
+// count.  Half ends at 65504: P carries 2^14; dS, which is as large or small as the
+// gradients are, has a power of two of its own (score_shift).
 //
 // Where there are few resident tiles the streamed axis is cut into ranges
 // whose fp32 parts k_attn_sum adds up in order.
@@ -34,13 +34,60 @@ namespace tasq {
 
 template <class T> struct Range;
 template <> struct Range<bf16_t> {
-    static constexpr float kShift = 32.0f, kScore = 1.0f;
-    static constexpr float kOutP = 0x1p-32f, kOutS = 0x1p-32f;  // of sums of P' and dS'
+    static constexpr int kShift = 32;
+    static constexpr bool kFits = false;            // dS' needs no power of its own
 };
 template <> struct Range<f16_t> {
-    static constexpr float kShift = 14.0f, kScore = 0x1p-14f;
-    static constexpr float kOutP = 0x1p-14f, kOutS = 1.0f;
+    static constexpr int kShift = 14;
+    static constexpr bool kFits = true;
 };
+
+// Largest magnitude of eight packed elements.
+template <class T> __device__ __forceinline__ float largest(u32x4 v)
+{
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 f = unpack2<T>(v[i]);
+        m = fmaxf(m, fmaxf(fabsf(f.x), fabsf(f.y)));
+    }
+    return m;
+}
+
+// The exponent that dS' of a column (a query of dQ, a key of dK) carries in half.
+// It follows `top`, the largest of the upstream gradients that a kernel sees first
+// (its query's, or its first tile's), to 2^8, which leaves room for |V| of 64 and
+// more where one key has all the weight: a dS is off by its own rounding or by
+// 2^-33 top.  Where that is too little room, sums come out infinite or NaN, and the
+// workgroup runs again with those columns' exponents kLess lower.  |dS'| is below
+// 2^55, so kRuns are enough for inputs that are finite themselves.
+// (us against dS without a power of its own, which lost up to all of its bits below
+// 2^-24 and overflowed above 65504: heads of 64, 4096 among themselves 231 and 224;
+// of 72 675 and 657, over 300 words 97 and 90; of 128, 2048 191 and 175.  A check of
+// every block with a branch instead took 248, 728, 97 and 193.)
+constexpr int kRuns = 4, kLess = 15;
+
+__device__ __forceinline__ int score_shift(float top)
+{
+    const uint32_t u = __float_as_uint(top);
+    const bool some = u - 1 < 0x7f800000u - 1;      // not zero, finite
+    return some ? min(8 + 127 - (int)(u >> 23), Range<f16_t>::kShift) : Range<f16_t>::kShift;
+}
+
+// Whether a column's sums, rows d below dim, hold an infinity or NaN.
+template <int DB> __device__ __forceinline__ bool not_finite(const v16f_t (&sum)[DB], int dim)
+{
+    const int h = (threadIdx.x & 63) >> 5;
+    float zero = 0.0f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (32 * db + 8 * (i / 4) + 4 * h < dim)
+                zero = fmaf(sum[db][i], 0.0f, zero);
+    zero = across_halves(zero, [](float a, float b) { return a + b; });
+    return zero != zero;
+}
 
 template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(AttnCall a)
 {
@@ -74,7 +121,7 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
                      ok, a.dim, gf);
     u32x4 of[KS];
     load_columns<KS>(static_cast<const T *>(a.out) + at, ok, a.dim, of);
-    float lse2 = ok ? a.lse[row] * kLog2e - Range<T>::kShift : 0.0f;
+    const float lse = ok ? a.lse[row] : 0.0f;
 
     const int n = key_count(a, b);
     int t0, t1;
@@ -84,19 +131,22 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
     const long long step = kAttnTile * stride[1];
 
     v16f_t dq[DB];
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-        dq[db] = v16f_t{};
     const Tile<KS> tile;
     Stager<KS> stager;
     stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     uint64_t live = 0, now = 0;
     int next_byte = 0;
-    if (t0 < t1) {
-        now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
-        stager.request(kv + t0 * step, live, lds[0]);
-        next_byte = mask_byte(a, b, n, t0 + 1);
-    }
+    auto begin = [&] {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            dq[db] = v16f_t{};
+        if (t0 < t1) {
+            now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
+            stager.request(kv + t0 * step, live, lds[0]);
+            next_byte = mask_byte(a, b, n, t0 + 1);
+        }
+    };
+    begin();
     // While the first tile is on its way.
     float delta = 0.0f;
 #pragma unroll
@@ -109,61 +159,79 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
     delta = across_halves(delta, [](float p, float q) { return p + q; });
     if (ok && lane < 32 && sp == 0)
         a.delta[row] = delta;
-    delta *= Range<T>::kScore;
-    // A row without keys (lse = -inf) has P = 0.
-    if (lse2 == -__builtin_huge_valf())
-        lse2 = __builtin_huge_valf();
-    if (t0 < t1) {
-        stager.wait();
-        __syncthreads();
+    int carried = Range<T>::kShift;
+    if constexpr (Range<T>::kFits) {
+        float top = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            top = fmaxf(top, largest<T>(gf[ks]));
+        carried = score_shift(
+            across_halves(top, [](float p, float q) { return fmaxf(p, q); }));
     }
-    for (int t = t0; t < t1; ++t) {
-        const char *kt = lds[(t - t0) & 1], *vt = kt + SIZE;
-        if (t + 1 < t1) {
-            live = live_keys(a, n, t + 1, next_byte);
-            stager.request(kv + (t + 1) * step, live, lds[(t + 1 - t0) & 1]);
-            next_byte = mask_byte(a, b, n, t + 2);
+    for (int run = 1;; ++run) {
+        // A row without keys (lse = -inf) has P = 0.
+        float lse2 = lse * kLog2e - (float)carried;
+        if (lse2 == -__builtin_huge_valf())
+            lse2 = __builtin_huge_valf();
+        if (t0 < t1) {
+            stager.wait();
+            __syncthreads();
         }
-        if (busy && now) {
+        for (int t = t0; t < t1; ++t) {
+            const char *kt = lds[(t - t0) & 1], *vt = kt + SIZE;
+            if (t + 1 < t1) {
+                live = live_keys(a, n, t + 1, next_byte);
+                stager.request(kv + (t + 1) * step, live, lds[(t + 1 - t0) & 1]);
+                next_byte = mask_byte(a, b, n, t + 2);
+            }
+            if (busy && now) {
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {
-                v16f_t sa = {}, pa = {};
+                for (int rb = 0; rb < 2; ++rb) {
+                    v16f_t sa = {}, pa = {};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    sa = mfma(T{}, tile.rows(kt, rb, ks), qf[ks], sa);
-                    pa = mfma(T{}, tile.rows(vt, rb, ks), gf[ks], pa);
-                }
-                float x[16];
-                if (now != ~0ull) {
+                    for (int ks = 0; ks < KS; ++ks) {
+                        sa = mfma(T{}, tile.rows(kt, rb, ks), qf[ks], sa);
+                        pa = mfma(T{}, tile.rows(vt, rb, ks), gf[ks], pa);
+                    }
+                    float x[16];
+                    if (now != ~0ull) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        sa[i] += dead_row(now, rb, i);
-                }
+                        for (int i = 0; i < 16; ++i)
+                            sa[i] += dead_row(now, rb, i);
+                    }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(sa[i] * a.scale_log2 - lse2);
-                    x[i] = p * (pa[i] * Range<T>::kScore - delta);
-                }
+                    for (int i = 0; i < 16; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(sa[i] * a.scale_log2 - lse2);
+                        x[i] = p * (pa[i] - delta);
+                    }
 #pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    const u32x4 ds = pack_rows<T>(x, s2);
+                    for (int s2 = 0; s2 < 2; ++s2) {
+                        const u32x4 ds = pack_rows<T>(x, s2);
 #pragma unroll
-                    for (int db = 0; db < DB; ++db)
-                        dq[db] =
-                            mfma(T{}, tile.columns(kt, 32 * rb + 16 * s2, db), ds, dq[db]);
+                        for (int db = 0; db < DB; ++db)
+                            dq[db] =
+                                mfma(T{}, tile.columns(kt, 32 * rb + 16 * s2, db), ds, dq[db]);
+                    }
                 }
             }
+            now = live;
+            stager.wait();
+            __syncthreads();
         }
-        now = live;
-        stager.wait();
-        __syncthreads();
+        if (!Range<T>::kFits || run == kRuns)
+            break;
+        const bool over = ok && not_finite(dq, a.dim);
+        if (!__syncthreads_or(over))
+            break;
+        carried -= over ? kLess : 0;
+        begin();
     }
+    const float back = ldexpf(a.scale, -carried);
     if (a.splits > 1)
         store_columns_f32<DB>(a.part + (size_t)sp * a.batch * a.q_len * a.heads * a.dim + at, ok,
-                              a.dim, dq, a.scale * Range<T>::kOutS);
+                              a.dim, dq, back);
     else
-        store_columns<T, DB>(static_cast<T *>(a.dq) + at, ok, a.dim, dq,
-                             a.scale * Range<T>::kOutS);
+        store_columns<T, DB>(static_cast<T *>(a.dq) + at, ok, a.dim, dq, back);
 }
 
 template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv(AttnCall a)
@@ -197,9 +265,6 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
                      counts, a.dim, vf);
 
     v16f_t dk[DB], dv[DB];
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-        dk[db] = dv[db] = v16f_t{};
     // Tiles of 64 queries, the group's heads one after the other.
     const int per_head = (a.q_len + kAttnTile - 1) / kAttnTile;
     const int t0 = sp * a.kv_split_tiles;
@@ -210,8 +275,7 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
     Stager<KS> stager;
     stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     float st = 0.0f;
-    int g = per_head ? t0 / per_head : 0;       // head and first row of the next tile
-    int s0 = (t0 - g * per_head) * kAttnTile;
+    int g = 0, s0 = 0;          // head and first row of the next tile
     auto fetch = [&](int i) {
         const int left = a.q_len - s0, head = hk * group + g;
         const uint64_t live = left >= kAttnTile ? ~0ull : (1ull << left) - 1;
@@ -234,62 +298,111 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
     auto put = [&](int i) {
         stager.wait();
         if (wave == 0) {        // rows past the end and rows without keys have P = 0
-            const float l = st * kLog2e - Range<T>::kShift;
+            const float l = st * kLog2e - (float)Range<T>::kShift;
             stat[i][0][lane] = l == -__builtin_huge_valf() ? __builtin_huge_valf() : l;
         } else if (wave == 1) {
-            stat[i][1][lane] = st * Range<T>::kScore;
+            stat[i][1][lane] = Range<T>::kFits ? -st : st;
         }
     };
-    if (t0 < t1) {
-        fetch(0);
-        put(0);
-        __syncthreads();
+    auto begin = [&] {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            dk[db] = dv[db] = v16f_t{};
+        g = per_head ? t0 / per_head : 0;
+        s0 = (t0 - g * per_head) * kAttnTile;
+        if (t0 < t1) {
+            fetch(0);
+            put(0);
+            __syncthreads();
+        }
+    };
+    begin();
+    int carried = Range<T>::kShift;
+    if constexpr (Range<T>::kFits) {
+        float top = 0.0f;
+        if (t0 < t1) {
+#pragma unroll
+            for (int i = 0; i < 2 * KS; ++i)
+                top = fmaxf(top, largest<T>(*reinterpret_cast<const u32x4 *>(
+                                     lds[0] + SIZE + 16 * (64 * i + lane))));
+        }
+        carried = score_shift(
+            group_reduce<64>(top, [](float p, float q) { return fmaxf(p, q); }));
     }
-    for (int t = t0; t < t1; ++t) {
-        const int cur = (t - t0) & 1;
-        const char *qt = lds[cur], *gt = qt + SIZE;
-        if (t + 1 < t1)
-            fetch(cur ^ 1);
-        if (busy) {
+    for (int run = 1;; ++run) {
+        const float lift = ldexpf(1.0f, carried - Range<T>::kShift);     // dS' over P' (..)
+        for (int t = t0; t < t1; ++t) {
+            const int cur = (t - t0) & 1;
+            const char *qt = lds[cur], *gt = qt + SIZE;
+            if (t + 1 < t1)
+                fetch(cur ^ 1);
+            if (busy) {
 #pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {
-                v16f_t sa = {}, pa = {};
+                for (int rb = 0; rb < 2; ++rb) {
+                    v16f_t sa = {}, pa = {};
+                    if constexpr (Range<T>::kFits) {    // minus delta to begin with
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    sa = mfma(T{}, tile.rows(qt, rb, ks), kf[ks], sa);
-                    pa = mfma(T{}, tile.rows(gt, rb, ks), vf[ks], pa);
-                }
-                float p[16], x[16];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int r = 32 * rb + 8 * q + 4 * (lane >> 5);
-                    const float4 l = *reinterpret_cast<const float4 *>(&stat[cur][0][r]);
-                    const float4 d = *reinterpret_cast<const float4 *>(&stat[cur][1][r]);
-                    const float ls[4] = {l.x, l.y, l.z, l.w}, de[4] = {d.x, d.y, d.z, d.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        p[4 * q + i] =
-                            __builtin_amdgcn_exp2f(sa[4 * q + i] * a.scale_log2 - ls[i]);
-                        x[4 * q + i] =
-                            p[4 * q + i] * (pa[4 * q + i] * Range<T>::kScore - de[i]);
+                        for (int q = 0; q < 4; ++q) {
+                            const float4 d = *reinterpret_cast<const float4 *>(
+                                &stat[cur][1][32 * rb + 8 * q + 4 * (lane >> 5)]);
+                            pa[4 * q] = d.x;
+                            pa[4 * q + 1] = d.y;
+                            pa[4 * q + 2] = d.z;
+                            pa[4 * q + 3] = d.w;
+                        }
                     }
-                }
 #pragma unroll
-                for (int s2 = 0; s2 < 2; ++s2) {
-                    const u32x4 pf = pack_rows<T>(p, s2), ds = pack_rows<T>(x, s2);
+                    for (int ks = 0; ks < KS; ++ks) {
+                        sa = mfma(T{}, tile.rows(qt, rb, ks), kf[ks], sa);
+                        pa = mfma(T{}, tile.rows(gt, rb, ks), vf[ks], pa);
+                    }
+                    float p[16], x[16];
 #pragma unroll
-                    for (int db = 0; db < DB; ++db) {
-                        dv[db] =
-                            mfma(T{}, tile.columns(gt, 32 * rb + 16 * s2, db), pf, dv[db]);
-                        dk[db] =
-                            mfma(T{}, tile.columns(qt, 32 * rb + 16 * s2, db), ds, dk[db]);
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = 32 * rb + 8 * q + 4 * (lane >> 5);
+                        const float4 l = *reinterpret_cast<const float4 *>(&stat[cur][0][r]);
+                        const float ls[4] = {l.x, l.y, l.z, l.w};
+                        float de[4] = {};
+                        if constexpr (!Range<T>::kFits) {
+                            const float4 d = *reinterpret_cast<const float4 *>(&stat[cur][1][r]);
+                            de[0] = d.x;
+                            de[1] = d.y;
+                            de[2] = d.z;
+                            de[3] = d.w;
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            p[4 * q + i] =
+                                __builtin_amdgcn_exp2f(sa[4 * q + i] * a.scale_log2 - ls[i]);
+                            x[4 * q + i] = p[4 * q + i] * (pa[4 * q + i] - de[i]);
+                            if constexpr (Range<T>::kFits)
+                                x[4 * q + i] *= lift;
+                        }
+                    }
+#pragma unroll
+                    for (int s2 = 0; s2 < 2; ++s2) {
+                        const u32x4 pf = pack_rows<T>(p, s2), ds = pack_rows<T>(x, s2);
+#pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            dv[db] =
+                                mfma(T{}, tile.columns(gt, 32 * rb + 16 * s2, db), pf, dv[db]);
+                            dk[db] =
+                                mfma(T{}, tile.columns(qt, 32 * rb + 16 * s2, db), ds, dk[db]);
+                        }
                     }
                 }
             }
+            if (t + 1 < t1)
+                put(cur ^ 1);
+            __syncthreads();
         }
-        if (t + 1 < t1)
-            put(cur ^ 1);
-        __syncthreads();
+        if (!Range<T>::kFits || run == kRuns)
+            break;
+        const bool over = counts && not_finite(dk, a.dim);
+        if (!__syncthreads_or(over))
+            break;
+        carried -= over ? kLess : 0;
+        begin();
     }
     // Keys that do not count have gradients of zero.
     if (!counts) {
@@ -298,16 +411,14 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
             dk[db] = dv[db] = v16f_t{};
     }
     const size_t at = (((size_t)b * a.kv_len + key) * a.kv_heads + hk) * a.dim;
+    const float back = ldexpf(a.scale, -carried), back_v = ldexpf(1.0f, -Range<T>::kShift);
     if (a.kv_splits > 1) {
         const size_t all = (size_t)a.batch * a.kv_len * a.kv_heads * a.dim;
-        store_columns_f32<DB>(a.kv_part + 2 * sp * all + at, ok, a.dim, dk,
-                              a.scale * Range<T>::kOutS);
-        store_columns_f32<DB>(a.kv_part + (2 * sp + 1) * all + at, ok, a.dim, dv,
-                              Range<T>::kOutP);
+        store_columns_f32<DB>(a.kv_part + 2 * sp * all + at, ok, a.dim, dk, back);
+        store_columns_f32<DB>(a.kv_part + (2 * sp + 1) * all + at, ok, a.dim, dv, back_v);
     } else {
-        store_columns<T, DB>(static_cast<T *>(a.dk) + at, ok, a.dim, dk,
-                             a.scale * Range<T>::kOutS);
-        store_columns<T, DB>(static_cast<T *>(a.dv) + at, ok, a.dim, dv, Range<T>::kOutP);
+        store_columns<T, DB>(static_cast<T *>(a.dk) + at, ok, a.dim, dk, back);
+        store_columns<T, DB>(static_cast<T *>(a.dv) + at, ok, a.dim, dv, back_v);
     }
 }
 
