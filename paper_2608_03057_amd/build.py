@@ -58,15 +58,11 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-I", INCLUDE, "-I", CSRC]
 
-# Forward attention takes maxima of scores: without this each operand of a
-# maximum is first multiplied by one, in case it is a signalling NaN.
-FLAGS = {"attn_fwd_bf16.hip": ["-fno-honor-nans"], "attn_fwd_f16.hip": ["-fno-honor-nans"]}
-
 
 def _compile(src: str) -> str:
     obj = os.path.join(OBJDIR, os.path.splitext(src)[0] + ".o")
     lang = ["-x", "hip"]
-    cmd = [HIPCC, *COMMON, *FLAGS.get(src, []), *lang, "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [HIPCC, *COMMON, *lang, "-c", os.path.join(CSRC, src), "-o", obj]
     subprocess.check_call(cmd)
     return obj
 
