@@ -25,14 +25,15 @@
 namespace tasq {
 
 // A row's weights are 2^(z - base), z in units of log2.  Floating-point weights
-// keep their precision whatever the base, which only has to keep them inside
-// the range.  So it starts at 0 and no maximum is computed, unless a lane's sum
-// over a tile reaches kMost, or is below kLeast in the first tile: the tile's
-// weights are then computed again with the base at the row's maximum, and its
-// sums so far are rescaled.
+// keep their precision whatever the base, which only has to keep them and their
+// products with values inside the range.  So it starts at 0 and no maximum is
+// computed, unless a lane's sum over a tile reaches kMost, or is below kLeast in the
+// first tile: the tile's weights are then computed again with the base at the row's
+// maximum, and its sums so far are rescaled.  In bfloat16 the sums thus hold values
+// from 2^-110 to 2^110 over a hundred keys, and scores from -11 to 11 need no maximum.
 template <class T> struct Weights;
 template <> struct Weights<bf16_t> {
-    static constexpr float kLeast = 0x1p-60f, kMost = 0x1p60f;
+    static constexpr float kLeast = 0x1p-16f, kMost = 0x1p16f;
 };
 template <> struct Weights<f16_t> {
     static constexpr float kLeast = 1.0f, kMost = 0x1p15f;      // the largest half is 65504
