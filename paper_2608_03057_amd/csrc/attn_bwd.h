@@ -12,8 +12,8 @@
 // A weight of a long row is small, and as fp32 or half it would lose bits or
 // vanish, so the kernels hold P' = 2^kShift P (kShift is taken off the exponent's
 // lse) and dS' = 2^at P (dO V^T - delta), and take the factors out of the sums at
-// the end.  bfloat16 has fp32's range: both carry 2^32, and weights down to 2^-158
-// count.  Half ends at 65504: P carries 2^14; dS, which is as large or small as the
+// the end.  bfloat16 has fp32's range: both carry 2^12, so that weights down to 2^-138
+// count and score gradients up to 2^115 do.  Half ends at 65504: P carries 2^14; dS, which is as large or small as the
 // gradients are, has a power of two of its own (score_shift).
 //
 // Where there are few resident tiles the streamed axis is cut into ranges
@@ -34,7 +34,7 @@ namespace tasq {
 
 template <class T> struct Range;
 template <> struct Range<bf16_t> {
-    static constexpr int kShift = 32;
+    static constexpr int kShift = 12;
     static constexpr bool kFits = false;            // dS' needs no power of its own
 };
 template <> struct Range<f16_t> {

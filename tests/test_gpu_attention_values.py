@@ -43,3 +43,15 @@ def test_small_values(shape, height):
     ex = Exact(q, k, v)
     out, _ = T.attention(q, k, v)
     near(out, *ex.forward()[:2], "out")
+
+
+@pytest.mark.parametrize("shape", [(1, 40, 90, 2, 2, 64), (2, 130, 700, 4, 2, 72)])
+def test_gradients_of_large_values(shape):
+    """Values of 2^60 and upstream gradients of 2^50: score gradients of 2^112."""
+    q, k, v, do, _ = draw(*shape, torch.bfloat16)
+    v, do = ((t.float() * 2.0 ** s).to(torch.bfloat16) for t, s in ((v, 60), (do, 50)))
+    out, lse = T.attention(q, k, v, want_lse=True)
+    got = T.attention_backward(do, q, k, v, out, lse)
+    for g, r, t, name in zip(got, *Exact(q, k, v).backward(do, out, lse), ("dq", "dk", "dv")):
+        assert bool(torch.isfinite(g).all()), name
+        near(g, r, t, name)
