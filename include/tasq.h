@@ -603,7 +603,10 @@ enum { TASQ_TYPE_F32 = 0, TASQ_TYPE_BF16 = 1, TASQ_TYPE_F16 = 2 };
  * decided in IEEE single precision (one product with the fp32 value nearest
  * 1/127; a correctly rounded division, then ties to even), codes in
  * [-127, 127]; a token whose scale is zero has codes 0.
- *   x         [M][K] of x_type, row m at x + m * x_stride; finite values.
+ *   x         [M][K] of x_type, row m at x + m * x_stride.  A token with a NaN
+ *             has scale NaN, one with an infinity and no NaN scale infinity: no
+ *             output of a product that is scaled by it is finite.  Its codes are
+ *             any.
  *   X_out     int8 [M][K]; sx_out fp32 [M] (4-byte aligned).
  * M == 0 enqueues nothing; K == 0 writes sx = 0.  Errors: TASQ_ERR_NULL,
  * _DIM (a negative size, M > 2^30, x_stride < K), _OVERFLOW (K >

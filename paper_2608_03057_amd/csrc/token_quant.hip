@@ -3,7 +3,8 @@
 //   s[m] = max_k |x[m][k]| * RN(1 / 127),   Q[m][k] = round(x[m][k] / s[m]),
 //
 // decided in IEEE single precision (one product; a correctly rounded division,
-// then ties to even); a token of zeros has s = 0 and codes 0.
+// then ties to even); a token of zeros has s = 0 and codes 0.  The maximum keeps
+// NaN, so that a token that is not finite has a scale that is not.
 //
 // One read of x: a row stays in the registers of the threads that loaded it
 // between its maximum and its codes, a wave to a row up to 2048 elements, which
@@ -49,10 +50,16 @@ struct TokenScale {
     }
 };
 
+// The larger, or NaN if either is (fmaxf would take the other).
+__device__ __forceinline__ float larger(float a, float b)
+{
+    return __builtin_elementwise_maximum(a, b);
+}
+
 // Maximum over the TPR threads of a row (TPR 64: a wave; 256: a workgroup).
 template <int TPR> __device__ __forceinline__ float row_max(float v)
 {
-    v = group_reduce<64>(v, [](float a, float b) { return fmaxf(a, b); });
+    v = group_reduce<64>(v, larger);
     if constexpr (TPR > 64) {
         __shared__ float part[TPR / 64];
         if ((threadIdx.x & 63) == 0)
@@ -61,7 +68,7 @@ template <int TPR> __device__ __forceinline__ float row_max(float v)
         v = part[0];
 #pragma unroll
         for (int w = 1; w < TPR / 64; ++w)
-            v = fmaxf(v, part[w]);
+            v = larger(v, part[w]);
     }
     return v;
 }
@@ -98,7 +105,7 @@ __global__ void __launch_bounds__(256) k_quantize_tokens(const T *__restrict__ x
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            top = fmaxf(top, fabsf(v[i][e]));
+            top = larger(top, fabsf(v[i][e]));
     const TokenScale ts(row_max<TPR>(top));
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -128,7 +135,7 @@ __global__ void __launch_bounds__(256) k_quantize_tokens_any(const T *__restrict
     const T *row = x + (size_t)m * stride;
     float top = 0.0f;
     for (int k = threadIdx.x; k < K; k += 256)
-        top = fmaxf(top, fabsf((float)row[k]));
+        top = larger(top, fabsf((float)row[k]));
     const TokenScale ts(row_max<256>(top));
     for (int k = threadIdx.x; k < K; k += 256)
         q[(size_t)m * K + k] = (int8_t)(int)ts.code<false>((float)row[k]);
