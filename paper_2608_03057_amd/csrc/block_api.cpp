@@ -29,8 +29,8 @@ int check_heads(const tasq_heads &h, int type, int dim, bool grad)
     for (int i = 0; i < 3; ++i)
         if (h.x_stride[i] < 0 || (grad && h.dy_stride[i] < 0))
             return TASQ_ERR_DIM;
-    // Units of a launch are counted in 32 bits, and so are tokens.
-    if ((long long)h.batch * h.tokens > (1LL << 30) ||
+    // Units of a call are counted in 32 bits, and so are tokens and heads.
+    if (h.heads > (1 << 30) || (long long)h.batch * h.tokens > (1LL << 30) ||
         (long long)h.batch * h.tokens * ((h.heads + 3LL) / 4) > (1LL << 30))
         return TASQ_ERR_DIM;
     if (!aligned_to(h.weight, 4) || !aligned_to(h.dweight, 4))

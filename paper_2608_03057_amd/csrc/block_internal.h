@@ -45,6 +45,7 @@ struct HeadCall {
     int n, type, dim, interleaved;
     float eps;
     float inv_dim;              // set by launch_norm_rotate
+    int first_block;            // of the launch
 };
 // part: n * kHeadGroups * dim floats (grad only).
 hipError_t launch_norm_rotate(const HeadCall &call, bool grad, float *part, hipStream_t stream);

@@ -191,9 +191,10 @@ __global__ void __launch_bounds__(256) k_norm_rotate(HeadCall call)
     constexpr int GROUPS = 256 / LPR;
     // The first blocks are the first job's, so that a workgroup's job is one.
     const int first = (call.job[0].units + GROUPS - 1) / GROUPS;
-    const int job = (int)blockIdx.x >= first;
+    const int block = call.first_block + (int)blockIdx.x;
+    const int job = block >= first;
     const HeadJob &j = call.job[job];
-    const int u = ((int)blockIdx.x - (job ? first : 0)) * GROUPS + (int)threadIdx.x / LPR;
+    const int u = (block - (job ? first : 0)) * GROUPS + (int)threadIdx.x / LPR;
     if (u >= j.units)
         return;                 // whole groups, which exchange among themselves only
     const int l = threadIdx.x % LPR;
@@ -452,8 +453,10 @@ int grad_groups(const HeadCall &c, int units_per_group)
     return all < kHeadGroups ? all : kHeadGroups;
 }
 
+// (Workgroups of the forward pass go out 2^22 at a time: a launch has fewer than 2^32
+// threads.)
 template <class T, Form FORM, int LPR>
-void launch_vectors(const HeadCall &c, bool grad, float *part, int *groups, hipStream_t stream)
+void launch_vectors(HeadCall c, bool grad, float *part, int *groups, hipStream_t stream)
 {
     constexpr int GROUPS = 256 / LPR;
     if (grad) {
@@ -462,7 +465,11 @@ void launch_vectors(const HeadCall &c, bool grad, float *part, int *groups, hipS
     } else {
         const int blocks = (c.job[0].units + GROUPS - 1) / GROUPS +
                            (c.job[1].units + GROUPS - 1) / GROUPS;
-        k_norm_rotate<T, FORM, LPR><<<blocks, 256, 0, stream>>>(c);
+        constexpr int MOST = 1 << 22;
+        for (c.first_block = 0; c.first_block < blocks; c.first_block += MOST) {
+            const int left = blocks - c.first_block;
+            k_norm_rotate<T, FORM, LPR><<<left < MOST ? left : MOST, 256, 0, stream>>>(c);
+        }
     }
 }
 
@@ -495,9 +502,8 @@ hipError_t launch_norm_rotate(const HeadCall &in, bool grad, float *part, hipStr
     }
     if (plain)
         c.interleaved = 1;
-    const int units = c.job[0].units + c.job[1].units;
     int groups = 0;
-    hipError_t e = units == 0 ? hipSuccess : with_type(c.type, [&](auto zero) {
+    hipError_t e = c.job[0].units == 0 && c.job[1].units == 0 ? hipSuccess : with_type(c.type, [&](auto zero) {
         using T = decltype(zero);
         if (c.dim % 8 == 0 && c.interleaved) {
             launch_lanes<T, kInterleaved>(c, grad, part, &groups, stream);

@@ -31,3 +31,27 @@ def test_no_eps(heads, dim, rot, inter, dtype):
         dx, mag, rw, wmag = backward(d, x, w, rope, inter, 0.0)
         near(got, dx, mag, 48)
         near(dw, rw, wmag, 24 + x.numel() / dim / 256 + 64)
+
+
+def test_more_workgroups_than_a_launch_takes():
+    """2^24 groups of eight heads of 136 and some: tokens one element apart, 36 GB out."""
+    torch.cuda.empty_cache()
+    S, D = (1 << 27) + 5000, 136
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    g = torch.Generator(device=DEV).manual_seed(2)
+    buf = torch.randn(S + D, generator=g, device=DEV).to(torch.bfloat16)
+    x = torch.as_strided(buf, (1, S, 1, D), (0, 1, 0, 1))
+    w = torch.randn(D, generator=g, device=DEV)
+    k = torch.randn(1, 9, 3, D, generator=g, device=DEV).to(torch.bfloat16)
+    y = torch.full((1, S, 1, D), float("nan"), dtype=torch.bfloat16, device=DEV)
+    _, yk = T.qk_norm_rotate(x, k, w, w, out_q=y)
+    torch.cuda.synchronize()
+    near(yk, *forward(k, w, None, False), 24)
+    for first in [i * (1 << 25) - 3000 for i in range(1, 5)] + [0, S - 6000]:
+        at = slice(first, first + 6000)
+        near(y[:, at], *forward(x[:, at], w, None, False), 24)
+    for first in range(0, S, 1 << 24):
+        assert not bool(y[:, first:first + (1 << 24)].isnan().any())
+    del y
+    torch.cuda.empty_cache()
