@@ -294,12 +294,13 @@ __device__ __forceinline__ int mask_byte(const AttnCall &a, int b, int n, int t)
 }
 
 // Workgroups are dispatched round-robin over the 8 XCDs; this bijection gives
-// each XCD one contiguous run of logical workgroups, so that those which read
-// the same keys meet in one L2.
-__device__ __forceinline__ int attn_unit(int pid, int G)
+// each XCD one contiguous run of a launch's logical workgroups, so that those which
+// read the same keys meet in one L2.
+__device__ __forceinline__ int attn_unit(const AttnCall &a)
 {
+    const int pid = blockIdx.x, G = gridDim.x;
     const int per = G / 8, more = G % 8, x = pid % 8;
-    return x * per + min(x, more) + pid / 8;
+    return a.first_unit + x * per + min(x, more) + pid / 8;
 }
 
 }  // namespace tasq

@@ -95,7 +95,7 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dq(A
     __shared__ __attribute__((aligned(16))) char lds[2][2 * SIZE];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int u = attn_unit(blockIdx.x, gridDim.x);
+    int u = attn_unit(a);
     const int mt = u % a.row_tiles;
     u /= a.row_tiles;
     const int sp = u % a.splits;
@@ -241,7 +241,7 @@ template <class T, int KS> __global__ void __launch_bounds__(256, 2) k_attn_dkdv
     __shared__ __attribute__((aligned(16))) float stat[2][2][kAttnTile];    // lse, delta
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int u = attn_unit(blockIdx.x, gridDim.x);
+    int u = attn_unit(a);
     const int kt_ = u % a.key_tiles;
     u /= a.key_tiles;
     const int sp = u % a.kv_splits;
@@ -458,15 +458,9 @@ template <class T, int KS> hipError_t attn_backward_ks(const AttnCall &a, hipStr
 {
     const long long rows = (long long)a.batch * a.kv_heads * a.splits * a.row_tiles;
     const long long keys = (long long)a.batch * a.kv_heads * a.kv_splits * a.key_tiles;
-    hipError_t e = hipSuccess;
-    if (rows > 0) {
-        k_attn_dq<T, KS><<<(unsigned)rows, 256, 0, stream>>>(a);
-        e = hipGetLastError();
-    }
-    if (e == hipSuccess && keys > 0) {
-        k_attn_dkdv<T, KS><<<(unsigned)keys, 256, 0, stream>>>(a);
-        e = hipGetLastError();
-    }
+    hipError_t e = launch_units(k_attn_dq<T, KS>, a, rows, stream);
+    if (e == hipSuccess)
+        e = launch_units(k_attn_dkdv<T, KS>, a, keys, stream);
     const size_t nq = (size_t)a.batch * a.q_len * a.heads * a.dim;
     const size_t nk = (size_t)a.batch * a.kv_len * a.kv_heads * a.dim;
     Sums sums{};

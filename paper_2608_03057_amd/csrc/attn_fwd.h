@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
     constexpr int BM = 128 * QB, SIZE = Tile<KS>::kBytes;
     __shared__ __attribute__((aligned(16))) char lds[2][2 * SIZE];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int u = attn_unit(blockIdx.x, gridDim.x);
+    int u = attn_unit(a);
     const int mt = u % a.row_tiles;
     u /= a.row_tiles;
     const int sp = u % a.splits;
@@ -351,14 +351,11 @@ template <class T, int SLICES> __global__ void __launch_bounds__(256) k_attn_joi
 template <class T, int KS> hipError_t attn_forward_ks(const AttnCall &a, hipStream_t stream)
 {
     const long long grid = (long long)a.batch * a.kv_heads * a.splits * a.row_tiles;
-    if (grid == 0)
-        return hipSuccess;
     void (*kernel)(AttnCall) = k_attn_forward<T, KS, 1>;
     if constexpr (KS >= kAttnWideFrom && KS <= kAttnWideSteps)
         if (a.row_blocks == 2)
             kernel = k_attn_forward<T, KS, 2>;
-    kernel<<<(unsigned)grid, 256, 0, stream>>>(a);
-    return hipGetLastError();
+    return launch_units(kernel, a, grid, stream);
 }
 
 template <class T> hipError_t attn_forward_typed(const AttnCall &a, hipStream_t stream)

@@ -73,7 +73,24 @@ struct AttnCall {
     float *part, *part_lse;     // [splits][batch][..] parts of out (or dq) and lse
     float *kv_part;             // [kv_splits][2][batch][kv_len][kv_heads][dim]
     float *delta;               // [batch][heads][q_len]
+    int first_unit;             // of the launch
 };
+
+// The kernel in launches of at most 2^22 workgroups: one has fewer than 2^32
+// threads.
+inline hipError_t launch_units(void (*kernel)(AttnCall), AttnCall a, long long units,
+                               hipStream_t stream)
+{
+    constexpr long long MOST = 1 << 22;
+    hipError_t e = hipSuccess;
+    for (long long u = 0; u < units && e == hipSuccess; u += MOST) {
+        a.first_unit = (int)u;
+        kernel<<<(unsigned)(units - u < MOST ? units - u : MOST), 256, 0, stream>>>(a);
+        e = hipGetLastError();
+    }
+    return e;
+}
+
 hipError_t attn_forward_bf16(const AttnCall &a, hipStream_t stream);
 hipError_t attn_forward_f16(const AttnCall &a, hipStream_t stream);
 hipError_t attn_backward_bf16(const AttnCall &a, hipStream_t stream);
