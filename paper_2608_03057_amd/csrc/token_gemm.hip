@@ -393,7 +393,9 @@ hipError_t launch_linear_tokens(const TokenLinear &t, hipStream_t stream)
                          (long long)t.M * t.K < (1LL << 31) && (long long)t.N * t.K < (1LL << 31);
     return with_type(t.type, [&](auto zero) {
         using T = decltype(zero);
-        if (t.M <= (aligned ? kFewTokens : kFewTokensAnywhere) && (aligned || t.K >= 16))
+        // (16 channels to a workgroup: from 2^28 on they are more than a launch takes.)
+        if (t.M <= (aligned ? kFewTokens : kFewTokensAnywhere) && (aligned || t.K >= 16) &&
+            t.N < (1 << 28))
             return launch_few<T>(t, aligned, stream);
         // Tiles of 64x64 where larger ones would leave compute units idle, else
         // 128x128, and from about half a tile per compute unit on 256x256, as a

@@ -98,3 +98,18 @@ def test_rows_past_the_end_of_a_very_wide_output(N, dtype):
     X, W, sx, sw, bias = problem(M, N, K, True)
     y = T.masked_linear_tokens(X, W, sx, sw, 8, bias, out_dtype=dtype)
     compare(y, X, W, sx, sw, 8, bias)
+
+
+@pytest.mark.parametrize("K", [0, 17])
+def test_one_token_and_more_channels_than_a_launch_of_few_takes(K):
+    """2^28 channels and some: 16 to a workgroup would be 2^32 threads."""
+    N = (1 << 28) + 40
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of device memory")
+    X, W, sx, sw, bias = problem(1, 64, K, True)
+    sx += 0.01
+    W, sw, bias = (t.repeat((N + 63) // 64, *[1] * (t.dim() - 1))[:N] for t in (W, sw, bias))
+    y = T.masked_linear_tokens(X, W, sx, sw, 8, bias)
+    compare(y[:, :4096], X, W[:4096], sx, sw[:4096], 8, bias[:4096])
+    assert torch.equal(y[0, :N // 64 * 64].view(-1, 64), y[0, :64].expand(N // 64, 64))
+    assert torch.equal(y[0, N // 64 * 64:], y[0, :N % 64])
