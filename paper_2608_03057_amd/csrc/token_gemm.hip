@@ -21,6 +21,14 @@ namespace {
 // an accumulator register spans do not meet in one bank.
 template <class C> constexpr int kOutPitch = C::WTN * 2 + 16;
 
+// Between the lanes of a wave that write LDS and those that read it: the hardware
+// keeps the order, and with this the compiler does too.
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Applies the factors and stores one wave's sub-tile.  Register v of a 32x32
 // accumulator in lane l is row 8*(v/4) + 4*(l/32) + v%4, column l%32.
 template <class C, class T>
@@ -67,7 +75,7 @@ __device__ __forceinline__ void token_epilogue(const TokenLinear &t, int m0, int
             }
         }
         if constexpr (sizeof(T) == 2) {
-            __builtin_amdgcn_wave_barrier();
+            wave_fence();
             constexpr int CH = C::WTN / 8;          // 16-byte chunks per row
             const bool wide = t.N % 8 == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0;
             for (int e = lane; e < 32 * CH; e += 64) {
@@ -84,7 +92,7 @@ __device__ __forceinline__ void token_epilogue(const TokenLinear &t, int m0, int
                         y[(size_t)m * t.N + n + k] = reinterpret_cast<const T *>(p)[k];
                 }
             }
-            __builtin_amdgcn_wave_barrier();
+            wave_fence();
         }
     }
 }
@@ -190,6 +198,7 @@ template <class C, class T> struct TokenEpilogue {
             }
             if constexpr (ES == 2) {
                 constexpr int CH = C::WTN / 8;
+                wave_fence();
 #pragma unroll
                 for (int e = 0; e < CH / 2; ++e) {
                     const int r = (64 * e + lane) / CH, c = lane % CH;
@@ -199,6 +208,7 @@ template <class C, class T> struct TokenEpilogue {
                         u, ry, n < d.N ? ((uint32_t)m * (uint32_t)d.N + (uint32_t)n) * 2u : kOOB,
                         0, 0);
                 }
+                wave_fence();
             }
         }
         pers::wait_lgkm0();
