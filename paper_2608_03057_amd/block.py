@@ -153,10 +153,10 @@ def _heads(x, weight, rope: Optional[Rope], out, name, dy=None, dweight=None, li
         turn = like[2]
     else:
         turn = _rope(rope, B, S)
-    gat, gst, dwat = 0, (0, 0, 0, 0), 0
+    gat, gst, dwat = 0, (0, 0, 0, 0), 0 if dweight is None else dweight.data_ptr()
     if dy is not None:
         gst = _strided(dy, dtype, shape, f"gradient of {name}")
-        gat, dwat = dy.data_ptr(), 0 if dweight is None else dweight.data_ptr()
+        gat = dy.data_ptr()
     return _HEADS.pack(x.data_ptr(), gat, out.data_ptr(),
                        _at(weight, torch.float32, (D,), f"weight of {name}"), dwat, turn[0],
                        turn[1], turn[2], st[0], st[1], st[2], gst[0], gst[1], gst[2], B, S, H,

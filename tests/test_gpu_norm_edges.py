@@ -33,6 +33,20 @@ def test_no_eps(heads, dim, rot, inter, dtype):
         near(dw, rw, wmag, 24 + x.numel() / dim / 256 + 64)
 
 
+def test_no_gradient_of_keys_that_are_none():
+    """Keys of no token need no gradient; their weight's is zeros, not what the
+    memory held."""
+    g = torch.Generator().manual_seed(1)
+    q = torch.randn(1, 5, 3, 64, generator=g).to(DEV)
+    w = torch.ones(64, device=DEV)
+    full = [torch.full((64,), 7.0, device=DEV) for _ in range(64)]
+    del full                                # the memory that is allocated next
+    _, gk, _, dwk = T.qk_norm_rotate_backward(q, None, q, q[:, :0], w, w)
+    assert gk.shape == (1, 0, 3, 64) and torch.equal(dwk, torch.zeros_like(w))
+    with pytest.raises(T.TasqError):        # keys that need one
+        T.qk_norm_rotate_backward(q, None, q, q, w, w)
+
+
 def test_more_workgroups_than_a_launch_takes():
     """2^24 groups of eight heads of 136 and some: tokens one element apart, 36 GB out."""
     torch.cuda.empty_cache()
