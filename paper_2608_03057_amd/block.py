@@ -39,6 +39,13 @@ def _type(t: torch.Tensor, name: str) -> int:
     return code
 
 
+_MOST = 0x7fffffff          # of an int of the C ABI: ctypes would cut larger ones off
+
+
+def _too_large(*sizes: int) -> ValueError:
+    return ValueError(f"sizes must be below 2^31, got {sizes}")
+
+
 def _strided(t: torch.Tensor, dtype, shape, name):
     """Strides of a GPU tensor with a contiguous innermost dimension."""
     st = t.stride()
@@ -83,6 +90,8 @@ def quantize_tokens(x: torch.Tensor, out: Optional[torch.Tensor] = None,
     floating type, rows at any stride: scale max|x| * fl(1/127) per token,
     codes round(x / scale)."""
     M, K = shape = x.shape
+    if M > _MOST or K > _MOST:
+        raise _too_large(M, K)
     st = _strided(x, x.dtype, shape, "x")
     if out is None:
         out = _like(x, torch.int8)
@@ -108,6 +117,8 @@ def masked_linear_tokens(X: torch.Tensor, W: torch.Tensor, sx: torch.Tensor, sw:
     (X W_b^T) sx[m] sw[n] + bias[n], W int8 [N, K] at b bits."""
     M, K = X.shape
     N = W.shape[0]
+    if M > _MOST or N > _MOST or K > _MOST:
+        raise _too_large(M, N, K)
     _need(X, torch.int8, (M, K), "X")
     _need(W, torch.int8, (N, K), "W")
     _need(sx, torch.float32, (M,), "sx")
