@@ -27,16 +27,20 @@ namespace tasq {
 // A row's weights are 2^(z - base), z in units of log2.  Floating-point weights
 // keep their precision whatever the base, which only has to keep them and their
 // products with values inside the range.  So it starts at 0 and no maximum is
-// computed, unless a lane's sum over a tile reaches kMost, or is below kLeast in the
-// first tile: the tile's weights are then computed again with the base at the row's
-// maximum, and its sums so far are rescaled.  In bfloat16 the sums thus hold values
-// from 2^-110 to 2^110 over a hundred keys, and scores from -11 to 11 need no maximum.
+// computed, unless a lane's sum over the first tile is outside [kLeast, kFirst) or
+// over a later one reaches kMost: the tile's weights are then computed again with
+// the base kRoom above the row's maximum, and its sums so far are rescaled.  In
+// bfloat16 the sums thus hold values from 2^-100 to 2^105 over a hundred keys, and
+// a base serves for scores that rise by 25 above the maximum it was taken from.
+// (4096 tokens among themselves, 16 heads of 72, scores with a deviation of 1, 4, 8
+// and 20: 192, 186, 186 and 210 us; with kFirst at 2^16 and no room 195, 212, 210 and
+// 230.)
 template <class T> struct Weights;
 template <> struct Weights<bf16_t> {
-    static constexpr float kLeast = 0x1p-16f, kMost = 0x1p16f;
+    static constexpr float kLeast = 0x1p-16f, kFirst = 0x1p8f, kMost = 0x1p16f, kRoom = 20.0f;
 };
-template <> struct Weights<f16_t> {
-    static constexpr float kLeast = 1.0f, kMost = 0x1p15f;      // the largest half is 65504
+template <> struct Weights<f16_t> {     // the largest half is 65504
+    static constexpr float kLeast = 1.0f, kFirst = 0x1p15f, kMost = 0x1p15f, kRoom = 0.0f;
 };
 
 // What a wave holds of its QB blocks of 32 rows.
@@ -78,14 +82,24 @@ template <class T, int KS, int QB> struct Rows {
         }
     }
 
+    // Sums of a tile that leave the base as it is, as bits: of the first tile and
+    // of a later one.
+    struct Sums {
+        uint32_t least = __float_as_uint(Weights<T>::kLeast);
+        uint32_t span = __float_as_uint(Weights<T>::kFirst) - __float_as_uint(Weights<T>::kLeast);
+        __device__ __forceinline__ void later()
+        {
+            least = 0;
+            span = __float_as_uint(Weights<T>::kMost);
+        }
+    };
+
     // 32 NR keys of a tile from row 32 rb on: x = K Q^T, the weights p,
     // o += V^T P^T.
     template <int NR>
     __device__ __forceinline__ void keys(const Tile<KS> &tile, const char *kt, const char *vt,
-                                         int rb, float scale_log2, uint64_t live, bool first)
+                                         int rb, float scale_log2, uint64_t live, Sums in)
     {
-        const uint32_t least = first ? __float_as_uint(Weights<T>::kLeast) : 0;
-        const uint32_t span = __float_as_uint(Weights<T>::kMost) - least;
         v16f_t x[QB][NR];
         u32x4 p[QB][NR][2];
 #pragma unroll
@@ -106,16 +120,19 @@ template <class T, int KS, int QB> struct Rows {
         for (int qb = 0; qb < QB; ++qb) {
             float part = weights(scale_log2, base[qb], x[qb], p[qb]);
             // As bits, where NaN is above everything and less than least wraps.
-            const bool out = __float_as_uint(part) - least >= span;
+            const bool out = __float_as_uint(part) - in.least >= in.span;
             if (__ballot(out)) {
                 // The other rows keep their base, so that no row's result depends
                 // on those beside it.
                 const bool row_out =
                     across_halves(out ? 1.0f : 0.0f, [](float u, float v) { return u + v; }) != 0;
+                const bool first = in.least != 0;
                 float to = first ? -__builtin_huge_valf() : base[qb];
+                float room = Weights<T>::kRoom;
+                asm volatile("" : "+s"(room));      // or it holds a register all the time
 #pragma unroll
                 for (int r = 0; r < NR; ++r)
-                    to = fmaxf(to, maximum(x[qb][r]) * scale_log2);
+                    to = fmaxf(to, maximum(x[qb][r]) * scale_log2 + room);
                 to = row_out ? to : base[qb];
                 // No score above -inf: weights of zero.
                 const float from = to == -__builtin_huge_valf() ? 0.0f : to;
@@ -259,7 +276,7 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
     stager.init(wave, 2u * (uint32_t)stride[1], a.dim);
     uint64_t live = 0, now = 0;
     int next_byte = 0;
-    bool fresh = true;
+    typename Rows<T, KS, QB>::Sums in;
     if (t0 < t1) {
         now = live = live_keys(a, n, t0, mask_byte(a, b, n, t0));
         stager.request(kv + t0 * step, live, lds[0]);
@@ -275,8 +292,8 @@ __global__ void __launch_bounds__(256, QB == 1 && KS <= 5 ? 3 : 2) k_attn_forwar
             next_byte = mask_byte(a, b, n, t + 2);
         }
         if (busy && now) {
-            rows.template keys<2>(tile, kt, vt, 0, a.scale_log2, now, fresh);
-            fresh = false;
+            rows.template keys<2>(tile, kt, vt, 0, a.scale_log2, now, in);
+            in.later();
         }
         now = live;
         stager.wait();
