@@ -113,3 +113,13 @@ def test_one_token_and_more_channels_than_a_launch_of_few_takes(K):
     compare(y[:, :4096], X, W[:4096], sx, sw[:4096], 8, bias[:4096])
     assert torch.equal(y[0, :N // 64 * 64].view(-1, 64), y[0, :64].expand(N // 64, 64))
     assert torch.equal(y[0, N // 64 * 64:], y[0, :N % 64])
+
+
+@pytest.mark.parametrize("M,N,K", [(66000, 300, 32768), (300, 66000, 32768), (9, 66000, 32768)])
+def test_operands_past_two_gigabytes(M, N, K):
+    """More codes than a 32-bit byte offset reaches: the first, last and some rows."""
+    X, W, sx, sw, bias = problem(M, N, K, True)
+    y = T.masked_linear_tokens(X, W, sx, sw, 6, bias)
+    m, n = (torch.cat([torch.arange(s - 200 if s > 400 else 0, s),
+                       torch.arange(0, s, max(1, s // 150))]).to(DEV) for s in (M, N))
+    compare(y[m][:, n], X[m].contiguous(), W[n].contiguous(), sx[m], sw[n], 6, bias[n])
