@@ -4,7 +4,8 @@ only): token-scaled linears, the norm and rotation of heads, attention.
 As in ``api``: tensors are checked, pointers and the current stream go to the
 C ABI of ``include/tasq.h``, an error raises ``TasqError``, and the work is
 asynchronous on the current stream.  Outputs and workspaces are allocated
-when they are not given.
+when they are not given.  Results carry no autograd graph, whatever the inputs
+require: the ``_backward`` calls give the gradients, and a program chains them.
 
 Descriptor structs are packed with ``struct`` (0.3 us; filling a ctypes
 Structure field by field takes 5): a call on one token is as long as its host

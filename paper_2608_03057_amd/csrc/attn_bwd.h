@@ -22,8 +22,8 @@
 // Bound by chains of products and vector instructions with two waves to a SIMD
 // (matrix units busy for a quarter to a third of the time, vector units for a
 // third to a half): 4096 queries over 300 masked keys, batch 2, 16 heads of 72 in
-// bfloat16 40 us for dQ and 44 for dK and dV; 4096 tokens among themselves, 10
-// heads of 64 in half 105 and 135 (320 workgroups on 256 compute units); batch 2,
+// bfloat16 41 us for dQ and 45 for dK and dV; 4096 tokens among themselves, 10
+// heads of 64 in half 114 and 138 (320 workgroups on 256 compute units); batch 2,
 // 8 heads of 128 in bfloat16 489 together, 0.70 PFLOP/s of the five products that
 // a gradient cannot do without.
 #pragma once

@@ -116,13 +116,15 @@ constexpr Pass kForward = {0.0087, 0.35, 0, 0, 1}, kQueryGrad = {0.0161, 0.48, 0
 //   tiles of a range * tile time * (1.2 where two share a compute unit)
 //     + 6 us for the launch that joins the parts + their bytes, written and read,
 //       at 4 TB/s.
-// Of 232 shapes of 32 to 320 workgroups and 8 to 64 tiles its choice takes 1.1%
-// more than the best of one to twelve ranges in the geometric mean, 11% at most.
-// us uncut and cut (ranges): forward, heads of 72, 32 workgroups of 64 tiles 65.1
-// and 20.1 (8), 160 of 64 66.1 and 44.6 (3), 160 of 16 19.8 and 26.1 (3); one query
-// over 8191 keys of 128 162 and 16 (32); both gradients with dK and dV cut, heads
-// of 72, 96 of 64 156 and 80 (5), 160 of 64 174 and 124 (3), 256 of 16 61.7 and 68
-// (2); with dQ cut, 160 of 64 151 and 121 (3), 160 of 16 49.4 and 52.4 (3).
+// Of 224 shapes of 32 to 256 workgroups and 8 to 64 tiles its choice takes 2.1%
+// more forward than the best of one to twelve ranges in the geometric mean, 28% at
+// most (13.2 us against 10.3), and 83% of uncut; of 96 each 1 to 2% and up to 17% in
+// the gradients.
+// us uncut and cut (ranges): forward, heads of 72, 32 workgroups of 64 tiles 63.6
+// and 20.8 (8), 160 of 64 67.9 and 45.8 (3), 160 of 16 20.2 and 26.0 (3); one query
+// over 8191 keys of 128 160 and 12 (64); both gradients with dK and dV cut, heads
+// of 72, 96 of 64 157 and 87 (5), 160 of 64 176 and 130 (3), 256 of 16 62.1 and 67.5
+// (2); with dQ cut, 160 of 64 159 and 134 (3), 160 of 16 52.0 and 53.2 (3).
 void plan_ranges(long long base, int tiles, int dim, size_t rows, const Pass &pass, int *ranges,
                  int *range_tiles)
 {
@@ -159,12 +161,12 @@ size_t plan_attention(tasq::AttnCall &c, bool backward, bool cut)
     // Two blocks of rows to a wave halve what a row reads of LDS, but take registers:
     // two workgroups of 256 rows to a compute unit where three of 128 fit.  So they
     // run where one round of them replaces two of the smaller, and where rounds
-    // are many for dims up to 64.  us with one block and two over 1024 keys, by
-    // workgroups of 256 rows: heads of 72 256 30.3 and 39.9, 352 40.7 and 50.4, 392
-    // 52.3 and 50.1, 512 over 4096 198 and 190, 544 over 2048 115 and 152, 2048 387
-    // and 400; of 64 352 34.4 and 38.3, 416 46.0 and 39.6, 544 100 and 111, 704 63.6
-    // and 61.6, 2048 321 and 305.  (Heads up to 32: 392 29.0 and 29.8, 704 43.0 and
-    // 44.8.)
+    // are many for dims up to 64.  us with one block and two, by workgroups of 256
+    // rows: heads of 64 over 1024 keys 384 34.8 and 38.8, 400 45.2 and 39.6, 512 46.5
+    // and 41.9, 544 52.2 and 59.5, 704 61.1 and 61.1, 1024 81.8 and 77.0; of 72 384
+    // 42.7 and 53.7, 512 56.5 and 57.1, over 4096 512 191.7 and 186.7, 544 214 and 299,
+    // 1024 361 and 384.  (Heads of 72 lose 4% over 300 keys, 26.7 and 28.3, and heads up
+    // to 32 gain nothing: 512 34.8 and 33.1, 704 45.2 and 44.9.)
     const int steps = (c.dim + 15) / 16;
     const long long wide = pairs * ((pair_rows + 255) / 256);
     const bool fits = steps >= tasq::kAttnWideFrom && steps <= tasq::kAttnWideSteps;

@@ -263,12 +263,12 @@ hipError_t launch_cfg(const TokenLinear &t, bool aligned, hipStream_t stream)
 // waves have every fourth 64 bytes of K each, straight from memory as matrix
 // operands (lane l: channel l%16, bytes 16 (l/16) .. of the 64), against the
 // tokens' codes read alike; the waves' int32 sums meet in LDS.  Bound by the
-// latency of one round of loads and the launch: 1x1152 -> 3456 (4 MB) 3.9 us,
-// 16x4608 -> 1152 7.1 (13.0 with 64x64 tiles).
+// latency of one round of loads and the launch: 1x1152 -> 3456 (4 MB) 3.7 us,
+// 16x4608 -> 1152 7.2 (13.7 with 64x64 tiles), 64x1152 -> 3456 6.2 (5.8).
 // Off the alignment of 16 bytes (a row's length is enough for that) each load is
 // several, and the tokens' are repeated by every workgroup: up to eight tokens,
-// 1x5538 -> 4090 12.6 a call and 24.1 with 64x64 tiles, 8x2315 -> 4436 10.8 and 12.1,
-// 16x1151 -> 3456 8.3 and 7.2.
+// 1x5538 -> 4090 12.7 a call and 24.4 with 64x64 tiles, 8x2315 -> 4436 11.4 and 12.7,
+// 16x1151 -> 3456 8.8 and 7.6.
 constexpr int kFewTokens = 64, kFewTokensAnywhere = 8;
 
 // Sixteen codes of a row of K >= 16 from byte k on, zeros past its end, at any
@@ -410,10 +410,11 @@ hipError_t launch_linear_tokens(const TokenLinear &t, hipStream_t stream)
         // Tiles of 64x64 where larger ones would leave compute units idle, else
         // 128x128, and from about half a tile per compute unit on 256x256, as a
         // persistent walk where the operands allow it.  us, 64x64 / 128x128 /
-        // walk, bfloat16 out: 300x1152 -> 3456 7.0 / 9.3 / 16.7, 1024x1280 -> 3840
-        // 13.5 / 11.9 / 19.1, 8192x1152 -> 1152 (160 tiles of 256x256) 23.9 / 22.9 /
-        // 19.6, 4096x640 -> 5120 (320) 33.2 / 26.1 / 26.1, 8192x1152 -> 3456 (448)
-        // 64.8 / 49.8 / 40.2; 4096x2240 -> 6720 fp32 147 / 125 / 76.
+        // walk, bfloat16 out: 300x1152 -> 3456 7.5 / 9.9 / 17.0, 1024x1280 -> 3840
+        // 13.5 / 12.2 / 19.3, 8192x1152 -> 1152 (160 tiles of 256x256) 22.5 / 23.1 /
+        // 20.9, 4096x640 -> 5120 (320) 30.5 / 25.9 / 26.6, 8192x1152 -> 3456 (448)
+        // 61.5 / 49.0 / 39.7; 4096x2240 -> 6720 fp32 131 / 108 / 74.  (fp32 out leaves
+        // 128x128 slowly: 1024x1152 -> 4608 17.9 / 21.6 / 16.9.)
         const long long t128 = ((t.M + 127LL) / 128) * ((t.N + 127LL) / 128);
         const long long t256 = ((t.M + 255LL) / 256) * ((t.N + 255LL) / 256);
         if (t256 >= 140) {
