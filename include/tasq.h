@@ -748,6 +748,75 @@ int tasq_attention_backward(const tasq_attention *a, void *stream);
  * 0 where they are not valid. */
 size_t tasq_attention_workspace_bytes(const tasq_attention *a, int backward);
 
+/* ------------------------------------------------------------------------
+ * What stands around a block's quantized linears: the residual stream's norm,
+ * linears on 4-bit microscaled codes, and the gradient of the token-scaled
+ * linear.  Types, strides and roundings as in the section before.
+ * ------------------------------------------------------------------------ */
+
+/* Widest row of tasq_residual_norm, and its most batch entries. */
+#define TASQ_MAX_RESIDUAL_WIDTH 16384
+#define TASQ_MAX_RESIDUAL_BATCH (1 << 20)
+
+enum { TASQ_NORM_LAYER = 0, TASQ_NORM_RMS = 1 };
+/* Modulations that all batch entries share: stride ignored, gradient [width]. */
+enum { TASQ_SHARED_GATE = 1, TASQ_SHARED_SCALE = 2, TASQ_SHARED_SHIFT = 4 };
+
+/*
+ * The residual stream x takes a branch's output y through its gate, and is normed
+ * and modulated for the next branch:
+ *   r = residual_scale x + gate P(y),  P(y) = y, or N(y) post_weight where given,
+ *   h = N(r) weight (1 + scale) + shift,
+ *   N(v) = (v - mean v) / sqrt(mean (v - mean v)^2 + eps)   (TASQ_NORM_LAYER)
+ *   N(v) = v / sqrt(mean v^2 + eps)                         (TASQ_NORM_RMS)
+ * over the width of each token; h is of r before it is rounded.  A factor that is
+ * NULL is one (scale, shift: zero).  Without y, r is x, is not written, and gate,
+ * post_weight and r are ignored.  With eps 0 a token without deviation gives NaN.
+ */
+typedef struct tasq_residual {
+    int32_t type;               /* of x, y, r, h and their gradients */
+    int32_t mod_type;           /* of gate, scale and shift: TASQ_TYPE_F32, or type */
+    int32_t kind;               /* TASQ_NORM_* */
+    int32_t shared;             /* TASQ_SHARED_* bits */
+    int32_t batch, tokens, width;
+    float eps, residual_scale;  /* eps finite, >= 0; residual_scale finite */
+    const void *x;              /* [batch][tokens][width]; backward: the forward call's r */
+    const void *y;              /* the same, or NULL */
+    long long x_stride[2], y_stride[2];         /* of batch and token */
+    const void *gate, *scale, *shift;           /* [batch][width], or [width] shared */
+    long long gate_stride, scale_stride, shift_stride;  /* of batch */
+    const float *weight, *post_weight;          /* fp32 [width] */
+    void *r, *h;                /* forward: contiguous [batch][tokens][width] */
+    const void *dh, *dr;        /* backward: gradients of h and of r (dr may be NULL) */
+    long long dh_stride[2], dr_stride[2];
+    void *dx, *dy;              /* backward: contiguous; dy with y */
+    float *dgate, *dscale, *dshift;     /* backward: fp32, shaped as gate, .. ; NULL:
+                                           not wanted */
+    float *dweight, *dpost_weight;      /* backward: fp32 [width], or NULL */
+    void *workspace;            /* backward: 256-byte aligned device scratch */
+    size_t workspace_bytes;
+} tasq_residual;
+
+/*
+ * Writes r (with y) and h.  Any width up to TASQ_MAX_RESIDUAL_WIDTH at any
+ * alignment of the elements; multiples of 8 take whole vectors.  r may be x.  No
+ * tokens or no width: enqueues nothing.  Errors: TASQ_ERR_NULL, _DIM (a size, a
+ * stride, batch > TASQ_MAX_RESIDUAL_BATCH, more than 2^30 tokens), _KIND (a type or
+ * kind), _RANGE (eps, residual_scale, unknown bits of shared), _ALIGN (a pointer
+ * not aligned to its elements), _HIP.
+ */
+int tasq_residual_norm(const tasq_residual *a, void *stream);
+
+/*
+ * Its gradient from dh and dr, with x the r of the forward call (without y: its
+ * x): writes dx, dy and those of dgate .. dpost_weight that are given, sums over
+ * the tokens in a fixed order (the same bits each time; zeros where there are no
+ * tokens).  A sum needs a workspace of tasq_residual_norm_workspace_bytes(batch,
+ * tokens, width) bytes (TASQ_ERR_WORKSPACE); a call without sums needs none.
+ */
+int tasq_residual_norm_backward(const tasq_residual *a, void *stream);
+size_t tasq_residual_norm_workspace_bytes(int batch, int tokens, int width);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,9 @@ from .block import (  # noqa: F401
     quantize_tokens, masked_linear_tokens, qk_norm_rotate, qk_norm_rotate_backward,
     qk_norm_rotate_workspace_bytes, attention, attention_backward, attention_workspace_bytes,
 )
+from .branch import (  # noqa: F401
+    residual_norm, residual_norm_backward, residual_norm_workspace_bytes, ResidualGrads,
+)
 from ._lib import (  # noqa: F401
     TasqError, VARIANT_AUTO, VARIANT_MASKED_I8, VARIANT_BITPLANE, VARIANT_PACKED, KIND_LINEAR,
     KIND_CONV3X3, TASQ_ACT_PARAMS_FLOATS,

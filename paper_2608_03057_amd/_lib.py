@@ -44,6 +44,14 @@ TASQ_MAX_NORM_DIM = 256
 TASQ_MAX_NORM_JOBS = 2
 TASQ_MAX_ATTENTION_DIM = 128
 
+NORM_LAYER = 0
+NORM_RMS = 1
+SHARED_GATE = 1
+SHARED_SCALE = 2
+SHARED_SHIFT = 4
+TASQ_MAX_RESIDUAL_WIDTH = 16384
+TASQ_MAX_RESIDUAL_BATCH = 1 << 20
+
 # Every exported symbol the header declares.
 EXPORTS = (
     "tasq_masked_linear", "tasq_masked_conv3x3", "tasq_pack_planes", "tasq_planes_bytes",
@@ -56,6 +64,7 @@ EXPORTS = (
     "tasq_quantize_tokens", "tasq_masked_linear_tokens",
     "tasq_norm_rotate", "tasq_norm_rotate_backward", "tasq_norm_rotate_workspace_bytes",
     "tasq_attention_forward", "tasq_attention_backward", "tasq_attention_workspace_bytes",
+    "tasq_residual_norm", "tasq_residual_norm_backward", "tasq_residual_norm_workspace_bytes",
 )
 
 
@@ -129,6 +138,27 @@ class Attention(ctypes.Structure):
                 ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("dout", ctypes.c_void_p),
                 ("dout_stride", ctypes.c_longlong * 3), ("dq", ctypes.c_void_p),
                 ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class Residual(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("mod_type", ctypes.c_int32), ("kind", ctypes.c_int32),
+                ("shared", ctypes.c_int32), ("batch", ctypes.c_int32),
+                ("tokens", ctypes.c_int32), ("width", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("residual_scale", ctypes.c_float),
+                ("x", ctypes.c_void_p), ("y", ctypes.c_void_p),
+                ("x_stride", ctypes.c_longlong * 2), ("y_stride", ctypes.c_longlong * 2),
+                ("gate", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("shift", ctypes.c_void_p),
+                ("gate_stride", ctypes.c_longlong), ("scale_stride", ctypes.c_longlong),
+                ("shift_stride", ctypes.c_longlong),
+                ("weight", ctypes.c_void_p), ("post_weight", ctypes.c_void_p),
+                ("r", ctypes.c_void_p), ("h", ctypes.c_void_p),
+                ("dh", ctypes.c_void_p), ("dr", ctypes.c_void_p),
+                ("dh_stride", ctypes.c_longlong * 2), ("dr_stride", ctypes.c_longlong * 2),
+                ("dx", ctypes.c_void_p), ("dy", ctypes.c_void_p),
+                ("dgate", ctypes.c_void_p), ("dscale", ctypes.c_void_p),
+                ("dshift", ctypes.c_void_p), ("dweight", ctypes.c_void_p),
+                ("dpost_weight", ctypes.c_void_p),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
@@ -211,6 +241,12 @@ def lib() -> ctypes.CDLL:
             f.restype = i32
         L.tasq_attention_workspace_bytes.argtypes = [vp, i32]
         L.tasq_attention_workspace_bytes.restype = size
+        for name in ("tasq_residual_norm", "tasq_residual_norm_backward"):
+            f = getattr(L, name)
+            f.argtypes = [vp, vp]
+            f.restype = i32
+        L.tasq_residual_norm_workspace_bytes.argtypes = [i32, i32, i32]
+        L.tasq_residual_norm_workspace_bytes.restype = size
         L.tasq_status_string.argtypes = [i32]
         L.tasq_status_string.restype = ctypes.c_char_p
         _lib = L

@@ -1,0 +1,172 @@
+"""Torch-facing wrappers of what stands around a block's quantized linears
+(argument marshalling only): the residual stream's norm with its gradient.
+
+As in ``block``: tensors are checked, pointers and the current stream go to the
+C ABI of ``include/tasq.h``, an error raises ``TasqError``, the work is
+asynchronous on the current stream, and results carry no autograd graph.
+"""
+from __future__ import annotations
+
+import struct
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import _lib
+from ._lib import check
+from .api import _stream
+from .block import _MOST, _at, _like, _need, _strided, _too_large, _type, _workspace
+
+_RESIDUAL = struct.Struct("7i2f4x2P4q3P3q6P4q8PN")       # tasq_residual
+_KINDS = {"layer": _lib.NORM_LAYER, "rms": _lib.NORM_RMS}
+_NONE = (0, 0)                  # strides of a tensor that is not there
+
+
+def _here(t: torch.Tensor, name: str) -> None:
+    """Calls go to the current device's stream: a tensor of another is refused."""
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+
+
+class ResidualGrads(NamedTuple):
+    """Gradients of residual_norm, None where there is no such input: of x and y
+    in their type, of the rest in fp32."""
+    dx: torch.Tensor
+    dy: Optional[torch.Tensor]
+    dgate: Optional[torch.Tensor]
+    dweight: Optional[torch.Tensor]
+    dscale: Optional[torch.Tensor]
+    dshift: Optional[torch.Tensor]
+    dpost_weight: Optional[torch.Tensor]
+
+
+def _rows(t: Optional[torch.Tensor], dtype, shape, name):
+    """(address, strides of batch and token) of a [batch, tokens, width] operand."""
+    if t is None:
+        return 0, _NONE
+    return t.data_ptr(), _strided(t, dtype, shape, name)
+
+
+def _residual(x, y, gate, weight, scale, shift, post_weight, kind, residual_scale, eps):
+    """(fields of a tasq_residual up to the weights, and which modulations are
+    shared), checked."""
+    shape, dtype = x.shape, x.dtype
+    if len(shape) != 3:
+        raise ValueError("x must be [batch, tokens, width]")
+    B, S, C = shape
+    if B > _MOST or S > _MOST or C > _MOST:
+        raise _too_large(B, S, C)
+    code = _type(x, "x")
+    xs = _strided(x, dtype, shape, "x")
+    _here(x, "x")
+    yat, ys = _rows(y, dtype, shape, "y")
+    if kind not in _KINDS:
+        raise ValueError(f"kind must be 'layer' or 'rms', got {kind!r}")
+    if y is None and (gate is not None or post_weight is not None or residual_scale != 1.0):
+        raise ValueError("gate, post_weight and residual_scale need y")
+    mod_type, shared, at, strides = None, 0, [], []
+    for bit, m, name in ((1, gate, "gate"), (2, scale, "scale"), (4, shift, "shift")):
+        if m is None:
+            at.append(0)
+            strides.append(0)
+            continue
+        if mod_type is None:
+            mod_type = m.dtype
+            if mod_type != torch.float32 and mod_type != dtype:
+                raise ValueError(f"{name} must be float32 or {dtype}, got {mod_type}")
+        one = m.dim() == 1
+        st = _strided(m, mod_type, (C,) if one else (B, C), name)
+        shared |= bit if one else 0
+        at.append(m.data_ptr())
+        strides.append(0 if one else st[0])
+    wat = _at(weight, torch.float32, (C,), "weight")
+    pat = _at(post_weight, torch.float32, (C,), "post_weight")
+    return (code, _lib.TYPE_F32 if mod_type == torch.float32 else code, _KINDS[kind], shared, B, S,
+            C, eps, residual_scale, x.data_ptr(), yat, xs[0], xs[1], ys[0], ys[1], *at, *strides,
+            wat, pat), shared
+
+
+def residual_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None,
+                  gate: Optional[torch.Tensor] = None, *,
+                  weight: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                  shift: Optional[torch.Tensor] = None,
+                  post_weight: Optional[torch.Tensor] = None, kind: str = "layer",
+                  residual_scale: float = 1.0, eps: float = 1e-6,
+                  out_r: Optional[torch.Tensor] = None, out_h: Optional[torch.Tensor] = None):
+    """(r, h) of a residual stream x [B, S, C] that takes a branch's output y
+    through its gate and is normed for the next branch:
+    r = residual_scale x + gate P(y), h = N(r) weight (1 + scale) + shift, with
+    P(y) = y, or N(y) post_weight where that is given, and N the layer or the
+    root-mean-square norm over C ("layer", "rms").  Without y, r is x.
+
+    x and y of one floating type at any strides with contiguous channels; gate,
+    scale and shift [B, C], or [C] for all entries, all fp32 or all of x's type;
+    weight and post_weight fp32 [C]."""
+    head, _ = _residual(x, y, gate, weight, scale, shift, post_weight, kind, residual_scale, eps)
+    if out_h is None:
+        out_h = _like(x)
+    else:
+        _need(out_h, x.dtype, x.shape, "out_h")
+    if y is None:
+        out_r, rat = x, 0
+    else:
+        if out_r is None:
+            out_r = _like(x)
+        else:
+            _need(out_r, x.dtype, x.shape, "out_r")
+        rat = out_r.data_ptr()
+    a = _RESIDUAL.pack(*head, rat, out_h.data_ptr(), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    rc = _lib.lib().tasq_residual_norm(a, _stream())
+    if rc:
+        check(rc, "tasq_residual_norm")
+    return out_r, out_h
+
+
+def residual_norm_workspace_bytes(batch: int, tokens: int, width: int) -> int:
+    """Workspace of residual_norm_backward for [batch, tokens, width]."""
+    return _lib.lib().tasq_residual_norm_workspace_bytes(batch, tokens, width)
+
+
+def residual_norm_backward(dh: torch.Tensor, dr: Optional[torch.Tensor], r: torch.Tensor,
+                           y: Optional[torch.Tensor] = None,
+                           gate: Optional[torch.Tensor] = None, *,
+                           weight: Optional[torch.Tensor] = None,
+                           scale: Optional[torch.Tensor] = None,
+                           shift: Optional[torch.Tensor] = None,
+                           post_weight: Optional[torch.Tensor] = None, kind: str = "layer",
+                           residual_scale: float = 1.0, eps: float = 1e-6,
+                           workspace: Optional[torch.Tensor] = None) -> ResidualGrads:
+    """Gradients of residual_norm from those of its outputs, dh and dr (None:
+    r has no other use), with the r that the forward call gave and its other
+    arguments.  Sums run in a fixed order."""
+    head, shared = _residual(r, y, gate, weight, scale, shift, post_weight, kind, residual_scale,
+                             eps)
+    shape, dtype = r.shape, r.dtype
+    hat, hs = _rows(dh, dtype, shape, "dh")
+    rat, rs = _rows(dr, dtype, shape, "dr")
+    dx, dy = _like(r), None if y is None else _like(r)
+    B, S, C = shape
+    sizes = [C if shared & bit else B * C for bit in (1, 2, 4)] + [C, C]
+    given = (gate, scale, shift, weight, post_weight)
+    # One buffer of all sums' results: an allocation takes longer than a view.
+    total = sum(n for n, t in zip(sizes, given) if t is not None)
+    grads, ats, ws, nbytes = [None] * 5, [0] * 5, None, 0
+    if total:
+        flat = torch.empty(total, dtype=torch.float32, device=r.device)
+        first, base = 0, flat.data_ptr()
+        for i, (n, t) in enumerate(zip(sizes, given)):
+            if t is not None:
+                grads[i] = flat[first:first + n].view(t.shape)
+                ats[i] = base + 4 * first
+                first += n
+        ws = _workspace(workspace, residual_norm_workspace_bytes(B, S, C), r.device,
+                        "residual_norm_backward")
+        nbytes = ws.numel() * ws.element_size()
+    a = _RESIDUAL.pack(*head, 0, 0, hat, rat, hs[0], hs[1], rs[0], rs[1], dx.data_ptr(),
+                       0 if dy is None else dy.data_ptr(), *ats,
+                       0 if ws is None else ws.data_ptr(), nbytes)
+    rc = _lib.lib().tasq_residual_norm_backward(a, _stream())
+    if rc:
+        check(rc, "tasq_residual_norm_backward")
+    dgate, dscale, dshift, dweight, dpost = grads
+    return ResidualGrads(dx, dy, dgate, dweight, dscale, dshift, dpost)

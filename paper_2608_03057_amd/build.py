@@ -47,6 +47,8 @@ SOURCES = [
     "attn_bwd_bf16.hip",
     "attn_bwd_f16.hip",
     "block_api.cpp",
+    "residual_norm.hip",
+    "branch_api.cpp",
     "cost.cpp",
     "tasq_api.cpp",
 ]

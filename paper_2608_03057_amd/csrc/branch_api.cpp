@@ -1,0 +1,155 @@
+// C ABI of what stands around a block's quantized linears (include/tasq.h):
+// argument checks, then one launcher each.
+#include <math.h>
+
+#include "branch_internal.h"
+#include "floats.h"
+
+namespace {
+
+constexpr int kMostRows = 1 << 30;  // rounded up to tiles in 32 bits
+
+bool type_known(int t)
+{
+    return t == TASQ_TYPE_F32 || t == TASQ_TYPE_BF16 || t == TASQ_TYPE_F16;
+}
+
+bool aligned_to(const void *p, size_t bytes)
+{
+    return reinterpret_cast<uintptr_t>(p) % bytes == 0;
+}
+
+int status(hipError_t e) { return e == hipSuccess ? TASQ_OK : TASQ_ERR_HIP; }
+
+bool finite(float v) { return !isnan(v) && !isinf(v); }
+
+// Sizes that tasq_residual_norm_workspace_bytes needs to be valid.
+bool residual_sizes(int batch, int tokens, int width)
+{
+    return batch >= 0 && batch <= TASQ_MAX_RESIDUAL_BATCH && tokens >= 0 && width >= 0 &&
+           width <= TASQ_MAX_RESIDUAL_WIDTH && (long long)batch * tokens <= kMostRows;
+}
+
+int residual_norm(const tasq_residual *a, bool grad, void *stream)
+{
+    if (!a)
+        return TASQ_ERR_NULL;
+    if (!type_known(a->type) || (a->mod_type != TASQ_TYPE_F32 && a->mod_type != a->type) ||
+        (a->kind != TASQ_NORM_LAYER && a->kind != TASQ_NORM_RMS))
+        return TASQ_ERR_KIND;
+    if (!(a->eps >= 0.0f) || !finite(a->eps) || !finite(a->residual_scale) ||
+        (a->shared & ~(TASQ_SHARED_GATE | TASQ_SHARED_SCALE | TASQ_SHARED_SHIFT)))
+        return TASQ_ERR_RANGE;
+    if (!residual_sizes(a->batch, a->tokens, a->width))
+        return TASQ_ERR_DIM;
+    tasq::NormCall c{};
+    const int extent[2] = {a->batch, a->tokens};
+    const long long *in[4] = {a->x_stride, a->y_stride, a->dh_stride, a->dr_stride};
+    long long *out[4] = {c.x_stride, c.y_stride, c.dh_stride, c.dr_stride};
+    const bool used[4] = {true, a->y != nullptr, grad, grad && a->dr};
+    for (int t = 0; t < 4; ++t)
+        for (int i = 0; i < 2; ++i) {
+            if (!used[t] || extent[i] < 2)
+                continue;
+            if (in[t][i] < 0)
+                return TASQ_ERR_DIM;
+            out[t][i] = in[t][i];
+        }
+    // A factor of the branch does nothing without one.
+    const void *gate = a->y ? a->gate : nullptr;
+    const float *post = a->y ? a->post_weight : nullptr;
+    const void *mods[3] = {gate, a->scale, a->shift};
+    const long long strides[3] = {a->gate_stride, a->scale_stride, a->shift_stride};
+    tasq::Modulation *to[3] = {&c.gate, &c.scale, &c.shift};
+    for (int i = 0; i < 3; ++i) {
+        const bool each = a->batch > 1 && !(a->shared & (1 << i));
+        if (mods[i] && each && strides[i] < 0)
+            return TASQ_ERR_DIM;
+        *to[i] = {mods[i], each ? strides[i] : 0};
+    }
+    const bool none = (long long)a->batch * a->tokens * a->width == 0;
+    float *sums[5] = {a->dgate, a->dscale, a->dshift, a->dweight, a->dpost_weight};
+    if (!a->y && !none)         // (an empty y may be NULL: its gate's gradient is zeros)
+        sums[0] = sums[4] = nullptr;
+    bool some_sum = false;
+    for (int i = 0; grad && i < 5; ++i) {
+        if (!aligned_to(sums[i], 4))
+            return TASQ_ERR_ALIGN;
+        some_sum = some_sum || sums[i];
+    }
+    if (none && !(some_sum && a->width))
+        return TASQ_OK;
+    const size_t es = (size_t)tasq::type_bytes(a->type), ms = (size_t)tasq::type_bytes(a->mod_type);
+    if (!none) {
+        if (!a->x || (grad ? !a->dh || !a->dx || (a->y && !a->dy) : !a->h || (a->y && !a->r)))
+            return TASQ_ERR_NULL;
+        const void *wide[] = {a->x, a->y, grad ? a->dh : a->h, grad ? a->dr : a->r,
+                              grad ? a->dx : nullptr, grad ? a->dy : nullptr};
+        for (const void *p : wide)
+            if (!aligned_to(p, es))
+                return TASQ_ERR_ALIGN;
+    }
+    if (!aligned_to(gate, ms) || !aligned_to(a->scale, ms) || !aligned_to(a->shift, ms) ||
+        !aligned_to(a->weight, 4) || !aligned_to(post, 4))
+        return TASQ_ERR_ALIGN;
+    if (some_sum) {
+        if (!aligned_to(a->workspace, 256))
+            return TASQ_ERR_ALIGN;
+        const size_t need = tasq_residual_norm_workspace_bytes(a->batch, a->tokens, a->width);
+        if (need && (!a->workspace || a->workspace_bytes < need))
+            return TASQ_ERR_WORKSPACE;
+        c.part = static_cast<float *>(a->workspace);
+    }
+    c.x = a->x;
+    c.y = a->y;
+    c.dh = a->dh;
+    c.dr = a->dr;
+    c.weight = a->weight;
+    c.post_weight = post;
+    c.r = a->r;
+    c.h = a->h;
+    c.dx = a->dx;
+    c.dy = a->dy;
+    c.dgate = sums[0];
+    c.dscale = sums[1];
+    c.dshift = sums[2];
+    c.dweight = sums[3];
+    c.dpost = sums[4];
+    c.sums = some_sum;
+    c.type = a->type;
+    c.wide_mods = a->mod_type == TASQ_TYPE_F32;
+    c.layer = a->kind == TASQ_NORM_LAYER;
+    c.batch = a->batch;
+    c.tokens = a->tokens;
+    c.width = a->width;
+    c.shared = a->shared;
+    c.eps = a->eps;
+    c.alpha = a->y ? a->residual_scale : 1.0f;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return status(grad ? tasq::launch_residual_norm_backward(c, st)
+                       : tasq::launch_residual_norm(c, st));
+}
+
+}  // namespace
+
+extern "C" {
+
+int tasq_residual_norm(const tasq_residual *a, void *stream)
+{
+    return residual_norm(a, false, stream);
+}
+
+int tasq_residual_norm_backward(const tasq_residual *a, void *stream)
+{
+    return residual_norm(a, true, stream);
+}
+
+size_t tasq_residual_norm_workspace_bytes(int batch, int tokens, int width)
+{
+    if (!residual_sizes(batch, tokens, width) || (long long)batch * tokens == 0)
+        return 0;
+    return (size_t)batch * (size_t)tasq::residual_norm_chunks(batch, tokens, width) * 3 *
+           (size_t)width * sizeof(float);
+}
+
+}  // extern "C"

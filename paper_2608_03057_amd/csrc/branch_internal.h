@@ -1,0 +1,41 @@
+// Internal declarations of what stands around a block's quantized linears: the
+// norm of the residual stream, 4-bit microscaled linears, and the gradient of the
+// token-scaled linear.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "tasq.h"
+#include "tasq_internal.h"
+
+namespace tasq {
+
+// The residual stream's norm and its gradient (residual_norm.hip).
+struct Modulation {             // of entry b at p + b * stride
+    const void *p;
+    long long stride;
+};
+struct NormCall {
+    const void *x, *y, *dh, *dr;
+    long long x_stride[2], y_stride[2], dh_stride[2], dr_stride[2];     // batch, token
+    Modulation gate, scale, shift;
+    const float *weight, *post_weight;
+    void *r, *h, *dx, *dy;
+    float *dgate, *dscale, *dshift, *dweight, *dpost;
+    int type, wide_mods;        // wide_mods: modulations are fp32, else of `type`
+    int layer, batch, tokens, width, shared;
+    float eps, alpha, inv_width;
+    int rows, chunks;           // rows of a group's run; runs (backward: workgroups) an entry
+    long long first_unit;       // of the launch
+    float *part;                // backward: [batch][chunks][3][width]
+    bool sums;                  // backward: some of dgate .. dpost are wanted
+};
+constexpr int kMaxNormWidth = TASQ_MAX_RESIDUAL_WIDTH;
+hipError_t launch_residual_norm(const NormCall &c, hipStream_t stream);
+hipError_t launch_residual_norm_backward(const NormCall &c, hipStream_t stream);
+// Workgroups of the gradient for each batch entry.
+int residual_norm_chunks(int batch, int tokens, int width);
+
+}  // namespace tasq

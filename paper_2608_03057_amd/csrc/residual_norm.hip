@@ -1,0 +1,613 @@
+// The residual stream between two branches of a block, and its gradient:
+//
+//   r = alpha x + g P(y),     P(y) = y or N(y) wp,
+//   h = N(r) w (1 + scale) + shift,
+//   N(v) = (v - mean v) / sqrt(var v + eps)  or  v / sqrt(mean v^2 + eps),
+//
+// g, scale and shift per channel and batch entry (or shared), w and wp per
+// channel.  Backward, with n = N(r), u = dh w (1 + scale), 1/s the factor of N:
+//   D = dr + (u - [mean u] - n mean(u n)) / s,   dx = alpha D,
+//   p = D g [wp],   dy = p  or  the same Jacobian of N at y applied to p,
+// and sums over tokens: dshift = sum dh, P = sum dh n, Q = sum D N(y) (or D y), of
+// which dscale = w P, dw = sum_b (1 + scale) P, dgate = wp Q, dwp = sum_b g Q.
+// The bracketed means are the layer kind's.  Everything between the loads and the
+// stores is fp32; the variance is that of the centred row, which two passes over
+// registers give without cancellation.
+//
+// Bound by memory: every operand is read once and every result written once.  A
+// row belongs to a wave (or a workgroup), which holds it in registers, eight
+// channels to a lane and vector, between its sums and its stores.
+#include "branch_internal.h"
+#include "floats.h"
+
+namespace tasq {
+
+namespace {
+
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+
+// Sums over the TPR threads of a row, K at a time.  (TPR above 64: the workgroup;
+// two buffers in turn, so that one barrier a call is enough.)
+template <int TPR, int K> struct RowSum {
+    __device__ __forceinline__ static void run(float (&v)[K], int &turn)
+    {
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+            v[i] = group_reduce<64>(v[i], add);
+        if constexpr (TPR > 64) {
+            constexpr int W = TPR / 64;
+            __shared__ float part[2][W][K];
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int i = 0; i < K; ++i)
+                    part[turn][threadIdx.x >> 6][i] = v[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                v[i] = part[turn][0][i];
+#pragma unroll
+                for (int w = 1; w < W; ++w)
+                    v[i] += part[turn][w][i];
+            }
+            turn ^= 1;
+        }
+    }
+};
+
+// Where a thread's vectors of eight channels lie.  FULL: the width is a multiple of
+// eight, so that a vector is whole or nothing.
+template <int TPR, int NV, bool FULL> struct Columns {
+    int width, t;
+    __device__ __forceinline__ int k(int i) const { return 8 * (t + i * TPR); }
+    __device__ __forceinline__ bool some(int i) const { return k(i) < width; }
+    __device__ __forceinline__ bool live(int i, int e) const
+    {
+        return FULL ? some(i) : k(i) + e < width;
+    }
+    // The vector's elements, zeros past the width.
+    template <class T> __device__ __forceinline__ Packed<T, 8> load(const T *row, int i) const
+    {
+        const int at = k(i);
+        Packed<T, 8> p = {};
+        if (FULL ? at < width : at + 8 <= width) {
+            p = *reinterpret_cast<const Packed<T, 8> *>(row + at);
+        } else if (!FULL && at < width) {
+            T e[8] = {};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at + j < width)
+                    e[j] = row[at + j];
+            p = __builtin_bit_cast(Packed<T, 8>, e);
+        }
+        return p;
+    }
+    template <class T>
+    __device__ __forceinline__ void store(T *row, int i, const float (&v)[8]) const
+    {
+        const int at = k(i);
+        if (FULL ? at < width : at + 8 <= width) {
+            Packed<T, 8> p;
+            p.set(v);
+            *reinterpret_cast<Packed<T, 8> *>(row + at) = p;
+        } else if (!FULL && at < width) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at + j < width)
+                    row[at + j] = (T)v[j];
+        }
+    }
+    // Eight factors of a per-channel vector: `none` where there is none.
+    template <class T>
+    __device__ __forceinline__ void factors(const T *p, int i, float none, float (&v)[8]) const
+    {
+        if (p) {
+            load(p, i).floats(v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = none;
+        }
+    }
+    template <class T>
+    __device__ __forceinline__ void modulation(const Modulation &m, bool wide, int b, int i,
+                                               float none, float (&v)[8]) const
+    {
+        if (wide)
+            factors(m.p ? static_cast<const float *>(m.p) + b * m.stride : nullptr, i, none, v);
+        else
+            factors(m.p ? static_cast<const T *>(m.p) + b * m.stride : nullptr, i, none, v);
+    }
+    // v less the mean, zeros past the width.
+    __device__ __forceinline__ void centre(float (&v)[NV][8], float mean) const
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[i][e] -= live(i, e) ? mean : 0.0f;
+    }
+};
+
+// v centred (layer kind), and 1 / deviation.
+template <int TPR, class Cols, int NV>
+__device__ __forceinline__ float normalise(const NormCall &c, const Cols &at, float (&v)[NV][8],
+                                           int &turn)
+{
+    if (c.layer) {
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                s[0] += v[i][e];
+        RowSum<TPR, 1>::run(s, turn);
+        at.centre(v, s[0] * c.inv_width);
+    }
+    float q[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            q[0] += v[i][e] * v[i][e];
+    RowSum<TPR, 1>::run(q, turn);
+    return rsqrtf(q[0] * c.inv_width + c.eps);
+}
+
+template <class T, int TPR, int NV, bool FULL>
+__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCall c)
+{
+    constexpr int GROUPS = TPR == 64 ? 4 : 1;
+    const long long unit =
+        c.first_unit + (long long)blockIdx.x * GROUPS + (int)threadIdx.x / TPR;
+    if (unit >= (long long)c.batch * c.chunks)
+        return;                 // whole waves (TPR 64), or nobody
+    const int b = (int)(unit / c.chunks), s0 = (int)(unit % c.chunks) * c.rows;
+    const int s1 = min(c.tokens, s0 + c.rows);
+    const Columns<TPR, NV, FULL> at{c.width, (int)threadIdx.x % TPR};
+    int turn = 0;
+    float factor[NV][8], shift[NV][8], gate[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float w[8];
+        at.factors(c.weight, i, 1.0f, w);
+        at.template modulation<T>(c.scale, c.wide_mods, b, i, 0.0f, factor[i]);
+        at.template modulation<T>(c.shift, c.wide_mods, b, i, 0.0f, shift[i]);
+        at.template modulation<T>(c.gate, c.wide_mods, b, i, 1.0f, gate[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            factor[i][e] = w[e] * (1.0f + factor[i][e]);
+    }
+    const T *x = static_cast<const T *>(c.x) + b * c.x_stride[0];
+    const T *y = static_cast<const T *>(c.y) + (c.y ? b * c.y_stride[0] : 0);
+    const size_t out = (size_t)b * c.tokens;
+    for (int s = s0; s < s1; ++s) {
+        Packed<T, 8> xr[NV], yr[NV] = {};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            xr[i] = at.load(x + s * c.x_stride[1], i);
+            if (c.y)
+                yr[i] = at.load(y + s * c.y_stride[1], i);
+        }
+        float v[NV][8];
+        if (c.y) {
+            float p[NV][8];
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                yr[i].floats(p[i]);
+            if (c.post_weight) {
+                const float d = normalise<TPR>(c, at, p, turn);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    float w[8];
+                    at.factors(c.post_weight, i, 1.0f, w);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        p[i][e] = p[i][e] * d * w[e];
+                }
+            }
+            T *r = static_cast<T *>(c.r) + (out + s) * c.width;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                xr[i].floats(v[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[i][e] = c.alpha * v[i][e] + gate[i][e] * p[i][e];
+                at.store(r, i, v[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                xr[i].floats(v[i]);
+        }
+        const float d = normalise<TPR>(c, at, v, turn);
+        T *h = static_cast<T *>(c.h) + (out + s) * c.width;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[i][e] = v[i][e] * d * factor[i][e] + shift[i][e];
+            at.store(h, i, v[i]);
+        }
+    }
+}
+
+// Threads of a workgroup of the gradient, and the rows that it has at a time.
+template <int TPR> constexpr int kBackThreads = TPR == 64 ? 512 : TPR;
+
+// A workgroup takes rows of one batch entry, every (chunks * GROUPS)-th for each of
+// its groups, with the sums over tokens in registers; the groups' meet in LDS and
+// the workgroup's go to part[b][chunk], which k_norm_sums adds up in order.  (No
+// atomics: their order would change the sums from run to run.)
+template <class T, int TPR, int NV, bool FULL>
+__global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(NormCall c)
+{
+    constexpr int GROUPS = kBackThreads<TPR> / TPR;
+    const int b = (int)(blockIdx.x / (unsigned)c.chunks), chunk = blockIdx.x % (unsigned)c.chunks;
+    const int group = threadIdx.x / TPR;
+    const Columns<TPR, NV, FULL> at{c.width, (int)threadIdx.x % TPR};
+    int turn = 0;
+    float factor[NV][8], gate[NV][8];
+    float dshift[NV][8] = {}, sum_p[NV][8] = {}, sum_q[NV][8] = {};
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        float w[8];
+        at.factors(c.weight, i, 1.0f, w);
+        at.template modulation<T>(c.scale, c.wide_mods, b, i, 0.0f, factor[i]);
+        at.template modulation<T>(c.gate, c.wide_mods, b, i, 1.0f, gate[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            factor[i][e] = w[e] * (1.0f + factor[i][e]);
+        at.factors(c.post_weight, i, 1.0f, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            gate[i][e] *= w[e];
+    }
+    const T *r = static_cast<const T *>(c.x) + b * c.x_stride[0];
+    const T *y = static_cast<const T *>(c.y) + (c.y ? b * c.y_stride[0] : 0);
+    const T *dh = static_cast<const T *>(c.dh) + b * c.dh_stride[0];
+    const T *dr = static_cast<const T *>(c.dr) + (c.dr ? b * c.dr_stride[0] : 0);
+    const size_t out = (size_t)b * c.tokens;
+    for (int s = chunk * GROUPS + group; s < c.tokens; s += c.chunks * GROUPS) {
+        Packed<T, 8> rr[NV], yr[NV] = {}, dhr[NV], drr[NV] = {};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            rr[i] = at.load(r + s * c.x_stride[1], i);
+            dhr[i] = at.load(dh + s * c.dh_stride[1], i);
+            if (c.y)
+                yr[i] = at.load(y + s * c.y_stride[1], i);
+            if (c.dr)
+                drr[i] = at.load(dr + s * c.dr_stride[1], i);
+        }
+        float n[NV][8], u[NV][8], mean_u = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            rr[i].floats(n[i]);
+            dhr[i].floats(u[i]);
+        }
+        if (c.layer) {
+            float m[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    m[0] += n[i][e];
+                    m[1] += u[i][e] * factor[i][e];
+                }
+            RowSum<TPR, 2>::run(m, turn);
+            at.centre(n, m[0] * c.inv_width);
+            mean_u = m[1] * c.inv_width;
+        }
+        float q[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                q[0] += n[i][e] * n[i][e];
+                q[1] += u[i][e] * factor[i][e] * n[i][e];
+            }
+        RowSum<TPR, 2>::run(q, turn);
+        const float d = rsqrtf(q[0] * c.inv_width + c.eps);
+        const float inner = q[1] * d * c.inv_width;
+        float D[NV][8];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float g[8], o[8];
+            drr[i].floats(g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float ne = n[i][e] * d;
+                dshift[i][e] += u[i][e];
+                sum_p[i][e] += u[i][e] * ne;
+                D[i][e] = g[e] + d * (u[i][e] * factor[i][e] - mean_u - ne * inner);
+                o[e] = c.alpha * D[i][e];
+            }
+            at.store(static_cast<T *>(c.dx) + (out + s) * c.width, i, o);
+        }
+        if (!c.y)
+            continue;
+        float p[NV][8];
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            yr[i].floats(p[i]);
+        T *dy = static_cast<T *>(c.dy) + (out + s) * c.width;
+        if (c.post_weight) {
+            const float dev = normalise<TPR>(c, at, p, turn);
+            float m[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[i][e] *= dev;
+                    sum_q[i][e] += D[i][e] * p[i][e];
+                    D[i][e] *= gate[i][e];
+                    m[0] += at.live(i, e) ? D[i][e] : 0.0f;
+                    m[1] += D[i][e] * p[i][e];
+                }
+            RowSum<TPR, 2>::run(m, turn);
+            const float mean = c.layer ? m[0] * c.inv_width : 0.0f, in = m[1] * c.inv_width;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    p[i][e] = dev * (D[i][e] - mean - p[i][e] * in);
+                at.store(dy, i, p[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sum_q[i][e] += D[i][e] * p[i][e];
+                    D[i][e] *= gate[i][e];
+                }
+                at.store(dy, i, D[i]);
+            }
+        }
+    }
+    if (!c.sums)
+        return;
+    float *part = c.part + (size_t)blockIdx.x * 3 * c.width;
+    if constexpr (GROUPS == 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            at.store(part, i, dshift[i]);
+            at.store(part + c.width, i, sum_p[i]);
+            at.store(part + 2 * c.width, i, sum_q[i]);
+        }
+    } else {
+        constexpr int CH = 8 * TPR * NV;
+        __shared__ __attribute__((aligned(16))) float sum[GROUPS][CH + 4];
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < 8; e += 4) {
+                    const float *v = &(j == 0 ? dshift : j == 1 ? sum_p : sum_q)[i][e];
+                    *reinterpret_cast<float4 *>(&sum[group][at.k(i) + e]) =
+                        make_float4(v[0], v[1], v[2], v[3]);
+                }
+            __syncthreads();
+            for (int k = threadIdx.x; k < c.width; k += kBackThreads<TPR>) {
+                float v = 0.0f;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g)
+                    v += sum[g][k];
+                part[j * c.width + k] = v;
+            }
+        }
+    }
+}
+
+// Adds the workgroups' parts up: a workgroup has 16 channels, 16 slices of the parts
+// side by side, of one batch entry, or (sums.entries of them further) of all entries
+// for what they share.
+constexpr int kSumColumns = 16, kSumSlices = 16;
+
+struct NormSums {
+    int entries;                // with sums of their own: the batch, or 0
+    int blocks;                 // of 16 channels
+    int first;                  // workgroup of the launch
+};
+
+template <class T>
+__global__ void __launch_bounds__(256) k_norm_sums(NormCall c, NormSums sums)
+{
+    const int col = threadIdx.x % kSumColumns, slice = threadIdx.x / kSumColumns;
+    const int unit = sums.first + (int)blockIdx.x, entry = unit / sums.blocks;
+    const int k = unit % sums.blocks * kSumColumns + col;
+    __shared__ float sum[5][kSumSlices][kSumColumns + 1];
+    const bool all = entry == sums.entries, on = k < c.width;
+    const int b0 = all ? 0 : entry, b1 = all ? c.batch : b0 + 1;
+    auto mod = [&](const Modulation &m, int b, float none) {
+        if (!m.p)
+            return none;
+        return c.wide_mods ? static_cast<const float *>(m.p)[b * m.stride + k]
+                           : (float)static_cast<const T *>(m.p)[b * m.stride + k];
+    };
+    // dshift, P, Q, sum_b (1 + scale) P, sum_b g Q
+    float v[5] = {};
+    if (on && c.chunks) {
+        // Entries in turn, or with fewer chunks than slices several side by side.
+        const int step = c.chunks >= kSumSlices ? 1 : kSumSlices / c.chunks;
+        const int per = kSumSlices / step;
+        const int eb = slice / per, first = slice % per;
+        for (int b = eb < step ? b0 + eb : b1; b < b1; b += step) {
+            const float *p = c.part + (size_t)b * c.chunks * 3 * c.width + k;
+            float w[3] = {};
+#pragma unroll 4
+            for (int g = first; g < c.chunks; g += per)
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    w[j] += p[((size_t)g * 3 + j) * c.width];
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                v[j] += w[j];
+            if (all) {
+                v[3] += w[1] * (1.0f + mod(c.scale, b, 0.0f));
+                v[4] += w[2] * mod(c.gate, b, 1.0f);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 5; ++j)
+        sum[j][slice][col] = v[j];
+    __syncthreads();
+    if (slice || !on)
+        return;
+#pragma unroll
+    for (int j = 0; j < 5; ++j) {
+        v[j] = 0.0f;
+#pragma unroll
+        for (int g = 0; g < kSumSlices; ++g)
+            v[j] += sum[j][g][col];
+    }
+    const float w = c.weight ? c.weight[k] : 1.0f, wp = c.post_weight ? c.post_weight[k] : 1.0f;
+    const size_t o = all ? (size_t)k : (size_t)b0 * c.width + k;
+    if (c.dgate && all == ((c.shared & TASQ_SHARED_GATE) != 0))
+        c.dgate[o] = wp * v[2];
+    if (c.dscale && all == ((c.shared & TASQ_SHARED_SCALE) != 0))
+        c.dscale[o] = w * v[1];
+    if (c.dshift && all == ((c.shared & TASQ_SHARED_SHIFT) != 0))
+        c.dshift[o] = v[0];
+    if (all && c.dweight)
+        c.dweight[k] = v[3];
+    if (all && c.dpost)
+        c.dpost[k] = v[4];
+}
+
+hipError_t launch_sums(const NormCall &c, hipStream_t stream)
+{
+    auto of_all = [&](int bit) { return (c.shared & bit) != 0; };
+    const bool each = (c.dgate && !of_all(TASQ_SHARED_GATE)) ||
+                      (c.dscale && !of_all(TASQ_SHARED_SCALE)) ||
+                      (c.dshift && !of_all(TASQ_SHARED_SHIFT));
+    const bool all = c.dweight || c.dpost || (c.dgate && of_all(TASQ_SHARED_GATE)) ||
+                     (c.dscale && of_all(TASQ_SHARED_SCALE)) ||
+                     (c.dshift && of_all(TASQ_SHARED_SHIFT));
+    NormSums s;
+    s.entries = each ? c.batch : 0;
+    s.blocks = (c.width + kSumColumns - 1) / kSumColumns;
+    const int units = (s.entries + (all ? 1 : 0)) * s.blocks;
+    constexpr int MOST = 1 << 22;
+    for (s.first = 0; s.first < units; s.first += MOST) {
+        const unsigned grid = (unsigned)(units - s.first < MOST ? units - s.first : MOST);
+        const hipError_t e = with_type(c.type, [&](auto zero) {
+            k_norm_sums<decltype(zero)><<<grid, 256, 0, stream>>>(c, s);
+            return hipGetLastError();
+        });
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
+}
+
+// Rows of a run in the forward pass: the modulations are read once for each run.
+int run_of(const NormCall &c)
+{
+    const long long rows = (long long)c.batch * c.tokens;
+    return rows >= 4 * 4096 ? 4 : rows >= 2 * 4096 ? 2 : 1;
+}
+
+template <class T, int TPR, int NV, bool FULL> hipError_t forward(NormCall c, hipStream_t stream)
+{
+    constexpr int GROUPS = TPR == 64 ? 4 : 1;
+    const long long units = (long long)c.batch * c.chunks;
+    constexpr long long MOST = 1 << 20;         // workgroups of a launch
+    for (c.first_unit = 0; c.first_unit < units; c.first_unit += MOST * GROUPS) {
+        const long long left = (units - c.first_unit + GROUPS - 1) / GROUPS;
+        k_residual_norm<T, TPR, NV, FULL>
+            <<<(unsigned)(left < MOST ? left : MOST), TPR == 64 ? 256 : TPR, 0, stream>>>(c);
+        if (hipError_t e = hipGetLastError())
+            return e;
+    }
+    return hipSuccess;
+}
+
+template <class T, bool FULL> hipError_t forward_width(const NormCall &c, hipStream_t stream)
+{
+    if (c.width <= 512)
+        return forward<T, 64, 1, FULL>(c, stream);
+    if (c.width <= 1024)
+        return forward<T, 64, 2, FULL>(c, stream);
+    if (c.width <= 1536)
+        return forward<T, 64, 3, FULL>(c, stream);
+    if (c.width <= 2048)
+        return forward<T, 256, 1, FULL>(c, stream);
+    if (c.width <= 4096)
+        return forward<T, 256, 2, FULL>(c, stream);
+    if (c.width <= 8192)
+        return forward<T, 512, 2, FULL>(c, stream);
+    return forward<T, 1024, 2, FULL>(c, stream);
+}
+
+template <class T, int TPR, int NV, bool FULL>
+hipError_t backward(const NormCall &c, hipStream_t stream)
+{
+    k_residual_norm_backward<T, TPR, NV, FULL>
+        <<<(unsigned)(c.batch * c.chunks), kBackThreads<TPR>, 0, stream>>>(c);
+    return hipGetLastError();
+}
+
+template <class T, bool FULL> hipError_t backward_width(const NormCall &c, hipStream_t stream)
+{
+    if (c.width <= 512)
+        return backward<T, 64, 1, FULL>(c, stream);
+    if (c.width <= 1024)
+        return backward<T, 64, 2, FULL>(c, stream);
+    if (c.width <= 1536)
+        return backward<T, 64, 3, FULL>(c, stream);
+    if (c.width <= 2048)
+        return backward<T, 256, 1, FULL>(c, stream);
+    if (c.width <= 4096)
+        return backward<T, 256, 2, FULL>(c, stream);
+    if (c.width <= 8192)
+        return backward<T, 512, 2, FULL>(c, stream);
+    return backward<T, 512, 4, FULL>(c, stream);
+}
+
+}  // namespace
+
+int residual_norm_chunks(int batch, int tokens, int width)
+{
+    const int groups = width <= 1536 ? 8 : 1;
+    const int want = ((width <= 1536 ? 256 : 512) + batch - 1) / (batch > 0 ? batch : 1);
+    const int most = (tokens + groups - 1) / groups;
+    return most < 1 ? 1 : want < most ? want : most;
+}
+
+hipError_t launch_residual_norm(const NormCall &in, hipStream_t stream)
+{
+    NormCall c = in;
+    c.inv_width = 1.0f / (float)c.width;
+    c.rows = run_of(c);
+    c.chunks = (c.tokens + c.rows - 1) / c.rows;
+    return with_type(c.type, [&](auto zero) {
+        using T = decltype(zero);
+        return c.width % 8 == 0 ? forward_width<T, true>(c, stream)
+                                : forward_width<T, false>(c, stream);
+    });
+}
+
+hipError_t launch_residual_norm_backward(const NormCall &in, hipStream_t stream)
+{
+    NormCall c = in;
+    c.inv_width = 1.0f / (float)c.width;
+    if (c.batch && c.tokens) {
+        c.chunks = residual_norm_chunks(c.batch, c.tokens, c.width);
+        const hipError_t e = with_type(c.type, [&](auto zero) {
+            using T = decltype(zero);
+            return c.width % 8 == 0 ? backward_width<T, true>(c, stream)
+                                    : backward_width<T, false>(c, stream);
+        });
+        if (e != hipSuccess)
+            return e;
+    } else {
+        c.chunks = 0;           // sums of nothing
+    }
+    return c.sums ? launch_sums(c, stream) : hipSuccess;
+}
+
+}  // namespace tasq
