@@ -817,6 +817,41 @@ int tasq_residual_norm(const tasq_residual *a, void *stream);
 int tasq_residual_norm_backward(const tasq_residual *a, void *stream);
 size_t tasq_residual_norm_workspace_bytes(int batch, int tokens, int width);
 
+/*
+ * Microscaled 4-bit floating-point codes (e2m1 elements with an e8m0 scale for each
+ * 32 neighbours of a row, as the OCP Microscaling Formats specification v1.0 has
+ * them and converts to them):
+ *   e = floor(log2(max |x|)) - 2 over the block, at least -127;
+ *   the block's scale byte is e + 127 and stands for 2^e,
+ *   an element's code stands for 0, .5, 1, 1.5, 2, 3, 4 or 6 (codes 0..7; 8..15 their
+ *   negatives), the nearest to x 2^-e, ties to the even code, 6 for what is beyond.
+ * A block of zeros has scale 0.  A block with a NaN or an infinity has the scale byte
+ * 255, NaN: no output of a product with it is finite.  Rows are filled up with zeros
+ * to K' = K rounded up to a multiple of 128 elements:
+ *   x         [M][K] of x_type, row m at x + m * x_stride, any alignment of elements;
+ *   codes_out uint8 [M][K' / 2], element 2 i in the low half of byte i; 16-byte aligned;
+ *   scales_out uint8 [M][K' / 32]; 4-byte aligned.
+ * Weights are quantized by the same call, once.  M == 0 or K == 0 enqueues nothing.
+ * Errors: TASQ_ERR_NULL, _DIM (a negative size, M > 2^30, x_stride < K), _OVERFLOW (K >
+ * TASQ_MAX_K), _KIND, _ALIGN, _HIP.
+ */
+int tasq_quantize_mx4(const void *x, int x_type, int M, int K, long long x_stride,
+                      uint8_t *codes_out, uint8_t *scales_out, void *stream);
+
+/*
+ * The linear on them, K a multiple of 128 (the K' above):
+ *   y[m][n] = sum over blocks of 2^(ex + ew) (sum over the block of x w) + bias[n],
+ * the products exact, sums fp32, y rounded once to y_type.  X [M][K / 2] with scales
+ * sx [M][K / 32], W [N][K / 2] with sw [N][K / 32], bias fp32 [N] or NULL, y_out
+ * [M][N], all contiguous; X and W 16-byte aligned, sx and sw 4-byte aligned.  M == 0
+ * or N == 0 enqueues nothing; K == 0 gives the bias.  Errors: TASQ_ERR_NULL, _DIM (a
+ * negative size, M or N > 2^30, K not a multiple of 128), _OVERFLOW (K > TASQ_MAX_K +
+ * 1), _KIND, _ALIGN, _HIP.
+ */
+int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const uint8_t *sw,
+                    const float *bias, int M, int N, int K, void *y_out, int y_type,
+                    void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -65,6 +65,7 @@ EXPORTS = (
     "tasq_norm_rotate", "tasq_norm_rotate_backward", "tasq_norm_rotate_workspace_bytes",
     "tasq_attention_forward", "tasq_attention_backward", "tasq_attention_workspace_bytes",
     "tasq_residual_norm", "tasq_residual_norm_backward", "tasq_residual_norm_workspace_bytes",
+    "tasq_quantize_mx4", "tasq_linear_mx4",
 )
 
 
@@ -247,6 +248,10 @@ def lib() -> ctypes.CDLL:
             f.restype = i32
         L.tasq_residual_norm_workspace_bytes.argtypes = [i32, i32, i32]
         L.tasq_residual_norm_workspace_bytes.restype = size
+        L.tasq_quantize_mx4.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
+        L.tasq_quantize_mx4.restype = i32
+        L.tasq_linear_mx4.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, i32, vp]
+        L.tasq_linear_mx4.restype = i32
         L.tasq_status_string.argtypes = [i32]
         L.tasq_status_string.restype = ctypes.c_char_p
         _lib = L

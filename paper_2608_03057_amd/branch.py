@@ -1,5 +1,6 @@
 """Torch-facing wrappers of what stands around a block's quantized linears
-(argument marshalling only): the residual stream's norm with its gradient.
+(argument marshalling only): the residual stream's norm with its gradient, linears
+on 4-bit microscaled codes.
 
 As in ``block``: tensors are checked, pointers and the current stream go to the
 C ABI of ``include/tasq.h``, an error raises ``TasqError``, the work is
@@ -170,3 +171,59 @@ def residual_norm_backward(dh: torch.Tensor, dr: Optional[torch.Tensor], r: torc
         check(rc, "tasq_residual_norm_backward")
     dgate, dscale, dshift, dweight, dpost = grads
     return ResidualGrads(dx, dy, dgate, dweight, dscale, dshift, dpost)
+
+
+def quantize_mx4(x: torch.Tensor, out: Optional[torch.Tensor] = None,
+                 scales: Optional[torch.Tensor] = None):
+    """(codes uint8 [M, K'/2], scales uint8 [M, K'/32]) of activations or a weight x
+    [M, K] of any floating type, rows at any stride: 4-bit floating-point codes
+    (e2m1), the even element of a pair in the low half, with one power of two for
+    each 32 of a row (exponent + 127), K' = K rounded up to a multiple of 128 with
+    zeros."""
+    M, K = shape = x.shape
+    if M > _MOST or K > _MOST:
+        raise _too_large(M, K)
+    st = _strided(x, x.dtype, shape, "x")
+    _here(x, "x")
+    whole = (K + 127) // 128
+    if out is None:
+        out = torch.empty_strided((M, 64 * whole), (64 * whole, 1), dtype=torch.uint8,
+                                  device=x.device)
+    else:
+        _need(out, torch.uint8, (M, 64 * whole), "out")
+    if scales is None:
+        scales = torch.empty_strided((M, 4 * whole), (4 * whole, 1), dtype=torch.uint8,
+                                     device=x.device)
+    else:
+        _need(scales, torch.uint8, (M, 4 * whole), "scales")
+    rc = _lib.lib().tasq_quantize_mx4(x.data_ptr(), _type(x, "x"), M, K, st[0], out.data_ptr(),
+                                      scales.data_ptr(), _stream())
+    if rc:
+        check(rc, "tasq_quantize_mx4")
+    return out, scales
+
+
+def linear_mx4(X: torch.Tensor, sx: torch.Tensor, W: torch.Tensor, sw: torch.Tensor,
+               bias: Optional[torch.Tensor] = None, *, out_dtype: torch.dtype = torch.bfloat16,
+               y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [M, N] = x w^T + bias of what quantize_mx4 gave for activations (X, sx) and,
+    once, for a weight [N, K] (W, sw); bias fp32 [N]."""
+    M, half = X.shape
+    N = W.shape[0]
+    if M > _MOST or N > _MOST or half > _MOST // 2:
+        raise _too_large(M, N, 2 * half)
+    _need(X, torch.uint8, (M, half), "X")
+    _need(W, torch.uint8, (N, half), "W")
+    _need(sx, torch.uint8, (M, half // 16), "sx")
+    _need(sw, torch.uint8, (N, half // 16), "sw")
+    _here(X, "X")
+    if y is None:
+        y = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=X.device)
+    else:
+        _need(y, y.dtype, (M, N), "y")
+    rc = _lib.lib().tasq_linear_mx4(X.data_ptr(), sx.data_ptr(), W.data_ptr(), sw.data_ptr(),
+                                    _at(bias, torch.float32, (N,), "bias"), M, N, 2 * half,
+                                    y.data_ptr(), _type(y, "y"), _stream())
+    if rc:
+        check(rc, "tasq_linear_mx4")
+    return y

@@ -48,6 +48,8 @@ SOURCES = [
     "attn_bwd_f16.hip",
     "block_api.cpp",
     "residual_norm.hip",
+    "mx4_quant.hip",
+    "mx4_gemm.hip",
     "branch_api.cpp",
     "cost.cpp",
     "tasq_api.cpp",

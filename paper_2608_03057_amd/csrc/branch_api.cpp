@@ -152,4 +152,44 @@ size_t tasq_residual_norm_workspace_bytes(int batch, int tokens, int width)
            (size_t)width * sizeof(float);
 }
 
+int tasq_quantize_mx4(const void *x, int x_type, int M, int K, long long x_stride,
+                      uint8_t *codes_out, uint8_t *scales_out, void *stream)
+{
+    if (!type_known(x_type))
+        return TASQ_ERR_KIND;
+    if (M < 0 || M > kMostRows || K < 0 || (M > 1 && x_stride < K))
+        return TASQ_ERR_DIM;
+    if (K > TASQ_MAX_K)
+        return TASQ_ERR_OVERFLOW;
+    if (M == 0 || K == 0)
+        return TASQ_OK;
+    if (!x || !codes_out || !scales_out)
+        return TASQ_ERR_NULL;
+    if (!aligned_to(x, (size_t)tasq::type_bytes(x_type)) || !aligned_to(codes_out, 16) ||
+        !aligned_to(scales_out, 4))
+        return TASQ_ERR_ALIGN;
+    return status(tasq::launch_quantize_mx4(x, x_type, M, K, M > 1 ? x_stride : K, codes_out,
+                                            scales_out, static_cast<hipStream_t>(stream)));
+}
+
+int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const uint8_t *sw,
+                    const float *bias, int M, int N, int K, void *y_out, int y_type, void *stream)
+{
+    if (!type_known(y_type))
+        return TASQ_ERR_KIND;
+    if (M < 0 || M > kMostRows || N < 0 || N > kMostRows || K < 0 || K % 128)
+        return TASQ_ERR_DIM;
+    if (K > TASQ_MAX_K + 1)
+        return TASQ_ERR_OVERFLOW;
+    if (M == 0 || N == 0)
+        return TASQ_OK;
+    if (!y_out || (K > 0 && (!X || !sx || !W || !sw)))
+        return TASQ_ERR_NULL;
+    if (!aligned_to(X, 16) || !aligned_to(W, 16) || !aligned_to(sx, 4) || !aligned_to(sw, 4) ||
+        !aligned_to(bias, 4) || !aligned_to(y_out, (size_t)tasq::type_bytes(y_type)))
+        return TASQ_ERR_ALIGN;
+    tasq::Mx4Linear a{X, sx, W, sw, bias, y_out, M, N, K / 128, y_type};
+    return status(tasq::launch_mx4_linear(a, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

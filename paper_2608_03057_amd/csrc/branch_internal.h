@@ -38,4 +38,16 @@ hipError_t launch_residual_norm_backward(const NormCall &c, hipStream_t stream);
 // Workgroups of the gradient for each batch entry.
 int residual_norm_chunks(int batch, int tokens, int width);
 
+// 4-bit microscaled codes (mx4_quant.hip) and the linear on them (mx4_gemm.hip): rows
+// of K128 * 128 elements, 64 bytes of codes and four scales each 128.
+hipError_t launch_quantize_mx4(const void *x, int type, int M, int K, long long stride,
+                               uint8_t *codes, uint8_t *scales, hipStream_t stream);
+struct Mx4Linear {
+    const uint8_t *X, *sx, *W, *sw;
+    const float *bias;
+    void *y;
+    int M, N, K128, type;
+};
+hipError_t launch_mx4_linear(const Mx4Linear &a, hipStream_t stream);
+
 }  // namespace tasq

@@ -151,7 +151,59 @@ def test_residual_norm_workspace_bytes():
         assert size(*no) == 0
 
 
+def quantize_mx4(x=FAKE, t=BF16, M=4, K=32, stride=32, q=FAKE, s=FAKE):
+    return L.tasq_quantize_mx4(x, t, M, K, stride, q, s, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(x=None), NULL), (dict(q=None), NULL), (dict(s=None), NULL),
+    (dict(M=-1), DIM), (dict(K=-1), DIM), (dict(stride=31), DIM), (dict(M=(1 << 30) + 1), DIM),
+    (dict(K=_lib.TASQ_MAX_K + 1, stride=1 << 20), OVERFLOW),
+    (dict(t=3), KIND), (dict(t=-1), KIND),
+    (dict(x=FAKE + 1), ALIGN), (dict(x=FAKE + 2, t=F32), ALIGN), (dict(q=FAKE + 8), ALIGN),
+    (dict(s=FAKE + 2), ALIGN),
+])
+def test_quantize_mx4_rejects(kw, code):
+    assert quantize_mx4(**kw) == code
+
+
+def linear_mx4(X=FAKE, sx=FAKE, W=FAKE, sw=FAKE, bias=None, M=4, N=4, K=128, y=FAKE, t=BF16):
+    return L.tasq_linear_mx4(X, sx, W, sw, bias, M, N, K, y, t, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(X=None), NULL), (dict(W=None), NULL), (dict(sx=None), NULL), (dict(sw=None), NULL),
+    (dict(y=None), NULL), (dict(K=0, y=None), NULL),
+    (dict(M=-1), DIM), (dict(N=-1), DIM), (dict(K=-128), DIM), (dict(K=96), DIM),
+    (dict(M=(1 << 30) + 1), DIM), (dict(N=(1 << 30) + 1), DIM),
+    (dict(K=_lib.TASQ_MAX_K + 129), OVERFLOW), (dict(t=7), KIND),
+    (dict(X=FAKE + 8), ALIGN), (dict(W=FAKE + 8), ALIGN), (dict(sx=FAKE + 2), ALIGN),
+    (dict(sw=FAKE + 1), ALIGN), (dict(bias=FAKE + 2), ALIGN), (dict(y=FAKE + 1), ALIGN),
+    (dict(y=FAKE + 2, t=F32), ALIGN),
+])
+def test_linear_mx4_rejects(kw, code):
+    assert linear_mx4(**kw) == code
+
+
+def test_mx4_of_nothing_is_noop():
+    assert quantize_mx4(M=0, x=None, q=None, s=None) == quantize_mx4(K=0, x=None, stride=0) == 0
+    assert linear_mx4(M=0, X=None, y=None) == linear_mx4(N=0, W=None, y=None) == 0
+
+
 # --------------------------------------------------------------------- wrappers
+
+def test_mx4_wrappers_refuse():
+    x, u = torch.zeros(4, 128), torch.zeros(4, 64, dtype=torch.uint8)
+    for call in (lambda: T.quantize_mx4(x), lambda: T.linear_mx4(u, u, u, u)):
+        with pytest.raises(ValueError, match="GPU tensor"):
+            call()
+    for shape in (((1 << 32) + 3, 1), (1, (1 << 32) + 3)):
+        with pytest.raises(ValueError, match="below 2\\^31"):
+            T.quantize_mx4(torch.empty(1).expand(*shape))
+        with pytest.raises(ValueError, match="below 2\\^31"):
+            big = torch.empty(1, dtype=torch.uint8).expand(*shape)
+            T.linear_mx4(big, big, big, big)
+
 
 def test_residual_wrappers_refuse():
     x = torch.zeros(2, 5, 72)
