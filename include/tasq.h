@@ -852,6 +852,36 @@ int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const
                     const float *bias, int M, int N, int K, void *y_out, int y_type,
                     void *stream);
 
+/*
+ * Gradient of tasq_masked_linear_tokens (its output's type being `type`), with the
+ * codes that it took as the activations' checkpoint in 8 bits:
+ *   dx[m][k] = sum_n dy[m][n] sw[n] W_b[n][k],
+ *   dw[n][k] = sum_m dy[m][n] sx[m] X[m][k],   dbias[n] = sum_m dy[m][n].
+ * dx is the gradient of the activations and dw that of the weight sw W_b, both straight
+ * through their rounding to codes; the gradient of sw[n] is sum_k dw[n][k] W_b[n][k].
+ * The 8-bit operand times its factor is rounded to `type` for the product (in half the
+ * factors of a sum are first divided by a power of two near their largest), sums are
+ * fp32 and in a fixed order (the same bits each time), results are rounded once.
+ *   dy        [M][N] of type (BF16 or F16), row m at dy + m * dy_stride
+ *   dx        [M][K] of type, dw [N][K] of type, dbias fp32 [N], contiguous; NULL: not
+ *             wanted.  dbias needs dw (TASQ_ERR_NULL).  X and sx are read for dw only,
+ *             W and sw for dx only, and may else be NULL.
+ *   workspace 256-byte aligned device scratch or NULL.  With
+ *             tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K) bytes, long sums
+ *             of small results are cut into ranges that run side by side; a smaller one
+ *             runs them uncut.
+ * N and dy_stride multiples of 8, K of 16 and 16-byte aligned dy, X and W take whole
+ * vector loads.  Sums of nothing are zeros.  Errors: TASQ_ERR_NULL, _DIM (a negative
+ * size, M or N > 2^30, dy_stride < N), _BITS, _OVERFLOW (K > TASQ_MAX_K), _KIND, _ALIGN,
+ * _HIP.
+ */
+int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_stride,
+                                       const int8_t *X, const float *sx, const int8_t *W,
+                                       const float *sw, int M, int N, int K, int b, void *dx,
+                                       void *dw, float *dbias, void *workspace,
+                                       size_t workspace_bytes, void *stream);
+size_t tasq_masked_linear_tokens_backward_workspace_bytes(int M, int N, int K);
+
 #ifdef __cplusplus
 }
 #endif

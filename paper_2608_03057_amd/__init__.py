@@ -20,7 +20,8 @@ from .block import (  # noqa: F401
 )
 from .branch import (  # noqa: F401
     residual_norm, residual_norm_backward, residual_norm_workspace_bytes, ResidualGrads,
-    quantize_mx4, linear_mx4,
+    quantize_mx4, linear_mx4, masked_linear_tokens_backward,
+    masked_linear_tokens_backward_workspace_bytes,
 )
 from ._lib import (  # noqa: F401
     TasqError, VARIANT_AUTO, VARIANT_MASKED_I8, VARIANT_BITPLANE, VARIANT_PACKED, KIND_LINEAR,

@@ -65,7 +65,8 @@ EXPORTS = (
     "tasq_norm_rotate", "tasq_norm_rotate_backward", "tasq_norm_rotate_workspace_bytes",
     "tasq_attention_forward", "tasq_attention_backward", "tasq_attention_workspace_bytes",
     "tasq_residual_norm", "tasq_residual_norm_backward", "tasq_residual_norm_workspace_bytes",
-    "tasq_quantize_mx4", "tasq_linear_mx4",
+    "tasq_quantize_mx4", "tasq_linear_mx4", "tasq_masked_linear_tokens_backward",
+    "tasq_masked_linear_tokens_backward_workspace_bytes",
 )
 
 
@@ -252,6 +253,11 @@ def lib() -> ctypes.CDLL:
         L.tasq_quantize_mx4.restype = i32
         L.tasq_linear_mx4.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, i32, vp]
         L.tasq_linear_mx4.restype = i32
+        L.tasq_masked_linear_tokens_backward.argtypes = [vp, i32, i64, vp, vp, vp, vp, i32, i32,
+                                                         i32, i32, vp, vp, vp, vp, size, vp]
+        L.tasq_masked_linear_tokens_backward.restype = i32
+        L.tasq_masked_linear_tokens_backward_workspace_bytes.argtypes = [i32, i32, i32]
+        L.tasq_masked_linear_tokens_backward_workspace_bytes.restype = size
         L.tasq_status_string.argtypes = [i32]
         L.tasq_status_string.restype = ctypes.c_char_p
         _lib = L

@@ -1,6 +1,6 @@
 """Torch-facing wrappers of what stands around a block's quantized linears
 (argument marshalling only): the residual stream's norm with its gradient, linears
-on 4-bit microscaled codes.
+on 4-bit microscaled codes, the gradient of the token-scaled linear.
 
 As in ``block``: tensors are checked, pointers and the current stream go to the
 C ABI of ``include/tasq.h``, an error raises ``TasqError``, the work is
@@ -227,3 +227,65 @@ def linear_mx4(X: torch.Tensor, sx: torch.Tensor, W: torch.Tensor, sw: torch.Ten
     if rc:
         check(rc, "tasq_linear_mx4")
     return y
+
+
+def masked_linear_tokens_backward_workspace_bytes(M: int, N: int, K: int) -> int:
+    """Workspace with which masked_linear_tokens_backward of these sizes runs ranges
+    of a long sum side by side."""
+    return _lib.lib().tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K)
+
+
+def masked_linear_tokens_backward(dy: torch.Tensor, X: torch.Tensor, W: torch.Tensor,
+                                  sx: torch.Tensor, sw: torch.Tensor, b: int, *,
+                                  need_input: bool = True, need_weight: bool = True,
+                                  dx: Optional[torch.Tensor] = None,
+                                  dw: Optional[torch.Tensor] = None,
+                                  dbias: Optional[torch.Tensor] = None,
+                                  workspace: Optional[torch.Tensor] = None):
+    """Gradients (dx [M, K], dw [N, K], dbias fp32 [N]) of masked_linear_tokens from
+    that of its output, dy [M, N] bfloat16 or half with rows at any stride, and its
+    arguments: the codes X with their scales sx are all that the program keeps of the
+    activations.  dx is the gradient of the activations, dw that of the weight
+    sw[n] W_b, both in dy's type and straight through the rounding to codes; the
+    gradient of sw is (dw * W_b).sum(1).  need_input=False leaves dx out (None),
+    need_weight=False dw and dbias."""
+    M, N = shape = dy.shape
+    K = W.shape[1]
+    if M > _MOST or N > _MOST or K > _MOST:
+        raise _too_large(M, N, K)
+    dtype = dy.dtype
+    if dtype != torch.bfloat16 and dtype != torch.float16:
+        raise ValueError(f"dy must be bfloat16 or float16, got {dtype}")
+    st = _strided(dy, dtype, shape, "dy")
+    _here(dy, "dy")
+    _need(X, torch.int8, (M, K), "X")
+    _need(W, torch.int8, (N, K), "W")
+    _need(sx, torch.float32, (M,), "sx")
+    _need(sw, torch.float32, (N,), "sw")
+
+    def grad(t, wanted, shape, dtype, name):
+        if not wanted:
+            return None, 0
+        if t is None:
+            t = torch.empty(shape, dtype=dtype, device=dy.device)
+        else:
+            _need(t, dtype, shape, name)
+        return t, t.data_ptr()
+    dx, xat = grad(dx, need_input, (M, K), dtype, "dx")
+    dw, wat = grad(dw, need_weight, (N, K), dtype, "dw")
+    dbias, bat = grad(dbias, need_weight, (N,), torch.float32, "dbias")
+    L = _lib.lib()
+    if workspace is None:
+        nbytes = L.tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    at = 0
+    if nbytes:
+        workspace = _workspace(workspace, nbytes, dy.device, "masked_linear_tokens_backward")
+        at = workspace.data_ptr()
+    rc = L.tasq_masked_linear_tokens_backward(dy.data_ptr(), _type(dy, "dy"), st[0], X.data_ptr(),
+                                              sx.data_ptr(), W.data_ptr(), sw.data_ptr(), M, N, K,
+                                              int(b), xat, wat, bat, at, nbytes, _stream())
+    if rc:
+        check(rc, "tasq_masked_linear_tokens_backward")
+    return dx, dw, dbias

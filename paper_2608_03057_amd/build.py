@@ -50,6 +50,8 @@ SOURCES = [
     "residual_norm.hip",
     "mx4_quant.hip",
     "mx4_gemm.hip",
+    "token_grad_bf16.hip",
+    "token_grad_f16.hip",
     "branch_api.cpp",
     "cost.cpp",
     "tasq_api.cpp",

@@ -130,6 +130,52 @@ int residual_norm(const tasq_residual *a, bool grad, void *stream)
                        : tasq::launch_residual_norm(c, st));
 }
 
+constexpr size_t round256(size_t v) { return (v + 255) / 256 * 256; }
+
+// Tiles and ranges of a product [R][C] over Z, and the bytes of its workspace.
+size_t plan_grad(tasq::GradJob &g, bool bias, bool cut)
+{
+    const int steps = (int)((g.Z + 63LL) / 64);
+    auto tiles = [&](int t) { return ((g.R + t - 1LL) / t) * ((g.C + t - 1LL) / t); };
+    g.tile = 64;
+    g.splits = 1;
+    for (const int t : {256, 128, 64}) {
+        const long long n = tiles(t);
+        long long s = n > 0 && cut ? 256 / n : 1;
+        s = s < 1 ? 1 : s > steps / 8 ? (steps / 8 > 1 ? steps / 8 : 1) : s;
+        g.tile = t;
+        g.splits = (int)s;
+        if (n * s >= 128)
+            break;
+    }
+    g.tiles_r = (int)((g.R + g.tile - 1LL) / g.tile);
+    g.tiles_c = (int)((g.C + g.tile - 1LL) / g.tile);
+    if (bias && g.tiles_c == 0)
+        g.tiles_c = 1;          // the rows' sums alone
+    g.split_steps = (steps + g.splits - 1) / g.splits;
+    if (g.split_steps > 0)
+        g.splits = (steps + g.split_steps - 1) / g.split_steps;
+    if (g.splits <= 1)
+        return 0;
+    return round256((size_t)g.splits * g.R * g.C * sizeof(float)) +
+           round256((size_t)g.splits * g.R * sizeof(float));
+}
+
+// The two products: of dx (turned false) and of dw.
+tasq::GradJob grad_job(int M, int N, int K, bool turned)
+{
+    tasq::GradJob g{};
+    g.R = turned ? N : M;
+    g.Z = turned ? M : N;
+    g.C = K;
+    return g;
+}
+
+bool grad_sizes(int M, int N, int K)
+{
+    return M >= 0 && M <= kMostRows && N >= 0 && N <= kMostRows && K >= 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -190,6 +236,73 @@ int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const
         return TASQ_ERR_ALIGN;
     tasq::Mx4Linear a{X, sx, W, sw, bias, y_out, M, N, K / 128, y_type};
     return status(tasq::launch_mx4_linear(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t tasq_masked_linear_tokens_backward_workspace_bytes(int M, int N, int K)
+{
+    if (!grad_sizes(M, N, K) || K > TASQ_MAX_K)
+        return 0;
+    size_t most = 0;
+    for (const bool turned : {false, true}) {
+        tasq::GradJob g = grad_job(M, N, K, turned);
+        const size_t bytes = plan_grad(g, turned, true);
+        most = bytes > most ? bytes : most;
+    }
+    return most;
+}
+
+int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_stride,
+                                       const int8_t *X, const float *sx, const int8_t *W,
+                                       const float *sw, int M, int N, int K, int b, void *dx,
+                                       void *dw, float *dbias, void *workspace,
+                                       size_t workspace_bytes, void *stream)
+{
+    if (type != TASQ_TYPE_BF16 && type != TASQ_TYPE_F16)
+        return TASQ_ERR_KIND;
+    if (!grad_sizes(M, N, K) || (M > 1 && dy_stride < N))
+        return TASQ_ERR_DIM;
+    if (K > TASQ_MAX_K)
+        return TASQ_ERR_OVERFLOW;
+    if (b < 1 || b > 8)
+        return TASQ_ERR_BITS;
+    if (!dw && dbias && N > 0 && K > 0)
+        return TASQ_ERR_NULL;
+    const bool want_x = dx && M > 0 && K > 0, want_w = (dw && N > 0 && K > 0) || (dbias && N > 0);
+    if (!want_x && !want_w)
+        return TASQ_OK;
+    if (M > 0 && N > 0 && (!dy || (want_x && (!W || !sw)) || (want_w && K > 0 && (!X || !sx))))
+        return TASQ_ERR_NULL;
+    if (!aligned_to(dy, 2) || !aligned_to(dx, 2) || !aligned_to(dw, 2) || !aligned_to(dbias, 4) ||
+        !aligned_to(sx, 4) || !aligned_to(sw, 4) || !aligned_to(workspace, 256))
+        return TASQ_ERR_ALIGN;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const size_t have = workspace ? workspace_bytes : 0;
+    for (const bool turned : {false, true}) {
+        if (!(turned ? want_w : want_x))
+            continue;
+        tasq::GradJob g = grad_job(M, N, K, turned);
+        g.A = dy;
+        g.a_stride = M > 1 ? dy_stride : N;
+        g.Q = turned ? X : W;
+        g.s = turned ? sx : sw;
+        g.mask = turned ? 0xffffffffu : tasq::keep_mask_dword(b);
+        g.out = turned ? dw : dx;
+        g.dbias = turned ? dbias : nullptr;
+        if (plan_grad(g, g.dbias, true) > have)
+            plan_grad(g, g.dbias, false);
+        if (g.splits > 1) {
+            g.part = static_cast<float *>(workspace);
+            g.bias_part = g.part + round256((size_t)g.splits * g.R * g.C * sizeof(float)) / 4;
+        }
+        // (Offsets within a tile of A are 32-bit.)
+        const bool whole = N % 8 == 0 && g.a_stride % 8 == 0 && K % 16 == 0 &&
+                           aligned_to(dy, 16) && aligned_to(g.Q, 16) && g.a_stride < (1 << 22);
+        const hipError_t e = type == TASQ_TYPE_BF16 ? tasq::token_grad_bf16(g, turned, whole, st)
+                                                    : tasq::token_grad_f16(g, turned, whole, st);
+        if (e != hipSuccess)
+            return TASQ_ERR_HIP;
+    }
+    return TASQ_OK;
 }
 
 }  // extern "C"

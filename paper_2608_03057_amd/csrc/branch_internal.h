@@ -50,4 +50,22 @@ struct Mx4Linear {
 };
 hipError_t launch_mx4_linear(const Mx4Linear &a, hipStream_t stream);
 
+// One product of the token-scaled linear's gradient (token_grad.h):
+// out[r][c] = sum_z A(r, z) s[z] Q[z][c], A [R][Z], or [Z][R] turned.
+struct GradJob {
+    const void *A;
+    long long a_stride;
+    const int8_t *Q;            // [Z][C]
+    const float *s;             // [Z]
+    uint32_t mask;              // of four codes
+    void *out;                  // [R][C]
+    float *dbias;               // [R], turned only, or null
+    int R, Z, C;
+    int tile, tiles_r, tiles_c;         // 64, 128 or 256 rows and columns
+    int splits, split_steps;            // ranges of Z, in steps of 64
+    float *part, *bias_part;            // [splits][R][C], [splits][R]
+};
+hipError_t token_grad_bf16(const GradJob &g, bool turned_a, bool whole, hipStream_t stream);
+hipError_t token_grad_f16(const GradJob &g, bool turned_a, bool whole, hipStream_t stream);
+
 }  // namespace tasq

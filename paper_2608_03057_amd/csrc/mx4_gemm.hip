@@ -12,13 +12,13 @@
 #include "branch_internal.h"
 #include "floats.h"
 #include "gemm_core.h"
+#include "tile_out.h"
 
 namespace tasq {
 
 namespace {
 
 typedef int v8i_t __attribute__((ext_vector_type(8)));
-typedef float v16f_t __attribute__((ext_vector_type(16)));
 typedef float v4f_t __attribute__((ext_vector_type(4)));
 
 constexpr int kFp4 = 4;         // the instruction's name for e2m1
@@ -33,21 +33,6 @@ __device__ __forceinline__ v16f_t mfma_mx4(v4i a, v4i b, v16f_t c, uint32_t sa, 
 {
     return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(a), operand(b), c, kFp4, kFp4,
                                                            STEP, (int)sa, STEP, (int)sb);
-}
-
-// A value that is the same in all lanes, in a scalar register.
-__device__ __forceinline__ uint32_t uniform(int v)
-{
-    return (uint32_t)__builtin_amdgcn_readfirstlane(v);
-}
-
-// Lane l's 16 bytes at `off` of the buffer to lds + 16 l; zeros out of bounds.
-__device__ __forceinline__ void load_to_lds(rsrc_t r, char *lds, uint32_t off)
-{
-#ifdef __HIP_DEVICE_COMPILE__       // the host pass knows no 16-byte form
-    typedef __attribute__((address_space(3))) void lds_t;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_t *)lds, 16, off, 0, 0, 0);
-#endif
 }
 
 // Tiles of BN channels by BM tokens, WN x WM waves of 32x32 blocks.  A step is 256
@@ -97,8 +82,7 @@ __device__ __forceinline__ uint32_t half_scales(uint2 u)
 
 template <class C, class T> __global__ void __launch_bounds__(C::NT) k_mx4_gemm(Mx4Linear a)
 {
-    constexpr int PITCH = C::FN * 32 * (int)sizeof(T) + 16;     // of the staged output
-    constexpr int OUT = C::WN * C::WM * 32 * PITCH;
+    constexpr int OUT = C::WN * C::WM * kOutBytes<T, C::FN>;
     __shared__ __attribute__((aligned(1024))) char sm[2 * C::STAGE > OUT ? 2 * C::STAGE : OUT];
     const int lane = threadIdx.x & 63;
     const int wave = (int)uniform(threadIdx.x >> 6);
@@ -124,7 +108,7 @@ template <class C, class T> __global__ void __launch_bounds__(C::NT) k_mx4_gemm(
             const bool w = i < C::BN / (8 * NW);                // known when unrolled
             const int first = 8 * (i * NW + wave);              // of the wave's eight rows
             const uint32_t row = (uint32_t)(first - (w ? 0 : C::BN) + (lane >> 3));
-            load_to_lds(w ? W.codes : X.codes, to + first * 128,
+            load_chunk_to_lds(w ? W.codes : X.codes, to + first * 128,
                         at < W.pitch ? row * W.pitch + at : kOOB);
         }
     };
@@ -186,59 +170,24 @@ template <class C, class T> __global__ void __launch_bounds__(C::NT) k_mx4_gemm(
         step(std::integral_constant<int, 3>{});
     }
     __syncthreads();            // the stages are free
-    // Register v of a block in lane l: channel 8 (v / 4) + 4 (l / 32) + v % 4, token
-    // l % 32.
-    char *out = sm + wave * 32 * PITCH;
     const int nw = n0 + wn * C::FN * 32;
     float bias[C::FN][16];
+    const rsrc_t rb = make_rsrc(a.bias + n0, a.bias ? 4u * uniform(min(a.N - n0, C::BN)) : 0u);
 #pragma unroll
     for (int i = 0; i < C::FN; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int n = nw + 32 * i + 8 * (v / 4) + 4 * h + v % 4;
-            bias[i][v] = a.bias && n < a.N ? a.bias[n] : 0.0f;
-        }
-    T *y = static_cast<T *>(a.y);
-    constexpr int PER = 16 / (int)sizeof(T), CH = C::FN * 32 / PER;     // chunks of a row
-    const bool wide = a.N % PER == 0 && (reinterpret_cast<uintptr_t>(y) & 15) == 0;
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-    for (int j = 0; j < C::FM; ++j) {
+            for (int e = 0; e < 4; ++e)
+                bias[i][4 * q + e] = __builtin_bit_cast(
+                    float, __builtin_amdgcn_raw_buffer_load_b32(
+                               rb, 4u * (uint32_t)(nw - n0 + 32 * i + 8 * q + 4 * h + e), 0, 0));
+    store_tile<T>(static_cast<T *>(a.y), a.M, a.N, m0 + wm * C::FM * 32, nw,
+                  sm + wave * kOutBytes<T, C::FN>, acc, [&](int i, int q, float (&v)[4]) {
 #pragma unroll
-        for (int i = 0; i < C::FN; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = acc[i][j][4 * q + e] + bias[i][4 * q + e];
-                T *p = reinterpret_cast<T *>(out + r32 * PITCH) + 32 * i + 8 * q + 4 * h;
-                store_vec<T, 4>(p, v);
-            }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        const int mw = m0 + (wm * C::FM + j) * 32;
-#pragma unroll
-        for (int e = 0; e < CH / 2; ++e) {
-            const int r = (64 * e + lane) / CH, c = (64 * e + lane) % CH;
-            const int m = mw + r, n = nw + PER * c;
-            const u32x4 u = *reinterpret_cast<const u32x4 *>(out + r * PITCH + 16 * c);
-            if (m >= a.M || n >= a.N)
-                continue;
-            T *to = y + (size_t)m * a.N + n;
-            if (wide) {
-                *reinterpret_cast<u32x4 *>(to) = u;
-            } else {
-                T one[PER];
-                __builtin_memcpy(one, &u, 16);
-#pragma unroll
-                for (int k = 0; k < PER; ++k)
-                    if (n + k < a.N)
-                        to[k] = one[k];
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    }
+                      for (int e = 0; e < 4; ++e)
+                          v[e] += bias[i][4 * q + e];
+                  });
 }
 
 // Few tokens: the weight is read once, by workgroups of 16 channels whose four waves

@@ -1,0 +1,483 @@
+// Gradient of the token-scaled masked linear, y = (X W_b^T) sx[m] sw[n] + bias[n],
+// from the 8-bit codes that the forward pass took:
+//
+//   dx[m][k] = sum_n dy[m][n] (sw[n] W_b[n][k]),
+//   dw[n][k] = sum_m dy[m][n] (sx[m] X[m][k]),     dbias[n] = sum_m dy[m][n].
+//
+// Both are products of dy (or its transpose) with an 8-bit matrix Q [Z][C] whose rows,
+// the summed axis, have a factor each: out[r][c] = sum_z A(r, z) s[z] Q[z][c].  The
+// 8-bit operand becomes one of dy's type on its way to LDS, s[z] q rounded once: codes
+// are exact in either type, so that this is the one rounding before the fp32 sums of
+// the matrix unit.  In half it is kept in the middle of the type's range: the factors
+// are divided by a power of two near the largest of a workgroup's and the sums are
+// multiplied by it again; a factor below 2^-21 of the largest loses bits, to values that
+// are below 2^-24 of the largest's.
+//
+// The matrix instruction takes Q's columns as its first operand, so that a lane has
+// four neighbouring columns of an output row (tile_out.h), and eight values of the
+// summed axis at a time: rows of dy give them as they lie, rows of Q and of dy's
+// transpose through the transposing LDS load (four rows of 16 columns per 16 lanes).
+#pragma once
+
+#include "branch_internal.h"
+#include "gemm_core.h"
+#include "tile_out.h"
+
+namespace tasq {
+
+namespace {
+
+typedef bf16_t v8bf_t __attribute__((ext_vector_type(8)));
+typedef f16_t v8h_t __attribute__((ext_vector_type(8)));
+typedef short v4s_t __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ v16f_t mfma_grad(bf16_t, u32x4 a, u32x4 b, v16f_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf_t, a),
+                                                   __builtin_bit_cast(v8bf_t, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ v16f_t mfma_grad(f16_t, u32x4 a, u32x4 b, v16f_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h_t, a),
+                                                  __builtin_bit_cast(v8h_t, b), c, 0, 0, 0);
+}
+
+constexpr int kGradStep = 64;   // of the summed axis
+
+// Tiles of BC columns of Q by BR rows of the output, WC x WR waves.
+template <int BC_, int BR_, int WC_, int WR_> struct GradCfg {
+    static constexpr int BC = BC_, BR = BR_, WC = WC_, WR = WR_;
+    static constexpr int NT = 64 * WC * WR;
+    static constexpr int FC = BC / WC / 32, FR = BR / WR / 32;
+    static constexpr int A_BYTES = BR * kGradStep * 2, Q_BYTES = BC * kGradStep * 2;
+    static constexpr int STAGE = A_BYTES + Q_BYTES;
+    static constexpr int Q_TASKS = kGradStep * BC / 16 / NT;    // 16 codes each
+    static constexpr int A_TASKS = kGradStep * BR / 8 / NT;     // 16 bytes each
+};
+
+// Place of 16-byte chunk c of row z of a tile with PITCH bytes a row that the
+// transposing load reads: the rows that it spans fall in distinct banks.
+template <int PITCH> __device__ __forceinline__ int turn_key(int z)
+{
+    return PITCH >= 256 ? z & 3 : (z >> 1) & 1;
+}
+
+template <int PITCH> __device__ __forceinline__ uint32_t turn_place(int z, int c)
+{
+    return (uint32_t)(z * PITCH + 16 * (c ^ (4 * turn_key<PITCH>(z))));
+}
+
+// Eight values z .. z + 7 of column `block * 32 + lane % 32` of such a tile, for lane
+// half h rows 8 h on, from `lds` at row 16 ks: `at` is this lane's part of the address
+// (turn_lane).
+template <int PITCH> __device__ __forceinline__ uint32_t turn_lane(int block)
+{
+    const int lane = threadIdx.x & 63, z = 8 * (lane >> 5) + ((lane & 15) >> 2);
+    const int c = 4 * block + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    return turn_place<PITCH>(z, c) + 8 * (lane & 1);
+}
+
+template <int PITCH>
+__device__ __forceinline__ u32x4 turned(const char *lds, uint32_t at, int ks)
+{
+    typedef __attribute__((address_space(3))) v4s_t lds_t;
+    const char *p = lds + at + 16 * ks * PITCH;
+    // (Rows z and z + 4 have the same key.)
+    static_assert(PITCH >= 256 || PITCH == 128, "keys repeat every four rows");
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)p));
+    const u32x2 hi = __builtin_bit_cast(
+        u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)(p + 4 * PITCH)));
+    return u32x4{lo.x, lo.y, hi.x, hi.y};
+}
+
+// 16 codes times their row's factor as 16 values of T.
+template <class T>
+__device__ __forceinline__ void dequantize(v4i q, float s, u32x4 &lo, u32x4 &hi)
+{
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            v[4 * i + j] = (float)(int8_t)((uint32_t)q[i] >> (8 * j)) * s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        lo[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
+        hi[i] = pack2<T>(v[8 + 2 * i], v[9 + 2 * i]);
+    }
+}
+
+// The power of two that brings the largest finite factor of [z0, z1) to 2^7: with
+// codes of up to 2^7 in magnitude a product stays below 2^15.
+template <class C> __device__ __forceinline__ int range_exponent(const float *s, int z0, int z1)
+{
+    __shared__ float part[C::NT / 64];
+    float top = 0.0f;
+    for (int z = z0 + (int)threadIdx.x; z < z1; z += C::NT) {
+        const float f = fabsf(s[z]);
+        top = f < __builtin_inff() ? fmaxf(top, f) : top;
+    }
+    top = group_reduce<64>(top, [](float a, float b) { return fmaxf(a, b); });
+    if ((threadIdx.x & 63) == 0)
+        part[threadIdx.x >> 6] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < C::NT / 64; ++w)
+        top = fmaxf(top, part[w]);
+    int e = 0;
+    if (top > 0.0f)
+        (void)frexpf(top, &e);          // top < 2^e
+    return 8 - e;
+}
+
+// out[r][c] of one tile and range of the summed axis.  TURNED: A is [Z][R], else
+// [R][Z].  WHOLE: rows of both operands are whole 16-byte chunks at 16-byte addresses,
+// and those of A go to LDS directly.
+template <class T, class C, bool TURNED, bool WHOLE>
+__device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int split, char *sm)
+{
+    constexpr int A_PITCH = TURNED ? 2 * C::BR : 2 * kGradStep;
+    constexpr int Q_PITCH = 2 * C::BC;
+    const int lane = threadIdx.x & 63;
+    const int wave = (int)uniform(threadIdx.x >> 6);
+    const int wc = wave % C::WC, wr = wave / C::WC;
+    const int r0 = tr * C::BR, c0 = tc * C::BC;
+    const int z0 = split * g.split_steps * kGradStep;
+    const int z1 = min(g.Z, z0 + g.split_steps * kGradStep);
+    const int steps = (z1 - z0 + kGradStep - 1) / kGradStep;
+    const T *A = static_cast<const T *>(g.A);
+    const int8_t *const q_end = g.Q + (size_t)g.Z * g.C;
+    int shift = 0;
+    if constexpr (sizeof(T) == 2 && __is_same(T, f16_t))
+        shift = range_exponent<C>(g.s, z0, z1);
+
+    // Two steps' codes and factors (and A's chunks, where they pass through
+    // registers) on their way.
+    struct Slot {
+        v4i q[C::Q_TASKS];
+        float s[C::Q_TASKS];
+        u32x4 a[WHOLE ? 1 : C::A_TASKS];
+    } slots[2];
+    // Step t's, zeros past the range.
+    auto request = [&](Slot &slot, int t) {
+        const int zt = z0 + kGradStep * t;
+        const uint32_t n = uniform(min(z1 - zt, kGradStep));
+        const rsrc_t rs = make_rsrc(g.s + zt, 4u * n);
+        const rsrc_t rq = make_rsrc(g.Q + (size_t)zt * g.C, WHOLE ? n * (uint32_t)g.C : 0u);
+#pragma unroll
+        for (int i = 0; i < C::Q_TASKS; ++i) {
+            const int task = (int)threadIdx.x + i * C::NT;
+            const int z = task / (C::BC / 16), c = c0 + 16 * (task % (C::BC / 16));
+            slot.s[i] = __builtin_bit_cast(
+                float, __builtin_amdgcn_raw_buffer_load_b32(rs, 4u * (uint32_t)z, 0, 0));
+            if constexpr (WHOLE) {
+                slot.q[i] = ld16(rq, c < g.C ? (uint32_t)z * (uint32_t)g.C + (uint32_t)c : kOOB);
+            } else {
+                slot.q[i] = v4i{0, 0, 0, 0};
+                if (zt + z >= z1 || c >= g.C)
+                    continue;
+                const int8_t *p = g.Q + (size_t)(zt + z) * g.C + c;
+                const long long left = (long long)(q_end - p);
+                if (left >= 16) {
+                    const Packed<int8_t, 16> w = *reinterpret_cast<const Packed<int8_t, 16> *>(p);
+                    slot.q[i] = v4i{(int)w.w[0], (int)w.w[1], (int)w.w[2], (int)w.w[3]};
+                } else {            // of the last row of all
+                    uint64_t w[2] = {0, 0};
+#pragma unroll 1
+                    for (int e = 0; e < (int)left; ++e)
+                        w[e >= 8] |= (uint64_t)(uint8_t)p[e] << (8 * (e & 7));
+                    slot.q[i] = v4i{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
+                }
+            }
+        }
+        if constexpr (!WHOLE) {
+#pragma unroll
+            for (int i = 0; i < C::A_TASKS; ++i) {
+                const int task = (int)threadIdx.x + i * C::NT;
+                const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
+                const int z = TURNED ? zt + row : zt + first, r = TURNED ? r0 + first : r0 + row;
+                const int left = TURNED ? g.R - r : z1 - z;     // of the row of A
+                slot.a[i] = u32x4{0, 0, 0, 0};
+                if ((TURNED ? z >= z1 : r >= g.R) || left <= 0)
+                    continue;
+                const T *p = A + (TURNED ? (size_t)z * g.a_stride + r : (size_t)r * g.a_stride + z);
+                if (left >= 8) {
+                    slot.a[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Packed<T, 8> *>(p));
+                } else {
+                    T e[8] = {};
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (k < left)
+                            e[k] = p[k];
+                    slot.a[i] = __builtin_bit_cast(u32x4, e);
+                }
+            }
+        }
+    };
+    // Step t's rows of A straight to LDS.
+    auto direct = [&](int t) {
+        if constexpr (WHOLE) {
+            char *to = sm + (t & 1) * C::STAGE;
+            const uint32_t pitch = 2u * (uint32_t)g.a_stride;
+            const int zt = z0 + kGradStep * t;
+            constexpr int CH = A_PITCH / 16;                    // chunks of a tile's row
+            constexpr int ROWS = 64 / CH > 0 ? 64 / CH : 1;     // of an instruction
+            rsrc_t rsrc;
+            if constexpr (TURNED) {
+                const uint32_t n = uniform(min(z1 - zt, kGradStep));
+                rsrc = make_rsrc(A + (size_t)zt * g.a_stride + r0,
+                                 (n - 1) * pitch + 2u * (uint32_t)uniform(min(g.R - r0, C::BR)));
+            } else {
+                const uint32_t n = uniform(min(g.R - r0, C::BR));
+                rsrc = make_rsrc(A + (size_t)r0 * g.a_stride,
+                                 (n - 1) * pitch + 2u * (uint32_t)g.Z);
+            }
+#pragma unroll
+            for (int i = 0; i < C::A_TASKS; ++i) {
+                const int first = (i * (C::NT / 64) + wave) * ROWS;     // the wave's first row
+                const int row = first + lane / CH, place = lane % CH;
+                uint32_t off;
+                if constexpr (TURNED) {
+                    const int c = place ^ (4 * turn_key<A_PITCH>(row));
+                    off = (uint32_t)row * pitch + 16u * (uint32_t)c;
+                    off = 8 * c < g.R - r0 ? off : kOOB;
+                } else {
+                    const int z = zt + 8 * (place ^ (row & 7));
+                    off = z < z1 ? (uint32_t)row * pitch + 2u * (uint32_t)z : kOOB;
+                }
+                load_chunk_unseen(rsrc, to + first * A_PITCH, off);
+            }
+        }
+    };
+    // What request() gave, into stage t.
+    auto put = [&](const Slot &slot, int t) {
+        char *to = sm + (t & 1) * C::STAGE;
+#pragma unroll
+        for (int i = 0; i < C::Q_TASKS; ++i) {
+            const int task = (int)threadIdx.x + i * C::NT;
+            const int z = task / (C::BC / 16), c = 2 * (task % (C::BC / 16));
+            v4i v = slot.q[i];
+            v.x &= (int)g.mask;
+            v.y &= (int)g.mask;
+            v.z &= (int)g.mask;
+            v.w &= (int)g.mask;
+            u32x4 lo, hi;
+            dequantize<T>(v, __is_same(T, f16_t) ? ldexpf(slot.s[i], shift) : slot.s[i], lo, hi);
+            *reinterpret_cast<u32x4 *>(to + C::A_BYTES + turn_place<Q_PITCH>(z, c)) = lo;
+            *reinterpret_cast<u32x4 *>(to + C::A_BYTES + turn_place<Q_PITCH>(z, c + 1)) = hi;
+        }
+        if constexpr (!WHOLE) {
+#pragma unroll
+            for (int i = 0; i < C::A_TASKS; ++i) {
+                const int task = (int)threadIdx.x + i * C::NT;
+                const int row = task / (A_PITCH / 16), c = task % (A_PITCH / 16);
+                const uint32_t at = TURNED ? turn_place<A_PITCH>(row, c)
+                                           : (uint32_t)(row * A_PITCH + 16 * (c ^ (row & 7)));
+                *reinterpret_cast<u32x4 *>(to + at) = slot.a[i];
+            }
+        }
+    };
+
+    uint32_t qa[C::FC], aa[C::FR];
+#pragma unroll
+    for (int i = 0; i < C::FC; ++i)
+        qa[i] = C::A_BYTES + turn_lane<Q_PITCH>(wc * C::FC + i);
+#pragma unroll
+    for (int j = 0; j < C::FR; ++j)
+        aa[j] = TURNED ? turn_lane<A_PITCH>(wr * C::FR + j) : 0;
+    v16f_t acc[C::FC][C::FR];
+#pragma unroll
+    for (int i = 0; i < C::FC; ++i)
+#pragma unroll
+        for (int j = 0; j < C::FR; ++j)
+            acc[i][j] = v16f_t{};
+    const bool sums = TURNED && g.dbias && tc == 0 && wc == 0;
+    float bias[C::FR] = {};
+
+    // A step: its operands are in stage t; those of t + 1 go there meanwhile, A's by
+    // themselves, Q's from `next`, into which those of t + 2 are requested.
+    auto step = [&](Slot &next, Slot &after, int t) {
+        // A's rows have landed (every request has: those of the step before), and
+        // every wave has put its part.
+        __builtin_amdgcn_s_waitcnt(0x0070);         // vmcnt(0) lgkmcnt(0)
+        __syncthreads();
+        if (t + 1 < steps)
+            direct(t + 1);
+        if (t + 2 < steps)
+            request(after, t + 2);
+        const char *at = sm + (t & 1) * C::STAGE;
+#pragma unroll
+        for (int ks = 0; ks < kGradStep / 16; ++ks) {
+            u32x4 a[C::FR], b[C::FC];
+#pragma unroll
+            for (int i = 0; i < C::FC; ++i)
+                b[i] = turned<Q_PITCH>(at, qa[i], ks);
+#pragma unroll
+            for (int j = 0; j < C::FR; ++j) {
+                if constexpr (TURNED) {
+                    a[j] = turned<A_PITCH>(at, aa[j], ks);
+                } else {
+                    const int row = (wr * C::FR + j) * 32 + (lane & 31);
+                    a[j] = *reinterpret_cast<const u32x4 *>(
+                        at + row * A_PITCH + 16 * ((2 * ks + (lane >> 5)) ^ (row & 7)));
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < C::FC; ++i)
+#pragma unroll
+                for (int j = 0; j < C::FR; ++j)
+                    acc[i][j] = mfma_grad(T{}, b[i], a[j], acc[i][j]);
+            if (TURNED && sums) {
+#pragma unroll
+                for (int j = 0; j < C::FR; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const f32x2 f = unpack2<T>(a[j][k]);
+                        bias[j] += f.x + f.y;
+                    }
+            }
+            if (ks == 1 && t + 1 < steps)
+                put(next, t + 1);
+        }
+    };
+    if (steps > 0) {
+        direct(0);
+        request(slots[0], 0);
+        put(slots[0], 0);
+    }
+    if (steps > 1)
+        request(slots[1], 1);
+    for (int t = 0; t < steps; t += 2) {
+        step(slots[1], slots[0], t);
+        if (t + 1 < steps)
+            step(slots[0], slots[1], t + 1);
+    }
+    __syncthreads();            // the stages are free
+    if (TURNED && sums) {
+#pragma unroll
+        for (int j = 0; j < C::FR; ++j) {
+            const int r = r0 + (wr * C::FR + j) * 32 + (lane & 31);
+            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(bias[j]),
+                                                            __float_as_uint(bias[j]), false, false);
+            if (lane < 32 && r < g.R)
+                g.dbias[(size_t)split * g.R + r] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        }
+    }
+    const int row0 = r0 + wr * C::FR * 32, col0 = c0 + wc * C::FC * 32;
+    const float back = ldexpf(1.0f, -shift);
+    auto scaled = [&](int, int, float (&v)[4]) {
+        if constexpr (__is_same(T, f16_t)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] *= back;
+        }
+    };
+    if (g.splits > 1)
+        store_tile<float>(g.part + (size_t)split * g.R * g.C, g.R, g.C, row0, col0,
+                          sm + wave * kOutBytes<float, C::FC>, acc, scaled);
+    else
+        store_tile<T>(static_cast<T *>(g.out), g.R, g.C, row0, col0,
+                      sm + wave * kOutBytes<T, C::FC>, acc, scaled);
+}
+
+template <class T, class C, bool TURNED, bool WHOLE>
+__global__ void __launch_bounds__(C::NT) k_token_grad(GradJob g, int first)
+{
+    constexpr int OUT = C::WC * C::WR * kOutBytes<float, C::FC>;
+    __shared__ __attribute__((aligned(1024))) char sm[2 * C::STAGE > OUT ? 2 * C::STAGE : OUT];
+    const int unit = first + xcd_remap(blockIdx.x, gridDim.x);
+    const int tiles = g.tiles_r * g.tiles_c, split = unit / tiles;
+    int tr, tc;
+    tile_coords(unit - split * tiles, g.tiles_r, g.tiles_c, tr, tc);
+    grad_tile<T, C, TURNED, WHOLE>(g, (int)uniform(tr), (int)uniform(tc), (int)uniform(split), sm);
+}
+
+// Adds the ranges' parts up in order and rounds: four values a thread, and after the
+// last of them the bias'.
+template <class T>
+__global__ void __launch_bounds__(256) k_join_grad(const float *part, T *out, size_t n, int splits,
+                                                   const float *bias_part, float *dbias, int bias_n)
+{
+    const size_t at = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
+    if (at < n) {
+        float v[4] = {};
+        const int live = n - at < 4 ? (int)(n - at) : 4;
+        if (live == 4) {
+            for (int s = 0; s < splits; ++s) {
+                const Packed<float, 4> p =
+                    *reinterpret_cast<const Packed<float, 4> *>(part + (size_t)s * n + at);
+                float f[4];
+                p.floats(f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] += f[e];
+            }
+            Packed<T, 4> o;
+            o.set(v);
+            *reinterpret_cast<Packed<T, 4> *>(out + at) = o;
+        } else {
+            for (int e = 0; e < live; ++e) {
+                float f = 0.0f;
+                for (int s = 0; s < splits; ++s)
+                    f += part[(size_t)s * n + at + e];
+                out[at + e] = (T)f;
+            }
+        }
+        return;
+    }
+    const size_t b = (size_t)blockIdx.x * 256 + threadIdx.x - (n + 3) / 4;
+    if (bias_part && b < (size_t)bias_n) {
+        float f = 0.0f;
+        for (int s = 0; s < splits; ++s)
+            f += bias_part[(size_t)s * bias_n + b];
+        dbias[b] = f;
+    }
+}
+
+template <class T, class C, bool TURNED> hipError_t launch_cfg(const GradJob &g, bool whole,
+                                                              hipStream_t stream)
+{
+    constexpr long long MOST = 1 << 22;
+    const long long units = (long long)g.tiles_r * g.tiles_c * g.splits;
+    for (long long u = 0; u < units; u += MOST) {
+        const unsigned grid = (unsigned)(units - u < MOST ? units - u : MOST);
+        if (whole)
+            k_token_grad<T, C, TURNED, true><<<grid, C::NT, 0, stream>>>(g, (int)u);
+        else
+            k_token_grad<T, C, TURNED, false><<<grid, C::NT, 0, stream>>>(g, (int)u);
+        if (hipError_t e = hipGetLastError())
+            return e;
+    }
+    return hipSuccess;
+}
+
+template <class T, bool TURNED>
+hipError_t launch_product(const GradJob &g, bool whole, hipStream_t stream)
+{
+    if (g.tile == 256)
+        return launch_cfg<T, GradCfg<256, 256, 4, 2>, TURNED>(g, whole, stream);
+    if (g.tile == 128)
+        return launch_cfg<T, GradCfg<128, 128, 2, 2>, TURNED>(g, whole, stream);
+    return launch_cfg<T, GradCfg<64, 64, 2, 2>, TURNED>(g, whole, stream);
+}
+
+// One of the two products and, where its range is cut, the sum of its parts.
+template <class T> hipError_t run_product(GradJob g, bool turned_a, bool whole, hipStream_t stream)
+{
+    float *dbias = g.dbias;
+    if (g.splits > 1)
+        g.dbias = dbias ? g.bias_part : nullptr;
+    hipError_t e = turned_a ? launch_product<T, true>(g, whole, stream)
+                            : launch_product<T, false>(g, whole, stream);
+    if (e != hipSuccess || g.splits == 1)
+        return e;
+    const size_t n = (size_t)g.R * g.C, threads = (n + 3) / 4 + (dbias ? g.R : 0);
+    k_join_grad<T><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(
+        g.part, static_cast<T *>(g.out), n, g.splits, dbias ? g.bias_part : nullptr, dbias, g.R);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+}  // namespace tasq

@@ -1,0 +1,11 @@
+// The token-scaled linear's gradient in bfloat16 (token_grad.h).
+#include "token_grad.h"
+
+namespace tasq {
+
+hipError_t token_grad_bf16(const GradJob &g, bool turned_a, bool whole, hipStream_t stream)
+{
+    return run_product<bf16_t>(g, turned_a, whole, stream);
+}
+
+}  // namespace tasq

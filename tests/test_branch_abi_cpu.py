@@ -190,7 +190,51 @@ def test_mx4_of_nothing_is_noop():
     assert linear_mx4(M=0, X=None, y=None) == linear_mx4(N=0, W=None, y=None) == 0
 
 
+def grad(dy=FAKE, t=BF16, stride=48, X=FAKE, sx=FAKE, W=FAKE, sw=FAKE, M=4, N=48, K=32, b=8,
+         dx=FAKE, dw=FAKE, dbias=FAKE, ws=FAKE, ws_bytes=1 << 30):
+    return L.tasq_masked_linear_tokens_backward(dy, t, stride, X, sx, W, sw, M, N, K, b, dx, dw,
+                                                dbias, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(dy=None), NULL), (dict(X=None), NULL), (dict(sx=None), NULL), (dict(W=None), NULL),
+    (dict(sw=None), NULL), (dict(dw=None), NULL),
+    (dict(M=-1), DIM), (dict(N=-1), DIM), (dict(K=-1), DIM), (dict(stride=47), DIM),
+    (dict(M=(1 << 30) + 1), DIM), (dict(N=(1 << 30) + 1, stride=1 << 31), DIM),
+    (dict(K=_lib.TASQ_MAX_K + 1), OVERFLOW), (dict(b=0), BITS), (dict(b=9), BITS),
+    (dict(t=F32), KIND), (dict(t=5), KIND),
+    (dict(dy=FAKE + 1), ALIGN), (dict(dx=FAKE + 1), ALIGN), (dict(dw=FAKE + 1), ALIGN),
+    (dict(dbias=FAKE + 2), ALIGN), (dict(sx=FAKE + 2), ALIGN), (dict(sw=FAKE + 2), ALIGN),
+    (dict(ws=FAKE + 16), ALIGN),
+])
+def test_token_grad_rejects(kw, code):
+    assert grad(**kw) == code
+
+
+def test_token_grad_of_nothing_is_noop():
+    assert grad(dx=None, dw=None, dbias=None) == 0
+    assert grad(M=0, dw=None, dbias=None) == grad(K=0, dbias=None) == grad(M=0, N=0) == 0
+
+
+def test_token_grad_workspace_bytes():
+    size = T.masked_linear_tokens_backward_workspace_bytes
+    assert size(8192, 128, 128) >= 2 * 128 * 128 * 4      # dw's ranges of tokens
+    for no in ((-1, 8, 8), (8, -1, 8), (8, 8, -1), (8, 8, _lib.TASQ_MAX_K + 1)):
+        assert size(*no) == 0
+
+
 # --------------------------------------------------------------------- wrappers
+
+def test_token_grad_wrapper_refuses():
+    dy, codes, s = torch.zeros(4, 8).bfloat16(), torch.zeros(4, 8, dtype=torch.int8), torch.ones(4)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        T.masked_linear_tokens_backward(dy, codes, codes, s, s, 8)
+    with pytest.raises(ValueError, match="bfloat16 or float16"):
+        T.masked_linear_tokens_backward(dy.float(), codes, codes, s, s, 8)
+    big = torch.empty(1).bfloat16().expand(1, (1 << 32) + 3)
+    with pytest.raises(ValueError, match="below 2\\^31"):
+        T.masked_linear_tokens_backward(big, codes, codes, s, s, 8)
+
 
 def test_mx4_wrappers_refuse():
     x, u = torch.zeros(4, 128), torch.zeros(4, 64, dtype=torch.uint8)
