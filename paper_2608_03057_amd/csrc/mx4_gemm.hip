@@ -96,10 +96,11 @@ template <class C, class T> __global__ void __launch_bounds__(C::NT) k_mx4_gemm(
     W.init(a.W, a.sw, a.N, n0, C::BN, a.K128);
     X.init(a.X, a.sx, a.M, m0, C::BM, a.K128);
     // Chunk i of this thread: row 8 (i NW + wave) + lane / 8 of the stage, place
-    // lane % 8, holding the row's chunk place ^ (row % 8), so that the rows that an
-    // operand read spans fall in distinct banks.
+    // lane % 8, holding the row's chunk place ^ (row / 2 % 8), so that 16 rows of an
+    // operand read fall in distinct banks.
     constexpr int NW = C::NT / 64;
-    const uint32_t chunk = 16u * (uint32_t)((lane & 7) ^ (lane >> 3));
+    static_assert(NW % 2 == 0, "rows of a wave differ by multiples of 16");
+    const uint32_t chunk = 16u * (uint32_t)((lane & 7) ^ (4 * (wave & 1) + (lane >> 4)));
     auto stage = [&](int t) {
         char *to = sm + (t & 1) * C::STAGE;
         const uint32_t at = 128u * (uint32_t)t + chunk;
@@ -147,7 +148,7 @@ template <class C, class T> __global__ void __launch_bounds__(C::NT) k_mx4_gemm(
         const char *at = sm + (t & 1) * C::STAGE;
         auto read = [&](int row, int ks) {
             return *reinterpret_cast<const v4i *>(at + (row + r32) * 128 +
-                                                  16 * ((2 * ks + h) ^ (r32 & 7)));
+                                                  16 * ((2 * ks + h) ^ ((r32 >> 1) & 7)));
         };
         auto step = [&](auto tag) {
             constexpr int ks = decltype(tag)::value;

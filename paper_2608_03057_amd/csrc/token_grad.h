@@ -20,7 +20,7 @@
 #pragma once
 
 #include "branch_internal.h"
-#include "gemm_core.h"
+#include "gemm_pers.h"
 #include "tile_out.h"
 
 namespace tasq {
@@ -51,7 +51,9 @@ template <int BC_, int BR_, int WC_, int WR_> struct GradCfg {
     static constexpr int NT = 64 * WC * WR;
     static constexpr int FC = BC / WC / 32, FR = BR / WR / 32;
     static constexpr int A_BYTES = BR * kGradStep * 2, Q_BYTES = BC * kGradStep * 2;
-    static constexpr int STAGE = A_BYTES + Q_BYTES;
+    // Three stages of A, two of Q.
+    static_assert(NT >= BR && 4 % WC == 0, "a thread to a row's sum");
+    static constexpr int LDS = 3 * A_BYTES + 2 * Q_BYTES;
     static constexpr int Q_TASKS = kGradStep * BC / 16 / NT;    // 16 codes each
     static constexpr int A_TASKS = kGradStep * BR / 8 / NT;     // 16 bytes each
 };
@@ -110,9 +112,9 @@ __device__ __forceinline__ void dequantize(v4i q, float s, u32x4 &lo, u32x4 &hi)
 
 // The power of two that brings the largest finite factor of [z0, z1) to 2^7: with
 // codes of up to 2^7 in magnitude a product stays below 2^15.
-template <class C> __device__ __forceinline__ int range_exponent(const float *s, int z0, int z1)
+template <class C>
+__device__ __forceinline__ int range_exponent(const float *s, int z0, int z1, float *part)
 {
-    __shared__ float part[C::NT / 64];
     float top = 0.0f;
     for (int z = z0 + (int)threadIdx.x; z < z1; z += C::NT) {
         const float f = fabsf(s[z]);
@@ -125,6 +127,7 @@ template <class C> __device__ __forceinline__ int range_exponent(const float *s,
 #pragma unroll
     for (int w = 0; w < C::NT / 64; ++w)
         top = fmaxf(top, part[w]);
+    __syncthreads();
     int e = 0;
     if (top > 0.0f)
         (void)frexpf(top, &e);          // top < 2^e
@@ -150,44 +153,44 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     const int8_t *const q_end = g.Q + (size_t)g.Z * g.C;
     int shift = 0;
     if constexpr (sizeof(T) == 2 && __is_same(T, f16_t))
-        shift = range_exponent<C>(g.s, z0, z1);
+        shift = range_exponent<C>(g.s, z0, z1, reinterpret_cast<float *>(sm));
 
-    // Two steps' codes and factors (and A's chunks, where they pass through
-    // registers) on their way.
-    struct Slot {
-        v4i q[C::Q_TASKS];
-        float s[C::Q_TASKS];
-        u32x4 a[WHOLE ? 1 : C::A_TASKS];
-    } slots[2];
+    // A step's codes and factors (and A's chunks, where they pass through registers)
+    // on their way.
+    v4i q[C::Q_TASKS];
+    float s[C::Q_TASKS];
+    u32x4 ar[WHOLE ? 1 : C::A_TASKS];
+    auto a_stage = [&](int t) { return sm + (t % 3) * C::A_BYTES; };
+    auto q_stage = [&](int t) { return sm + 3 * C::A_BYTES + (t & 1) * C::Q_BYTES; };
     // Step t's, zeros past the range.
-    auto request = [&](Slot &slot, int t) {
+    auto request = [&](int t) {
         const int zt = z0 + kGradStep * t;
-        const uint32_t n = uniform(min(z1 - zt, kGradStep));
+        const uint32_t n = uniform(max(min(z1 - zt, kGradStep), 0));
         const rsrc_t rs = make_rsrc(g.s + zt, 4u * n);
         const rsrc_t rq = make_rsrc(g.Q + (size_t)zt * g.C, WHOLE ? n * (uint32_t)g.C : 0u);
 #pragma unroll
         for (int i = 0; i < C::Q_TASKS; ++i) {
             const int task = (int)threadIdx.x + i * C::NT;
             const int z = task / (C::BC / 16), c = c0 + 16 * (task % (C::BC / 16));
-            slot.s[i] = __builtin_bit_cast(
+            s[i] = __builtin_bit_cast(
                 float, __builtin_amdgcn_raw_buffer_load_b32(rs, 4u * (uint32_t)z, 0, 0));
             if constexpr (WHOLE) {
-                slot.q[i] = ld16(rq, c < g.C ? (uint32_t)z * (uint32_t)g.C + (uint32_t)c : kOOB);
+                q[i] = ld16(rq, c < g.C ? (uint32_t)z * (uint32_t)g.C + (uint32_t)c : kOOB);
             } else {
-                slot.q[i] = v4i{0, 0, 0, 0};
+                q[i] = v4i{0, 0, 0, 0};
                 if (zt + z >= z1 || c >= g.C)
                     continue;
                 const int8_t *p = g.Q + (size_t)(zt + z) * g.C + c;
                 const long long left = (long long)(q_end - p);
                 if (left >= 16) {
                     const Packed<int8_t, 16> w = *reinterpret_cast<const Packed<int8_t, 16> *>(p);
-                    slot.q[i] = v4i{(int)w.w[0], (int)w.w[1], (int)w.w[2], (int)w.w[3]};
+                    q[i] = v4i{(int)w.w[0], (int)w.w[1], (int)w.w[2], (int)w.w[3]};
                 } else {            // of the last row of all
                     uint64_t w[2] = {0, 0};
 #pragma unroll 1
                     for (int e = 0; e < (int)left; ++e)
                         w[e >= 8] |= (uint64_t)(uint8_t)p[e] << (8 * (e & 7));
-                    slot.q[i] = v4i{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
+                    q[i] = v4i{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
                 }
             }
         }
@@ -198,19 +201,19 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
                 const int z = TURNED ? zt + row : zt + first, r = TURNED ? r0 + first : r0 + row;
                 const int left = TURNED ? g.R - r : z1 - z;     // of the row of A
-                slot.a[i] = u32x4{0, 0, 0, 0};
+                ar[i] = u32x4{0, 0, 0, 0};
                 if ((TURNED ? z >= z1 : r >= g.R) || left <= 0)
                     continue;
                 const T *p = A + (TURNED ? (size_t)z * g.a_stride + r : (size_t)r * g.a_stride + z);
                 if (left >= 8) {
-                    slot.a[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Packed<T, 8> *>(p));
+                    ar[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Packed<T, 8> *>(p));
                 } else {
                     T e[8] = {};
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
                         if (k < left)
                             e[k] = p[k];
-                    slot.a[i] = __builtin_bit_cast(u32x4, e);
+                    ar[i] = __builtin_bit_cast(u32x4, e);
                 }
             }
         }
@@ -218,16 +221,16 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     // Step t's rows of A straight to LDS.
     auto direct = [&](int t) {
         if constexpr (WHOLE) {
-            char *to = sm + (t & 1) * C::STAGE;
+            char *to = a_stage(t);
             const uint32_t pitch = 2u * (uint32_t)g.a_stride;
             const int zt = z0 + kGradStep * t;
             constexpr int CH = A_PITCH / 16;                    // chunks of a tile's row
             constexpr int ROWS = 64 / CH > 0 ? 64 / CH : 1;     // of an instruction
             rsrc_t rsrc;
             if constexpr (TURNED) {
-                const uint32_t n = uniform(min(z1 - zt, kGradStep));
+                const uint32_t n = uniform(max(min(z1 - zt, kGradStep), 0));
                 rsrc = make_rsrc(A + (size_t)zt * g.a_stride + r0,
-                                 (n - 1) * pitch + 2u * (uint32_t)uniform(min(g.R - r0, C::BR)));
+                                 n ? (n - 1) * pitch + 2u * uniform(min(g.R - r0, C::BR)) : 0u);
             } else {
                 const uint32_t n = uniform(min(g.R - r0, C::BR));
                 rsrc = make_rsrc(A + (size_t)r0 * g.a_stride,
@@ -243,7 +246,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                     off = (uint32_t)row * pitch + 16u * (uint32_t)c;
                     off = 8 * c < g.R - r0 ? off : kOOB;
                 } else {
-                    const int z = zt + 8 * (place ^ (row & 7));
+                    const int z = zt + 8 * (place ^ ((row >> 1) & 7));
                     off = z < z1 ? (uint32_t)row * pitch + 2u * (uint32_t)z : kOOB;
                 }
                 load_chunk_unseen(rsrc, to + first * A_PITCH, off);
@@ -251,21 +254,21 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
         }
     };
     // What request() gave, into stage t.
-    auto put = [&](const Slot &slot, int t) {
-        char *to = sm + (t & 1) * C::STAGE;
+    auto put = [&](int t) {
+        char *to = q_stage(t);
 #pragma unroll
         for (int i = 0; i < C::Q_TASKS; ++i) {
             const int task = (int)threadIdx.x + i * C::NT;
             const int z = task / (C::BC / 16), c = 2 * (task % (C::BC / 16));
-            v4i v = slot.q[i];
+            v4i v = q[i];
             v.x &= (int)g.mask;
             v.y &= (int)g.mask;
             v.z &= (int)g.mask;
             v.w &= (int)g.mask;
             u32x4 lo, hi;
-            dequantize<T>(v, __is_same(T, f16_t) ? ldexpf(slot.s[i], shift) : slot.s[i], lo, hi);
-            *reinterpret_cast<u32x4 *>(to + C::A_BYTES + turn_place<Q_PITCH>(z, c)) = lo;
-            *reinterpret_cast<u32x4 *>(to + C::A_BYTES + turn_place<Q_PITCH>(z, c + 1)) = hi;
+            dequantize<T>(v, __is_same(T, f16_t) ? ldexpf(s[i], shift) : s[i], lo, hi);
+            *reinterpret_cast<u32x4 *>(to + turn_place<Q_PITCH>(z, c)) = lo;
+            *reinterpret_cast<u32x4 *>(to + turn_place<Q_PITCH>(z, c + 1)) = hi;
         }
         if constexpr (!WHOLE) {
 #pragma unroll
@@ -273,8 +276,8 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 const int task = (int)threadIdx.x + i * C::NT;
                 const int row = task / (A_PITCH / 16), c = task % (A_PITCH / 16);
                 const uint32_t at = TURNED ? turn_place<A_PITCH>(row, c)
-                                           : (uint32_t)(row * A_PITCH + 16 * (c ^ (row & 7)));
-                *reinterpret_cast<u32x4 *>(to + at) = slot.a[i];
+                                           : (uint32_t)(row * A_PITCH + 16 * (c ^ ((row >> 1) & 7)));
+                *reinterpret_cast<u32x4 *>(a_stage(t) + at) = ar[i];
             }
         }
     };
@@ -282,7 +285,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     uint32_t qa[C::FC], aa[C::FR];
 #pragma unroll
     for (int i = 0; i < C::FC; ++i)
-        qa[i] = C::A_BYTES + turn_lane<Q_PITCH>(wc * C::FC + i);
+        qa[i] = turn_lane<Q_PITCH>(wc * C::FC + i);
 #pragma unroll
     for (int j = 0; j < C::FR; ++j)
         aa[j] = TURNED ? turn_lane<A_PITCH>(wr * C::FR + j) : 0;
@@ -292,77 +295,127 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
 #pragma unroll
         for (int j = 0; j < C::FR; ++j)
             acc[i][j] = v16f_t{};
-    const bool sums = TURNED && g.dbias && tc == 0 && wc == 0;
+    const bool sums = TURNED && g.dbias && tc == 0;
     float bias[C::FR] = {};
 
-    // A step: its operands are in stage t; those of t + 1 go there meanwhile, A's by
-    // themselves, Q's from `next`, into which those of t + 2 are requested.
-    auto step = [&](Slot &next, Slot &after, int t) {
-        // A's rows have landed (every request has: those of the step before), and
-        // every wave has put its part.
-        __builtin_amdgcn_s_waitcnt(0x0070);         // vmcnt(0) lgkmcnt(0)
-        __syncthreads();
-        if (t + 1 < steps)
-            direct(t + 1);
-        if (t + 2 < steps)
-            request(after, t + 2);
-        const char *at = sm + (t & 1) * C::STAGE;
+    struct Operands {
+        u32x4 a[C::FR], b[C::FC];
+    } f[2];
+    auto read = [&](int t, int ks, Operands &o) {
+        const char *A = a_stage(t), *Q = q_stage(t);
 #pragma unroll
-        for (int ks = 0; ks < kGradStep / 16; ++ks) {
-            u32x4 a[C::FR], b[C::FC];
-#pragma unroll
-            for (int i = 0; i < C::FC; ++i)
-                b[i] = turned<Q_PITCH>(at, qa[i], ks);
-#pragma unroll
-            for (int j = 0; j < C::FR; ++j) {
-                if constexpr (TURNED) {
-                    a[j] = turned<A_PITCH>(at, aa[j], ks);
-                } else {
-                    const int row = (wr * C::FR + j) * 32 + (lane & 31);
-                    a[j] = *reinterpret_cast<const u32x4 *>(
-                        at + row * A_PITCH + 16 * ((2 * ks + (lane >> 5)) ^ (row & 7)));
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < C::FC; ++i)
-#pragma unroll
-                for (int j = 0; j < C::FR; ++j)
-                    acc[i][j] = mfma_grad(T{}, b[i], a[j], acc[i][j]);
-            if (TURNED && sums) {
-#pragma unroll
-                for (int j = 0; j < C::FR; ++j)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const f32x2 f = unpack2<T>(a[j][k]);
-                        bias[j] += f.x + f.y;
-                    }
-            }
-            if (ks == 1 && t + 1 < steps)
-                put(next, t + 1);
-        }
-    };
-    if (steps > 0) {
-        direct(0);
-        request(slots[0], 0);
-        put(slots[0], 0);
-    }
-    if (steps > 1)
-        request(slots[1], 1);
-    for (int t = 0; t < steps; t += 2) {
-        step(slots[1], slots[0], t);
-        if (t + 1 < steps)
-            step(slots[0], slots[1], t + 1);
-    }
-    __syncthreads();            // the stages are free
-    if (TURNED && sums) {
+        for (int i = 0; i < C::FC; ++i)
+            o.b[i] = turned<Q_PITCH>(Q, qa[i], ks);
 #pragma unroll
         for (int j = 0; j < C::FR; ++j) {
-            const int r = r0 + (wr * C::FR + j) * 32 + (lane & 31);
+            if constexpr (TURNED) {
+                o.a[j] = turned<A_PITCH>(A, aa[j], ks);
+            } else {
+                const int row = (wr * C::FR + j) * 32 + (lane & 31);
+                o.a[j] = *reinterpret_cast<const u32x4 *>(
+                    A + row * A_PITCH + 16 * ((2 * ks + (lane >> 5)) ^ ((lane >> 1) & 7)));
+            }
+        }
+    };
+    auto multiply = [&](const Operands &o) {
+#pragma unroll
+        for (int i = 0; i < C::FC; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FR; ++j)
+                acc[i][j] = mfma_grad(T{}, o.b[i], o.a[j], acc[i][j]);
+    };
+    // Reads and products in turn, `valu` vector instructions to a product.
+    auto in_turn = [&](auto valu) {
+        constexpr int PRODUCTS = C::FC * C::FR, READS = 2 * C::FC + (TURNED ? 2 : 1) * C::FR;
+        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // a product
+            if (i * EACH < READS)
+                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);   // LDS reads
+            if constexpr (decltype(valu)::value > 0)
+                __builtin_amdgcn_sched_group_barrier(0x002, decltype(valu)::value, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr std::integral_constant<int, 0> NO_VALU{};
+    constexpr std::integral_constant<int, (46 * C::Q_TASKS + C::FC * C::FR - 1) / (C::FC * C::FR)>
+        PUT_VALU{};
+    if (steps > 0) {
+        // (Steps past the last are requested and put as zeros, so that the loop is
+        // the same each time.)
+        direct(0);
+        request(0);
+        put(0);
+        direct(1);
+        request(1);
+        pers::wait_vm_lgkm0<0>();
+        pers::barrier();
+        read(0, 0, f[0]);
+        for (int t = 0; t < steps; ++t) {
+            if (TURNED && sums) {
+                // (The WC waves that read the same rows of A take 16 of the step's
+                // 64 values each, or 32.)
+#pragma unroll
+                for (int ks = 0; ks < 4; ks += C::WC)
+#pragma unroll
+                    for (int j = 0; j < C::FR; ++j) {
+                        const u32x4 u = turned<A_PITCH>(a_stage(t), aa[j], ks + wc);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const f32x2 v = unpack2<T>(u[k]);
+                            bias[j] += v.x + v.y;
+                        }
+                    }
+            }
+            // What the step before requested has landed: Q's rows of step t + 1, which
+            // go to their stage now, and A's.
+            read(t, 1, f[1]);
+            __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0)
+            put(t + 1);
+            multiply(f[0]);
+            in_turn(PUT_VALU);
+            // Those of t + 2 are requested: their stage of A was read in step t - 1,
+            // before the last barrier.
+            direct(t + 2);
+            request(t + 2);
+            read(t, 2, f[0]);
+            multiply(f[1]);
+            in_turn(NO_VALU);
+            read(t, 3, f[1]);
+            multiply(f[0]);
+            in_turn(NO_VALU);
+            // This wave has read all of step t and written its part of t + 1.
+            pers::wait_lgkm0();
+            pers::barrier();
+            read(t + 1, 0, f[0]);
+            multiply(f[1]);
+            in_turn(NO_VALU);
+        }
+        pers::wait_vm_lgkm0<0>();
+    }
+    pers::barrier();            // the stages are free
+    if (TURNED && sums) {
+        // Both halves of a lane pair, then the WC waves' parts in order.
+        float *part = reinterpret_cast<float *>(sm);
+#pragma unroll
+        for (int j = 0; j < C::FR; ++j) {
             const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(bias[j]),
                                                             __float_as_uint(bias[j]), false, false);
-            if (lane < 32 && r < g.R)
-                g.dbias[(size_t)split * g.R + r] = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+            if (lane < 32)
+                part[wc * C::BR + (wr * C::FR + j) * 32 + lane] =
+                    __uint_as_float(p[0]) + __uint_as_float(p[1]);
         }
+        __syncthreads();
+        const int r = (int)threadIdx.x;
+        if (r < C::BR && r0 + r < g.R) {
+            float v = part[r];
+#pragma unroll
+            for (int w = 1; w < C::WC; ++w)
+                v += part[w * C::BR + r];
+            g.dbias[(size_t)split * g.R + r0 + r] = v;
+        }
+        __syncthreads();
     }
     const int row0 = r0 + wr * C::FR * 32, col0 = c0 + wc * C::FC * 32;
     const float back = ldexpf(1.0f, -shift);
@@ -385,7 +438,7 @@ template <class T, class C, bool TURNED, bool WHOLE>
 __global__ void __launch_bounds__(C::NT) k_token_grad(GradJob g, int first)
 {
     constexpr int OUT = C::WC * C::WR * kOutBytes<float, C::FC>;
-    __shared__ __attribute__((aligned(1024))) char sm[2 * C::STAGE > OUT ? 2 * C::STAGE : OUT];
+    __shared__ __attribute__((aligned(1024))) char sm[C::LDS > OUT ? C::LDS : OUT];
     const int unit = first + xcd_remap(blockIdx.x, gridDim.x);
     const int tiles = g.tiles_r * g.tiles_c, split = unit / tiles;
     int tr, tc;
