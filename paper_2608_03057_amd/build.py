@@ -52,6 +52,8 @@ SOURCES = [
     "mx4_gemm.hip",
     "token_grad_bf16.hip",
     "token_grad_f16.hip",
+    "grad_tiles_bf16.hip",
+    "grad_tiles_f16.hip",
     "branch_api.cpp",
     "cost.cpp",
     "tasq_api.cpp",

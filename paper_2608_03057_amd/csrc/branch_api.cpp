@@ -132,43 +132,109 @@ int residual_norm(const tasq_residual *a, bool grad, void *stream)
 
 constexpr size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 
-// Tiles and ranges of a product [R][C] over Z, and the bytes of its workspace.
-size_t plan_grad(tasq::GradJob &g, bool bias, bool cut)
+// One product of the gradient, [R][C] over Z, and how it runs: of values over 256-row
+// tiles, or of codes as they are.
+struct GradPlan {
+    int R, Z, C;
+    bool values;
+    int tile, tile_c;           // rows and columns of a tile
+    int tiles_r, tiles_c, splits, split_steps;
+    size_t parts;               // bytes of the ranges' parts
+};
+
+int tiles_of(int n, int t) { return (int)((n + t - 1LL) / t); }
+
+// Ranges of the sum: as many as give `units` workgroups, of at least `least` steps.
+void cut_sum(GradPlan &p, int steps, int units, int least, bool cut)
 {
-    const int steps = (int)((g.Z + 63LL) / 64);
-    auto tiles = [&](int t) { return ((g.R + t - 1LL) / t) * ((g.C + t - 1LL) / t); };
-    g.tile = 64;
-    g.splits = 1;
-    for (const int t : {256, 128, 64}) {
-        const long long n = tiles(t);
-        long long s = n > 0 && cut ? 256 / n : 1;
-        s = s < 1 ? 1 : s > steps / 8 ? (steps / 8 > 1 ? steps / 8 : 1) : s;
-        g.tile = t;
-        g.splits = (int)s;
-        if (n * s >= 128)
-            break;
-    }
-    g.tiles_r = (int)((g.R + g.tile - 1LL) / g.tile);
-    g.tiles_c = (int)((g.C + g.tile - 1LL) / g.tile);
-    if (bias && g.tiles_c == 0)
-        g.tiles_c = 1;          // the rows' sums alone
-    g.split_steps = (steps + g.splits - 1) / g.splits;
-    if (g.split_steps > 0)
-        g.splits = (steps + g.split_steps - 1) / g.split_steps;
-    if (g.splits <= 1)
-        return 0;
-    return round256((size_t)g.splits * g.R * g.C * sizeof(float)) +
-           round256((size_t)g.splits * g.R * sizeof(float));
+    const long long n = (long long)p.tiles_r * p.tiles_c;
+    long long s = n > 0 && cut ? units / n : 1;
+    const int most = steps / least;
+    s = s > most ? most : s;
+    p.splits = s < 1 ? 1 : (int)s;
+    p.split_steps = (steps + p.splits - 1) / p.splits;
+    if (p.split_steps > 0)
+        p.splits = (steps + p.split_steps - 1) / p.split_steps;
+    if (p.splits < 1)
+        p.splits = 1;
+    p.parts = p.splits == 1 ? 0
+                            : round256((size_t)p.splits * p.R * p.C * sizeof(float)) +
+                                  round256((size_t)p.splits * p.R * sizeof(float));
 }
 
-// The two products: of dx (turned false) and of dw.
-tasq::GradJob grad_job(int M, int N, int K, bool turned)
+// Of codes: tiles of 64 to 256 rows and columns, enough for half the compute units.
+void plan_codes(GradPlan &p, bool bias, bool cut)
 {
-    tasq::GradJob g{};
-    g.R = turned ? N : M;
-    g.Z = turned ? M : N;
-    g.C = K;
-    return g;
+    const int steps = (int)((p.Z + 63LL) / 64);
+    p.values = false;
+    for (const int t : {256, 128, 64}) {
+        p.tile = p.tile_c = t;
+        p.tiles_r = tiles_of(p.R, t);
+        p.tiles_c = tiles_of(p.C, t);
+        if (bias && p.tiles_c == 0)
+            p.tiles_c = 1;      // the rows' sums alone
+        cut_sum(p, steps, 256, 8, cut);
+        if ((long long)p.tiles_r * p.tiles_c * p.splits >= 128)
+            break;
+    }
+}
+
+// Of values: tiles of 256 rows by the width that takes the least time, counted in
+// rounds of one workgroup a compute unit.
+void plan_values(GradPlan &p, bool bias)
+{
+    const int steps = (int)((p.Z + 31LL) / 32);
+    GradPlan best{};
+    double least = 0;
+    for (const int c : {256, 192}) {
+        GradPlan q = p;
+        q.values = true;
+        q.tile = 256;
+        q.tile_c = c;
+        q.tiles_r = tiles_of(q.R, 256);
+        q.tiles_c = tiles_of(q.C, c);
+        if (bias && q.tiles_c == 0)
+            q.tiles_c = 1;
+        for (const int units : {256, 512}) {
+            cut_sum(q, steps, units, 16, true);
+            const long long n = (long long)q.tiles_r * q.tiles_c * q.splits;
+            const double us = (double)((n + 255) / 256) * (q.split_steps * 0.6 * c / 256.0 + 4.0) +
+                              (q.splits > 1 ? 2.0 + 2.0 * q.parts / 4e6 : 0.0);
+            if (least == 0 || us < least) {
+                least = us;
+                best = q;
+            }
+        }
+    }
+    p = best;
+}
+
+// Values pay where there are rows and columns enough to fill such tiles.
+bool values_pay(int M, int N, int K) { return M >= 512 && N >= 256 && K >= 128; }
+
+// The two products: of dx (turned false) and of dw.
+GradPlan grad_plan(int M, int N, int K, bool turned)
+{
+    GradPlan p{};
+    p.R = turned ? N : M;
+    p.Z = turned ? M : N;
+    p.C = K;
+    return p;
+}
+
+constexpr int whole_chunks(int n) { return (n + 7) / 8 * 8; }
+
+// Bytes of the values of both 8-bit operands and (copy) of dy, and of the two factors.
+struct ValueBytes {
+    size_t w, x, dy, back;
+    size_t all() const { return w + x + dy + back; }
+};
+
+ValueBytes value_bytes(int M, int N, int K, bool want_x, bool want_w, bool copy)
+{
+    const size_t row = 2 * (size_t)whole_chunks(K);
+    return {want_x ? round256(N * row) : 0, want_w ? round256(M * row) : 0,
+            copy ? round256((size_t)M * 2 * whole_chunks(N)) : 0, 256};
 }
 
 bool grad_sizes(int M, int N, int K)
@@ -242,13 +308,17 @@ size_t tasq_masked_linear_tokens_backward_workspace_bytes(int M, int N, int K)
 {
     if (!grad_sizes(M, N, K) || K > TASQ_MAX_K)
         return 0;
-    size_t most = 0;
+    size_t parts = 0;
+    const bool values = values_pay(M, N, K);
     for (const bool turned : {false, true}) {
-        tasq::GradJob g = grad_job(M, N, K, turned);
-        const size_t bytes = plan_grad(g, turned, true);
-        most = bytes > most ? bytes : most;
+        GradPlan p = grad_plan(M, N, K, turned);
+        if (values)
+            plan_values(p, turned);
+        else
+            plan_codes(p, turned, true);
+        parts = p.parts > parts ? p.parts : parts;
     }
-    return most;
+    return parts + (values ? value_bytes(M, N, K, true, true, N % 8 != 0).all() : 0);
 }
 
 int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_stride,
@@ -276,29 +346,128 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
         !aligned_to(sx, 4) || !aligned_to(sw, 4) || !aligned_to(workspace, 256))
         return TASQ_ERR_ALIGN;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const size_t have = workspace ? workspace_bytes : 0;
+    const bool bf16 = type == TASQ_TYPE_BF16;
+    const long long stride = M > 1 ? dy_stride : N;
+    size_t have = workspace ? workspace_bytes : 0;
+    char *at = static_cast<char *>(workspace);
+    GradPlan plan[2];
+    for (const bool turned : {false, true})
+        plan[turned] = grad_plan(M, N, K, turned);
+
+    // Values, where they pay and there is room for them.
+    const bool dy_whole = N % 8 == 0 && stride % 8 == 0 && aligned_to(dy, 16);
+    const ValueBytes vb = value_bytes(M, N, K, want_x, want_w, !dy_whole);
+    bool values = values_pay(M, N, K);
+    if (values) {
+        size_t parts = 0;
+        for (const bool turned : {false, true}) {
+            plan_values(plan[turned], turned && dbias);
+            const bool wanted = turned ? want_w : want_x;
+            parts = wanted && plan[turned].parts > parts ? plan[turned].parts : parts;
+        }
+        // (Offsets within a tile of dy are 32-bit.)
+        values = vb.all() + parts <= have && (dy_whole ? stride : whole_chunks(N)) < (1 << 22);
+    }
+    tasq::GradGemm gemm[2] = {};
+    if (values) {
+        tasq::GradValues v{};
+        auto take = [&](size_t bytes) {
+            char *p = at;
+            at += bytes;
+            return p;
+        };
+        float *back = reinterpret_cast<float *>(take(vb.back));
+        const void *A = dy;
+        long long a_stride = stride;
+        if (!dy_whole) {
+            auto &j = v.job[v.n++];
+            j = {};
+            j.from = dy;
+            j.from_stride = stride;
+            j.to = take(vb.dy);
+            j.rows = M;
+            j.width = N;
+            j.to_stride = whole_chunks(N);
+            A = j.to;
+            a_stride = j.to_stride;
+        }
+        for (const bool turned : {false, true}) {
+            if (!(turned ? want_w : want_x))
+                continue;
+            auto &j = v.job[v.n++];
+            j = {};
+            j.q = turned ? X : W;
+            j.s = turned ? sx : sw;
+            j.mask = turned ? 0xffffffffu : tasq::keep_mask_dword(b);
+            j.back = back + turned;
+            j.to = take(turned ? vb.x : vb.w);
+            j.rows = plan[turned].Z;
+            j.width = K;
+            j.to_stride = whole_chunks(K);
+            tasq::GradGemm &g = gemm[turned];
+            g.A = A;
+            g.a_stride = a_stride;
+            g.Q = j.to;
+            g.q_stride = j.to_stride;
+            g.back = bf16 ? nullptr : j.back;
+        }
+        if ((bf16 ? tasq::grad_values_bf16(v, st) : tasq::grad_values_f16(v, st)) != hipSuccess)
+            return TASQ_ERR_HIP;
+    }
     for (const bool turned : {false, true}) {
         if (!(turned ? want_w : want_x))
             continue;
-        tasq::GradJob g = grad_job(M, N, K, turned);
-        g.A = dy;
-        g.a_stride = M > 1 ? dy_stride : N;
-        g.Q = turned ? X : W;
-        g.s = turned ? sx : sw;
-        g.mask = turned ? 0xffffffffu : tasq::keep_mask_dword(b);
-        g.out = turned ? dw : dx;
-        g.dbias = turned ? dbias : nullptr;
-        if (plan_grad(g, g.dbias, true) > have)
-            plan_grad(g, g.dbias, false);
-        if (g.splits > 1) {
-            g.part = static_cast<float *>(workspace);
-            g.bias_part = g.part + round256((size_t)g.splits * g.R * g.C * sizeof(float)) / 4;
+        GradPlan &p = plan[turned];
+        float *const bias = turned ? dbias : nullptr;
+        if (!values) {
+            plan_codes(p, bias, true);
+            if (p.parts > have)
+                plan_codes(p, bias, false);
         }
-        // (Offsets within a tile of A are 32-bit.)
-        const bool whole = N % 8 == 0 && g.a_stride % 8 == 0 && K % 16 == 0 &&
-                           aligned_to(dy, 16) && aligned_to(g.Q, 16) && g.a_stride < (1 << 22);
-        const hipError_t e = type == TASQ_TYPE_BF16 ? tasq::token_grad_bf16(g, turned, whole, st)
-                                                    : tasq::token_grad_f16(g, turned, whole, st);
+        float *part = p.splits > 1 ? reinterpret_cast<float *>(at) : nullptr;
+        float *bias_part =
+            part ? part + round256((size_t)p.splits * p.R * p.C * sizeof(float)) / 4 : nullptr;
+        void *out = turned ? dw : dx;
+        hipError_t e;
+        if (values) {
+            tasq::GradGemm &g = gemm[turned];
+            g.out = out;
+            g.dbias = bias;
+            g.R = p.R;
+            g.Z = p.Z;
+            g.C = p.C;
+            g.tile_c = p.tile_c;
+            g.tiles_r = p.tiles_r;
+            g.tiles_c = p.tiles_c;
+            g.splits = p.splits;
+            g.split_steps = p.split_steps;
+            g.part = part;
+            g.bias_part = bias_part;
+            e = bf16 ? tasq::grad_gemm_bf16(g, turned, st) : tasq::grad_gemm_f16(g, turned, st);
+        } else {
+            tasq::GradJob g{};
+            g.A = dy;
+            g.a_stride = stride;
+            g.Q = turned ? X : W;
+            g.s = turned ? sx : sw;
+            g.mask = turned ? 0xffffffffu : tasq::keep_mask_dword(b);
+            g.out = out;
+            g.dbias = bias;
+            g.R = p.R;
+            g.Z = p.Z;
+            g.C = p.C;
+            g.tile = p.tile;
+            g.tiles_r = p.tiles_r;
+            g.tiles_c = p.tiles_c;
+            g.splits = p.splits;
+            g.split_steps = p.split_steps;
+            g.part = part;
+            g.bias_part = bias_part;
+            // (Offsets within a tile of dy are 32-bit.)
+            const bool whole = dy_whole && K % 16 == 0 && aligned_to(g.Q, 16) && stride < (1 << 22);
+            e = bf16 ? tasq::token_grad_bf16(g, turned, whole, st)
+                     : tasq::token_grad_f16(g, turned, whole, st);
+        }
         if (e != hipSuccess)
             return TASQ_ERR_HIP;
     }

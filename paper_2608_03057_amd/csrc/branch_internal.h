@@ -65,6 +65,38 @@ struct GradJob {
     int splits, split_steps;            // ranges of Z, in steps of 64
     float *part, *bias_part;            // [splits][R][C], [splits][R]
 };
+// The same over many tokens (grad_tiles.h): Q's values in A's type.
+struct GradGemm {
+    const void *A, *Q;          // rows of whole 16-byte chunks; Q [Z][q_stride]
+    long long a_stride;
+    int q_stride;
+    const float *back;          // factor of the sums, or null
+    void *out;
+    float *dbias;
+    int R, Z, C;
+    int tile_c, tiles_r, tiles_c;       // 256 rows by 256 or 192 columns
+    int splits, split_steps;            // ranges of Z, in steps of 32
+    float *part, *bias_part;
+};
+// Rows to be written as whole chunks of values: codes times factors, or values.
+struct GradValues {
+    struct Job {
+        const int8_t *q;        // [rows][width], or null: from
+        const float *s;         // [rows]
+        uint32_t mask;
+        float *back;            // receives the factor of the sums (half)
+        const void *from;
+        long long from_stride;
+        void *to;               // [rows][to_stride]
+        int rows, width, to_stride;
+    } job[3];
+    int n;
+};
+hipError_t grad_values_bf16(const GradValues &v, hipStream_t stream);
+hipError_t grad_values_f16(const GradValues &v, hipStream_t stream);
+hipError_t grad_gemm_bf16(const GradGemm &g, bool turned_a, hipStream_t stream);
+hipError_t grad_gemm_f16(const GradGemm &g, bool turned_a, hipStream_t stream);
+
 hipError_t token_grad_bf16(const GradJob &g, bool turned_a, bool whole, hipStream_t stream);
 hipError_t token_grad_f16(const GradJob &g, bool turned_a, bool whole, hipStream_t stream);
 

@@ -1,0 +1,345 @@
+// The token-scaled linear's gradient over many tokens: both operands in dy's type.
+//
+// Turning codes into values costs the K loop of token_grad.h as much as it can hide (88
+// vector instructions a wave and 64 rows beside 32 products), and every tile of rows
+// does it again.  Here a pass of its own writes s[z] q[z][c] once, rounded to dy's type
+// (rows filled up to whole 16-byte chunks; dy too, where its own are not), and the
+// product is one of two 16-bit matrices whose rows go to LDS directly: no registers and
+// no vector instructions but addresses between memory and the matrix unit.
+#pragma once
+
+#include "token_grad.h"
+
+namespace tasq {
+
+namespace {
+
+constexpr int kTileStep = 32;   // of the summed axis
+
+// Tiles of BC columns by BR rows, WC x WR waves, a ring of NS stages.
+template <int BC_, int BR_, int WC_, int WR_> struct TileCfg {
+    static constexpr int BC = BC_, BR = BR_, WC = WC_, WR = WR_, NT = 512, NS = 5;
+    static_assert(64 * WC * WR == NT, "eight waves");
+    static constexpr int FC = BC / WC / 32, FR = BR / WR / 32;
+    static constexpr int A_BYTES = BR * kTileStep * 2, Q_BYTES = BC * kTileStep * 2;
+    static constexpr int STAGE = A_BYTES + Q_BYTES;
+    static constexpr int A_LOADS = A_BYTES / 16 / NT;           // of a thread
+    static constexpr int Q_LOADS = (Q_BYTES / 16 + NT - 1) / NT;
+    static_assert(A_BYTES % (16 * NT) == 0, "whole loads of A");
+    // Threads without a chunk of Q in the last load write zeros behind the stages.
+    static constexpr int SPARE = Q_LOADS * 16 * NT - Q_BYTES;
+    static constexpr int LDS = NS * STAGE + SPARE;
+};
+
+template <class T, class C, bool TURNED>
+__device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc, int split,
+                                               char *sm)
+{
+    constexpr int A_PITCH = TURNED ? 2 * C::BR : 2 * kTileStep;
+    constexpr int Q_PITCH = 2 * C::BC;
+    const int lane = threadIdx.x & 63;
+    const int wave = (int)uniform(threadIdx.x >> 6);
+    const int wc = wave % C::WC, wr = wave / C::WC;
+    const int r0 = tr * C::BR, c0 = tc * C::BC;
+    const int z0 = split * g.split_steps * kTileStep;
+    const int z1 = min(g.Z, z0 + g.split_steps * kTileStep);
+    const int steps = (z1 - z0 + kTileStep - 1) / kTileStep;
+    const T *A = static_cast<const T *>(g.A), *Q = static_cast<const T *>(g.Q);
+    const uint32_t lds0 = lds_offset(sm);
+
+    // This lane's chunks: of A one column in all its rows, of Q each its own.
+    constexpr int A_CH = A_PITCH / 16, Q_CH = Q_PITCH / 16;
+    constexpr int A_NEXT = C::NT / A_CH;            // rows between a thread's chunks
+    static_assert(C::NT % A_CH == 0 && A_NEXT % 16 == 0, "one column a lane");
+    const int a_row = (int)threadIdx.x / A_CH, a_place = (int)threadIdx.x % A_CH;
+    const int a_col = 8 * (TURNED ? a_place ^ (4 * turn_key<A_PITCH>(a_row))
+                                  : a_place ^ ((a_row >> 2) & 3));
+    const uint32_t a_pitch = 2u * (uint32_t)g.a_stride, q_pitch = 2u * (uint32_t)g.q_stride;
+    const uint32_t a_off = TURNED && a_col >= g.R - r0
+                               ? kOOB
+                               : (uint32_t)a_row * a_pitch + 2u * (uint32_t)a_col;
+    const uint32_t a_rows = uniform(min(g.R - r0, C::BR));
+    uint32_t q_off[C::Q_LOADS];
+#pragma unroll
+    for (int i = 0; i < C::Q_LOADS; ++i) {
+        const int p = i * C::NT + (int)threadIdx.x, row = p / Q_CH;
+        const int c = 8 * ((p % Q_CH) ^ (4 * turn_key<Q_PITCH>(row)));
+        q_off[i] = row < kTileStep && c0 + c < g.C
+                       ? (uint32_t)row * q_pitch + 2u * (uint32_t)(c0 + c)
+                       : kOOB;
+    }
+    // Step t's rows to its stage, zeros past the range.
+    auto fetch = [&](uint32_t stage, int t) {
+        const int zt = z0 + kTileStep * t;
+        const int left = (int)uniform(max(z1 - zt, 0));
+        const uint32_t n = (uint32_t)min(left, kTileStep);
+        rsrc_t ra;
+        uint32_t off = a_off;
+        if constexpr (TURNED) {
+            ra = make_rsrc(A + (size_t)zt * g.a_stride + r0, n ? (n - 1) * a_pitch + 2u * a_rows : 0u);
+        } else {
+            // (From column zt on: the last row ends with the range.)
+            ra = make_rsrc(A + (size_t)r0 * g.a_stride + zt,
+                           left ? (a_rows - 1) * a_pitch + 2u * (uint32_t)left : 0u);
+            off = a_col < left ? off : kOOB;
+        }
+        const rsrc_t rq = make_rsrc(Q + (size_t)zt * g.q_stride, n * q_pitch);
+#pragma unroll
+        for (int i = 0; i < C::A_LOADS; ++i)
+            load_chunk_unseen(ra, lds0 + stage + (uint32_t)(i * C::NT + 64 * wave) * 16u,
+                              off + (uint32_t)(i * A_NEXT) * a_pitch);
+#pragma unroll
+        for (int i = 0; i < C::Q_LOADS; ++i) {
+            const uint32_t at = (uint32_t)(i * C::NT + 64 * wave) * 16u;
+            const uint32_t to = at < C::Q_BYTES ? stage + C::A_BYTES + at
+                                                : C::NS * C::STAGE + at - C::Q_BYTES;
+            load_chunk_unseen(rq, lds0 + to, q_off[i]);
+        }
+    };
+
+    uint32_t qa[C::FC], aa[C::FR];
+#pragma unroll
+    for (int i = 0; i < C::FC; ++i)
+        qa[i] = C::A_BYTES + turn_lane<Q_PITCH>(wc * C::FC + i);
+#pragma unroll
+    for (int j = 0; j < C::FR; ++j)
+        aa[j] = TURNED ? turn_lane<A_PITCH>(wr * C::FR + j) : 0;
+    uint32_t rows[2];           // of A as it lies: this lane's place in steps of 16
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+        rows[ks] = (uint32_t)((wr * C::FR * 32 + (lane & 31)) * A_PITCH +
+                              16 * ((2 * ks + (lane >> 5)) ^ ((lane >> 2) & 3)));
+    v16f_t acc[C::FC][C::FR];
+#pragma unroll
+    for (int i = 0; i < C::FC; ++i)
+#pragma unroll
+        for (int j = 0; j < C::FR; ++j)
+            acc[i][j] = v16f_t{};
+    const bool sums = TURNED && g.dbias && tc == 0;
+    float bias[C::FR] = {};
+
+    struct Operands {
+        u32x4 a[C::FR], b[C::FC];
+    } f[2];
+    auto read = [&](uint32_t stage, int ks, Operands &o) {
+        const char *p = sm + stage;
+#pragma unroll
+        for (int i = 0; i < C::FC; ++i)
+            o.b[i] = turned<Q_PITCH>(p, qa[i], ks);
+#pragma unroll
+        for (int j = 0; j < C::FR; ++j) {
+            if constexpr (TURNED)
+                o.a[j] = turned<A_PITCH>(p, aa[j], ks);
+            else
+                o.a[j] = *reinterpret_cast<const u32x4 *>(p + rows[ks] + j * 32 * A_PITCH);
+        }
+    };
+    auto multiply = [&](const Operands &o) {
+#pragma unroll
+        for (int i = 0; i < C::FC; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FR; ++j)
+                acc[i][j] = mfma_grad(T{}, o.b[i], o.a[j], acc[i][j]);
+    };
+    // Reads and products in turn.
+    auto in_turn = [&] {
+        constexpr int PRODUCTS = C::FC * C::FR, READS = 2 * C::FC + (TURNED ? 2 : 1) * C::FR;
+        constexpr int EACH = (READS + PRODUCTS - 1) / PRODUCTS;
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);          // a product
+            if (i * EACH < READS)
+                __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);   // LDS reads
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // A wave's requests of a step, and those of all steps but the next two.
+    constexpr int LOADS = C::A_LOADS + C::Q_LOADS, AHEAD = (C::NS - 2) * LOADS;
+    if (steps > 0) {
+        // (Steps past the last are fetched as zeros, so that the loop and its counts
+        // are the same each time.)
+#pragma unroll
+        for (int t = 0; t < C::NS - 1; ++t)
+            fetch((uint32_t)(t * C::STAGE), t);
+        pers::wait_vm_lgkm0<AHEAD>();
+        pers::barrier();
+        uint32_t st = 0, ahead = (C::NS - 1) * C::STAGE;        // stages of t and t + NS - 1
+        read(st, 0, f[0]);
+        for (int t = 0; t < steps; ++t) {
+            // Step t - 1's stage, which every wave had read before the last barrier.
+            fetch(ahead, t + C::NS - 1);
+            if constexpr (TURNED) {
+                // (The waves that read the same rows of A take the steps of 16 in
+                // turn.)
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+                    if (!sums || (2 * t + ks) % C::WC != wc)
+                        continue;
+#pragma unroll
+                    for (int j = 0; j < C::FR; ++j) {
+                        const u32x4 u = turned<A_PITCH>(sm + st, aa[j], ks);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const f32x2 v = unpack2<T>(u[k]);
+                            bias[j] += v.x + v.y;
+                        }
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            read(st, 1, f[1]);
+            multiply(f[0]);
+            in_turn();
+            // Step t + 1's rows have landed, and this wave has read all of step t.
+            pers::wait_vm_lgkm0<AHEAD>();
+            pers::barrier();
+            ahead = st;
+            st = st == (C::NS - 1) * C::STAGE ? 0 : st + C::STAGE;
+            read(st, 0, f[0]);
+            multiply(f[1]);
+            in_turn();
+        }
+        pers::wait_vm_lgkm0<0>();
+    }
+    pers::barrier();            // the stages are free
+    if (TURNED && sums)
+        store_row_sums<C>(bias, wr, wc, r0, g.R, g.dbias + (size_t)split * g.R, sm);
+    const int row0 = r0 + wr * C::FR * 32, col0 = c0 + wc * C::FC * 32;
+    const float back = g.back ? *g.back : 1.0f;
+    auto scaled = [&](int, int, float (&v)[4]) {
+        if constexpr (__is_same(T, f16_t)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] *= back;
+        }
+    };
+    if (g.splits > 1)
+        store_tile<float>(g.part + (size_t)split * g.R * g.C, g.R, g.C, row0, col0,
+                          sm + wave * kOutBytes<float, C::FC>, acc, scaled);
+    else
+        store_tile<T>(static_cast<T *>(g.out), g.R, g.C, row0, col0,
+                      sm + wave * kOutBytes<T, C::FC>, acc, scaled);
+}
+
+template <class T, class C, bool TURNED>
+__global__ void __launch_bounds__(C::NT) k_grad_gemm(GradGemm g, int first)
+{
+    constexpr int OUT = C::WC * C::WR * kOutBytes<float, C::FC>;
+    __shared__ __attribute__((aligned(1024))) char sm[C::LDS > OUT ? C::LDS : OUT];
+    const int unit = first + xcd_remap(blockIdx.x, gridDim.x);
+    const int tiles = g.tiles_r * g.tiles_c, split = unit / tiles;
+    int tr, tc;
+    tile_coords(unit - split * tiles, g.tiles_r, g.tiles_c, tr, tc);
+    grad_gemm_tile<T, C, TURNED>(g, (int)uniform(tr), (int)uniform(tc), (int)uniform(split), sm);
+}
+
+struct ValueThreads {
+    static constexpr int NT = 256;
+};
+
+// Writes codes times their rows' factors as rows of T, and copies rows of T, into rows
+// of whole 16-byte chunks (zeros past the width).
+template <class T> __global__ void __launch_bounds__(256) k_grad_values(GradValues v)
+{
+    __shared__ float part[4];
+    const int job = blockIdx.y;
+    const GradValues::Job &j = v.job[job];
+    const int chunks = j.to_stride / 8;
+    const size_t n = (size_t)j.rows * chunks;
+    int shift = 0;
+    if constexpr (__is_same(T, f16_t)) {
+        if (j.q) {
+            shift = range_exponent<ValueThreads>(j.s, 0, j.rows, part);
+            if (blockIdx.x == 0 && threadIdx.x == 0)
+                *j.back = ldexpf(1.0f, -shift);
+        }
+    }
+    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (size_t)gridDim.x * 256) {
+        const int row = (int)(at / chunks), c = 8 * (int)(at - (size_t)row * chunks);
+        u32x4 o = {0, 0, 0, 0};
+        if (j.q) {
+            const int8_t *p = j.q + (size_t)row * j.width + c;
+            u32x2 w = {0, 0};
+            if (c + 8 <= j.width) {
+                const Packed<int8_t, 8> e = *reinterpret_cast<const Packed<int8_t, 8> *>(p);
+                w = u32x2{e.w[0], e.w[1]};
+            } else {
+                uint64_t u = 0;
+                for (int e = 0; e < j.width - c; ++e)
+                    u |= (uint64_t)(uint8_t)p[e] << (8 * e);
+                w = u32x2{(uint32_t)u, (uint32_t)(u >> 32)};
+            }
+            const float s = __is_same(T, f16_t) ? ldexpf(j.s[row], shift) : j.s[row];
+            // (Zeros past the width, also where the factor is not finite.)
+            o = dequantize<T>(u32x2{w.x & j.mask, w.y & j.mask}, s);
+            if (c + 8 > j.width) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (c + e >= j.width)
+                        o[e / 2] &= e % 2 ? 0x0000ffffu : 0xffff0000u;
+            }
+        } else {
+            const T *p = static_cast<const T *>(j.from) + (size_t)row * j.from_stride + c;
+            if (c + 8 <= j.width) {
+                o = __builtin_bit_cast(u32x4, *reinterpret_cast<const Packed<T, 8> *>(p));
+            } else {
+                T e[8] = {};
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < j.width)
+                        e[k] = p[k];
+                o = __builtin_bit_cast(u32x4, e);
+            }
+        }
+        static_cast<u32x4 *>(j.to)[at] = o;
+    }
+}
+
+template <class T> hipError_t write_values(const GradValues &v, hipStream_t stream)
+{
+    size_t most = 0;
+    for (int i = 0; i < v.n; ++i) {
+        const size_t n = (size_t)v.job[i].rows * (v.job[i].to_stride / 8);
+        most = n > most ? n : most;
+    }
+    const size_t blocks = (most + 255) / 256;
+    k_grad_values<T><<<dim3((unsigned)(blocks < 2048 ? blocks : 2048), v.n), 256, 0, stream>>>(v);
+    return hipGetLastError();
+}
+
+template <class T, class C, bool TURNED> hipError_t launch_gemm(const GradGemm &g, hipStream_t stream)
+{
+    constexpr long long MOST = 1 << 22;
+    const long long units = (long long)g.tiles_r * g.tiles_c * g.splits;
+    for (long long u = 0; u < units; u += MOST) {
+        const unsigned grid = (unsigned)(units - u < MOST ? units - u : MOST);
+        k_grad_gemm<T, C, TURNED><<<grid, C::NT, 0, stream>>>(g, (int)u);
+        if (hipError_t e = hipGetLastError())
+            return e;
+    }
+    return hipSuccess;
+}
+
+template <class T, bool TURNED> hipError_t launch_gemm_tile(const GradGemm &g, hipStream_t stream)
+{
+    if (g.tile_c == 256)
+        return launch_gemm<T, TileCfg<256, 256, 4, 2>, TURNED>(g, stream);
+    return launch_gemm<T, TileCfg<192, 256, 2, 4>, TURNED>(g, stream);
+}
+
+template <class T> hipError_t run_gemm(GradGemm g, bool turned_a, hipStream_t stream)
+{
+    float *dbias = g.dbias;
+    if (g.splits > 1)
+        g.dbias = dbias ? g.bias_part : nullptr;
+    const hipError_t e = turned_a ? launch_gemm_tile<T, true>(g, stream)
+                                  : launch_gemm_tile<T, false>(g, stream);
+    if (e != hipSuccess || g.splits == 1)
+        return e;
+    return join_parts<T>(g.part, g.out, (size_t)g.R * g.C, g.splits, dbias ? g.bias_part : nullptr,
+                         dbias, g.R, stream);
+}
+
+}  // namespace
+
+}  // namespace tasq

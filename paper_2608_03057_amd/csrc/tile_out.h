@@ -26,17 +26,26 @@ __device__ __forceinline__ void load_chunk_to_lds(rsrc_t r, char *lds, uint32_t 
 
 // The same, not known to the compiler as a write to LDS, for which it would wait
 // before every transposing load: the caller waits (vmcnt) before the barrier that hands
-// the bytes on.  lds is the same in all lanes.  (m0 cannot be named as overwritten: a
+// the bytes on.  lds, an offset in LDS, is the same in all lanes.  (m0 cannot be named as overwritten: a
 // kernel uses this form or the one above, not both.)
-__device__ __forceinline__ void load_chunk_unseen(rsrc_t r, const char *lds, uint32_t off)
+__device__ __forceinline__ void load_chunk_unseen(rsrc_t r, uint32_t lds, uint32_t off)
+{
+#ifdef __HIP_DEVICE_COMPILE__
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(uniform((int)lds)), "v"(off), "s"(r)
+                 : "memory");
+#endif
+}
+
+// Where in LDS p is.
+__device__ __forceinline__ uint32_t lds_offset(const char *p)
 {
 #ifdef __HIP_DEVICE_COMPILE__
     typedef __attribute__((address_space(3))) const char lds_t;
-    const uint32_t to = uniform((int)(uint32_t)(uintptr_t)(lds_t *)lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 :
-                 : "s"(to), "v"(off), "s"(r)
-                 : "memory");
+    return (uint32_t)(uintptr_t)(lds_t *)p;
+#else
+    return 0;
 #endif
 }
 

@@ -54,7 +54,7 @@ template <int BC_, int BR_, int WC_, int WR_> struct GradCfg {
     // Three stages of A, two of Q.
     static_assert(NT >= BR && 4 % WC == 0, "a thread to a row's sum");
     static constexpr int LDS = 3 * A_BYTES + 2 * Q_BYTES;
-    static constexpr int Q_TASKS = kGradStep * BC / 16 / NT;    // 16 codes each
+    static constexpr int Q_TASKS = kGradStep * BC / 8 / NT;     // 8 codes each
     static constexpr int A_TASKS = kGradStep * BR / 8 / NT;     // 16 bytes each
 };
 
@@ -62,7 +62,7 @@ template <int BC_, int BR_, int WC_, int WR_> struct GradCfg {
 // transposing load reads: the rows that it spans fall in distinct banks.
 template <int PITCH> __device__ __forceinline__ int turn_key(int z)
 {
-    return PITCH >= 256 ? z & 3 : (z >> 1) & 1;
+    return PITCH % 256 == 0 ? z & 3 : (z >> 1) & 1;
 }
 
 template <int PITCH> __device__ __forceinline__ uint32_t turn_place(int z, int c)
@@ -85,29 +85,23 @@ __device__ __forceinline__ u32x4 turned(const char *lds, uint32_t at, int ks)
 {
     typedef __attribute__((address_space(3))) v4s_t lds_t;
     const char *p = lds + at + 16 * ks * PITCH;
-    // (Rows z and z + 4 have the same key.)
-    static_assert(PITCH >= 256 || PITCH == 128, "keys repeat every four rows");
+    static_assert(PITCH % 128 == 0, "rows z and z + 4 have the same key");
     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)p));
     const u32x2 hi = __builtin_bit_cast(
         u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)(p + 4 * PITCH)));
     return u32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
-// 16 codes times their row's factor as 16 values of T.
-template <class T>
-__device__ __forceinline__ void dequantize(v4i q, float s, u32x4 &lo, u32x4 &hi)
+// Eight codes times their row's factor as eight values of T.
+template <class T> __device__ __forceinline__ u32x4 dequantize(u32x2 q, float s)
 {
-    float v[16];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[4 * i + j] = (float)(int8_t)((uint32_t)q[i] >> (8 * j)) * s;
+    u32x4 o;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        lo[i] = pack2<T>(v[2 * i], v[2 * i + 1]);
-        hi[i] = pack2<T>(v[8 + 2 * i], v[9 + 2 * i]);
+        const uint32_t w = q[i / 2] >> (16 * (i & 1));
+        o[i] = pack2<T>((float)(int8_t)w * s, (float)(int8_t)(w >> 8) * s);
     }
+    return o;
 }
 
 // The power of two that brings the largest finite factor of [z0, z1) to 2^7: with
@@ -134,6 +128,34 @@ __device__ __forceinline__ int range_exponent(const float *s, int z0, int z1, fl
     return 8 - e;
 }
 
+// The sums of a tile's rows that its waves hold, a row to the lanes l and l + 32 and to
+// C::WC waves, added up in order into out[r0 ..]; LDS is free before and after.
+template <class C>
+__device__ __forceinline__ void store_row_sums(const float (&sum)[C::FR], int wr, int wc, int r0,
+                                               int R, float *out, char *sm)
+{
+    const int lane = threadIdx.x & 63;
+    float *part = reinterpret_cast<float *>(sm);
+#pragma unroll
+    for (int j = 0; j < C::FR; ++j) {
+        const uint32_t u = __float_as_uint(sum[j]);
+        const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        if (lane < 32)
+            part[wc * C::BR + (wr * C::FR + j) * 32 + lane] =
+                __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    __syncthreads();
+    const int r = (int)threadIdx.x;
+    if (r < C::BR && r0 + r < R) {
+        float v = part[r];
+#pragma unroll
+        for (int w = 1; w < C::WC; ++w)
+            v += part[w * C::BR + r];
+        out[r0 + r] = v;
+    }
+    __syncthreads();
+}
+
 // out[r][c] of one tile and range of the summed axis.  TURNED: A is [Z][R], else
 // [R][Z].  WHOLE: rows of both operands are whole 16-byte chunks at 16-byte addresses,
 // and those of A go to LDS directly.
@@ -157,40 +179,52 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
 
     // A step's codes and factors (and A's chunks, where they pass through registers)
     // on their way.
-    v4i q[C::Q_TASKS];
-    float s[C::Q_TASKS];
-    u32x4 ar[WHOLE ? 1 : C::A_TASKS];
-    auto a_stage = [&](int t) { return sm + (t % 3) * C::A_BYTES; };
-    auto q_stage = [&](int t) { return sm + 3 * C::A_BYTES + (t & 1) * C::Q_BYTES; };
+    struct Raw {
+        u32x2 q[C::Q_TASKS];
+        float s[C::Q_TASKS];
+        u32x4 a[WHOLE ? 1 : C::A_TASKS];
+    };
+    // Offsets in LDS of a step's stage of A, and of Q.
+    struct Stage {
+        uint32_t a, q;
+    };
+    const uint32_t lds0 = lds_offset(sm);
+    // This thread's first eight codes of a step: row qz, column c0 + qc, in every part.
+    // (Neighbouring lanes write neighbouring chunks.)
+    constexpr int Q_ROWS = C::NT / (C::BC / 8);     // between a thread's parts
+    const int qz = (int)threadIdx.x / (C::BC / 8), qc = 8 * ((int)threadIdx.x % (C::BC / 8));
+    const uint32_t q_off =
+        c0 + qc < g.C ? (uint32_t)qz * (uint32_t)g.C + (uint32_t)(c0 + qc) : kOOB;
     // Step t's, zeros past the range.
-    auto request = [&](int t) {
+    auto request = [&](Raw &raw, int t) {
         const int zt = z0 + kGradStep * t;
         const uint32_t n = uniform(max(min(z1 - zt, kGradStep), 0));
         const rsrc_t rs = make_rsrc(g.s + zt, 4u * n);
         const rsrc_t rq = make_rsrc(g.Q + (size_t)zt * g.C, WHOLE ? n * (uint32_t)g.C : 0u);
 #pragma unroll
         for (int i = 0; i < C::Q_TASKS; ++i) {
-            const int task = (int)threadIdx.x + i * C::NT;
-            const int z = task / (C::BC / 16), c = c0 + 16 * (task % (C::BC / 16));
-            s[i] = __builtin_bit_cast(
+            const int z = qz + i * Q_ROWS, c = c0 + qc;
+            raw.s[i] = __builtin_bit_cast(
                 float, __builtin_amdgcn_raw_buffer_load_b32(rs, 4u * (uint32_t)z, 0, 0));
             if constexpr (WHOLE) {
-                q[i] = ld16(rq, c < g.C ? (uint32_t)z * (uint32_t)g.C + (uint32_t)c : kOOB);
+                raw.q[i] = __builtin_bit_cast(
+                    u32x2, __builtin_amdgcn_raw_buffer_load_b64(
+                               rq, q_off + (uint32_t)(i * Q_ROWS) * (uint32_t)g.C, 0, 0));
             } else {
-                q[i] = v4i{0, 0, 0, 0};
+                raw.q[i] = u32x2{0, 0};
                 if (zt + z >= z1 || c >= g.C)
                     continue;
                 const int8_t *p = g.Q + (size_t)(zt + z) * g.C + c;
                 const long long left = (long long)(q_end - p);
-                if (left >= 16) {
-                    const Packed<int8_t, 16> w = *reinterpret_cast<const Packed<int8_t, 16> *>(p);
-                    q[i] = v4i{(int)w.w[0], (int)w.w[1], (int)w.w[2], (int)w.w[3]};
+                if (left >= 8) {
+                    const Packed<int8_t, 8> w = *reinterpret_cast<const Packed<int8_t, 8> *>(p);
+                    raw.q[i] = u32x2{w.w[0], w.w[1]};
                 } else {            // of the last row of all
-                    uint64_t w[2] = {0, 0};
+                    uint64_t w = 0;
 #pragma unroll 1
                     for (int e = 0; e < (int)left; ++e)
-                        w[e >= 8] |= (uint64_t)(uint8_t)p[e] << (8 * (e & 7));
-                    q[i] = v4i{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
+                        w |= (uint64_t)(uint8_t)p[e] << (8 * e);
+                    raw.q[i] = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
                 }
             }
         }
@@ -201,75 +235,72 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
                 const int z = TURNED ? zt + row : zt + first, r = TURNED ? r0 + first : r0 + row;
                 const int left = TURNED ? g.R - r : z1 - z;     // of the row of A
-                ar[i] = u32x4{0, 0, 0, 0};
+                raw.a[i] = u32x4{0, 0, 0, 0};
                 if ((TURNED ? z >= z1 : r >= g.R) || left <= 0)
                     continue;
                 const T *p = A + (TURNED ? (size_t)z * g.a_stride + r : (size_t)r * g.a_stride + z);
                 if (left >= 8) {
-                    ar[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Packed<T, 8> *>(p));
+                    raw.a[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Packed<T, 8> *>(p));
                 } else {
                     T e[8] = {};
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
                         if (k < left)
                             e[k] = p[k];
-                    ar[i] = __builtin_bit_cast(u32x4, e);
+                    raw.a[i] = __builtin_bit_cast(u32x4, e);
                 }
             }
         }
     };
-    // Step t's rows of A straight to LDS.
-    auto direct = [&](int t) {
+    // This lane's first chunk of a step's rows of A: A_ROWS rows an instruction, every
+    // A_NEXT-th of a wave's.  Its column is the same in all of them.
+    constexpr int CH = A_PITCH / 16, A_ROWS = 64 / CH, A_NEXT = C::NT / 64 * A_ROWS;
+    static_assert(TURNED ? A_NEXT % 4 == 0 : A_NEXT % 16 == 0, "one column a lane");
+    const int a_row = wave * A_ROWS + lane / CH;
+    const int a_col = 8 * (TURNED ? (lane % CH) ^ (4 * turn_key<A_PITCH>(a_row))
+                                  : (lane % CH) ^ ((a_row >> 1) & 7));
+    const uint32_t a_pitch = 2u * (uint32_t)g.a_stride;
+    const uint32_t a_off = TURNED && a_col >= g.R - r0
+                               ? kOOB
+                               : (uint32_t)a_row * a_pitch + 2u * (uint32_t)a_col;
+    const uint32_t a_last = 2u * uniform(min(g.R - r0, C::BR));
+    // Step t's rows of A straight to LDS, zeros past the range.
+    auto direct = [&](uint32_t stage, int t) {
         if constexpr (WHOLE) {
-            char *to = a_stage(t);
-            const uint32_t pitch = 2u * (uint32_t)g.a_stride;
             const int zt = z0 + kGradStep * t;
-            constexpr int CH = A_PITCH / 16;                    // chunks of a tile's row
-            constexpr int ROWS = 64 / CH > 0 ? 64 / CH : 1;     // of an instruction
+            const int left = (int)uniform(max(z1 - zt, 0));
             rsrc_t rsrc;
+            uint32_t off = a_off;
             if constexpr (TURNED) {
-                const uint32_t n = uniform(max(min(z1 - zt, kGradStep), 0));
-                rsrc = make_rsrc(A + (size_t)zt * g.a_stride + r0,
-                                 n ? (n - 1) * pitch + 2u * uniform(min(g.R - r0, C::BR)) : 0u);
+                const uint32_t n = (uint32_t)min(left, kGradStep);
+                rsrc = make_rsrc(A + (size_t)zt * g.a_stride + r0, n ? (n - 1) * a_pitch + a_last : 0u);
             } else {
-                const uint32_t n = uniform(min(g.R - r0, C::BR));
-                rsrc = make_rsrc(A + (size_t)r0 * g.a_stride,
-                                 (n - 1) * pitch + 2u * (uint32_t)g.Z);
+                // (From column zt on: the last row ends with the range.)
+                rsrc = make_rsrc(A + (size_t)r0 * g.a_stride + zt,
+                                 left ? (a_last / 2 - 1) * a_pitch + 2u * (uint32_t)left : 0u);
+                off = a_col < left ? off : kOOB;
             }
 #pragma unroll
-            for (int i = 0; i < C::A_TASKS; ++i) {
-                const int first = (i * (C::NT / 64) + wave) * ROWS;     // the wave's first row
-                const int row = first + lane / CH, place = lane % CH;
-                uint32_t off;
-                if constexpr (TURNED) {
-                    const int c = place ^ (4 * turn_key<A_PITCH>(row));
-                    off = (uint32_t)row * pitch + 16u * (uint32_t)c;
-                    off = 8 * c < g.R - r0 ? off : kOOB;
-                } else {
-                    const int z = zt + 8 * (place ^ ((row >> 1) & 7));
-                    off = z < z1 ? (uint32_t)row * pitch + 2u * (uint32_t)z : kOOB;
-                }
-                load_chunk_unseen(rsrc, to + first * A_PITCH, off);
-            }
+            for (int i = 0; i < C::A_TASKS; ++i)
+                load_chunk_unseen(rsrc, lds0 + stage + (uint32_t)((wave * A_ROWS + i * A_NEXT) * A_PITCH),
+                                  off + (uint32_t)(i * A_NEXT) * a_pitch);
         }
     };
-    // What request() gave, into stage t.
-    auto put = [&](int t) {
-        char *to = q_stage(t);
+    // What request() gave, into its stage: Q's parts i0 .. i1 - 1; A's chunks.
+    const uint32_t q_to = turn_place<Q_PITCH>(qz, qc / 8);
+    static_assert(Q_ROWS % 4 == 0, "rows of a thread have one key");
+    auto put = [&](const Raw &raw, Stage st, int i0, int i1) {
+        char *to = sm + st.q;
 #pragma unroll
         for (int i = 0; i < C::Q_TASKS; ++i) {
-            const int task = (int)threadIdx.x + i * C::NT;
-            const int z = task / (C::BC / 16), c = 2 * (task % (C::BC / 16));
-            v4i v = q[i];
-            v.x &= (int)g.mask;
-            v.y &= (int)g.mask;
-            v.z &= (int)g.mask;
-            v.w &= (int)g.mask;
-            u32x4 lo, hi;
-            dequantize<T>(v, __is_same(T, f16_t) ? ldexpf(s[i], shift) : s[i], lo, hi);
-            *reinterpret_cast<u32x4 *>(to + turn_place<Q_PITCH>(z, c)) = lo;
-            *reinterpret_cast<u32x4 *>(to + turn_place<Q_PITCH>(z, c + 1)) = hi;
+            if (i < i0 || i >= i1)
+                continue;
+            const float s = __is_same(T, f16_t) ? ldexpf(raw.s[i], shift) : raw.s[i];
+            *reinterpret_cast<u32x4 *>(to + q_to + i * Q_ROWS * Q_PITCH) =
+                dequantize<T>(u32x2{raw.q[i].x & g.mask, raw.q[i].y & g.mask}, s);
         }
+    };
+    auto put_chunks = [&](const Raw &raw, Stage st) {
         if constexpr (!WHOLE) {
 #pragma unroll
             for (int i = 0; i < C::A_TASKS; ++i) {
@@ -277,7 +308,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 const int row = task / (A_PITCH / 16), c = task % (A_PITCH / 16);
                 const uint32_t at = TURNED ? turn_place<A_PITCH>(row, c)
                                            : (uint32_t)(row * A_PITCH + 16 * (c ^ ((row >> 1) & 7)));
-                *reinterpret_cast<u32x4 *>(a_stage(t) + at) = ar[i];
+                *reinterpret_cast<u32x4 *>(sm + st.a + at) = raw.a[i];
             }
         }
     };
@@ -301,8 +332,8 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     struct Operands {
         u32x4 a[C::FR], b[C::FC];
     } f[2];
-    auto read = [&](int t, int ks, Operands &o) {
-        const char *A = a_stage(t), *Q = q_stage(t);
+    auto read = [&](Stage st, int ks, Operands &o) {
+        const char *A = sm + st.a, *Q = sm + st.q;
 #pragma unroll
         for (int i = 0; i < C::FC; ++i)
             o.b[i] = turned<Q_PITCH>(Q, qa[i], ks);
@@ -339,19 +370,25 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
         __builtin_amdgcn_sched_barrier(0);
     };
     constexpr std::integral_constant<int, 0> NO_VALU{};
-    constexpr std::integral_constant<int, (46 * C::Q_TASKS + C::FC * C::FR - 1) / (C::FC * C::FR)>
+    constexpr int HALF = (C::Q_TASKS + 1) / 2;
+    constexpr std::integral_constant<int, (23 * HALF + C::FC * C::FR - 1) / (C::FC * C::FR)>
         PUT_VALU{};
     if (steps > 0) {
         // (Steps past the last are requested and put as zeros, so that the loop is
         // the same each time.)
-        direct(0);
-        request(0);
-        put(0);
-        direct(1);
-        request(1);
+        constexpr uint32_t Q0 = 3 * C::A_BYTES, A1 = C::A_BYTES, Q1 = C::Q_BYTES;
+        Stage st = {0, Q0}, after = {A1, Q0 + Q1};      // of steps t and t + 1
+        uint32_t free_a = 2 * A1;                       // of step t + 2
+        Raw now, next;
+        direct(st.a, 0);
+        request(now, 0);
+        put(now, st, 0, C::Q_TASKS);
+        put_chunks(now, st);
+        direct(after.a, 1);
+        request(next, 1);
         pers::wait_vm_lgkm0<0>();
         pers::barrier();
-        read(0, 0, f[0]);
+        read(st, 0, f[0]);
         for (int t = 0; t < steps; ++t) {
             if (TURNED && sums) {
                 // (The WC waves that read the same rows of A take 16 of the step's
@@ -360,7 +397,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 for (int ks = 0; ks < 4; ks += C::WC)
 #pragma unroll
                     for (int j = 0; j < C::FR; ++j) {
-                        const u32x4 u = turned<A_PITCH>(a_stage(t), aa[j], ks + wc);
+                        const u32x4 u = turned<A_PITCH>(sm + st.a, aa[j], ks + wc);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const f32x2 v = unpack2<T>(u[k]);
@@ -369,54 +406,40 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                     }
             }
             // What the step before requested has landed: Q's rows of step t + 1, which
-            // go to their stage now, and A's.
-            read(t, 1, f[1]);
+            // go to their stage now, and A's.  Those of t + 2 are requested: their
+            // stage of A was read in step t - 1, before the last barrier.
+            read(st, 1, f[1]);
             __builtin_amdgcn_s_waitcnt(0x0f70);     // vmcnt(0)
-            put(t + 1);
+            now = next;
+            direct(free_a, t + 2);
+            request(next, t + 2);
+            put(now, after, 0, HALF);
             multiply(f[0]);
             in_turn(PUT_VALU);
-            // Those of t + 2 are requested: their stage of A was read in step t - 1,
-            // before the last barrier.
-            direct(t + 2);
-            request(t + 2);
-            read(t, 2, f[0]);
+            read(st, 2, f[0]);
+            put(now, after, HALF, C::Q_TASKS);
             multiply(f[1]);
-            in_turn(NO_VALU);
-            read(t, 3, f[1]);
+            in_turn(PUT_VALU);
+            read(st, 3, f[1]);
+            put_chunks(now, after);
             multiply(f[0]);
             in_turn(NO_VALU);
             // This wave has read all of step t and written its part of t + 1.
             pers::wait_lgkm0();
             pers::barrier();
-            read(t + 1, 0, f[0]);
+            const uint32_t done = st.a;
+            st = after;
+            after = {free_a, 2 * Q0 + Q1 - st.q};
+            free_a = done;
+            read(st, 0, f[0]);
             multiply(f[1]);
             in_turn(NO_VALU);
         }
         pers::wait_vm_lgkm0<0>();
     }
     pers::barrier();            // the stages are free
-    if (TURNED && sums) {
-        // Both halves of a lane pair, then the WC waves' parts in order.
-        float *part = reinterpret_cast<float *>(sm);
-#pragma unroll
-        for (int j = 0; j < C::FR; ++j) {
-            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(bias[j]),
-                                                            __float_as_uint(bias[j]), false, false);
-            if (lane < 32)
-                part[wc * C::BR + (wr * C::FR + j) * 32 + lane] =
-                    __uint_as_float(p[0]) + __uint_as_float(p[1]);
-        }
-        __syncthreads();
-        const int r = (int)threadIdx.x;
-        if (r < C::BR && r0 + r < g.R) {
-            float v = part[r];
-#pragma unroll
-            for (int w = 1; w < C::WC; ++w)
-                v += part[w * C::BR + r];
-            g.dbias[(size_t)split * g.R + r0 + r] = v;
-        }
-        __syncthreads();
-    }
+    if (TURNED && sums)
+        store_row_sums<C>(bias, wr, wc, r0, g.R, g.dbias + (size_t)split * g.R, sm);
     const int row0 = r0 + wr * C::FR * 32, col0 = c0 + wc * C::FC * 32;
     const float back = ldexpf(1.0f, -shift);
     auto scaled = [&](int, int, float (&v)[4]) {
@@ -515,6 +538,16 @@ hipError_t launch_product(const GradJob &g, bool whole, hipStream_t stream)
     return launch_cfg<T, GradCfg<64, 64, 2, 2>, TURNED>(g, whole, stream);
 }
 
+template <class T>
+hipError_t join_parts(const float *part, void *out, size_t n, int splits, const float *bias_part,
+                      float *dbias, int bias_n, hipStream_t stream)
+{
+    const size_t threads = (n + 3) / 4 + (dbias ? bias_n : 0);
+    k_join_grad<T><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(
+        part, static_cast<T *>(out), n, splits, bias_part, dbias, bias_n);
+    return hipGetLastError();
+}
+
 // One of the two products and, where its range is cut, the sum of its parts.
 template <class T> hipError_t run_product(GradJob g, bool turned_a, bool whole, hipStream_t stream)
 {
@@ -525,10 +558,8 @@ template <class T> hipError_t run_product(GradJob g, bool turned_a, bool whole, 
                             : launch_product<T, false>(g, whole, stream);
     if (e != hipSuccess || g.splits == 1)
         return e;
-    const size_t n = (size_t)g.R * g.C, threads = (n + 3) / 4 + (dbias ? g.R : 0);
-    k_join_grad<T><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(
-        g.part, static_cast<T *>(g.out), n, g.splits, dbias ? g.bias_part : nullptr, dbias, g.R);
-    return hipGetLastError();
+    return join_parts<T>(g.part, g.out, (size_t)g.R * g.C, g.splits, dbias ? g.bias_part : nullptr,
+                         dbias, g.R, stream);
 }
 
 }  // namespace
