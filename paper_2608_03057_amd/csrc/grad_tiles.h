@@ -16,26 +16,41 @@ namespace {
 
 constexpr int kTileStep = 32;   // of the summed axis
 
-// Tiles of BC columns by BR rows, WC x WR waves, a ring of NS stages.
-template <int BC_, int BR_, int WC_, int WR_> struct TileCfg {
-    static constexpr int BC = BC_, BR = BR_, WC = WC_, WR = WR_, NT = 512, NS = 5;
-    static_assert(64 * WC * WR == NT, "eight waves");
+// Tiles of BC columns by BR rows, WC x WR waves.  Rows of Q, and of A turned, are a
+// step's stage in a ring of NS; of A as it lies a stage has two steps, so that a row's
+// part is a whole cache line.  (With one step to a stage, half lines, 4096x2240 ->
+// 11200 took 231 us for dx.)
+template <int BC_, int BR_, int WC_, int WR_, int NS_, int NA_, bool TURNED_> struct TileCfg {
+    static constexpr int BC = BC_, BR = BR_, WC = WC_, WR = WR_, NT = 64 * WC * WR;
+    static constexpr bool TURNED = TURNED_;
     static constexpr int FC = BC / WC / 32, FR = BR / WR / 32;
-    static constexpr int A_BYTES = BR * kTileStep * 2, Q_BYTES = BC * kTileStep * 2;
-    static constexpr int STAGE = A_BYTES + Q_BYTES;
+    static constexpr int SPAN = TURNED ? 1 : 2;                 // steps of a stage of A
+    static constexpr int NS = NS_, NA = TURNED ? NS_ : NA_;     // stages of Q and A
+    static_assert(NS - 2 < SPAN * (NA - 1), "rows of A are asked for before those of Q");
+    static constexpr int A_BYTES = BR * SPAN * kTileStep * 2, Q_BYTES = BC * kTileStep * 2;
     static constexpr int A_LOADS = A_BYTES / 16 / NT;           // of a thread
     static constexpr int Q_LOADS = (Q_BYTES / 16 + NT - 1) / NT;
     static_assert(A_BYTES % (16 * NT) == 0, "whole loads of A");
     // Threads without a chunk of Q in the last load write zeros behind the stages.
-    static constexpr int SPARE = Q_LOADS * 16 * NT - Q_BYTES;
-    static constexpr int LDS = NS * STAGE + SPARE;
+    static constexpr int Q0 = NA * A_BYTES, SPARE0 = Q0 + NS * Q_BYTES;
+    static constexpr int LDS = SPARE0 + Q_LOADS * 16 * NT - Q_BYTES;
+    // Requests of a wave that follow those of step t + 1 (and of its rows of A) when
+    // step t, part `half` of a stage of A, ends: of NS - 2 steps.
+    static constexpr int ahead(int half)
+    {
+        int n = 0;
+        for (int d = 0; d < NS - 2; ++d)
+            n += Q_LOADS + ((half + SPAN * NS - d) % SPAN == 0 ? A_LOADS : 0);
+        return n;
+    }
 };
 
-template <class T, class C, bool TURNED>
+template <class T, class C>
 __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc, int split,
                                                char *sm)
 {
-    constexpr int A_PITCH = TURNED ? 2 * C::BR : 2 * kTileStep;
+    constexpr bool TURNED = C::TURNED;
+    constexpr int A_PITCH = TURNED ? 2 * C::BR : 2 * C::SPAN * kTileStep;
     constexpr int Q_PITCH = 2 * C::BC;
     const int lane = threadIdx.x & 63;
     const int wave = (int)uniform(threadIdx.x >> 6);
@@ -53,7 +68,7 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
     static_assert(C::NT % A_CH == 0 && A_NEXT % 16 == 0, "one column a lane");
     const int a_row = (int)threadIdx.x / A_CH, a_place = (int)threadIdx.x % A_CH;
     const int a_col = 8 * (TURNED ? a_place ^ (4 * turn_key<A_PITCH>(a_row))
-                                  : a_place ^ ((a_row >> 2) & 3));
+                                  : a_place ^ ((a_row >> 1) & 7));
     const uint32_t a_pitch = 2u * (uint32_t)g.a_stride, q_pitch = 2u * (uint32_t)g.q_stride;
     const uint32_t a_off = TURNED && a_col >= g.R - r0
                                ? kOOB
@@ -68,14 +83,15 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
                        ? (uint32_t)row * q_pitch + 2u * (uint32_t)(c0 + c)
                        : kOOB;
     }
-    // Step t's rows to its stage, zeros past the range.
-    auto fetch = [&](uint32_t stage, int t) {
+    // Rows of A of step t (and the next, C::SPAN of them), and of Q, to a stage; zeros
+    // past the range.
+    auto fetch_a = [&](uint32_t stage, int t) {
         const int zt = z0 + kTileStep * t;
         const int left = (int)uniform(max(z1 - zt, 0));
-        const uint32_t n = (uint32_t)min(left, kTileStep);
         rsrc_t ra;
         uint32_t off = a_off;
         if constexpr (TURNED) {
+            const uint32_t n = (uint32_t)min(left, kTileStep);
             ra = make_rsrc(A + (size_t)zt * g.a_stride + r0, n ? (n - 1) * a_pitch + 2u * a_rows : 0u);
         } else {
             // (From column zt on: the last row ends with the range.)
@@ -83,32 +99,35 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
                            left ? (a_rows - 1) * a_pitch + 2u * (uint32_t)left : 0u);
             off = a_col < left ? off : kOOB;
         }
-        const rsrc_t rq = make_rsrc(Q + (size_t)zt * g.q_stride, n * q_pitch);
 #pragma unroll
         for (int i = 0; i < C::A_LOADS; ++i)
             load_chunk_unseen(ra, lds0 + stage + (uint32_t)(i * C::NT + 64 * wave) * 16u,
                               off + (uint32_t)(i * A_NEXT) * a_pitch);
+    };
+    auto fetch_q = [&](uint32_t stage, int t) {
+        const int zt = z0 + kTileStep * t;
+        const uint32_t n = uniform(min(max(z1 - zt, 0), kTileStep));
+        const rsrc_t rq = make_rsrc(Q + (size_t)zt * g.q_stride, n * q_pitch);
 #pragma unroll
         for (int i = 0; i < C::Q_LOADS; ++i) {
             const uint32_t at = (uint32_t)(i * C::NT + 64 * wave) * 16u;
-            const uint32_t to = at < C::Q_BYTES ? stage + C::A_BYTES + at
-                                                : C::NS * C::STAGE + at - C::Q_BYTES;
-            load_chunk_unseen(rq, lds0 + to, q_off[i]);
+            load_chunk_unseen(rq, lds0 + (at < C::Q_BYTES ? stage + at : C::SPARE0 + at - C::Q_BYTES),
+                              q_off[i]);
         }
     };
 
     uint32_t qa[C::FC], aa[C::FR];
 #pragma unroll
     for (int i = 0; i < C::FC; ++i)
-        qa[i] = C::A_BYTES + turn_lane<Q_PITCH>(wc * C::FC + i);
+        qa[i] = turn_lane<Q_PITCH>(wc * C::FC + i);
 #pragma unroll
     for (int j = 0; j < C::FR; ++j)
         aa[j] = TURNED ? turn_lane<A_PITCH>(wr * C::FR + j) : 0;
-    uint32_t rows[2];           // of A as it lies: this lane's place in steps of 16
+    uint32_t rows[2 * C::SPAN]; // of A as it lies: this lane's place in steps of 16
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < 2 * C::SPAN; ++ks)
         rows[ks] = (uint32_t)((wr * C::FR * 32 + (lane & 31)) * A_PITCH +
-                              16 * ((2 * ks + (lane >> 5)) ^ ((lane >> 2) & 3)));
+                              16 * ((2 * ks + (lane >> 5)) ^ ((lane >> 1) & 7)));
     v16f_t acc[C::FC][C::FR];
 #pragma unroll
     for (int i = 0; i < C::FC; ++i)
@@ -121,17 +140,18 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
     struct Operands {
         u32x4 a[C::FR], b[C::FC];
     } f[2];
-    auto read = [&](uint32_t stage, int ks, Operands &o) {
-        const char *p = sm + stage;
+    // Half ks of a step: of Q's stage, and of A's from its part `half` on.
+    auto read = [&](uint32_t a_stage, int half, uint32_t q_stage, int ks, Operands &o) {
 #pragma unroll
         for (int i = 0; i < C::FC; ++i)
-            o.b[i] = turned<Q_PITCH>(p, qa[i], ks);
+            o.b[i] = turned<Q_PITCH>(sm + q_stage, qa[i], ks);
 #pragma unroll
         for (int j = 0; j < C::FR; ++j) {
             if constexpr (TURNED)
-                o.a[j] = turned<A_PITCH>(p, aa[j], ks);
+                o.a[j] = turned<A_PITCH>(sm + a_stage, aa[j], ks);
             else
-                o.a[j] = *reinterpret_cast<const u32x4 *>(p + rows[ks] + j * 32 * A_PITCH);
+                o.a[j] = *reinterpret_cast<const u32x4 *>(sm + a_stage + rows[2 * half + ks] +
+                                                          j * 32 * A_PITCH);
         }
     };
     auto multiply = [&](const Operands &o) {
@@ -153,21 +173,30 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    // A wave's requests of a step, and those of all steps but the next two.
-    constexpr int LOADS = C::A_LOADS + C::Q_LOADS, AHEAD = (C::NS - 2) * LOADS;
     if (steps > 0) {
         // (Steps past the last are fetched as zeros, so that the loop and its counts
         // are the same each time.)
+        constexpr int PAIRS = C::NA - 1;        // stages of A that are filled at first
 #pragma unroll
-        for (int t = 0; t < C::NS - 1; ++t)
-            fetch((uint32_t)(t * C::STAGE), t);
-        pers::wait_vm_lgkm0<AHEAD>();
+        for (int t = 0; t < C::NS - 1 || t < PAIRS * C::SPAN; ++t) {
+            if (t % C::SPAN == 0 && t / C::SPAN < PAIRS)
+                fetch_a((uint32_t)(t / C::SPAN * C::A_BYTES), t);
+            if (t < C::NS - 1)
+                fetch_q((uint32_t)(C::Q0 + t * C::Q_BYTES), t);
+        }
+        pers::wait_vm_lgkm0<0>();
         pers::barrier();
-        uint32_t st = 0, ahead = (C::NS - 1) * C::STAGE;        // stages of t and t + NS - 1
-        read(st, 0, f[0]);
-        for (int t = 0; t < steps; ++t) {
-            // Step t - 1's stage, which every wave had read before the last barrier.
-            fetch(ahead, t + C::NS - 1);
+        // Stages of step t, and those that its requests go to: step t - 1's, which every
+        // wave had read before the last barrier.
+        uint32_t sa = 0, qs = C::Q0;
+        uint32_t next_a = PAIRS * C::A_BYTES, next_q = C::Q0 + (C::NS - 1) * C::Q_BYTES;
+        read(sa, 0, qs, 0, f[0]);
+        auto step = [&](auto part, int t) {
+            constexpr int half = decltype(part)::value;         // of A's stage
+            constexpr bool last = half == C::SPAN - 1;
+            if constexpr (half == 0)
+                fetch_a(next_a, t + PAIRS * C::SPAN);
+            fetch_q(next_q, t + C::NS - 1);
             if constexpr (TURNED) {
                 // (The waves that read the same rows of A take the steps of 16 in
                 // turn.)
@@ -177,7 +206,7 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
                         continue;
 #pragma unroll
                     for (int j = 0; j < C::FR; ++j) {
-                        const u32x4 u = turned<A_PITCH>(sm + st, aa[j], ks);
+                        const u32x4 u = turned<A_PITCH>(sm + sa, aa[j], ks);
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const f32x2 v = unpack2<T>(u[k]);
@@ -187,17 +216,26 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-            read(st, 1, f[1]);
+            read(sa, half, qs, 1, f[1]);
             multiply(f[0]);
             in_turn();
             // Step t + 1's rows have landed, and this wave has read all of step t.
-            pers::wait_vm_lgkm0<AHEAD>();
+            pers::wait_vm_lgkm0<C::ahead(half)>();
             pers::barrier();
-            ahead = st;
-            st = st == (C::NS - 1) * C::STAGE ? 0 : st + C::STAGE;
-            read(st, 0, f[0]);
+            next_q = qs;
+            qs = qs == C::Q0 + (C::NS - 1) * C::Q_BYTES ? C::Q0 : qs + C::Q_BYTES;
+            if constexpr (last) {
+                next_a = sa;
+                sa = sa == (C::NA - 1) * C::A_BYTES ? 0 : sa + C::A_BYTES;
+            }
+            read(sa, last ? 0 : half + 1, qs, 0, f[0]);
             multiply(f[1]);
             in_turn();
+        };
+        for (int t = 0; t < steps; t += C::SPAN) {
+            step(std::integral_constant<int, 0>{}, t);
+            if constexpr (C::SPAN == 2)
+                step(std::integral_constant<int, 1>{}, t + 1);
         }
         pers::wait_vm_lgkm0<0>();
     }
@@ -221,7 +259,7 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
                       sm + wave * kOutBytes<T, C::FC>, acc, scaled);
 }
 
-template <class T, class C, bool TURNED>
+template <class T, class C>
 __global__ void __launch_bounds__(C::NT) k_grad_gemm(GradGemm g, int first)
 {
     constexpr int OUT = C::WC * C::WR * kOutBytes<float, C::FC>;
@@ -230,7 +268,7 @@ __global__ void __launch_bounds__(C::NT) k_grad_gemm(GradGemm g, int first)
     const int tiles = g.tiles_r * g.tiles_c, split = unit / tiles;
     int tr, tc;
     tile_coords(unit - split * tiles, g.tiles_r, g.tiles_c, tr, tc);
-    grad_gemm_tile<T, C, TURNED>(g, (int)uniform(tr), (int)uniform(tc), (int)uniform(split), sm);
+    grad_gemm_tile<T, C>(g, (int)uniform(tr), (int)uniform(tc), (int)uniform(split), sm);
 }
 
 struct ValueThreads {
@@ -307,13 +345,13 @@ template <class T> hipError_t write_values(const GradValues &v, hipStream_t stre
     return hipGetLastError();
 }
 
-template <class T, class C, bool TURNED> hipError_t launch_gemm(const GradGemm &g, hipStream_t stream)
+template <class T, class C> hipError_t launch_gemm(const GradGemm &g, hipStream_t stream)
 {
     constexpr long long MOST = 1 << 22;
     const long long units = (long long)g.tiles_r * g.tiles_c * g.splits;
     for (long long u = 0; u < units; u += MOST) {
         const unsigned grid = (unsigned)(units - u < MOST ? units - u : MOST);
-        k_grad_gemm<T, C, TURNED><<<grid, C::NT, 0, stream>>>(g, (int)u);
+        k_grad_gemm<T, C><<<grid, C::NT, 0, stream>>>(g, (int)u);
         if (hipError_t e = hipGetLastError())
             return e;
     }
@@ -323,8 +361,8 @@ template <class T, class C, bool TURNED> hipError_t launch_gemm(const GradGemm &
 template <class T, bool TURNED> hipError_t launch_gemm_tile(const GradGemm &g, hipStream_t stream)
 {
     if (g.tile_c == 256)
-        return launch_gemm<T, TileCfg<256, 256, 4, 2>, TURNED>(g, stream);
-    return launch_gemm<T, TileCfg<192, 256, 2, 4>, TURNED>(g, stream);
+        return launch_gemm<T, TileCfg<256, 256, 4, 2, TURNED ? 5 : 4, 3, TURNED>>(g, stream);
+    return launch_gemm<T, TileCfg<192, 256, 2, 4, TURNED ? 5 : 4, 3, TURNED>>(g, stream);
 }
 
 template <class T> hipError_t run_gemm(GradGemm g, bool turned_a, hipStream_t stream)
