@@ -26,34 +26,35 @@ namespace {
 
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
-// Sums over the TPR threads of a row, K at a time.  (TPR above 64: the workgroup;
-// two buffers in turn, so that one barrier a call is enough.)
-template <int TPR, int K> struct RowSum {
-    __device__ __forceinline__ static void run(float (&v)[K], int &turn)
-    {
+// Sums over the TPR threads of a row, K at a time, in a workgroup of THREADS.  (TPR
+// above 64: all rows of the workgroup together; two buffers in turn, so that one
+// barrier a call is enough.)
+template <int TPR, int THREADS, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], int &turn)
+{
 #pragma unroll
-        for (int i = 0; i < K; ++i)
-            v[i] = group_reduce<64>(v[i], add);
-        if constexpr (TPR > 64) {
-            constexpr int W = TPR / 64;
-            __shared__ float part[2][W][K];
-            if ((threadIdx.x & 63) == 0) {
+    for (int i = 0; i < K; ++i)
+        v[i] = group_reduce<64>(v[i], add);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        __shared__ float part[2][THREADS / 64][K];
+        const int wave = threadIdx.x >> 6, first = wave / W * W;
+        if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-                for (int i = 0; i < K; ++i)
-                    part[turn][threadIdx.x >> 6][i] = v[i];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < K; ++i) {
-                v[i] = part[turn][0][i];
-#pragma unroll
-                for (int w = 1; w < W; ++w)
-                    v[i] += part[turn][w][i];
-            }
-            turn ^= 1;
+            for (int i = 0; i < K; ++i)
+                part[turn][wave][i] = v[i];
         }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            v[i] = part[turn][first][i];
+#pragma unroll
+            for (int w = 1; w < W; ++w)
+                v[i] += part[turn][first + w][i];
+        }
+        turn ^= 1;
     }
-};
+}
 
 // Where a thread's vectors of eight channels lie.  FULL: the width is a multiple of
 // eight, so that a vector is whole or nothing.
@@ -130,7 +131,7 @@ template <int TPR, int NV, bool FULL> struct Columns {
 };
 
 // v centred (layer kind), and 1 / deviation.
-template <int TPR, class Cols, int NV>
+template <int TPR, int THREADS, class Cols, int NV>
 __device__ __forceinline__ float normalise(const NormCall &c, const Cols &at, float (&v)[NV][8],
                                            int &turn)
 {
@@ -141,7 +142,7 @@ __device__ __forceinline__ float normalise(const NormCall &c, const Cols &at, fl
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 s[0] += v[i][e];
-        RowSum<TPR, 1>::run(s, turn);
+        row_sums<TPR, THREADS>(s, turn);
         at.centre(v, s[0] * c.inv_width);
     }
     float q[1] = {0.0f};
@@ -150,14 +151,14 @@ __device__ __forceinline__ float normalise(const NormCall &c, const Cols &at, fl
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             q[0] += v[i][e] * v[i][e];
-    RowSum<TPR, 1>::run(q, turn);
+    row_sums<TPR, THREADS>(q, turn);
     return rsqrtf(q[0] * c.inv_width + c.eps);
 }
 
 template <class T, int TPR, int NV, bool FULL>
 __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCall c)
 {
-    constexpr int GROUPS = TPR == 64 ? 4 : 1;
+    constexpr int THREADS = TPR == 64 ? 256 : TPR, GROUPS = THREADS / TPR;
     const long long unit =
         c.first_unit + (long long)blockIdx.x * GROUPS + (int)threadIdx.x / TPR;
     if (unit >= (long long)c.batch * c.chunks)
@@ -181,14 +182,25 @@ __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCal
     const T *x = static_cast<const T *>(c.x) + b * c.x_stride[0];
     const T *y = static_cast<const T *>(c.y) + (c.y ? b * c.y_stride[0] : 0);
     const size_t out = (size_t)b * c.tokens;
-    for (int s = s0; s < s1; ++s) {
-        Packed<T, 8> xr[NV], yr[NV] = {};
+    Packed<T, 8> xn[NV], yn[NV] = {};           // the next row, on its way
+    auto fetch = [&](int s) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            xr[i] = at.load(x + s * c.x_stride[1], i);
+            xn[i] = at.load(x + s * c.x_stride[1], i);
             if (c.y)
-                yr[i] = at.load(y + s * c.y_stride[1], i);
+                yn[i] = at.load(y + s * c.y_stride[1], i);
         }
+    };
+    fetch(s0);
+    for (int s = s0; s < s1; ++s) {
+        Packed<T, 8> xr[NV], yr[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            xr[i] = xn[i];
+            yr[i] = yn[i];
+        }
+        if (s + 1 < s1)
+            fetch(s + 1);
         float v[NV][8];
         if (c.y) {
             float p[NV][8];
@@ -196,7 +208,7 @@ __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCal
             for (int i = 0; i < NV; ++i)
                 yr[i].floats(p[i]);
             if (c.post_weight) {
-                const float d = normalise<TPR>(c, at, p, turn);
+                const float d = normalise<TPR, THREADS>(c, at, p, turn);
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     float w[8];
@@ -220,7 +232,7 @@ __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCal
             for (int i = 0; i < NV; ++i)
                 xr[i].floats(v[i]);
         }
-        const float d = normalise<TPR>(c, at, v, turn);
+        const float d = normalise<TPR, THREADS>(c, at, v, turn);
         T *h = static_cast<T *>(c.h) + (out + s) * c.width;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -232,8 +244,8 @@ __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCal
     }
 }
 
-// Threads of a workgroup of the gradient, and the rows that it has at a time.
-template <int TPR> constexpr int kBackThreads = TPR == 64 ? 512 : TPR;
+// Threads of a workgroup of the gradient, of TPR a row.
+template <int TPR> constexpr int kBackThreads = TPR == 192 ? 768 : TPR < 512 ? 512 : TPR;
 
 // A workgroup takes rows of one batch entry, every (chunks * GROUPS)-th for each of
 // its groups, with the sums over tokens in registers; the groups' meet in LDS and
@@ -242,7 +254,8 @@ template <int TPR> constexpr int kBackThreads = TPR == 64 ? 512 : TPR;
 template <class T, int TPR, int NV, bool FULL>
 __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(NormCall c)
 {
-    constexpr int GROUPS = kBackThreads<TPR> / TPR;
+    constexpr int THREADS = kBackThreads<TPR>, GROUPS = THREADS / TPR;
+    constexpr bool AHEAD = TPR < 1024;
     const int b = (int)(blockIdx.x / (unsigned)c.chunks), chunk = blockIdx.x % (unsigned)c.chunks;
     const int group = threadIdx.x / TPR;
     const Columns<TPR, NV, FULL> at{c.width, (int)threadIdx.x % TPR};
@@ -268,100 +281,145 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
     const T *dh = static_cast<const T *>(c.dh) + b * c.dh_stride[0];
     const T *dr = static_cast<const T *>(c.dr) + (c.dr ? b * c.dr_stride[0] : 0);
     const size_t out = (size_t)b * c.tokens;
-    for (int s = chunk * GROUPS + group; s < c.tokens; s += c.chunks * GROUPS) {
-        Packed<T, 8> rr[NV], yr[NV] = {}, dhr[NV], drr[NV] = {};
+    const int step = c.chunks * GROUPS;
+    struct Rows {
+        Packed<T, 8> r[NV], y[NV], dh[NV], dr[NV];
+    } row = {}, next = {};
+    // (A group past the last row has zeros.)
+    auto fetch = [&](Rows &to, int s) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            rr[i] = at.load(r + s * c.x_stride[1], i);
-            dhr[i] = at.load(dh + s * c.dh_stride[1], i);
+            to.r[i] = to.y[i] = to.dh[i] = to.dr[i] = {};
+            if (s >= c.tokens)
+                continue;
+            to.r[i] = at.load(r + s * c.x_stride[1], i);
+            to.dh[i] = at.load(dh + s * c.dh_stride[1], i);
             if (c.y)
-                yr[i] = at.load(y + s * c.y_stride[1], i);
+                to.y[i] = at.load(y + s * c.y_stride[1], i);
             if (c.dr)
-                drr[i] = at.load(dr + s * c.dr_stride[1], i);
+                to.dr[i] = at.load(dr + s * c.dr_stride[1], i);
         }
-        float n[NV][8], u[NV][8], mean_u = 0.0f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            rr[i].floats(n[i]);
-            dhr[i].floats(u[i]);
+    };
+    if constexpr (AHEAD)
+        fetch(next, chunk * GROUPS + group);
+    // All groups of a workgroup together: they meet at its barriers.
+    for (int s0 = chunk * GROUPS; s0 < c.tokens; s0 += step) {
+        const int s = s0 + group;
+        const bool real = s < c.tokens;
+        if constexpr (AHEAD) {
+            row = next;
+            fetch(next, s + step);
+        } else {
+            fetch(row, s);
         }
+        float mean = 0.0f, mean_u = 0.0f;
         if (c.layer) {
             float m[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                float n[8], u[8];
+                row.r[i].floats(n);
+                row.dh[i].floats(u);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    m[0] += n[i][e];
-                    m[1] += u[i][e] * factor[i][e];
+                    m[0] += n[e];
+                    m[1] += u[e] * factor[i][e];
                 }
-            RowSum<TPR, 2>::run(m, turn);
-            at.centre(n, m[0] * c.inv_width);
+            }
+            row_sums<TPR, THREADS>(m, turn);
+            mean = m[0] * c.inv_width;
             mean_u = m[1] * c.inv_width;
         }
         float q[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                q[0] += n[i][e] * n[i][e];
-                q[1] += u[i][e] * factor[i][e] * n[i][e];
-            }
-        RowSum<TPR, 2>::run(q, turn);
-        const float d = rsqrtf(q[0] * c.inv_width + c.eps);
-        const float inner = q[1] * d * c.inv_width;
-        float D[NV][8];
-#pragma unroll
         for (int i = 0; i < NV; ++i) {
-            float g[8], o[8];
-            drr[i].floats(g);
+            float n[8], u[8];
+            row.r[i].floats(n);
+            row.dh[i].floats(u);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float ne = n[i][e] * d;
-                dshift[i][e] += u[i][e];
-                sum_p[i][e] += u[i][e] * ne;
-                D[i][e] = g[e] + d * (u[i][e] * factor[i][e] - mean_u - ne * inner);
-                o[e] = c.alpha * D[i][e];
+                n[e] -= at.live(i, e) ? mean : 0.0f;
+                q[0] += n[e] * n[e];
+                q[1] += u[e] * factor[i][e] * n[e];
             }
-            at.store(static_cast<T *>(c.dx) + (out + s) * c.width, i, o);
         }
-        if (!c.y)
-            continue;
-        float p[NV][8];
+        row_sums<TPR, THREADS>(q, turn);
+        const float d = real ? rsqrtf(q[0] * c.inv_width + c.eps) : 0.0f;
+        const float inner = q[1] * d * c.inv_width;
+        // D of vector i (and its part of the sums).
+        auto back = [&](int i, float (&D)[8]) {
+            float n[8], u[8];
+            row.r[i].floats(n);
+            row.dh[i].floats(u);
+            row.dr[i].floats(D);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            yr[i].floats(p[i]);
+            for (int e = 0; e < 8; ++e) {
+                const float ne = (n[e] - (at.live(i, e) ? mean : 0.0f)) * d;
+                dshift[i][e] += u[e];
+                sum_p[i][e] += u[e] * ne;
+                D[e] += d * (u[e] * factor[i][e] - mean_u - ne * inner);
+            }
+        };
+        T *dx = static_cast<T *>(c.dx) + (out + s) * c.width;
         T *dy = static_cast<T *>(c.dy) + (out + s) * c.width;
-        if (c.post_weight) {
-            const float dev = normalise<TPR>(c, at, p, turn);
-            float m[2] = {0.0f, 0.0f};
+        if (!c.y) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i) {
+                float D[8];
+                back(i, D);
+                if (real)
+                    at.store(dx, i, D);
+            }
+        } else if (!c.post_weight) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float D[8], o[8], p[8];
+                back(i, D);
+                row.y[i].floats(p);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    p[i][e] *= dev;
-                    sum_q[i][e] += D[i][e] * p[i][e];
-                    D[i][e] *= gate[i][e];
-                    m[0] += at.live(i, e) ? D[i][e] : 0.0f;
-                    m[1] += D[i][e] * p[i][e];
+                    o[e] = c.alpha * D[e];
+                    sum_q[i][e] += D[e] * p[e];
+                    D[e] *= gate[i][e];
                 }
-            RowSum<TPR, 2>::run(m, turn);
-            const float mean = c.layer ? m[0] * c.inv_width : 0.0f, in = m[1] * c.inv_width;
+                if (real)
+                    at.store(dx, i, o);
+                if (real)
+                    at.store(dy, i, D);
+            }
+        } else {
+            float p[NV][8], g[NV][8];
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                row.y[i].floats(p[i]);
+            const float factor_y = normalise<TPR, THREADS>(c, at, p, turn);
+            const float dev = real ? factor_y : 0.0f;
+            float m[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                float o[8];
+                back(i, g[i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    o[e] = c.alpha * g[i][e];
+                    p[i][e] *= dev;
+                    sum_q[i][e] += g[i][e] * p[i][e];
+                    g[i][e] *= gate[i][e];
+                    m[0] += at.live(i, e) ? g[i][e] : 0.0f;
+                    m[1] += g[i][e] * p[i][e];
+                }
+                if (real)
+                    at.store(dx, i, o);
+            }
+            row_sums<TPR, THREADS>(m, turn);
+            const float mean_g = c.layer ? m[0] * c.inv_width : 0.0f, in = m[1] * c.inv_width;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    p[i][e] = dev * (D[i][e] - mean - p[i][e] * in);
-                at.store(dy, i, p[i]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum_q[i][e] += D[i][e] * p[i][e];
-                    D[i][e] *= gate[i][e];
-                }
-                at.store(dy, i, D[i]);
+                    p[i][e] = dev * (g[i][e] - mean_g - p[i][e] * in);
+                if (real)
+                    at.store(dy, i, p[i]);
             }
         }
     }
@@ -508,7 +566,7 @@ hipError_t launch_sums(const NormCall &c, hipStream_t stream)
 int run_of(const NormCall &c)
 {
     const long long rows = (long long)c.batch * c.tokens;
-    return rows >= 4 * 4096 ? 4 : rows >= 2 * 4096 ? 2 : 1;
+    return rows >= 2 * 4096 ? 4 : rows >= 4096 ? 2 : 1;
 }
 
 template <class T, int TPR, int NV, bool FULL> hipError_t forward(NormCall c, hipStream_t stream)
@@ -530,14 +588,21 @@ template <class T, bool FULL> hipError_t forward_width(const NormCall &c, hipStr
 {
     if (c.width <= 512)
         return forward<T, 64, 1, FULL>(c, stream);
+#if VAR == 1
     if (c.width <= 1024)
         return forward<T, 64, 2, FULL>(c, stream);
     if (c.width <= 1536)
         return forward<T, 64, 3, FULL>(c, stream);
+#else
+    if (c.width <= 1024)
+        return forward<T, 128, 1, FULL>(c, stream);
+    if (c.width <= 1536)
+        return forward<T, 192, 1, FULL>(c, stream);
+#endif
     if (c.width <= 2048)
         return forward<T, 256, 1, FULL>(c, stream);
     if (c.width <= 4096)
-        return forward<T, 256, 2, FULL>(c, stream);
+        return forward<T, 512, 1, FULL>(c, stream);
     if (c.width <= 8192)
         return forward<T, 512, 2, FULL>(c, stream);
     return forward<T, 1024, 2, FULL>(c, stream);
@@ -556,24 +621,24 @@ template <class T, bool FULL> hipError_t backward_width(const NormCall &c, hipSt
     if (c.width <= 512)
         return backward<T, 64, 1, FULL>(c, stream);
     if (c.width <= 1024)
-        return backward<T, 64, 2, FULL>(c, stream);
+        return backward<T, 128, 1, FULL>(c, stream);
     if (c.width <= 1536)
-        return backward<T, 64, 3, FULL>(c, stream);
+        return backward<T, 192, 1, FULL>(c, stream);
     if (c.width <= 2048)
         return backward<T, 256, 1, FULL>(c, stream);
     if (c.width <= 4096)
-        return backward<T, 256, 2, FULL>(c, stream);
+        return backward<T, 512, 1, FULL>(c, stream);
     if (c.width <= 8192)
-        return backward<T, 512, 2, FULL>(c, stream);
-    return backward<T, 512, 4, FULL>(c, stream);
+        return backward<T, 1024, 1, FULL>(c, stream);
+    return backward<T, 1024, 2, FULL>(c, stream);
 }
 
 }  // namespace
 
 int residual_norm_chunks(int batch, int tokens, int width)
 {
-    const int groups = width <= 1536 ? 8 : 1;
-    const int want = ((width <= 1536 ? 256 : 512) + batch - 1) / (batch > 0 ? batch : 1);
+    const int groups = width <= 512 ? 8 : width <= 1536 ? 4 : width <= 2048 ? 2 : 1;
+    const int want = (512 + batch - 1) / (batch > 0 ? batch : 1);
     const int most = (tokens + groups - 1) / groups;
     return most < 1 ? 1 : want < most ? want : most;
 }
