@@ -811,11 +811,11 @@ int tasq_residual_norm(const tasq_residual *a, void *stream);
  * Its gradient from dh and dr, with x the r of the forward call (without y: its
  * x): writes dx, dy and those of dgate .. dpost_weight that are given, sums over
  * the tokens in a fixed order (the same bits each time; zeros where there are no
- * tokens).  A sum needs a workspace of tasq_residual_norm_workspace_bytes(batch,
- * tokens, width) bytes (TASQ_ERR_WORKSPACE); a call without sums needs none.
+ * tokens).  A sum needs a workspace of tasq_residual_norm_workspace_bytes(type,
+ * batch, tokens, width) bytes (TASQ_ERR_WORKSPACE); a call without sums needs none.
  */
 int tasq_residual_norm_backward(const tasq_residual *a, void *stream);
-size_t tasq_residual_norm_workspace_bytes(int batch, int tokens, int width);
+size_t tasq_residual_norm_workspace_bytes(int type, int batch, int tokens, int width);
 
 /*
  * Microscaled 4-bit floating-point codes (e2m1 elements with an e8m0 scale for each

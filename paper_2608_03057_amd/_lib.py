@@ -247,7 +247,7 @@ def lib() -> ctypes.CDLL:
             f = getattr(L, name)
             f.argtypes = [vp, vp]
             f.restype = i32
-        L.tasq_residual_norm_workspace_bytes.argtypes = [i32, i32, i32]
+        L.tasq_residual_norm_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.tasq_residual_norm_workspace_bytes.restype = size
         L.tasq_quantize_mx4.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp]
         L.tasq_quantize_mx4.restype = i32

@@ -123,9 +123,9 @@ def residual_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None,
     return out_r, out_h
 
 
-def residual_norm_workspace_bytes(batch: int, tokens: int, width: int) -> int:
-    """Workspace of residual_norm_backward for [batch, tokens, width]."""
-    return _lib.lib().tasq_residual_norm_workspace_bytes(batch, tokens, width)
+def residual_norm_workspace_bytes(x: torch.Tensor) -> int:
+    """Workspace of residual_norm_backward for a stream like x [B, S, C]."""
+    return _lib.lib().tasq_residual_norm_workspace_bytes(_type(x, "x"), *x.shape)
 
 
 def residual_norm_backward(dh: torch.Tensor, dr: Optional[torch.Tensor], r: torch.Tensor,
@@ -147,25 +147,26 @@ def residual_norm_backward(dh: torch.Tensor, dr: Optional[torch.Tensor], r: torc
     rat, rs = _rows(dr, dtype, shape, "dr")
     dx, dy = _like(r), None if y is None else _like(r)
     B, S, C = shape
-    sizes = [C if shared & bit else B * C for bit in (1, 2, 4)] + [C, C]
     given = (gate, scale, shift, weight, post_weight)
-    # One buffer of all sums' results: an allocation takes longer than a view.
-    total = sum(n for n, t in zip(sizes, given) if t is not None)
-    grads, ats, ws, nbytes = [None] * 5, [0] * 5, None, 0
-    if total:
-        flat = torch.empty(total, dtype=torch.float32, device=r.device)
-        first, base = 0, flat.data_ptr()
-        for i, (n, t) in enumerate(zip(sizes, given)):
-            if t is not None:
-                grads[i] = flat[first:first + n].view(t.shape)
-                ats[i] = base + 4 * first
-                first += n
-        ws = _workspace(workspace, residual_norm_workspace_bytes(B, S, C), r.device,
-                        "residual_norm_backward")
-        nbytes = ws.numel() * ws.element_size()
+    grads, ats, at, nbytes = [None] * 5, [0] * 5, 0, 0
+    # One buffer of all sums of a shape: an allocation takes longer than a view.
+    each = [i for i in range(3) if given[i] is not None and not shared >> i & 1]
+    flat = [i for i in range(5) if given[i] is not None and (i > 2 or shared >> i & 1)]
+    for which, size in ((each, (len(each), B, C)), (flat, (len(flat), C))):
+        if which:
+            sums = torch.empty(size, dtype=torch.float32, device=r.device)
+            first = sums.data_ptr()
+            step = 4 * (B * C if which is each else C)
+            for n, (i, view) in enumerate(zip(which, sums.unbind(0))):
+                grads[i] = view
+                ats[i] = first + n * step
+    if each or flat:
+        workspace = _workspace(
+            workspace, _lib.lib().tasq_residual_norm_workspace_bytes(head[0], B, S, C), r.device,
+            "residual_norm_backward")
+        at, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     a = _RESIDUAL.pack(*head, 0, 0, hat, rat, hs[0], hs[1], rs[0], rs[1], dx.data_ptr(),
-                       0 if dy is None else dy.data_ptr(), *ats,
-                       0 if ws is None else ws.data_ptr(), nbytes)
+                       0 if dy is None else dy.data_ptr(), *ats, at, nbytes)
     rc = _lib.lib().tasq_residual_norm_backward(a, _stream())
     if rc:
         check(rc, "tasq_residual_norm_backward")
@@ -263,17 +264,17 @@ def masked_linear_tokens_backward(dy: torch.Tensor, X: torch.Tensor, W: torch.Te
     _need(sx, torch.float32, (M,), "sx")
     _need(sw, torch.float32, (N,), "sw")
 
-    def grad(t, wanted, shape, dtype, name):
+    def grad(t, wanted, like, dtype, name):
         if not wanted:
             return None, 0
         if t is None:
-            t = torch.empty(shape, dtype=dtype, device=dy.device)
+            t = _like(like, dtype)
         else:
-            _need(t, dtype, shape, name)
+            _need(t, dtype, like.shape, name)
         return t, t.data_ptr()
-    dx, xat = grad(dx, need_input, (M, K), dtype, "dx")
-    dw, wat = grad(dw, need_weight, (N, K), dtype, "dw")
-    dbias, bat = grad(dbias, need_weight, (N,), torch.float32, "dbias")
+    dx, xat = grad(dx, need_input, X, dtype, "dx")
+    dw, wat = grad(dw, need_weight, W, dtype, "dw")
+    dbias, bat = grad(dbias, need_weight, sw, torch.float32, "dbias")
     L = _lib.lib()
     if workspace is None:
         nbytes = L.tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K)

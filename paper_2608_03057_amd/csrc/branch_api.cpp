@@ -95,7 +95,7 @@ int residual_norm(const tasq_residual *a, bool grad, void *stream)
     if (some_sum) {
         if (!aligned_to(a->workspace, 256))
             return TASQ_ERR_ALIGN;
-        const size_t need = tasq_residual_norm_workspace_bytes(a->batch, a->tokens, a->width);
+        const size_t need = tasq_residual_norm_workspace_bytes(a->type, a->batch, a->tokens, a->width);
         if (need && (!a->workspace || a->workspace_bytes < need))
             return TASQ_ERR_WORKSPACE;
         c.part = static_cast<float *>(a->workspace);
@@ -256,12 +256,13 @@ int tasq_residual_norm_backward(const tasq_residual *a, void *stream)
     return residual_norm(a, true, stream);
 }
 
-size_t tasq_residual_norm_workspace_bytes(int batch, int tokens, int width)
+size_t tasq_residual_norm_workspace_bytes(int type, int batch, int tokens, int width)
 {
-    if (!residual_sizes(batch, tokens, width) || (long long)batch * tokens == 0)
+    if (!type_known(type) || !residual_sizes(batch, tokens, width) ||
+        (long long)batch * tokens == 0)
         return 0;
-    return (size_t)batch * (size_t)tasq::residual_norm_chunks(batch, tokens, width) * 3 *
-           (size_t)width * sizeof(float);
+    return (size_t)batch * (size_t)tasq::residual_norm_teams(type, batch, tokens, width).chunks *
+           3 * (size_t)width * sizeof(float);
 }
 
 int tasq_quantize_mx4(const void *x, int x_type, int M, int K, long long x_stride,

@@ -27,7 +27,8 @@ struct NormCall {
     int type, wide_mods;        // wide_mods: modulations are fp32, else of `type`
     int layer, batch, tokens, width, shared;
     float eps, alpha, inv_width;
-    int rows, chunks;           // rows of a group's run; runs (backward: workgroups) an entry
+    int rows, chunks;           // rows of a team's run; runs (backward: workgroups) an entry
+    int waves, groups;          // of a row; rows of a workgroup at a time (backward)
     long long first_unit;       // of the launch
     float *part;                // backward: [batch][chunks][3][width]
     bool sums;                  // backward: some of dgate .. dpost are wanted
@@ -35,8 +36,11 @@ struct NormCall {
 constexpr int kMaxNormWidth = TASQ_MAX_RESIDUAL_WIDTH;
 hipError_t launch_residual_norm(const NormCall &c, hipStream_t stream);
 hipError_t launch_residual_norm_backward(const NormCall &c, hipStream_t stream);
-// Workgroups of the gradient for each batch entry.
-int residual_norm_chunks(int batch, int tokens, int width);
+// Waves of a row, rows at a time and workgroups for each batch entry of the gradient.
+struct NormTeams {
+    int waves, groups, chunks;
+};
+NormTeams residual_norm_teams(int type, int batch, int tokens, int width);
 
 // 4-bit microscaled codes (mx4_quant.hip) and the linear on them (mx4_gemm.hip): rows
 // of K128 * 128 elements, 64 bytes of codes and four scales each 128.

@@ -26,31 +26,41 @@ namespace {
 
 __device__ __forceinline__ float add(float a, float b) { return a + b; }
 
-// Sums over the TPR threads of a row, K at a time, in a workgroup of THREADS.  (TPR
-// above 64: all rows of the workgroup together; two buffers in turn, so that one
-// barrier a call is enough.)
-template <int TPR, int THREADS, int K>
-__device__ __forceinline__ void row_sums(float (&v)[K], int &turn)
+// The threads of a row: a wave, or as many waves as its width takes.
+template <bool WAVE> struct Team {
+    int waves, first, group, t;         // first: the row's first wave; t: of its threads
+    __device__ __forceinline__ explicit Team(int waves_) : waves(WAVE ? 1 : waves_)
+    {
+        const int wave = threadIdx.x >> 6;
+        group = wave / waves;
+        first = group * waves;
+        t = (int)threadIdx.x - 64 * first;
+    }
+};
+
+// Sums over the threads of a row, K at a time.  (Several waves a row: all rows of the
+// workgroup together; two buffers in turn, so that one barrier a call is enough.)
+constexpr int kMostWaves = 16;
+template <bool WAVE, int K>
+__device__ __forceinline__ void row_sums(const Team<WAVE> &team, float (&v)[K], int &turn)
 {
 #pragma unroll
     for (int i = 0; i < K; ++i)
         v[i] = group_reduce<64>(v[i], add);
-    if constexpr (TPR > 64) {
-        constexpr int W = TPR / 64;
-        __shared__ float part[2][THREADS / 64][K];
-        const int wave = threadIdx.x >> 6, first = wave / W * W;
+    if constexpr (!WAVE) {
+        __shared__ float part[2][kMostWaves][K];
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
             for (int i = 0; i < K; ++i)
-                part[turn][wave][i] = v[i];
+                part[turn][threadIdx.x >> 6][i] = v[i];
         }
         __syncthreads();
+        // A lane a wave's part, the rest zeros.
+        const int w = (int)(threadIdx.x & 15);
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            v[i] = part[turn][first][i];
-#pragma unroll
-            for (int w = 1; w < W; ++w)
-                v[i] += part[turn][first + w][i];
+            const float p = part[turn][min(team.first + w, kMostWaves - 1)][i];
+            v[i] = group_reduce<kMostWaves>(w < team.waves ? p : 0.0f, add);
         }
         turn ^= 1;
     }
@@ -58,9 +68,9 @@ __device__ __forceinline__ void row_sums(float (&v)[K], int &turn)
 
 // Where a thread's vectors of eight channels lie.  FULL: the width is a multiple of
 // eight, so that a vector is whole or nothing.
-template <int TPR, int NV, bool FULL> struct Columns {
-    int width, t;
-    __device__ __forceinline__ int k(int i) const { return 8 * (t + i * TPR); }
+template <int NV, bool FULL> struct Columns {
+    int width, t, threads;
+    __device__ __forceinline__ int k(int i) const { return 8 * (t + i * threads); }
     __device__ __forceinline__ bool some(int i) const { return k(i) < width; }
     __device__ __forceinline__ bool live(int i, int e) const
     {
@@ -131,9 +141,9 @@ template <int TPR, int NV, bool FULL> struct Columns {
 };
 
 // v centred (layer kind), and 1 / deviation.
-template <int TPR, int THREADS, class Cols, int NV>
-__device__ __forceinline__ float normalise(const NormCall &c, const Cols &at, float (&v)[NV][8],
-                                           int &turn)
+template <bool WAVE, class Cols, int NV>
+__device__ __forceinline__ float normalise(const NormCall &c, const Team<WAVE> &team,
+                                           const Cols &at, float (&v)[NV][8], int &turn)
 {
     if (c.layer) {
         float s[1] = {0.0f};
@@ -142,7 +152,7 @@ __device__ __forceinline__ float normalise(const NormCall &c, const Cols &at, fl
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 s[0] += v[i][e];
-        row_sums<TPR, THREADS>(s, turn);
+        row_sums(team, s, turn);
         at.centre(v, s[0] * c.inv_width);
     }
     float q[1] = {0.0f};
@@ -151,21 +161,21 @@ __device__ __forceinline__ float normalise(const NormCall &c, const Cols &at, fl
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             q[0] += v[i][e] * v[i][e];
-    row_sums<TPR, THREADS>(q, turn);
+    row_sums(team, q, turn);
     return rsqrtf(q[0] * c.inv_width + c.eps);
 }
 
-template <class T, int TPR, int NV, bool FULL>
-__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCall c)
+// WAVE: rows of a wave each, four to a workgroup; else a row at a time.
+template <class T, int NV, bool FULL, bool WAVE>
+__global__ void __launch_bounds__(WAVE ? 256 : NV == 1 ? 512 : 1024) k_residual_norm(NormCall c)
 {
-    constexpr int THREADS = TPR == 64 ? 256 : TPR, GROUPS = THREADS / TPR;
-    const long long unit =
-        c.first_unit + (long long)blockIdx.x * GROUPS + (int)threadIdx.x / TPR;
+    const Team<WAVE> team(c.waves);
+    const long long unit = c.first_unit + (long long)blockIdx.x * (WAVE ? 4 : 1) + team.group;
     if (unit >= (long long)c.batch * c.chunks)
-        return;                 // whole waves (TPR 64), or nobody
+        return;                 // whole waves (WAVE), or nobody
     const int b = (int)(unit / c.chunks), s0 = (int)(unit % c.chunks) * c.rows;
     const int s1 = min(c.tokens, s0 + c.rows);
-    const Columns<TPR, NV, FULL> at{c.width, (int)threadIdx.x % TPR};
+    const Columns<NV, FULL> at{c.width, team.t, 64 * team.waves};
     int turn = 0;
     float factor[NV][8], shift[NV][8], gate[NV][8];
 #pragma unroll
@@ -208,7 +218,7 @@ __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCal
             for (int i = 0; i < NV; ++i)
                 yr[i].floats(p[i]);
             if (c.post_weight) {
-                const float d = normalise<TPR, THREADS>(c, at, p, turn);
+                const float d = normalise(c, team, at, p, turn);
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     float w[8];
@@ -232,7 +242,7 @@ __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCal
             for (int i = 0; i < NV; ++i)
                 xr[i].floats(v[i]);
         }
-        const float d = normalise<TPR, THREADS>(c, at, v, turn);
+        const float d = normalise(c, team, at, v, turn);
         T *h = static_cast<T *>(c.h) + (out + s) * c.width;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -244,21 +254,24 @@ __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR) k_residual_norm(NormCal
     }
 }
 
-// Threads of a workgroup of the gradient, of TPR a row.
-template <int TPR> constexpr int kBackThreads = TPR == 192 ? 768 : TPR < 512 ? 512 : TPR;
+// Most threads of a workgroup of the gradient: three waves a SIMD, whose registers
+// hold a row of 16-bit values and its sums, or two for fp32.  (The widest rows take
+// what there is.)
+template <class T, int NV> constexpr int kBackThreads = NV > 1 ? 1024 : sizeof(T) == 4 ? 512 : 768;
 
-// A workgroup takes rows of one batch entry, every (chunks * GROUPS)-th for each of
+// A workgroup takes rows of one batch entry, every (chunks * groups)-th for each of
 // its groups, with the sums over tokens in registers; the groups' meet in LDS and
 // the workgroup's go to part[b][chunk], which k_norm_sums adds up in order.  (No
 // atomics: their order would change the sums from run to run.)
-template <class T, int TPR, int NV, bool FULL>
-__global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(NormCall c)
+template <class T, int NV, bool FULL, bool WAVE>
+__global__ void __launch_bounds__((kBackThreads<T, NV>)) k_residual_norm_backward(NormCall c)
 {
-    constexpr int THREADS = kBackThreads<TPR>, GROUPS = THREADS / TPR;
-    constexpr bool AHEAD = TPR < 1024;
+    constexpr bool AHEAD = NV == 1;
+    const Team<WAVE> team(c.waves);
+    const int groups = c.groups;
     const int b = (int)(blockIdx.x / (unsigned)c.chunks), chunk = blockIdx.x % (unsigned)c.chunks;
-    const int group = threadIdx.x / TPR;
-    const Columns<TPR, NV, FULL> at{c.width, (int)threadIdx.x % TPR};
+    const int group = team.group;
+    const Columns<NV, FULL> at{c.width, team.t, 64 * team.waves};
     int turn = 0;
     float factor[NV][8], gate[NV][8];
     float dshift[NV][8] = {}, sum_p[NV][8] = {}, sum_q[NV][8] = {};
@@ -281,7 +294,7 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
     const T *dh = static_cast<const T *>(c.dh) + b * c.dh_stride[0];
     const T *dr = static_cast<const T *>(c.dr) + (c.dr ? b * c.dr_stride[0] : 0);
     const size_t out = (size_t)b * c.tokens;
-    const int step = c.chunks * GROUPS;
+    const int step = c.chunks * groups;
     struct Rows {
         Packed<T, 8> r[NV], y[NV], dh[NV], dr[NV];
     } row = {}, next = {};
@@ -301,9 +314,9 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
         }
     };
     if constexpr (AHEAD)
-        fetch(next, chunk * GROUPS + group);
+        fetch(next, chunk * groups + group);
     // All groups of a workgroup together: they meet at its barriers.
-    for (int s0 = chunk * GROUPS; s0 < c.tokens; s0 += step) {
+    for (int s0 = chunk * groups; s0 < c.tokens; s0 += step) {
         const int s = s0 + group;
         const bool real = s < c.tokens;
         if constexpr (AHEAD) {
@@ -326,7 +339,7 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
                     m[1] += u[e] * factor[i][e];
                 }
             }
-            row_sums<TPR, THREADS>(m, turn);
+            row_sums(team, m, turn);
             mean = m[0] * c.inv_width;
             mean_u = m[1] * c.inv_width;
         }
@@ -343,7 +356,7 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
                 q[1] += u[e] * factor[i][e] * n[e];
             }
         }
-        row_sums<TPR, THREADS>(q, turn);
+        row_sums(team, q, turn);
         const float d = real ? rsqrtf(q[0] * c.inv_width + c.eps) : 0.0f;
         const float inner = q[1] * d * c.inv_width;
         // D of vector i (and its part of the sums).
@@ -392,7 +405,7 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 row.y[i].floats(p[i]);
-            const float factor_y = normalise<TPR, THREADS>(c, at, p, turn);
+            const float factor_y = normalise(c, team, at, p, turn);
             const float dev = real ? factor_y : 0.0f;
             float m[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -411,7 +424,7 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
                 if (real)
                     at.store(dx, i, o);
             }
-            row_sums<TPR, THREADS>(m, turn);
+            row_sums(team, m, turn);
             const float mean_g = c.layer ? m[0] * c.inv_width : 0.0f, in = m[1] * c.inv_width;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -426,7 +439,7 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
     if (!c.sums)
         return;
     float *part = c.part + (size_t)blockIdx.x * 3 * c.width;
-    if constexpr (GROUPS == 1) {
+    if (groups == 1) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             at.store(part, i, dshift[i]);
@@ -434,25 +447,23 @@ __global__ void __launch_bounds__(kBackThreads<TPR>) k_residual_norm_backward(No
             at.store(part + 2 * c.width, i, sum_q[i]);
         }
     } else {
-        constexpr int CH = 8 * TPR * NV;
-        __shared__ __attribute__((aligned(16))) float sum[GROUPS][CH + 4];
+        // (Groups of one row each have at most a workgroup's eight channels a thread.)
+        __shared__ __attribute__((aligned(16))) float sum[8 * kBackThreads<T, 1>];
+        const int channels = 8 * 64 * team.waves;
 #pragma unroll
         for (int j = 0; j < 3; ++j) {
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                    const float *v = &(j == 0 ? dshift : j == 1 ? sum_p : sum_q)[i][e];
-                    *reinterpret_cast<float4 *>(&sum[group][at.k(i) + e]) =
-                        make_float4(v[0], v[1], v[2], v[3]);
-                }
+            for (int e = 0; e < 8; e += 4) {
+                const float *v = &(j == 0 ? dshift : j == 1 ? sum_p : sum_q)[0][e];
+                *reinterpret_cast<float4 *>(&sum[group * channels + 8 * team.t + e]) =
+                    make_float4(v[0], v[1], v[2], v[3]);
+            }
             __syncthreads();
-            for (int k = threadIdx.x; k < c.width; k += kBackThreads<TPR>) {
+            for (int k = threadIdx.x; k < c.width; k += 64 * team.waves * groups) {
                 float v = 0.0f;
-#pragma unroll
-                for (int g = 0; g < GROUPS; ++g)
-                    v += sum[g][k];
+                for (int g = 0; g < groups; ++g)
+                    v += sum[g * channels + k];
                 part[j * c.width + k] = v;
             }
         }
@@ -562,85 +573,78 @@ hipError_t launch_sums(const NormCall &c, hipStream_t stream)
     return hipSuccess;
 }
 
-// Rows of a run in the forward pass: the modulations are read once for each run.
+// Waves of a row with NV vectors of eight channels a lane.
+int waves_of(int width, int nv) { return (width + 512 * nv - 1) / (512 * nv); }
+
+// Rows of a run in the forward pass: the modulations are read once for each run, and a
+// row is requested while the one before is worked on.
 int run_of(const NormCall &c)
 {
     const long long rows = (long long)c.batch * c.tokens;
     return rows >= 2 * 4096 ? 4 : rows >= 4096 ? 2 : 1;
 }
 
-template <class T, int TPR, int NV, bool FULL> hipError_t forward(NormCall c, hipStream_t stream)
+template <class T, int NV, bool FULL, bool WAVE> hipError_t forward(NormCall c, hipStream_t stream)
 {
-    constexpr int GROUPS = TPR == 64 ? 4 : 1;
+    constexpr int GROUPS = WAVE ? 4 : 1;
+    c.waves = waves_of(c.width, NV);
     const long long units = (long long)c.batch * c.chunks;
     constexpr long long MOST = 1 << 20;         // workgroups of a launch
     for (c.first_unit = 0; c.first_unit < units; c.first_unit += MOST * GROUPS) {
         const long long left = (units - c.first_unit + GROUPS - 1) / GROUPS;
-        k_residual_norm<T, TPR, NV, FULL>
-            <<<(unsigned)(left < MOST ? left : MOST), TPR == 64 ? 256 : TPR, 0, stream>>>(c);
+        k_residual_norm<T, NV, FULL, WAVE><<<(unsigned)(left < MOST ? left : MOST),
+                                             64 * GROUPS * c.waves, 0, stream>>>(c);
         if (hipError_t e = hipGetLastError())
             return e;
     }
     return hipSuccess;
 }
 
+template <class T, int NV, bool FULL, bool WAVE>
+hipError_t backward(const NormCall &c, hipStream_t stream)
+{
+    k_residual_norm_backward<T, NV, FULL, WAVE>
+        <<<(unsigned)(c.batch * c.chunks), 64 * c.waves * c.groups, 0, stream>>>(c);
+    return hipGetLastError();
+}
+
+// Eight channels a lane up to the workgroups' most, and sixteen.  (Rows of 1152 in
+// bfloat16 with 24 channels a lane, a wave to a row: 17.5 us for 8192, 14.7 with three
+// waves.)
+constexpr int kWideForward = 8 * 512;
+
 template <class T, bool FULL> hipError_t forward_width(const NormCall &c, hipStream_t stream)
 {
     if (c.width <= 512)
-        return forward<T, 64, 1, FULL>(c, stream);
-#if VAR == 1
-    if (c.width <= 1024)
-        return forward<T, 64, 2, FULL>(c, stream);
-    if (c.width <= 1536)
-        return forward<T, 64, 3, FULL>(c, stream);
-#else
-    if (c.width <= 1024)
-        return forward<T, 128, 1, FULL>(c, stream);
-    if (c.width <= 1536)
-        return forward<T, 192, 1, FULL>(c, stream);
-#endif
-    if (c.width <= 2048)
-        return forward<T, 256, 1, FULL>(c, stream);
-    if (c.width <= 4096)
-        return forward<T, 512, 1, FULL>(c, stream);
-    if (c.width <= 8192)
-        return forward<T, 512, 2, FULL>(c, stream);
-    return forward<T, 1024, 2, FULL>(c, stream);
-}
-
-template <class T, int TPR, int NV, bool FULL>
-hipError_t backward(const NormCall &c, hipStream_t stream)
-{
-    k_residual_norm_backward<T, TPR, NV, FULL>
-        <<<(unsigned)(c.batch * c.chunks), kBackThreads<TPR>, 0, stream>>>(c);
-    return hipGetLastError();
+        return forward<T, 1, FULL, true>(c, stream);
+    if (c.width <= kWideForward)
+        return forward<T, 1, FULL, false>(c, stream);
+    return forward<T, 2, FULL, false>(c, stream);
 }
 
 template <class T, bool FULL> hipError_t backward_width(const NormCall &c, hipStream_t stream)
 {
     if (c.width <= 512)
-        return backward<T, 64, 1, FULL>(c, stream);
-    if (c.width <= 1024)
-        return backward<T, 128, 1, FULL>(c, stream);
-    if (c.width <= 1536)
-        return backward<T, 192, 1, FULL>(c, stream);
-    if (c.width <= 2048)
-        return backward<T, 256, 1, FULL>(c, stream);
-    if (c.width <= 4096)
-        return backward<T, 512, 1, FULL>(c, stream);
-    if (c.width <= 8192)
-        return backward<T, 1024, 1, FULL>(c, stream);
-    return backward<T, 1024, 2, FULL>(c, stream);
+        return backward<T, 1, FULL, true>(c, stream);
+    if (c.width <= 8 * kBackThreads<T, 1>)
+        return backward<T, 1, FULL, false>(c, stream);
+    return backward<T, 2, FULL, false>(c, stream);
 }
 
 }  // namespace
 
-int residual_norm_chunks(int batch, int tokens, int width)
+NormTeams residual_norm_teams(int type, int batch, int tokens, int width)
 {
-    const int groups = width <= 512 ? 8 : width <= 1536 ? 4 : width <= 2048 ? 2 : 1;
-    const int want = (512 + batch - 1) / (batch > 0 ? batch : 1);
-    const int most = (tokens + groups - 1) / groups;
-    return most < 1 ? 1 : want < most ? want : most;
+    const int threads = type == TASQ_TYPE_F32 ? kBackThreads<float, 1> : kBackThreads<bf16_t, 1>;
+    const int nv = width <= 8 * threads ? 1 : 2;
+    NormTeams n;
+    n.waves = waves_of(width, nv);
+    n.groups = nv == 1 && n.waves ? threads / 64 / n.waves : 1;
+    n.groups = tokens < n.groups ? (tokens > 1 ? tokens : 1) : n.groups;
+    const int want = (256 + batch - 1) / (batch > 0 ? batch : 1);
+    const int most = (tokens + n.groups - 1) / n.groups;
+    n.chunks = most < 1 ? 1 : want < most ? want : most;
+    return n;
 }
 
 hipError_t launch_residual_norm(const NormCall &in, hipStream_t stream)
@@ -661,7 +665,10 @@ hipError_t launch_residual_norm_backward(const NormCall &in, hipStream_t stream)
     NormCall c = in;
     c.inv_width = 1.0f / (float)c.width;
     if (c.batch && c.tokens) {
-        c.chunks = residual_norm_chunks(c.batch, c.tokens, c.width);
+        const NormTeams n = residual_norm_teams(c.type, c.batch, c.tokens, c.width);
+        c.chunks = n.chunks;
+        c.waves = n.waves;
+        c.groups = n.groups;
         const hipError_t e = with_type(c.type, [&](auto zero) {
             using T = decltype(zero);
             return c.width % 8 == 0 ? backward_width<T, true>(c, stream)

@@ -127,7 +127,7 @@ def test_residual_norm_forward_rejects(kw, code):
     (dict(dpost_weight=FAKE + 2), ALIGN), (dict(workspace=FAKE + 16), ALIGN),
     (dict(dh_stride=(-1, 72)), DIM), (dict(dr_stride=(360, -1)), DIM),
     (dict(workspace=None), WORKSPACE),
-    (dict(workspace_bytes=T.residual_norm_workspace_bytes(2, 5, 72) - 1), WORKSPACE),
+    (dict(workspace_bytes=L.tasq_residual_norm_workspace_bytes(BF16, 2, 5, 72) - 1), WORKSPACE),
 ])
 def test_residual_norm_backward_rejects(kw, code):
     assert backward(**kw) == code
@@ -142,13 +142,16 @@ def test_residual_norm_of_nothing():
 
 
 def test_residual_norm_workspace_bytes():
-    size = T.residual_norm_workspace_bytes
-    assert size(2, 5, 72) >= 2 * 3 * 72 * 4 and size(2, 5, 72) % (3 * 72 * 4) == 0
-    # A few parts for each compute unit, however many tokens there are.
-    assert size(2, 1 << 20, 1152) <= 1024 * 3 * 1152 * 4
-    for no in ((0, 5, 72), (2, 0, 72), (2, 5, 0), (-1, 5, 72),
-               (2, 5, _lib.TASQ_MAX_RESIDUAL_WIDTH + 1)):
+    size = L.tasq_residual_norm_workspace_bytes
+    for t in (F32, BF16, F16):
+        assert size(t, 2, 5, 72) >= 2 * 3 * 72 * 4 and size(t, 2, 5, 72) % (3 * 72 * 4) == 0
+        # A few parts for each compute unit, however many tokens there are.
+        assert size(t, 2, 1 << 20, 1152) <= 1024 * 3 * 1152 * 4
+    for no in ((BF16, 0, 5, 72), (BF16, 2, 0, 72), (BF16, 2, 5, 0), (BF16, -1, 5, 72), (3, 2, 5, 72),
+               (BF16, 2, 5, _lib.TASQ_MAX_RESIDUAL_WIDTH + 1)):
         assert size(*no) == 0
+    x = torch.empty(2, 5, 72, dtype=torch.float16)
+    assert T.residual_norm_workspace_bytes(x) == size(F16, 2, 5, 72)
 
 
 def quantize_mx4(x=FAKE, t=BF16, M=4, K=32, stride=32, q=FAKE, s=FAKE):
