@@ -84,7 +84,8 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
                        : kOOB;
     }
     // Rows of A of step t (and the next, C::SPAN of them), and of Q, to a stage; zeros
-    // past the range.
+    // past the range.  A buffer ends with a whole chunk of its last row (a dword that
+    // reaches past the end would be dropped, with its first element): rows have them.
     auto fetch_a = [&](uint32_t stage, int t) {
         const int zt = z0 + kTileStep * t;
         const int left = (int)uniform(max(z1 - zt, 0));
@@ -92,11 +93,12 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
         uint32_t off = a_off;
         if constexpr (TURNED) {
             const uint32_t n = (uint32_t)min(left, kTileStep);
-            ra = make_rsrc(A + (size_t)zt * g.a_stride + r0, n ? (n - 1) * a_pitch + 2u * a_rows : 0u);
+            ra = make_rsrc(A + (size_t)zt * g.a_stride + r0,
+                           n ? (n - 1) * a_pitch + 2u * ((a_rows + 7) & ~7u) : 0u);
         } else {
             // (From column zt on: the last row ends with the range.)
             ra = make_rsrc(A + (size_t)r0 * g.a_stride + zt,
-                           left ? (a_rows - 1) * a_pitch + 2u * (uint32_t)left : 0u);
+                           left ? (a_rows - 1) * a_pitch + 2u * (((uint32_t)left + 7) & ~7u) : 0u);
             off = a_col < left ? off : kOOB;
         }
 #pragma unroll

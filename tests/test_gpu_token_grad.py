@@ -78,6 +78,19 @@ def test_sizes(M, N, K, dtype):
     check(make(M, N, K, dtype, M + N), 8)
 
 
+@pytest.mark.parametrize("N", range(257, 264))
+@pytest.mark.parametrize("dtype", BOTH)
+def test_rows_that_end_inside_a_chunk_over_many_tokens(N, dtype):
+    check(make(513, N, 130, dtype, N), 8)
+
+
+@pytest.mark.parametrize("M,N,K", [(700, 1283, 640), (1001, 1000, 129), (2049, 513, 1001),
+                                   (1283, 2051, 641)])
+@pytest.mark.parametrize("dtype", BOTH)
+def test_odd_sizes_over_many_tokens(M, N, K, dtype):
+    check(make(M, N, K, dtype, M + N), 8)
+
+
 @pytest.mark.parametrize("b", range(1, 9))
 def test_bits(b):
     check(make(70, 136, 96, torch.bfloat16), b)
