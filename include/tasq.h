@@ -852,6 +852,8 @@ int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const
                     const float *bias, int M, int N, int K, void *y_out, int y_type,
                     void *stream);
 
+#define TASQ_MAX_GRAD_STRIDE (1 << 22)
+
 /*
  * Gradient of tasq_masked_linear_tokens (its output's type being `type`), with the
  * codes that it took as the activations' checkpoint in 8 bits:
@@ -872,7 +874,7 @@ int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const
  *             runs them uncut.
  * N and dy_stride multiples of 8, K of 16 and 16-byte aligned dy, X and W take whole
  * vector loads.  Sums of nothing are zeros.  Errors: TASQ_ERR_NULL, _DIM (a negative
- * size, M or N > 2^30, dy_stride < N), _BITS, _OVERFLOW (K > TASQ_MAX_K), _KIND, _ALIGN,
+ * size, M or N > 2^30, and where M > 1 dy_stride < N or >= TASQ_MAX_GRAD_STRIDE), _BITS, _OVERFLOW (K > TASQ_MAX_K), _KIND, _ALIGN,
  * _HIP.
  */
 int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_stride,

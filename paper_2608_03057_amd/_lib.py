@@ -51,6 +51,7 @@ SHARED_SCALE = 2
 SHARED_SHIFT = 4
 TASQ_MAX_RESIDUAL_WIDTH = 16384
 TASQ_MAX_RESIDUAL_BATCH = 1 << 20
+TASQ_MAX_GRAD_STRIDE = 1 << 22
 
 # Every exported symbol the header declares.
 EXPORTS = (

@@ -162,21 +162,27 @@ void cut_sum(GradPlan &p, int steps, int units, int least, bool cut)
                                   round256((size_t)p.splits * p.R * sizeof(float));
 }
 
-// Of codes: tiles of 64 to 256 rows and columns, enough for half the compute units.
-void plan_codes(GradPlan &p, bool bias, bool cut)
+// Of codes.  Counted in tiles of 64 x 64 and their steps of 64, with three more for a
+// tile's first loads and its result, small work is spread wide and large work kept in
+// tiles that read less.  (Measured at tiles of 64 / 128 / 256, us with the joins: 576
+// steps of 256 x 1152, 700 tokens, for dx 13 / 18 / 24; 1152 x 1152 over 2000 tokens
+// 22 / 22 / 28; 9280 x 2288 over 400 tokens 48 / 38 / 37; 11144 x 2400 over 868 tokens
+// 110 / 81 / 66.  Rows that are no whole chunks pass through registers and LDS, which a
+// tile of 256 has too little else to do beside: 9273 x 2278 over 405 tokens 91 / 73 /
+// 125.)  Ranges of the sum: for 6 tokens of 10536 x 3344 64-row tiles in 212 / 477 / 1007
+// workgroups take 26 / 19 / 17 us for dx.
+void plan_codes(GradPlan &p, bool bias, bool whole, bool cut)
 {
     const int steps = (int)((p.Z + 63LL) / 64);
+    const long long work = (long long)tiles_of(p.R, 64) * tiles_of(p.C, 64) * (steps + 3);
+    const int t = work < 9500 ? 64 : work < 36000 || !whole ? 128 : 256;
     p.values = false;
-    for (const int t : {256, 128, 64}) {
-        p.tile = p.tile_c = t;
-        p.tiles_r = tiles_of(p.R, t);
-        p.tiles_c = tiles_of(p.C, t);
-        if (bias && p.tiles_c == 0)
-            p.tiles_c = 1;      // the rows' sums alone
-        cut_sum(p, steps, 256, 8, cut);
-        if ((long long)p.tiles_r * p.tiles_c * p.splits >= 128)
-            break;
-    }
+    p.tile = p.tile_c = t;
+    p.tiles_r = tiles_of(p.R, t);
+    p.tiles_c = tiles_of(p.C, t);
+    if (bias && p.tiles_c == 0)
+        p.tiles_c = 1;          // the rows' sums alone
+    cut_sum(p, steps, t == 256 ? 256 : 512, t == 64 ? 4 : 8, cut);
 }
 
 // Of values: tiles of 256 rows by the width that takes the least time, counted in
@@ -209,8 +215,14 @@ void plan_values(GradPlan &p, bool bias)
     p = best;
 }
 
-// Values pay where there are rows and columns enough to fill such tiles.
-bool values_pay(int M, int N, int K) { return M >= 512 && N >= 256 && K >= 128; }
+// Values pay where there is work enough to fill such tiles and to make up for the pass
+// that writes them.  (Codes / values, us of all kernels: 2000 x 1152 x 1152 52 / 52, 4096
+// tokens of it 55 / 64, 8192 tokens 81 / 73; 2048 x 2240 x 2240 87 / 84; 512 x 4608 x 4608
+// 82 / 80; 3001 x 4447 x 982 143 / 128.)
+bool values_pay(int M, int N, int K)
+{
+    return M >= 512 && N >= 256 && K >= 256 && (double)M * N * K >= 1e10;
+}
 
 // The two products: of dx (turned false) and of dw.
 GradPlan grad_plan(int M, int N, int K, bool turned)
@@ -222,7 +234,8 @@ GradPlan grad_plan(int M, int N, int K, bool turned)
     return p;
 }
 
-constexpr int whole_chunks(int n) { return (n + 7) / 8 * 8; }
+// Elements of a row of values: whole cache lines.
+constexpr int value_row(int n) { return (n + 63) / 64 * 64; }
 
 // Bytes of the values of both 8-bit operands and (copy) of dy, and of the two factors.
 struct ValueBytes {
@@ -232,9 +245,9 @@ struct ValueBytes {
 
 ValueBytes value_bytes(int M, int N, int K, bool want_x, bool want_w, bool copy)
 {
-    const size_t row = 2 * (size_t)whole_chunks(K);
+    const size_t row = 2 * (size_t)value_row(K);
     return {want_x ? round256(N * row) : 0, want_w ? round256(M * row) : 0,
-            copy ? round256((size_t)M * 2 * whole_chunks(N)) : 0, 256};
+            copy ? round256((size_t)M * 2 * value_row(N)) : 0, 256};
 }
 
 bool grad_sizes(int M, int N, int K)
@@ -316,7 +329,15 @@ size_t tasq_masked_linear_tokens_backward_workspace_bytes(int M, int N, int K)
         if (values)
             plan_values(p, turned);
         else
-            plan_codes(p, turned, true);
+            {
+            // (Either of the two ways that rows may lie.)
+            size_t most = 0;
+            for (const bool whole : {false, true}) {
+                plan_codes(p, turned, whole, true);
+                most = p.parts > most ? p.parts : most;
+            }
+            p.parts = most;
+        }
         parts = p.parts > parts ? p.parts : parts;
     }
     return parts + (values ? value_bytes(M, N, K, true, true, N % 8 != 0).all() : 0);
@@ -330,7 +351,7 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
 {
     if (type != TASQ_TYPE_BF16 && type != TASQ_TYPE_F16)
         return TASQ_ERR_KIND;
-    if (!grad_sizes(M, N, K) || (M > 1 && dy_stride < N))
+    if (!grad_sizes(M, N, K) || (M > 1 && (dy_stride < N || dy_stride >= TASQ_MAX_GRAD_STRIDE)))
         return TASQ_ERR_DIM;
     if (K > TASQ_MAX_K)
         return TASQ_ERR_OVERFLOW;
@@ -348,7 +369,8 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
         return TASQ_ERR_ALIGN;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool bf16 = type == TASQ_TYPE_BF16;
-    const long long stride = M > 1 ? dy_stride : N;
+    // (One row has any; 32-bit offsets within a tile.)
+    const long long stride = M > 1 ? dy_stride : N < 4096 ? (N + 7) / 8 * 8 : 4096;
     size_t have = workspace ? workspace_bytes : 0;
     char *at = static_cast<char *>(workspace);
     GradPlan plan[2];
@@ -366,8 +388,7 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
             const bool wanted = turned ? want_w : want_x;
             parts = wanted && plan[turned].parts > parts ? plan[turned].parts : parts;
         }
-        // (Offsets within a tile of dy are 32-bit.)
-        values = vb.all() + parts <= have && (dy_whole ? stride : whole_chunks(N)) < (1 << 22);
+        values = vb.all() + parts <= have;
     }
     tasq::GradGemm gemm[2] = {};
     if (values) {
@@ -388,7 +409,7 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
             j.to = take(vb.dy);
             j.rows = M;
             j.width = N;
-            j.to_stride = whole_chunks(N);
+            j.to_stride = value_row(N);
             A = j.to;
             a_stride = j.to_stride;
         }
@@ -404,7 +425,7 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
             j.to = take(turned ? vb.x : vb.w);
             j.rows = plan[turned].Z;
             j.width = K;
-            j.to_stride = whole_chunks(K);
+            j.to_stride = value_row(K);
             tasq::GradGemm &g = gemm[turned];
             g.A = A;
             g.a_stride = a_stride;
@@ -420,10 +441,11 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
             continue;
         GradPlan &p = plan[turned];
         float *const bias = turned ? dbias : nullptr;
+        const bool codes_whole = dy_whole && K % 16 == 0 && aligned_to(turned ? X : W, 16);
         if (!values) {
-            plan_codes(p, bias, true);
+            plan_codes(p, bias, codes_whole, true);
             if (p.parts > have)
-                plan_codes(p, bias, false);
+                plan_codes(p, bias, codes_whole, false);
         }
         float *part = p.splits > 1 ? reinterpret_cast<float *>(at) : nullptr;
         float *bias_part =
@@ -464,10 +486,8 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
             g.split_steps = p.split_steps;
             g.part = part;
             g.bias_part = bias_part;
-            // (Offsets within a tile of dy are 32-bit.)
-            const bool whole = dy_whole && K % 16 == 0 && aligned_to(g.Q, 16) && stride < (1 << 22);
-            e = bf16 ? tasq::token_grad_bf16(g, turned, whole, st)
-                     : tasq::token_grad_f16(g, turned, whole, st);
+            e = bf16 ? tasq::token_grad_bf16(g, turned, codes_whole, st)
+                     : tasq::token_grad_f16(g, turned, codes_whole, st);
         }
         if (e != hipSuccess)
             return TASQ_ERR_HIP;

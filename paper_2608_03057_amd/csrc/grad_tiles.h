@@ -284,7 +284,7 @@ template <class T> __global__ void __launch_bounds__(256) k_grad_values(GradValu
     __shared__ float part[4];
     const int job = blockIdx.y;
     const GradValues::Job &j = v.job[job];
-    const int chunks = j.to_stride / 8;
+    const int chunks = (j.width + 7) / 8;
     const size_t n = (size_t)j.rows * chunks;
     int shift = 0;
     if constexpr (__is_same(T, f16_t)) {
@@ -331,7 +331,7 @@ template <class T> __global__ void __launch_bounds__(256) k_grad_values(GradValu
                 o = __builtin_bit_cast(u32x4, e);
             }
         }
-        static_cast<u32x4 *>(j.to)[at] = o;
+        *reinterpret_cast<u32x4 *>(static_cast<T *>(j.to) + (size_t)row * j.to_stride + c) = o;
     }
 }
 
@@ -339,7 +339,7 @@ template <class T> hipError_t write_values(const GradValues &v, hipStream_t stre
 {
     size_t most = 0;
     for (int i = 0; i < v.n; ++i) {
-        const size_t n = (size_t)v.job[i].rows * (v.job[i].to_stride / 8);
+        const size_t n = (size_t)v.job[i].rows * ((v.job[i].width + 7) / 8);
         most = n > most ? n : most;
     }
     const size_t blocks = (most + 255) / 256;

@@ -110,9 +110,14 @@ template <class C>
 __device__ __forceinline__ int range_exponent(const float *s, int z0, int z1, float *part)
 {
     float top = 0.0f;
-    for (int z = z0 + (int)threadIdx.x; z < z1; z += C::NT) {
-        const float f = fabsf(s[z]);
-        top = f < __builtin_inff() ? fmaxf(top, f) : top;
+    for (int z = z0 + (int)threadIdx.x; z < z1; z += 8 * C::NT) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)     // (on their way together)
+            f[i] = fabsf(s[min(z + i * C::NT, z1 - 1)]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            top = f[i] < __builtin_inff() ? fmaxf(top, f[i]) : top;
     }
     top = group_reduce<64>(top, [](float a, float b) { return fmaxf(a, b); });
     if ((threadIdx.x & 63) == 0)
@@ -195,59 +200,81 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     const int qz = (int)threadIdx.x / (C::BC / 8), qc = 8 * ((int)threadIdx.x % (C::BC / 8));
     const uint32_t q_off =
         c0 + qc < g.C ? (uint32_t)qz * (uint32_t)g.C + (uint32_t)(c0 + qc) : kOOB;
+    // Where rows that are no whole chunks lie, a chunk reaches past its row: into the
+    // next, or, of the last ones, past the operand's end.  The dword across that end is
+    // dropped, and its first bytes are loaded one by one.
+    const uint32_t a_pitch = 2u * (uint32_t)g.a_stride;
+    const T *const a_end = A + (TURNED ? (size_t)(g.Z - 1) * g.a_stride + g.R
+                                       : (size_t)(g.R - 1) * g.a_stride + g.Z);
     // Step t's, zeros past the range.
     auto request = [&](Raw &raw, int t) {
         const int zt = z0 + kGradStep * t;
         const uint32_t n = uniform(max(min(z1 - zt, kGradStep), 0));
         const rsrc_t rs = make_rsrc(g.s + zt, 4u * n);
-        const rsrc_t rq = make_rsrc(g.Q + (size_t)zt * g.C, WHOLE ? n * (uint32_t)g.C : 0u);
+        const int8_t *const q0 = g.Q + (size_t)zt * g.C;
+        uint32_t bytes = n * (uint32_t)g.C;
+        if (!WHOLE && n) {
+            const long long rest = q_end - q0;
+            bytes = rest < bytes + 7 ? (uint32_t)rest : bytes + 7;
+        }
+        const rsrc_t rq = make_rsrc(q0, bytes);
 #pragma unroll
         for (int i = 0; i < C::Q_TASKS; ++i) {
-            const int z = qz + i * Q_ROWS, c = c0 + qc;
-            raw.s[i] = __builtin_bit_cast(
-                float, __builtin_amdgcn_raw_buffer_load_b32(rs, 4u * (uint32_t)z, 0, 0));
-            if constexpr (WHOLE) {
-                raw.q[i] = __builtin_bit_cast(
-                    u32x2, __builtin_amdgcn_raw_buffer_load_b64(
-                               rq, q_off + (uint32_t)(i * Q_ROWS) * (uint32_t)g.C, 0, 0));
-            } else {
-                raw.q[i] = u32x2{0, 0};
-                if (zt + z >= z1 || c >= g.C)
-                    continue;
-                const int8_t *p = g.Q + (size_t)(zt + z) * g.C + c;
-                const long long left = (long long)(q_end - p);
-                if (left >= 8) {
-                    const Packed<int8_t, 8> w = *reinterpret_cast<const Packed<int8_t, 8> *>(p);
-                    raw.q[i] = u32x2{w.w[0], w.w[1]};
-                } else {            // of the last row of all
-                    uint64_t w = 0;
-#pragma unroll 1
-                    for (int e = 0; e < (int)left; ++e)
-                        w |= (uint64_t)(uint8_t)p[e] << (8 * e);
-                    raw.q[i] = u32x2{(uint32_t)w, (uint32_t)(w >> 32)};
-                }
-            }
+            raw.s[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
+                                                     rs, 4u * (uint32_t)(qz + i * Q_ROWS), 0, 0));
+            raw.q[i] = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_raw_buffer_load_b64(
+                           rq, q_off + (uint32_t)(i * Q_ROWS) * (uint32_t)g.C, 0, 0));
         }
         if constexpr (!WHOLE) {
+            const T *const a0 = A + (TURNED ? (size_t)zt * g.a_stride + r0 : (size_t)r0 * g.a_stride + zt);
+            uint32_t a_bytes = 0;
+            if (n) {
+                const uint32_t rows = TURNED ? n : (uint32_t)min(g.R - r0, C::BR);
+                const uint32_t cols = TURNED ? (uint32_t)min(g.R - r0, C::BR) : n;
+                const long long want = (long long)(rows - 1) * a_pitch + 2 * cols + 14;
+                const long long rest = 2 * (a_end - a0);
+                a_bytes = (uint32_t)(rest < want ? rest : want);
+            }
+            const rsrc_t ra = make_rsrc(a0, uniform(a_bytes));
 #pragma unroll
             for (int i = 0; i < C::A_TASKS; ++i) {
                 const int task = (int)threadIdx.x + i * C::NT;
                 const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
-                const int z = TURNED ? zt + row : zt + first, r = TURNED ? r0 + first : r0 + row;
-                const int left = TURNED ? g.R - r : z1 - z;     // of the row of A
-                raw.a[i] = u32x4{0, 0, 0, 0};
-                if ((TURNED ? z >= z1 : r >= g.R) || left <= 0)
-                    continue;
-                const T *p = A + (TURNED ? (size_t)z * g.a_stride + r : (size_t)r * g.a_stride + z);
-                if (left >= 8) {
-                    raw.a[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const Packed<T, 8> *>(p));
-                } else {
-                    T e[8] = {};
+                const bool in = TURNED ? row < (int)n && first < g.R - r0
+                                       : r0 + row < g.R && first < (int)n;
+                raw.a[i] = __builtin_bit_cast(
+                    u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                               ra, in ? (uint32_t)row * a_pitch + 2u * (uint32_t)first : kOOB, 0, 0));
+            }
+            // The last dword of either operand (its rows are near the end of the range).
+            if (n && zt + (int)n == g.Z) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        if (k < left)
-                            e[k] = p[k];
-                    raw.a[i] = __builtin_bit_cast(u32x4, e);
+                for (int i = 0; i < C::Q_TASKS; ++i) {
+                    const int z = qz + i * Q_ROWS, c = c0 + qc;
+                    const int8_t *p = q0 + (size_t)z * g.C + c;
+                    const int left = z < (int)n && c < g.C && q_end - p < 8 ? (int)(q_end - p) : 0;
+                    uint32_t u = 0;
+#pragma unroll 1
+                    for (int e = left & ~3; e < left; ++e)
+                        u |= (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
+                    if (left & 3)
+                        raw.q[i] = left < 4 ? u32x2{u, 0} : u32x2{raw.q[i].x, u};
+                }
+#pragma unroll
+                for (int i = 0; i < C::A_TASKS; ++i) {
+                    const int task = (int)threadIdx.x + i * C::NT;
+                    const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
+                    const bool in = TURNED ? row < (int)n && first < g.R - r0
+                                           : r0 + row < g.R && first < (int)n;
+                    const T *p = a0 + (size_t)row * g.a_stride + first;
+                    const int left = in && a_end - p < 8 ? (int)(a_end - p) : 0;
+                    if (left & 1) {
+                        const uint32_t u = __builtin_bit_cast(uint16_t, p[left - 1]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            raw.a[i][k] = k == left / 2 ? u : raw.a[i][k];
+                    }
                 }
             }
         }
@@ -259,7 +286,6 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     const int a_row = wave * A_ROWS + lane / CH;
     const int a_col = 8 * (TURNED ? (lane % CH) ^ (4 * turn_key<A_PITCH>(a_row))
                                   : (lane % CH) ^ ((a_row >> 1) & 7));
-    const uint32_t a_pitch = 2u * (uint32_t)g.a_stride;
     const uint32_t a_off = TURNED && a_col >= g.R - r0
                                ? kOOB
                                : (uint32_t)a_row * a_pitch + 2u * (uint32_t)a_col;
@@ -300,8 +326,18 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 dequantize<T>(u32x2{raw.q[i].x & g.mask, raw.q[i].y & g.mask}, s);
         }
     };
-    auto put_chunks = [&](const Raw &raw, Stage st) {
+    auto put_chunks = [&](Raw &raw, Stage st, int t) {
         if constexpr (!WHOLE) {
+            const int n = (int)uniform(z1 - z0 - kGradStep * t);    // rows of step t
+            if (!TURNED && n < kGradStep) {     // zeros past the range within a chunk
+#pragma unroll
+                for (int i = 0; i < C::A_TASKS; ++i) {
+                    const int left = n - 8 * (((int)threadIdx.x + i * C::NT) % (A_PITCH / 16));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        raw.a[i][k] &= left >= 2 * k + 2 ? ~0u : left == 2 * k + 1 ? 0xffffu : 0u;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < C::A_TASKS; ++i) {
                 const int task = (int)threadIdx.x + i * C::NT;
@@ -383,7 +419,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
         direct(st.a, 0);
         request(now, 0);
         put(now, st, 0, C::Q_TASKS);
-        put_chunks(now, st);
+        put_chunks(now, st, 0);
         direct(after.a, 1);
         request(next, 1);
         pers::wait_vm_lgkm0<0>();
@@ -421,7 +457,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
             multiply(f[1]);
             in_turn(PUT_VALU);
             read(st, 3, f[1]);
-            put_chunks(now, after);
+            put_chunks(now, after, t + 1);
             multiply(f[0]);
             in_turn(NO_VALU);
             // This wave has read all of step t and written its part of t + 1.
@@ -480,14 +516,20 @@ __global__ void __launch_bounds__(256) k_join_grad(const float *part, T *out, si
         float v[4] = {};
         const int live = n - at < 4 ? (int)(n - at) : 4;
         if (live == 4) {
-            for (int s = 0; s < splits; ++s) {
-                const Packed<float, 4> p =
-                    *reinterpret_cast<const Packed<float, 4> *>(part + (size_t)s * n + at);
-                float f[4];
-                p.floats(f);
+            for (int s = 0; s < splits; s += 8) {       // (eight on their way together)
+                Packed<float, 4> p[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] += f[e];
+                for (int i = 0; i < 8; ++i)
+                    p[i] = *reinterpret_cast<const Packed<float, 4> *>(
+                        part + (size_t)min(s + i, splits - 1) * n + at);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float f[4];
+                    p[i].floats(f);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[e] += s + i < splits ? f[e] : 0.0f;
+                }
             }
             Packed<T, 4> o;
             o.set(v);

@@ -214,6 +214,14 @@ def test_token_grad_rejects(kw, code):
     assert grad(**kw) == code
 
 
+def test_token_grad_rejects_rows_too_far_apart():
+    text = open(os.path.join(ROOT, "include", "tasq.h")).read()
+    value = re.search(r"#define TASQ_MAX_GRAD_STRIDE (\(?[\d <]+\)?)", text)[1]
+    assert eval(value) == _lib.TASQ_MAX_GRAD_STRIDE
+    assert grad(stride=_lib.TASQ_MAX_GRAD_STRIDE) == DIM
+    assert grad(M=0, stride=_lib.TASQ_MAX_GRAD_STRIDE, dw=None, dbias=None) == 0
+
+
 def test_token_grad_of_nothing_is_noop():
     assert grad(dx=None, dw=None, dbias=None) == 0
     assert grad(M=0, dw=None, dbias=None) == grad(K=0, dbias=None) == grad(M=0, N=0) == 0

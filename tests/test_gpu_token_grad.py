@@ -91,6 +91,21 @@ def test_odd_sizes_over_many_tokens(M, N, K, dtype):
     check(make(M, N, K, dtype, M + N), 8)
 
 
+@pytest.mark.parametrize("M,N,K", [(512, 4449, 4400), (513, 4450, 4401), (515, 4451, 4402),
+                                   (519, 4453, 4403), (520, 4455, 4407), (2049, 2563, 2001),
+                                   (8195, 1153, 1100)])
+@pytest.mark.parametrize("dtype", BOTH)
+def test_odd_sizes_of_much_work(M, N, K, dtype):
+    check(make(M, N, K, dtype, M + N), 8)
+
+
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 2), (2, 1), (3, 1), (1, 5), (5, 3), (6, 7), (9, 9)])
+@pytest.mark.parametrize("M", [1, 2, 3, 66])
+def test_rows_of_less_than_a_chunk(M, N, K):
+    """Chunks of these reach over many rows, and past the last one."""
+    check(make(M, N, K, torch.bfloat16, M), 8)
+
+
 @pytest.mark.parametrize("b", range(1, 9))
 def test_bits(b):
     check(make(70, 136, 96, torch.bfloat16), b)
