@@ -167,9 +167,9 @@ void cut_sum(GradPlan &p, int steps, int units, int least, bool cut)
 // tiles that read less.  (Measured at tiles of 64 / 128 / 256, us with the joins: 576
 // steps of 256 x 1152, 700 tokens, for dx 13 / 18 / 24; 1152 x 1152 over 2000 tokens
 // 22 / 22 / 28; 9280 x 2288 over 400 tokens 48 / 38 / 37; 11144 x 2400 over 868 tokens
-// 110 / 81 / 66.  Rows that are no whole chunks pass through registers and LDS, which a
-// tile of 256 has too little else to do beside: 9273 x 2278 over 405 tokens 91 / 73 /
-// 125.)  Ranges of the sum: for 6 tokens of 10536 x 3344 64-row tiles in 212 / 477 / 1007
+// 110 / 81 / 66.  Rows that are no whole chunks pass through registers, and a tile of 256
+// is alone on its compute unit with that: 9273 x 2278 over 405 tokens 48 at 128, 93 at
+// 256.)  Ranges of the sum: for 6 tokens of 10536 x 3344 tiles of 64 in 212 / 477 / 1007
 // workgroups take 26 / 19 / 17 us for dx.
 void plan_codes(GradPlan &p, bool bias, bool whole, bool cut)
 {

@@ -26,8 +26,8 @@ __device__ __forceinline__ void load_chunk_to_lds(rsrc_t r, char *lds, uint32_t 
 
 // The same, not known to the compiler as a write to LDS, for which it would wait
 // before every transposing load: the caller waits (vmcnt) before the barrier that hands
-// the bytes on.  lds, an offset in LDS, is the same in all lanes.  (m0 cannot be named as overwritten: a
-// kernel uses this form or the one above, not both.)
+// the bytes on.  lds, an offset in LDS, is the same in all lanes.  (m0 cannot be named
+// as overwritten: a kernel uses this form or the one above, not both.)
 __device__ __forceinline__ void load_chunk_unseen(rsrc_t r, uint32_t lds, uint32_t off)
 {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -99,6 +99,8 @@ __device__ __forceinline__ void store_tile(T *y, int rows, int cols, int row0, i
             T *to = y + (size_t)m * cols + n;
             if (wide) {
                 *reinterpret_cast<u32x4 *>(to) = u;
+            } else if (n + PER <= cols) {       // at any address
+                *reinterpret_cast<Packed<T, PER> *>(to) = __builtin_bit_cast(Packed<T, PER>, u);
             } else {
                 T one[PER];
                 __builtin_memcpy(one, &u, 16);
