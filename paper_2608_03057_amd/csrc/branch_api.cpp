@@ -142,6 +142,14 @@ struct GradPlan {
     size_t parts;               // bytes of the ranges' parts
 };
 
+// Floats of a product's parts, before the bias'.
+size_t part_floats(const GradPlan &p)
+{
+    return round256((size_t)p.splits * p.R * p.C * sizeof(float)) / sizeof(float);
+}
+
+long long units_of(const GradPlan &p) { return (long long)p.tiles_r * p.tiles_c * p.splits; }
+
 int tiles_of(int n, int t) { return (int)((n + t - 1LL) / t); }
 
 // Ranges of the sum: as many as give `units` workgroups, of at least `least` steps.
@@ -158,7 +166,7 @@ void cut_sum(GradPlan &p, int steps, int units, int least, bool cut)
     if (p.splits < 1)
         p.splits = 1;
     p.parts = p.splits == 1 ? 0
-                            : round256((size_t)p.splits * p.R * p.C * sizeof(float)) +
+                            : part_floats(p) * sizeof(float) +
                                   round256((size_t)p.splits * p.R * sizeof(float));
 }
 
@@ -170,7 +178,8 @@ void cut_sum(GradPlan &p, int steps, int units, int least, bool cut)
 // 110 / 81 / 66.  Rows that are no whole chunks pass through registers, and a tile of 256
 // is alone on its compute unit with that: 9273 x 2278 over 405 tokens 48 at 128, 93 at
 // 256.)  Ranges of the sum: for 6 tokens of 10536 x 3344 tiles of 64 in 212 / 477 / 1007
-// workgroups take 26 / 19 / 17 us for dx.
+// workgroups take 26 / 19 / 17 us for dx; tiles of 128 for 2000 tokens of 1152 x 1152 in up
+// to 256 / 512 of each product 29 / 38 for both.
 void plan_codes(GradPlan &p, bool bias, bool whole, bool cut)
 {
     const int steps = (int)((p.Z + 63LL) / 64);
@@ -182,7 +191,7 @@ void plan_codes(GradPlan &p, bool bias, bool whole, bool cut)
     p.tiles_c = tiles_of(p.C, t);
     if (bias && p.tiles_c == 0)
         p.tiles_c = 1;          // the rows' sums alone
-    cut_sum(p, steps, t == 256 ? 256 : 512, t == 64 ? 4 : 8, cut);
+    cut_sum(p, steps, t == 64 ? 512 : 256, t == 64 ? 4 : 8, cut);
 }
 
 // Of values: tiles of 256 rows by the width that takes the least time, counted in
@@ -322,23 +331,23 @@ size_t tasq_masked_linear_tokens_backward_workspace_bytes(int M, int N, int K)
 {
     if (!grad_sizes(M, N, K) || K > TASQ_MAX_K)
         return 0;
-    size_t parts = 0;
+    // Of values one product's parts after the other's, of codes both (whichever of the
+    // two ways their rows may lie).
     const bool values = values_pay(M, N, K);
-    for (const bool turned : {false, true}) {
-        GradPlan p = grad_plan(M, N, K, turned);
-        if (values)
-            plan_values(p, turned);
-        else
-            {
-            // (Either of the two ways that rows may lie.)
-            size_t most = 0;
-            for (const bool whole : {false, true}) {
+    size_t parts = 0;
+    for (const bool whole : {false, true}) {
+        size_t sum = 0, most = 0;
+        for (const bool turned : {false, true}) {
+            GradPlan p = grad_plan(M, N, K, turned);
+            if (values)
+                plan_values(p, turned);
+            else
                 plan_codes(p, turned, whole, true);
-                most = p.parts > most ? p.parts : most;
-            }
-            p.parts = most;
+            sum += p.parts;
+            most = p.parts > most ? p.parts : most;
         }
-        parts = p.parts > parts ? p.parts : parts;
+        const size_t need = values ? most : sum;
+        parts = need > parts ? need : parts;
     }
     return parts + (values ? value_bytes(M, N, K, true, true, N % 8 != 0).all() : 0);
 }
@@ -436,26 +445,14 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
         if ((bf16 ? tasq::grad_values_bf16(v, st) : tasq::grad_values_f16(v, st)) != hipSuccess)
             return TASQ_ERR_HIP;
     }
-    for (const bool turned : {false, true}) {
-        if (!(turned ? want_w : want_x))
-            continue;
-        GradPlan &p = plan[turned];
-        float *const bias = turned ? dbias : nullptr;
-        const bool codes_whole = dy_whole && K % 16 == 0 && aligned_to(turned ? X : W, 16);
-        if (!values) {
-            plan_codes(p, bias, codes_whole, true);
-            if (p.parts > have)
-                plan_codes(p, bias, codes_whole, false);
-        }
-        float *part = p.splits > 1 ? reinterpret_cast<float *>(at) : nullptr;
-        float *bias_part =
-            part ? part + round256((size_t)p.splits * p.R * p.C * sizeof(float)) / 4 : nullptr;
-        void *out = turned ? dw : dx;
-        hipError_t e;
-        if (values) {
+    if (values) {
+        for (const bool turned : {false, true}) {
+            if (!(turned ? want_w : want_x))
+                continue;
+            const GradPlan &p = plan[turned];
             tasq::GradGemm &g = gemm[turned];
-            g.out = out;
-            g.dbias = bias;
+            g.out = turned ? dw : dx;
+            g.dbias = turned ? dbias : nullptr;
             g.R = p.R;
             g.Z = p.Z;
             g.C = p.C;
@@ -464,32 +461,64 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
             g.tiles_c = p.tiles_c;
             g.splits = p.splits;
             g.split_steps = p.split_steps;
-            g.part = part;
-            g.bias_part = bias_part;
-            e = bf16 ? tasq::grad_gemm_bf16(g, turned, st) : tasq::grad_gemm_f16(g, turned, st);
-        } else {
-            tasq::GradJob g{};
-            g.A = dy;
-            g.a_stride = stride;
-            g.Q = turned ? X : W;
-            g.s = turned ? sx : sw;
-            g.mask = turned ? 0xffffffffu : tasq::keep_mask_dword(b);
-            g.out = out;
-            g.dbias = bias;
-            g.R = p.R;
-            g.Z = p.Z;
-            g.C = p.C;
-            g.tile = p.tile;
-            g.tiles_r = p.tiles_r;
-            g.tiles_c = p.tiles_c;
-            g.splits = p.splits;
-            g.split_steps = p.split_steps;
-            g.part = part;
-            g.bias_part = bias_part;
-            e = bf16 ? tasq::token_grad_bf16(g, turned, codes_whole, st)
-                     : tasq::token_grad_f16(g, turned, codes_whole, st);
+            if (p.splits > 1) {
+                g.part = reinterpret_cast<float *>(at);
+                g.bias_part = g.part + part_floats(p);
+            }
+            if ((bf16 ? tasq::grad_gemm_bf16(g, turned, st) : tasq::grad_gemm_f16(g, turned, st)) !=
+                hipSuccess)
+                return TASQ_ERR_HIP;
         }
-        if (e != hipSuccess)
+        return TASQ_OK;
+    }
+    tasq::GradJob job[2] = {};
+    bool whole[2];
+    for (const bool cut : {true, false}) {
+        size_t need = 0;
+        for (const bool turned : {false, true}) {
+            whole[turned] = dy_whole && K % 16 == 0 && aligned_to(turned ? X : W, 16);
+            plan_codes(plan[turned], turned && dbias, whole[turned], cut);
+            need += (turned ? want_w : want_x) ? plan[turned].parts : 0;
+        }
+        if (need <= have)
+            break;
+    }
+    for (const bool turned : {false, true}) {
+        const GradPlan &p = plan[turned];
+        tasq::GradJob &g = job[turned];
+        g.A = dy;
+        g.a_stride = stride;
+        g.Q = turned ? X : W;
+        g.s = turned ? sx : sw;
+        g.mask = turned ? 0xffffffffu : tasq::keep_mask_dword(b);
+        g.out = turned ? dw : dx;
+        g.dbias = turned ? dbias : nullptr;
+        g.R = p.R;
+        g.Z = p.Z;
+        g.C = p.C;
+        g.tile = p.tile;
+        g.tiles_r = p.tiles_r;
+        g.tiles_c = p.tiles_c;
+        g.splits = p.splits;
+        g.split_steps = p.split_steps;
+        if ((turned ? want_w : want_x) && p.splits > 1) {
+            g.part = reinterpret_cast<float *>(at);
+            g.bias_part = g.part + part_floats(p);
+            at += p.parts;
+        }
+    }
+    // Small products share a launch (on its own each takes 3 us of the host's, and fills
+    // less of the card).
+    const long long units = units_of(plan[0]) + units_of(plan[1]);
+    if (want_x && want_w && plan[0].tile == plan[1].tile && plan[0].tile <= 128 &&
+        whole[0] == whole[1] && units < (1 << 22))
+        return status(bf16 ? tasq::token_grads_bf16(job[0], job[1], whole[0], st)
+                           : tasq::token_grads_f16(job[0], job[1], whole[0], st));
+    for (const bool turned : {false, true}) {
+        if (!(turned ? want_w : want_x))
+            continue;
+        if ((bf16 ? tasq::token_grad_bf16(job[turned], turned, whole[turned], st)
+                  : tasq::token_grad_f16(job[turned], turned, whole[turned], st)) != hipSuccess)
             return TASQ_ERR_HIP;
     }
     return TASQ_OK;

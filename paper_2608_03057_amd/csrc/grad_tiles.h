@@ -369,15 +369,13 @@ template <class T, bool TURNED> hipError_t launch_gemm_tile(const GradGemm &g, h
 
 template <class T> hipError_t run_gemm(GradGemm g, bool turned_a, hipStream_t stream)
 {
-    float *dbias = g.dbias;
-    if (g.splits > 1)
-        g.dbias = dbias ? g.bias_part : nullptr;
+    const GradParts p = {g.part, g.out, (size_t)g.R * g.C, g.splits,
+                         g.dbias ? g.bias_part : nullptr, g.dbias, g.R};
+    if (g.splits > 1 && g.dbias)
+        g.dbias = g.bias_part;
     const hipError_t e = turned_a ? launch_gemm_tile<T, true>(g, stream)
                                   : launch_gemm_tile<T, false>(g, stream);
-    if (e != hipSuccess || g.splits == 1)
-        return e;
-    return join_parts<T>(g.part, g.out, (size_t)g.R * g.C, g.splits, dbias ? g.bias_part : nullptr,
-                         dbias, g.R, stream);
+    return e != hipSuccess || g.splits == 1 ? e : join_parts<T>(&p, 1, stream);
 }
 
 }  // namespace

@@ -505,12 +505,50 @@ __global__ void __launch_bounds__(C::NT) k_token_grad(GradJob g, int first)
     grad_tile<T, C, TURNED, WHOLE>(g, (int)uniform(tr), (int)uniform(tc), (int)uniform(split), sm);
 }
 
-// Adds the ranges' parts up in order and rounds: four values a thread, and after the
-// last of them the bias'.
-template <class T>
-__global__ void __launch_bounds__(256) k_join_grad(const float *part, T *out, size_t n, int splits,
-                                                   const float *bias_part, float *dbias, int bias_n)
+// Both products of a small gradient in one launch: dx's `first` workgroups, then dw's.
+template <class T, class C, bool WHOLE>
+__global__ void __launch_bounds__(C::NT) k_token_grads(GradJob x, GradJob w, int first)
 {
+    constexpr int OUT = C::WC * C::WR * kOutBytes<float, C::FC>;
+    __shared__ __attribute__((aligned(1024))) char sm[C::LDS > OUT ? C::LDS : OUT];
+    // (Each XCD has its share of both.)
+    const bool turned_a = (int)blockIdx.x >= first;
+    const int u = turned_a ? xcd_remap(blockIdx.x - first, gridDim.x - first)
+                           : xcd_remap(blockIdx.x, first);
+    const int tiles_r = turned_a ? w.tiles_r : x.tiles_r;
+    const int tiles_c = turned_a ? w.tiles_c : x.tiles_c;
+    const int tiles = tiles_r * tiles_c, split = u / tiles;
+    int tr, tc;
+    tile_coords(u - split * tiles, tiles_r, tiles_c, tr, tc);
+    tr = (int)uniform(tr);
+    tc = (int)uniform(tc);
+    if (turned_a)
+        grad_tile<T, C, true, WHOLE>(w, tr, tc, (int)uniform(split), sm);
+    else
+        grad_tile<T, C, false, WHOLE>(x, tr, tc, (int)uniform(split), sm);
+}
+
+// Parts of a result that its ranges left, and of the bias'.
+struct GradParts {
+    const float *part;
+    void *out;
+    size_t n;
+    int splits;
+    const float *bias_part;
+    float *dbias;
+    int bias_n;
+};
+
+// Adds the ranges' parts up in order and rounds, of one result or two: four values a
+// thread, and after the last of them the bias'.
+template <class T>
+__global__ void __launch_bounds__(256) k_join_grad(GradParts one, GradParts two)
+{
+    const GradParts &j = blockIdx.y ? two : one;
+    const float *const part = j.part;
+    T *const out = static_cast<T *>(j.out);
+    const size_t n = j.n;
+    const int splits = j.splits;
     const size_t at = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
     if (at < n) {
         float v[4] = {};
@@ -545,11 +583,11 @@ __global__ void __launch_bounds__(256) k_join_grad(const float *part, T *out, si
         return;
     }
     const size_t b = (size_t)blockIdx.x * 256 + threadIdx.x - (n + 3) / 4;
-    if (bias_part && b < (size_t)bias_n) {
+    if (j.bias_part && b < (size_t)j.bias_n) {
         float f = 0.0f;
         for (int s = 0; s < splits; ++s)
-            f += bias_part[(size_t)s * bias_n + b];
-        dbias[b] = f;
+            f += j.bias_part[(size_t)s * j.bias_n + b];
+        j.dbias[b] = f;
     }
 }
 
@@ -580,28 +618,61 @@ hipError_t launch_product(const GradJob &g, bool whole, hipStream_t stream)
     return launch_cfg<T, GradCfg<64, 64, 2, 2>, TURNED>(g, whole, stream);
 }
 
-template <class T>
-hipError_t join_parts(const float *part, void *out, size_t n, int splits, const float *bias_part,
-                      float *dbias, int bias_n, hipStream_t stream)
+// What is left to add up of a product whose range is cut.
+inline GradParts parts_of(const GradJob &g, float *dbias)
 {
-    const size_t threads = (n + 3) / 4 + (dbias ? bias_n : 0);
-    k_join_grad<T><<<(unsigned)((threads + 255) / 256), 256, 0, stream>>>(
-        part, static_cast<T *>(out), n, splits, bias_part, dbias, bias_n);
+    return {g.part, g.out, (size_t)g.R * g.C, g.splits, dbias ? g.bias_part : nullptr, dbias, g.R};
+}
+
+template <class T> hipError_t join_parts(const GradParts *p, int n, hipStream_t stream)
+{
+    size_t most = 0;
+    for (int i = 0; i < n; ++i) {
+        const size_t threads = (p[i].n + 3) / 4 + (p[i].dbias ? p[i].bias_n : 0);
+        most = threads > most ? threads : most;
+    }
+    k_join_grad<T><<<dim3((unsigned)((most + 255) / 256), n), 256, 0, stream>>>(p[0], p[n - 1]);
     return hipGetLastError();
 }
 
 // One of the two products and, where its range is cut, the sum of its parts.
 template <class T> hipError_t run_product(GradJob g, bool turned_a, bool whole, hipStream_t stream)
 {
-    float *dbias = g.dbias;
-    if (g.splits > 1)
-        g.dbias = dbias ? g.bias_part : nullptr;
+    const GradParts p = parts_of(g, g.dbias);
+    if (g.splits > 1 && g.dbias)
+        g.dbias = g.bias_part;
     hipError_t e = turned_a ? launch_product<T, true>(g, whole, stream)
                             : launch_product<T, false>(g, whole, stream);
-    if (e != hipSuccess || g.splits == 1)
-        return e;
-    return join_parts<T>(g.part, g.out, (size_t)g.R * g.C, g.splits, dbias ? g.bias_part : nullptr,
-                         dbias, g.R, stream);
+    return e != hipSuccess || g.splits == 1 ? e : join_parts<T>(&p, 1, stream);
+}
+
+template <class T, class C>
+hipError_t launch_both(const GradJob &x, const GradJob &w, bool whole, hipStream_t stream)
+{
+    const int first = x.tiles_r * x.tiles_c * x.splits;
+    const unsigned grid = (unsigned)(first + w.tiles_r * w.tiles_c * w.splits);
+    if (whole)
+        k_token_grads<T, C, true><<<grid, C::NT, 0, stream>>>(x, w, first);
+    else
+        k_token_grads<T, C, false><<<grid, C::NT, 0, stream>>>(x, w, first);
+    return hipGetLastError();
+}
+
+// Both products, of one tile size of 64 or 128 and fewer than 2^22 workgroups in all.
+template <class T> hipError_t run_products(GradJob x, GradJob w, bool whole, hipStream_t stream)
+{
+    GradParts p[2];
+    int n = 0;
+    if (x.splits > 1)
+        p[n++] = parts_of(x, nullptr);
+    if (w.splits > 1) {
+        p[n++] = parts_of(w, w.dbias);
+        if (w.dbias)
+            w.dbias = w.bias_part;
+    }
+    const hipError_t e = x.tile == 64 ? launch_both<T, GradCfg<64, 64, 2, 2>>(x, w, whole, stream)
+                                      : launch_both<T, GradCfg<128, 128, 2, 2>>(x, w, whole, stream);
+    return e != hipSuccess || n == 0 ? e : join_parts<T>(p, n, stream);
 }
 
 }  // namespace
