@@ -5,7 +5,10 @@
 // does it again.  Here a pass of its own writes s[z] q[z][c] once, rounded to dy's type
 // (rows filled up to whole 16-byte chunks; dy too, where its own are not), and the
 // product is one of two 16-bit matrices whose rows go to LDS directly: no registers and
-// no vector instructions but addresses between memory and the matrix unit.
+// no vector instructions but addresses between memory and the matrix unit.  Bound by the
+// matrix unit at the clock that the power allows it (2.0 to 2.2 GHz, busy 0.42 to 0.48):
+// 8192 tokens of 1152 -> 3456 70 us a product and 9.5 for the values, 4096 of 2240 ->
+// 11200 207 and 18.
 #pragma once
 
 #include "token_grad.h"

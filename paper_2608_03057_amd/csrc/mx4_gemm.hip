@@ -9,6 +9,11 @@
 // The weight's rows are the first operand, so that a lane's accumulators are four
 // neighbouring channels of one token: they cross LDS as whole dwords on their way to
 // rows of 16-byte stores.
+//
+// Bound, where there are many tokens, by what the products wait for: their share of the
+// matrix units' time is 0.45 over long sums (8192^3 in 285 us), 0.27 for 4096x2240 ->
+// 11200 (77 us) and 0.2 for 8192x1152 -> 4608 (41 us), where a tile's results take as
+// long as two steps.  With few tokens it is the launch and one round of loads.
 #include "branch_internal.h"
 #include "floats.h"
 #include "gemm_pers.h"
@@ -218,7 +223,10 @@ template <class C, class T> __global__ void __launch_bounds__(C::NT) k_mx4_gemm(
 // ahead of its products across tiles: those of a tile's first steps are asked for
 // before the stores of the tile before, which nothing waits for but the step after the
 // next (one in-order counter covers loads and stores).  Outputs cross 4 KB of LDS a
-// wave, whole lines of rows at a time.
+// wave, whole lines of rows at a time.  (8192x1152 -> 4608 in bfloat16: 41 us, a
+// workgroup a tile 45; 4096x2240 -> 11200 into fp32 77 and 88.  In tiles of 128, 45 and
+// 107; two workgroups of 128 x 256 a compute unit in steps of half cache lines 47 and
+// more, bound by requests to L2.)
 template <class C, class T> struct Mx4Walk {
     static constexpr int OUT = 4096;                            // of a wave
     static constexpr int LDS = 2 * C::STAGE + C::NT / 64 * OUT;
@@ -490,11 +498,11 @@ __global__ void __launch_bounds__(C::NT) k_mx4_walk(Mx4Linear a, int tiles_m, in
 // have every fourth 128 elements each, straight from memory as matrix operands (lane
 // l: channel l % 16, block l / 16 of the four), against the tokens' codes read alike;
 // the waves' sums meet in LDS.
-constexpr int kMx4Few = 64;
+constexpr int kMx4Few = 32;
 
 template <class T, int MB> __global__ void __launch_bounds__(256) k_mx4_few(Mx4Linear a)
 {
-    constexpr int UNROLL = MB <= 2 ? 4 : 2;
+    constexpr int UNROLL = 4;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int n0 = blockIdx.x * 16, r = lane & 15, kb = lane >> 4;
     Mx4Rows W, X;
@@ -586,19 +594,22 @@ hipError_t launch_mx4_linear(const Mx4Linear &a, hipStream_t stream)
 {
     return with_type(a.type, [&](auto zero) {
         using T = decltype(zero);
-        // (16 channels to a workgroup: from 2^28 on they are more than a launch takes.)
-        if (a.M <= kMx4Few && a.N < (1 << 28)) {
+        // (Few / tiles of 64, us: 1152 -> 3456 of 16 tokens 3.1 / 4.0, 32 3.5 / 4.1, 64 4.2
+        // / 4.1; 1152 -> 9000 of 1 3.8 / 3.9, 16 4.4 / 4.1, 32 5.7 / 4.2; 4608 -> 1152 of
+        // 32 7.2 / 7.9, 64 10.2 / 8.0.)
+        if (a.M <= kMx4Few && (long long)a.M * a.N <= 1 << 17) {
             const unsigned grid = (unsigned)((a.N + 15LL) / 16);
             if (a.M <= 16)
                 k_mx4_few<T, 1><<<grid, 256, 0, stream>>>(a);
-            else if (a.M <= 32)
-                k_mx4_few<T, 2><<<grid, 256, 0, stream>>>(a);
             else
-                k_mx4_few<T, 4><<<grid, 256, 0, stream>>>(a);
+                k_mx4_few<T, 2><<<grid, 256, 0, stream>>>(a);
             return hipGetLastError();
         }
         const long long t128 = ((a.M + 127LL) / 128) * ((a.N + 127LL) / 128);
         const long long t256 = ((a.M + 255LL) / 256) * ((a.N + 255LL) / 256);
+        // Tiles as large as still come to half a round.  (64 / 128 / 256, us, 1152
+        // channels in: 2304 x 4096 18.8 / 17.5 / 16.3, 1500 x 3000 11.0 / 10.6 / 14.1,
+        // 512 x 2304 6.9 / 7.6 / 12.6.)
         if (t256 >= 140) {
             // The walk stores whole 16-byte chunks at 32-bit offsets within a tile, and
             // takes two steps of 256 elements or more.

@@ -11,7 +11,9 @@
 //
 // A lane has eight elements, four lanes a block; rows are filled up to a multiple of
 // 128 elements with zeros, so that codes and scales of all rows are one run of whole
-// dwords.  Bound by memory: x is read once, a quarter of its bytes (bfloat16) written.
+// dwords.  Bound by memory: x is read once, a quarter of its bytes (bfloat16) written:
+// 8192 x 1152 in 6.9 us, 4096 x 2240 of fp32 in 8.5 (24 and 42 MB, short of a copy's
+// rate by the first loads' latency).
 #include "branch_internal.h"
 #include "floats.h"
 
