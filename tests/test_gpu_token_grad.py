@@ -311,3 +311,128 @@ def test_more_than_two_gib():
     close(dw, *product(a["dy"].t(), a["sx"], a["X"].double(), torch.bfloat16), torch.bfloat16, "dw")
     d = a["dy"].double()
     close(dbias, d.sum(0), 70 * 2.0 ** -24 * d.abs().sum(0), torch.float32, "dbias")
+
+
+# Much work: the codes become values first, in rows of whole cache lines.
+MUCH = (520, 4456, 4408)
+
+
+def arguments(a):
+    return [a[n] for n in ("dy", "X", "W", "sx", "sw")]
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("N", [4456, 4451])
+def test_much_work_with_values_that_are_not_finite(bad, N):
+    M, _, K = MUCH
+    a = make(M, N, K, torch.bfloat16)
+    dx, dw, dbias = check(a, 8)
+    args = arguments(a)
+    args[0] = a["dy"].clone()
+    args[0][300, N - 1] = bad
+    gx, gw, gb = T.masked_linear_tokens_backward(*args, 8)
+    rows = torch.arange(M, device=DEV) != 300
+    assert torch.equal(gx[rows], dx[rows]) and torch.equal(gw[:-1], dw[:-1])
+    assert torch.equal(gb[:-1], dbias[:-1]) and not torch.isfinite(gb[-1])
+    assert not torch.isfinite(gx[300]).any() and not torch.isfinite(gw[-1]).any()
+    args = arguments(a)
+    args[3] = a["sx"].clone()
+    args[3][M - 1] = bad
+    args[1] = a["X"].clone()
+    args[1][M - 1] = 5
+    gx, gw, gb = T.masked_linear_tokens_backward(*args, 8)
+    assert torch.equal(gx, dx) and torch.equal(gb, dbias) and not torch.isfinite(gw).any()
+
+
+def test_much_work_in_half_of_far_factors():
+    a = make(*MUCH, torch.float16)
+    for small in (1e-6, 2.0 ** -40):
+        check({**a, "sx": a["sx"] * small, "sw": a["sw"] * small}, 8)
+    a["sx"][::3] *= 2.0 ** -12
+    check(a, 8)
+    a["sx"] *= 1e5
+    check({**a, "dy": a["dy"] * 1e-3}, 8)
+    a["sx"].zero_()
+    dx, dw, _ = check(a, 8)
+    assert dx.any() and not dw.any()
+
+
+@pytest.mark.parametrize("N", [4456, 4455])
+def test_much_work_of_strided_rows_and_offset_outputs(N):
+    M, _, K = MUCH
+    a = make(M, N, K, torch.bfloat16)
+    plain = check(a, 7)
+    wide = torch.full((M, N + 9), math.nan, dtype=torch.bfloat16, device=DEV)
+    wide[:, 5:5 + N] = a["dy"]
+    even = torch.full((M, N + 16 - N % 8), math.nan, dtype=torch.bfloat16, device=DEV)
+    even[:, :N] = a["dy"]
+    for dy in (wide[:, 5:5 + N], even[:, :N]):
+        check({**a, "dy": dy}, 7)
+    flat = torch.zeros(M * K + 3, dtype=torch.int8, device=DEV)
+    X = flat[3:].view(M, K)
+    X.copy_(a["X"])
+    rooms = [torch.full((r * K + 11,), 7.0, dtype=torch.bfloat16, device=DEV) for r in (M, N)]
+    got = check({**a, "X": X}, 7, dx=rooms[0][3:3 + M * K].view(M, K),
+                dw=rooms[1][5:5 + N * K].view(N, K))
+    assert torch.equal(got[0], plain[0]) and torch.equal(got[1], plain[1])
+    for room, first, n in ((rooms[0], 3, M * K), (rooms[1], 5, N * K)):
+        assert bool((room[:first] == 7).all()) and bool((room[first + n:] == 7).all())
+
+
+@pytest.mark.parametrize("M,N,K", [MUCH, (2048, 4453, 1160), (9000, 1152, 1000)])
+def test_much_work_in_parts(M, N, K):
+    """One result alone, and workspaces without room for the values or for the ranges."""
+    a = make(M, N, K, torch.bfloat16)
+    both = check(a, 6)
+    dx, _, _ = check(a, 6, need_weight=False)
+    assert torch.equal(dx, both[0])
+    _, dw, dbias = check(a, 6, need_input=False)
+    assert torch.equal(dw, both[1]) and torch.equal(dbias, both[2])
+    n = T.masked_linear_tokens_backward_workspace_bytes(M, N, K)
+    for part in (n // 2, 256):
+        check(a, 6, workspace=torch.empty(part, dtype=torch.uint8, device=DEV))
+    # (Bytes behind the workspace asked for stay.)
+    room = torch.full((n + 512,), 9, dtype=torch.uint8, device=DEV)
+    again = check(a, 6, workspace=room[:n])
+    assert all(torch.equal(p, q) for p, q in zip(again, both)) and bool((room[n:] == 9).all())
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+def test_much_work_captured_and_replayed(dtype):
+    a = make(*MUCH, dtype)
+    args = arguments(a)
+
+    def f():
+        return T.masked_linear_tokens_backward(*args, 7)
+    f()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        f()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = f()
+    for seed in range(3):
+        new = make(*MUCH, dtype, seed + 3)
+        for n in ("dy", "X", "sx"):
+            a[n].copy_(new[n])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(out, f()))
+
+
+def test_much_work_of_more_than_two_gib():
+    M, N, K = 1_050_000, 2056, 256
+    a = make(64, N, K, torch.bfloat16)
+    dy = torch.zeros(M, N, dtype=torch.bfloat16, device=DEV)
+    X = torch.zeros(M, K, dtype=torch.int8, device=DEV)
+    sx = torch.ones(M, device=DEV)
+    dy[-64:], X[-64:], sx[-64:] = a["dy"], a["X"], a["sx"]
+    dx, dw, dbias = T.masked_linear_tokens_backward(dy, X, a["W"], sx, a["sw"], 8)
+    assert not dx[:-64].any()
+    close(dx[-64:].clone(), *product(a["dy"], a["sw"], masked(a["W"], 8), torch.bfloat16),
+          torch.bfloat16, "dx")
+    close(dw, *product(a["dy"].t(), a["sx"], a["X"].double(), torch.bfloat16), torch.bfloat16, "dw")
+    d = a["dy"].double()
+    close(dbias, d.sum(0), 70 * 2.0 ** -24 * d.abs().sum(0), torch.float32, "dbias")
