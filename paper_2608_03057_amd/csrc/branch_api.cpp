@@ -179,8 +179,9 @@ void cut_sum(GradPlan &p, int steps, int units, int least, bool cut)
 // is alone on its compute unit with that: 9273 x 2278 over 405 tokens 48 at 128, 93 at
 // 256.)  Ranges of the sum: for 6 tokens of 10536 x 3344 tiles of 64 in 212 / 477 / 1007
 // workgroups take 26 / 19 / 17 us for dx; tiles of 128 for 2000 tokens of 1152 x 1152 in up
-// to 256 / 512 of each product 29 / 38 for both.
-void plan_codes(GradPlan &p, bool bias, bool whole, bool cut)
+// to 256 / 512 of each product 29 / 38 for both; below 24 steps the join's launch is more
+// than the ranges save (700 x 1152 x 1152 17.3 / 12.5 without).
+void plan_codes(GradPlan &p, bool bias, bool whole, bool cut, int groups = 1)
 {
     const int steps = (int)((p.Z + 63LL) / 64);
     const long long work = (long long)tiles_of(p.R, 64) * tiles_of(p.C, 64) * (steps + 3);
@@ -191,7 +192,30 @@ void plan_codes(GradPlan &p, bool bias, bool whole, bool cut)
     p.tiles_c = tiles_of(p.C, t);
     if (bias && p.tiles_c == 0)
         p.tiles_c = 1;          // the rows' sums alone
-    cut_sum(p, steps, t == 64 ? 512 : 256, t == 64 ? 4 : 8, cut);
+    if (t == 64 && groups == 1)
+        cut_sum(p, steps, 512, 4, cut && steps >= 24);
+    else
+        cut_sum(p, steps, 256, 8 * groups, cut);
+}
+
+// Both products of codes, and in how many parts side by side workgroups of tiles of 64
+// have their range (alike for one product alone: the sums are the same).  Two where there
+// are few workgroups: with ranges of their own instead they need a launch more.  (One / two
+// parts, us a call: 1200 x 1152 x 640, 370 workgroups, 16.0 / 14.2; 1500 x 640 x 640, 340,
+// 15.9 / 13.7; 700 x 1152 x 1152, 522, 12.5 / 15.4.  Four parts: 8000 x 128 x 128 21.5 for
+// 15.8 of two.)
+int plan_both(GradPlan (&plan)[2], bool bias, const bool (&whole)[2], bool cut)
+{
+    long long small = 0;
+    for (const bool turned : {false, true}) {
+        plan_codes(plan[turned], turned && bias, whole[turned], false);
+        small += plan[turned].tile == 64 ? units_of(plan[turned]) : 0;
+    }
+    const int groups = small <= 416 ? 2 : 1;
+    for (const bool turned : {false, true})
+        plan_codes(plan[turned], turned && bias, whole[turned], cut,
+                   plan[turned].tile == 64 ? groups : 1);
+    return groups;
 }
 
 // Of values: tiles of 256 rows by the width that takes the least time, counted in
@@ -335,23 +359,20 @@ size_t tasq_masked_linear_tokens_backward_workspace_bytes(int M, int N, int K)
         return 0;
     // Of values one product's parts after the other's, of codes both (whichever of the
     // two ways their rows may lie).
-    const bool values = values_pay(M, N, K);
-    size_t parts = 0;
-    for (const bool whole : {false, true}) {
-        size_t sum = 0, most = 0;
-        for (const bool turned : {false, true}) {
-            GradPlan p = grad_plan(M, N, K, turned);
-            if (values)
-                plan_values(p, turned);
-            else
-                plan_codes(p, turned, whole, true);
-            sum += p.parts;
-            most = p.parts > most ? p.parts : most;
-        }
-        const size_t need = values ? most : sum;
-        parts = need > parts ? need : parts;
+    GradPlan plan[2] = {grad_plan(M, N, K, false), grad_plan(M, N, K, true)};
+    if (values_pay(M, N, K)) {
+        plan_values(plan[0], false);
+        plan_values(plan[1], true);
+        const size_t parts = plan[0].parts > plan[1].parts ? plan[0].parts : plan[1].parts;
+        return parts + value_bytes(M, N, K, true, true, N % 8 != 0).all();
     }
-    return parts + (values ? value_bytes(M, N, K, true, true, N % 8 != 0).all() : 0);
+    size_t most = 0;
+    for (const bool whole : {false, true}) {
+        plan_both(plan, true, {whole, whole}, true);
+        const size_t parts = plan[0].parts + plan[1].parts;
+        most = parts > most ? parts : most;
+    }
+    return most;
 }
 
 int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_stride,
@@ -474,17 +495,12 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
         return TASQ_OK;
     }
     tasq::GradJob job[2] = {};
-    bool whole[2];
-    for (const bool cut : {true, false}) {
-        size_t need = 0;
-        for (const bool turned : {false, true}) {
-            whole[turned] = dy_whole && K % 16 == 0 && aligned_to(turned ? X : W, 16);
-            plan_codes(plan[turned], turned && dbias, whole[turned], cut);
-            need += (turned ? want_w : want_x) ? plan[turned].parts : 0;
-        }
-        if (need <= have)
-            break;
-    }
+    const bool whole[2] = {dy_whole && K % 16 == 0 && aligned_to(W, 16),
+                           dy_whole && K % 16 == 0 && aligned_to(X, 16)};
+    const bool want[2] = {want_x, want_w};
+    int groups = plan_both(plan, dbias, whole, true);
+    if ((want_x ? plan[0].parts : 0) + (want_w ? plan[1].parts : 0) > have)
+        groups = plan_both(plan, dbias, whole, false);
     for (const bool turned : {false, true}) {
         const GradPlan &p = plan[turned];
         tasq::GradJob &g = job[turned];
@@ -503,7 +519,7 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
         g.tiles_c = p.tiles_c;
         g.splits = p.splits;
         g.split_steps = p.split_steps;
-        if ((turned ? want_w : want_x) && p.splits > 1) {
+        if (want[turned] && p.splits > 1) {
             g.part = reinterpret_cast<float *>(at);
             g.bias_part = g.part + part_floats(p);
             at += p.parts;
@@ -511,19 +527,20 @@ int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_st
     }
     // Small products share a launch (on its own each takes 3 us of the host's, and fills
     // less of the card).
-    const long long units = units_of(plan[0]) + units_of(plan[1]);
+    const auto run = [&](const tasq::GradJob *x, const tasq::GradJob *w) {
+        const bool chunks = whole[x ? 0 : 1];
+        if (x && w ? x->tile <= 128 : (x ? x : w)->tile == 64)
+            return bf16 ? tasq::token_grads_bf16(x, w, groups, chunks, st)
+                        : tasq::token_grads_f16(x, w, groups, chunks, st);
+        return bf16 ? tasq::token_grad_bf16(x ? *x : *w, !x, chunks, st)
+                    : tasq::token_grad_f16(x ? *x : *w, !x, chunks, st);
+    };
     if (want_x && want_w && plan[0].tile == plan[1].tile && plan[0].tile <= 128 &&
-        whole[0] == whole[1] && units < (1 << 22))
-        return status(bf16 ? tasq::token_grads_bf16(job[0], job[1], whole[0], st)
-                           : tasq::token_grads_f16(job[0], job[1], whole[0], st));
-    for (const bool turned : {false, true}) {
-        if (!(turned ? want_w : want_x))
-            continue;
-        if ((bf16 ? tasq::token_grad_bf16(job[turned], turned, whole[turned], st)
-                  : tasq::token_grad_f16(job[turned], turned, whole[turned], st)) != hipSuccess)
-            return TASQ_ERR_HIP;
-    }
-    return TASQ_OK;
+        whole[0] == whole[1])
+        return status(run(&job[0], &job[1]));
+    if (want_x && run(&job[0], nullptr) != hipSuccess)
+        return TASQ_ERR_HIP;
+    return want_w ? status(run(nullptr, &job[1])) : TASQ_OK;
 }
 
 }  // extern "C"

@@ -103,8 +103,11 @@ hipError_t grad_gemm_f16(const GradGemm &g, bool turned_a, hipStream_t stream);
 
 hipError_t token_grad_bf16(const GradJob &g, bool turned_a, bool whole, hipStream_t stream);
 hipError_t token_grad_f16(const GradJob &g, bool turned_a, bool whole, hipStream_t stream);
-// Both products in one launch: dx's x and dw's w, of one tile size of 64 or 128.
-hipError_t token_grads_bf16(const GradJob &x, const GradJob &w, bool whole, hipStream_t stream);
-hipError_t token_grads_f16(const GradJob &x, const GradJob &w, bool whole, hipStream_t stream);
+// Products in one launch: dx's x, dw's w or (neither null) both, of one tile size: 64,
+// with the range of a workgroup in 1 or 2 parts side by side, or both of 128.
+hipError_t token_grads_bf16(const GradJob *x, const GradJob *w, int groups, bool whole,
+                            hipStream_t stream);
+hipError_t token_grads_f16(const GradJob *x, const GradJob *w, int groups, bool whole,
+                           hipStream_t stream);
 
 }  // namespace tasq

@@ -246,7 +246,7 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
     }
     pers::barrier();            // the stages are free
     if (TURNED && sums)
-        store_row_sums<C>(bias, wr, wc, r0, g.R, g.dbias + (size_t)split * g.R, sm);
+        store_row_sums<C, C::WC>(bias, wr, wc, r0, g.R, g.dbias + (size_t)split * g.R, sm);
     const int row0 = r0 + wr * C::FR * 32, col0 = c0 + wc * C::FC * 32;
     const float back = g.back ? *g.back : 1.0f;
     auto scaled = [&](int, int, float (&v)[4]) {
@@ -276,10 +276,6 @@ __global__ void __launch_bounds__(C::NT) k_grad_gemm(GradGemm g, int first)
     grad_gemm_tile<T, C>(g, (int)uniform(tr), (int)uniform(tc), (int)uniform(split), sm);
 }
 
-struct ValueThreads {
-    static constexpr int NT = 256;
-};
-
 // Writes codes times their rows' factors as rows of T, and copies rows of T, into rows
 // of whole 16-byte chunks (zeros past the width).
 template <class T> __global__ void __launch_bounds__(256) k_grad_values(GradValues v)
@@ -292,7 +288,7 @@ template <class T> __global__ void __launch_bounds__(256) k_grad_values(GradValu
     int shift = 0;
     if constexpr (__is_same(T, f16_t)) {
         if (j.q) {
-            shift = range_exponent<ValueThreads>(j.s, 0, j.rows, part);
+            shift = range_exponent<256>(j.s, 0, j.rows, part);
             if (blockIdx.x == 0 && threadIdx.x == 0)
                 *j.back = ldexpf(1.0f, -shift);
         }

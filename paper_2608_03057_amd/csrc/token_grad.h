@@ -13,8 +13,8 @@
 // multiplied by it again; a factor below 2^-21 of the largest loses bits, to values that
 // are below 2^-24 of the largest's.
 //
-// Bound by latency: 300 tokens of 640 -> 1283 (1 GFLOP) take 10 us for both products,
-// five steps of loads, values, LDS and products after one another; large products by
+// Bound by latency: 300 tokens of 640 -> 1288 (1 GFLOP) take 10 us for both products,
+// eleven steps of loads, values, LDS and products after one another (1283 13); large products by
 // the vector instructions that turn codes into values, of which a wave has 88 beside 32
 // products, and which every tile of rows does again (grad_tiles.h).
 //
@@ -50,10 +50,11 @@ __device__ __forceinline__ v16f_t mfma_grad(f16_t, u32x4 a, u32x4 b, v16f_t c)
 
 constexpr int kGradStep = 64;   // of the summed axis
 
-// Tiles of BC columns of Q by BR rows of the output, WC x WR waves.
-template <int BC_, int BR_, int WC_, int WR_> struct GradCfg {
-    static constexpr int BC = BC_, BR = BR_, WC = WC_, WR = WR_;
-    static constexpr int NT = 64 * WC * WR;
+// Tiles of BC columns of Q by BR rows of the output, WC x WR waves; G groups of them
+// have a part of the tile's range each, with stages of their own, and add up at its end.
+template <int BC_, int BR_, int WC_, int WR_, int G_ = 1> struct GradCfg {
+    static constexpr int BC = BC_, BR = BR_, WC = WC_, WR = WR_, G = G_;
+    static constexpr int NT = 64 * WC * WR, ALL = G * NT;       // threads of a group, and all
     static constexpr int FC = BC / WC / 32, FR = BR / WR / 32;
     static constexpr int A_BYTES = BR * kGradStep * 2, Q_BYTES = BC * kGradStep * 2;
     // Three stages of A, two of Q.
@@ -110,16 +111,16 @@ template <class T> __device__ __forceinline__ u32x4 dequantize(u32x2 q, float s)
 }
 
 // The power of two that brings the largest finite factor of [z0, z1) to 2^7: with
-// codes of up to 2^7 in magnitude a product stays below 2^15.
-template <class C>
+// codes of up to 2^7 in magnitude a product stays below 2^15.  NT threads.
+template <int NT>
 __device__ __forceinline__ int range_exponent(const float *s, int z0, int z1, float *part)
 {
     float top = 0.0f;
-    for (int z = z0 + (int)threadIdx.x; z < z1; z += 8 * C::NT) {
+    for (int z = z0 + (int)threadIdx.x; z < z1; z += 8 * NT) {
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i)     // (on their way together)
-            f[i] = fabsf(s[min(z + i * C::NT, z1 - 1)]);
+            f[i] = fabsf(s[min(z + i * NT, z1 - 1)]);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             top = f[i] < __builtin_inff() ? fmaxf(top, f[i]) : top;
@@ -129,7 +130,7 @@ __device__ __forceinline__ int range_exponent(const float *s, int z0, int z1, fl
         part[threadIdx.x >> 6] = top;
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < C::NT / 64; ++w)
+    for (int w = 0; w < NT / 64; ++w)
         top = fmaxf(top, part[w]);
     __syncthreads();
     int e = 0;
@@ -139,9 +140,10 @@ __device__ __forceinline__ int range_exponent(const float *s, int z0, int z1, fl
 }
 
 // The sums of a tile's rows that its waves hold, a row to the lanes l and l + 32 and to
-// C::WC waves, added up in order into out[r0 ..]; LDS is free before and after.
-template <class C>
-__device__ __forceinline__ void store_row_sums(const float (&sum)[C::FR], int wr, int wc, int r0,
+// N waves, of which this is the n-th, added up in order into out[r0 ..]; LDS is free
+// before and after.
+template <class C, int N>
+__device__ __forceinline__ void store_row_sums(const float (&sum)[C::FR], int wr, int n, int r0,
                                                int R, float *out, char *sm)
 {
     const int lane = threadIdx.x & 63;
@@ -151,7 +153,7 @@ __device__ __forceinline__ void store_row_sums(const float (&sum)[C::FR], int wr
         const uint32_t u = __float_as_uint(sum[j]);
         const auto p = __builtin_amdgcn_permlane32_swap(u, u, false, false);
         if (lane < 32)
-            part[wc * C::BR + (wr * C::FR + j) * 32 + lane] =
+            part[n * C::BR + (wr * C::FR + j) * 32 + lane] =
                 __uint_as_float(p[0]) + __uint_as_float(p[1]);
     }
     __syncthreads();
@@ -159,7 +161,7 @@ __device__ __forceinline__ void store_row_sums(const float (&sum)[C::FR], int wr
     if (r < C::BR && r0 + r < R) {
         float v = part[r];
 #pragma unroll
-        for (int w = 1; w < C::WC; ++w)
+        for (int w = 1; w < N; ++w)
             v += part[w * C::BR + r];
         out[r0 + r] = v;
     }
@@ -170,22 +172,26 @@ __device__ __forceinline__ void store_row_sums(const float (&sum)[C::FR], int wr
 // [R][Z].  WHOLE: rows of both operands are whole 16-byte chunks at 16-byte addresses,
 // and those of A go to LDS directly.
 template <class T, class C, bool TURNED, bool WHOLE>
-__device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int split, char *sm)
+__device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int split, char *all)
 {
     constexpr int A_PITCH = TURNED ? 2 * C::BR : 2 * kGradStep;
     constexpr int Q_PITCH = 2 * C::BC;
     const int lane = threadIdx.x & 63;
-    const int wave = (int)uniform(threadIdx.x >> 6);
+    const int tid = (int)(threadIdx.x % C::NT), group = (int)uniform(threadIdx.x / C::NT);
+    const int wave = (int)uniform(tid >> 6);
     const int wc = wave % C::WC, wr = wave / C::WC;
     const int r0 = tr * C::BR, c0 = tc * C::BC;
-    const int z0 = split * g.split_steps * kGradStep;
-    const int z1 = min(g.Z, z0 + g.split_steps * kGradStep);
-    const int steps = (z1 - z0 + kGradStep - 1) / kGradStep;
+    const int first = split * g.split_steps * kGradStep;
+    const int end = min(g.Z, first + g.split_steps * kGradStep);
+    // A group's part of the range: as many steps for each, so that they meet at barriers.
+    const int steps = ((end - first + kGradStep - 1) / kGradStep + C::G - 1) / C::G;
+    const int z0 = first + group * steps * kGradStep, z1 = min(end, z0 + steps * kGradStep);
+    char *const sm = all + group * C::LDS;
     const T *A = static_cast<const T *>(g.A);
     const int8_t *const q_end = g.Q + (size_t)g.Z * g.C;
     int shift = 0;
     if constexpr (sizeof(T) == 2 && __is_same(T, f16_t))
-        shift = range_exponent<C>(g.s, z0, z1, reinterpret_cast<float *>(sm));
+        shift = range_exponent<C::ALL>(g.s, first, end, reinterpret_cast<float *>(all));
 
     // A step's codes and factors (and A's chunks, where they pass through registers)
     // on their way.
@@ -202,7 +208,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     // This thread's first eight codes of a step: row qz, column c0 + qc, in every part.
     // (Neighbouring lanes write neighbouring chunks.)
     constexpr int Q_ROWS = C::NT / (C::BC / 8);     // between a thread's parts
-    const int qz = (int)threadIdx.x / (C::BC / 8), qc = 8 * ((int)threadIdx.x % (C::BC / 8));
+    const int qz = tid / (C::BC / 8), qc = 8 * (tid % (C::BC / 8));
     const uint32_t q_off =
         c0 + qc < g.C ? (uint32_t)qz * (uint32_t)g.C + (uint32_t)(c0 + qc) : kOOB;
     // Where rows that are no whole chunks lie, a chunk reaches past its row: into the
@@ -244,7 +250,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
             const rsrc_t ra = make_rsrc(a0, uniform(a_bytes));
 #pragma unroll
             for (int i = 0; i < C::A_TASKS; ++i) {
-                const int task = (int)threadIdx.x + i * C::NT;
+                const int task = tid + i * C::NT;
                 const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
                 const bool in = TURNED ? row < (int)n && first < g.R - r0
                                        : r0 + row < g.R && first < (int)n;
@@ -268,7 +274,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 }
 #pragma unroll
                 for (int i = 0; i < C::A_TASKS; ++i) {
-                    const int task = (int)threadIdx.x + i * C::NT;
+                    const int task = tid + i * C::NT;
                     const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
                     const bool in = TURNED ? row < (int)n && first < g.R - r0
                                            : r0 + row < g.R && first < (int)n;
@@ -337,7 +343,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
             if (!TURNED && n < kGradStep) {     // zeros past the range within a chunk
 #pragma unroll
                 for (int i = 0; i < C::A_TASKS; ++i) {
-                    const int left = n - 8 * (((int)threadIdx.x + i * C::NT) % (A_PITCH / 16));
+                    const int left = n - 8 * ((tid + i * C::NT) % (A_PITCH / 16));
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         raw.a[i][k] &= left >= 2 * k + 2 ? ~0u : left == 2 * k + 1 ? 0xffffu : 0u;
@@ -345,7 +351,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
             }
 #pragma unroll
             for (int i = 0; i < C::A_TASKS; ++i) {
-                const int task = (int)threadIdx.x + i * C::NT;
+                const int task = tid + i * C::NT;
                 const int row = task / (A_PITCH / 16), c = task % (A_PITCH / 16);
                 const uint32_t at = TURNED ? turn_place<A_PITCH>(row, c)
                                            : (uint32_t)(row * A_PITCH + 16 * (c ^ ((row >> 1) & 7)));
@@ -480,7 +486,27 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     }
     pers::barrier();            // the stages are free
     if (TURNED && sums)
-        store_row_sums<C>(bias, wr, wc, r0, g.R, g.dbias + (size_t)split * g.R, sm);
+        store_row_sums<C, C::G * C::WC>(bias, wr, group * C::WC + wc, r0, g.R,
+                                        g.dbias + (size_t)split * g.R, all);
+    if constexpr (C::G > 1) {
+        // The other groups' sums, behind where the first's results go out.
+        constexpr int HELD = C::FC * C::FR * 16, OUT = C::NT / 64 * kOutBytes<float, C::FC>;
+        static_assert(OUT + (C::G - 1) * C::NT * HELD * 4 <= C::G * C::LDS, "room in the stages");
+        float *const part = reinterpret_cast<float *>(all + OUT);
+        if (group > 0) {
+#pragma unroll
+            for (int v = 0; v < HELD; ++v)
+                part[((group - 1) * HELD + v) * C::NT + tid] = acc[v / 16 / C::FR][v / 16 % C::FR][v % 16];
+        }
+        __syncthreads();
+        if (group > 0)
+            return;
+#pragma unroll
+        for (int o = 0; o < C::G - 1; ++o)
+#pragma unroll
+            for (int v = 0; v < HELD; ++v)
+                acc[v / 16 / C::FR][v / 16 % C::FR][v % 16] += part[(o * HELD + v) * C::NT + tid];
+    }
     const int row0 = r0 + wr * C::FR * 32, col0 = c0 + wc * C::FC * 32;
     const float back = ldexpf(1.0f, -shift);
     auto scaled = [&](int, int, float (&v)[4]) {
@@ -510,16 +536,18 @@ __global__ void __launch_bounds__(C::NT) k_token_grad(GradJob g, int first)
     grad_tile<T, C, TURNED, WHOLE>(g, (int)uniform(tr), (int)uniform(tc), (int)uniform(split), sm);
 }
 
-// Both products of a small gradient in one launch: dx's `first` workgroups, then dw's.
+// Both products of a small gradient in one launch, from workgroup `from` on: dx's
+// `first` workgroups, then dw's.
 template <class T, class C, bool WHOLE>
-__global__ void __launch_bounds__(C::NT) k_token_grads(GradJob x, GradJob w, int first)
+__global__ void __launch_bounds__(C::ALL) k_token_grads(GradJob x, GradJob w, int first, int from)
 {
-    constexpr int OUT = C::WC * C::WR * kOutBytes<float, C::FC>;
-    __shared__ __attribute__((aligned(1024))) char sm[C::LDS > OUT ? C::LDS : OUT];
+    constexpr int OUT = C::WC * C::WR * kOutBytes<float, C::FC>, STAGES = C::G * C::LDS;
+    __shared__ __attribute__((aligned(1024))) char sm[STAGES > OUT ? STAGES : OUT];
     // (Each XCD has its share of both.)
-    const bool turned_a = (int)blockIdx.x >= first;
-    const int u = turned_a ? xcd_remap(blockIdx.x - first, gridDim.x - first)
-                           : xcd_remap(blockIdx.x, first);
+    const int block = from + (int)blockIdx.x, end = from + (int)gridDim.x;
+    const bool turned_a = block >= first;
+    const int low = turned_a ? max(first, from) : from, high = turned_a ? end : min(first, end);
+    const int u = low - (turned_a ? first : 0) + xcd_remap(block - low, high - low);
     const int tiles_r = turned_a ? w.tiles_r : x.tiles_r;
     const int tiles_c = turned_a ? w.tiles_c : x.tiles_c;
     const int tiles = tiles_r * tiles_c, split = u / tiles;
@@ -618,9 +646,7 @@ hipError_t launch_product(const GradJob &g, bool whole, hipStream_t stream)
 {
     if (g.tile == 256)
         return launch_cfg<T, GradCfg<256, 256, 4, 2>, TURNED>(g, whole, stream);
-    if (g.tile == 128)
-        return launch_cfg<T, GradCfg<128, 128, 2, 2>, TURNED>(g, whole, stream);
-    return launch_cfg<T, GradCfg<64, 64, 2, 2>, TURNED>(g, whole, stream);
+    return launch_cfg<T, GradCfg<128, 128, 2, 2>, TURNED>(g, whole, stream);
 }
 
 // What is left to add up of a product whose range is cut.
@@ -640,7 +666,8 @@ template <class T> hipError_t join_parts(const GradParts *p, int n, hipStream_t 
     return hipGetLastError();
 }
 
-// One of the two products and, where its range is cut, the sum of its parts.
+// One of the two products, in tiles of 128 or 256, and, where its range is cut, the sum
+// of its parts.
 template <class T> hipError_t run_product(GradJob g, bool turned_a, bool whole, hipStream_t stream)
 {
     const GradParts p = parts_of(g, g.dbias);
@@ -651,21 +678,32 @@ template <class T> hipError_t run_product(GradJob g, bool turned_a, bool whole, 
     return e != hipSuccess || g.splits == 1 ? e : join_parts<T>(&p, 1, stream);
 }
 
+// In as many launches as keep one below 2^22 workgroups, as launch_cfg.
 template <class T, class C>
-hipError_t launch_both(const GradJob &x, const GradJob &w, bool whole, hipStream_t stream)
+hipError_t launch_small(const GradJob &x, const GradJob &w, bool whole, hipStream_t stream)
 {
-    const int first = x.tiles_r * x.tiles_c * x.splits;
-    const unsigned grid = (unsigned)(first + w.tiles_r * w.tiles_c * w.splits);
-    if (whole)
-        k_token_grads<T, C, true><<<grid, C::NT, 0, stream>>>(x, w, first);
-    else
-        k_token_grads<T, C, false><<<grid, C::NT, 0, stream>>>(x, w, first);
-    return hipGetLastError();
+    constexpr long long MOST = 1 << 22;
+    const long long first = (long long)x.tiles_r * x.tiles_c * x.splits;
+    const long long units = first + (long long)w.tiles_r * w.tiles_c * w.splits;
+    for (long long u = 0; u < units; u += MOST) {
+        const unsigned grid = (unsigned)(units - u < MOST ? units - u : MOST);
+        if (whole)
+            k_token_grads<T, C, true><<<grid, C::ALL, 0, stream>>>(x, w, (int)first, (int)u);
+        else
+            k_token_grads<T, C, false><<<grid, C::ALL, 0, stream>>>(x, w, (int)first, (int)u);
+        if (hipError_t e = hipGetLastError())
+            return e;
+    }
+    return hipSuccess;
 }
 
-// Both products, of one tile size of 64 or 128 and fewer than 2^22 workgroups in all.
-template <class T> hipError_t run_products(GradJob x, GradJob w, bool whole, hipStream_t stream)
+// Products of one tile size of 64 (in 1 or 2 groups) or 128.
+template <class T>
+hipError_t run_products(const GradJob *px, const GradJob *pw, int groups, bool whole,
+                        hipStream_t stream)
 {
+    GradJob x = px ? *px : GradJob{}, w = pw ? *pw : GradJob{};     // (of no workgroups)
+    const int tile = px ? x.tile : w.tile;
     GradParts p[2];
     int n = 0;
     if (x.splits > 1)
@@ -675,8 +713,10 @@ template <class T> hipError_t run_products(GradJob x, GradJob w, bool whole, hip
         if (w.dbias)
             w.dbias = w.bias_part;
     }
-    const hipError_t e = x.tile == 64 ? launch_both<T, GradCfg<64, 64, 2, 2>>(x, w, whole, stream)
-                                      : launch_both<T, GradCfg<128, 128, 2, 2>>(x, w, whole, stream);
+    const hipError_t e =
+        tile == 128   ? launch_small<T, GradCfg<128, 128, 2, 2>>(x, w, whole, stream)
+        : groups == 2 ? launch_small<T, GradCfg<64, 64, 2, 2, 2>>(x, w, whole, stream)
+                      : launch_small<T, GradCfg<64, 64, 2, 2>>(x, w, whole, stream);
     return e != hipSuccess || n == 0 ? e : join_parts<T>(p, n, stream);
 }
 

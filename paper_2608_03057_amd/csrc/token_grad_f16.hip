@@ -8,9 +8,10 @@ hipError_t token_grad_f16(const GradJob &g, bool turned_a, bool whole, hipStream
     return run_product<f16_t>(g, turned_a, whole, stream);
 }
 
-hipError_t token_grads_f16(const GradJob &x, const GradJob &w, bool whole, hipStream_t stream)
+hipError_t token_grads_f16(const GradJob *x, const GradJob *w, int groups, bool whole,
+                           hipStream_t stream)
 {
-    return run_products<f16_t>(x, w, whole, stream);
+    return run_products<f16_t>(x, w, groups, whole, stream);
 }
 
 }  // namespace tasq
