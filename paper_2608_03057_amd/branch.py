@@ -245,10 +245,10 @@ def masked_linear_tokens_backward(dy: torch.Tensor, X: torch.Tensor, W: torch.Te
                                   workspace: Optional[torch.Tensor] = None):
     """Gradients (dx [M, K], dw [N, K], dbias fp32 [N]) of masked_linear_tokens from
     that of its output, dy [M, N] bfloat16 or half with rows at any stride (below 2^22
-    elements), and its arguments: the codes X with their scales sx are all that the program keeps of the
-    activations.  dx is the gradient of the activations, dw that of the weight
-    sw[n] W_b, both in dy's type and straight through the rounding to codes; the
-    gradient of sw is (dw * W_b).sum(1).  need_input=False leaves dx out (None),
+    elements), and its arguments: the codes X with their scales sx are all that the
+    program keeps of the activations.  dx is the gradient of the activations, dw that of
+    the weight sw[n] W_b, both in dy's type and straight through the rounding to codes;
+    the gradient of sw is (dw * W_b).sum(1).  need_input=False leaves dx out (None),
     need_weight=False dw and dbias."""
     M, N = shape = dy.shape
     K = W.shape[1]

@@ -95,7 +95,8 @@ int residual_norm(const tasq_residual *a, bool grad, void *stream)
     if (some_sum) {
         if (!aligned_to(a->workspace, 256))
             return TASQ_ERR_ALIGN;
-        const size_t need = tasq_residual_norm_workspace_bytes(a->type, a->batch, a->tokens, a->width);
+        const size_t need =
+            tasq_residual_norm_workspace_bytes(a->type, a->batch, a->tokens, a->width);
         if (need && (!a->workspace || a->workspace_bytes < need))
             return TASQ_ERR_WORKSPACE;
         c.part = static_cast<float *>(a->workspace);

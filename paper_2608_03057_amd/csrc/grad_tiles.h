@@ -116,8 +116,8 @@ __device__ __forceinline__ void grad_gemm_tile(const GradGemm &g, int tr, int tc
 #pragma unroll
         for (int i = 0; i < C::Q_LOADS; ++i) {
             const uint32_t at = (uint32_t)(i * C::NT + 64 * wave) * 16u;
-            load_chunk_unseen(rq, lds0 + (at < C::Q_BYTES ? stage + at : C::SPARE0 + at - C::Q_BYTES),
-                              q_off[i]);
+            const uint32_t to = at < C::Q_BYTES ? stage + at : C::SPARE0 + at - C::Q_BYTES;
+            load_chunk_unseen(rq, lds0 + to, q_off[i]);
         }
     };
 

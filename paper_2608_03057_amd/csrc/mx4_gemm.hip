@@ -348,7 +348,8 @@ __global__ void __launch_bounds__(C::NT) k_mx4_walk(Mx4Linear a, int tiles_m, in
             o.w[i ? i - C::FM : 0] = *reinterpret_cast<const v4i *>(
                 p + (wn * C::FN + (i ? i - C::FM : 0)) * 32 * 128);
         else
-            o.x[i - 1] = *reinterpret_cast<const v4i *>(p + (C::BN + (wm * C::FM + i - 1) * 32) * 128);
+            o.x[i - 1] =
+                *reinterpret_cast<const v4i *>(p + (C::BN + (wm * C::FM + i - 1) * 32) * 128);
     };
     auto reads = [&](uint32_t stage, int ks, Operands &o) {
         return [&, stage, ks](int i) {
@@ -441,7 +442,8 @@ __global__ void __launch_bounds__(C::NT) k_mx4_walk(Mx4Linear a, int tiles_m, in
         bias = (int)ask_bias(n0);
         // Rows of whole lines through LDS, BLOCKS of 32 channels at a time.
         T *y = static_cast<T *>(a.y) + (size_t)m1 * a.N;
-        const rsrc_t ry = make_rsrc(y, uniform(min(a.M - m1, C::BM)) * (uint32_t)a.N * (uint32_t)sizeof(T));
+        const uint32_t rows = uniform(min(a.M - m1, C::BM));
+        const rsrc_t ry = make_rsrc(y, rows * (uint32_t)a.N * (uint32_t)sizeof(T));
         char *out = sm + 2 * C::STAGE + wave * Walk::OUT;
         // (A lane number of its own, or the compiler forms all addresses before the
         // loop and has no registers left in it.)

@@ -238,7 +238,8 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                            rq, q_off + (uint32_t)(i * Q_ROWS) * (uint32_t)g.C, 0, 0));
         }
         if constexpr (!WHOLE) {
-            const T *const a0 = A + (TURNED ? (size_t)zt * g.a_stride + r0 : (size_t)r0 * g.a_stride + zt);
+            const T *const a0 =
+                A + (TURNED ? (size_t)zt * g.a_stride + r0 : (size_t)r0 * g.a_stride + zt);
             uint32_t a_bytes = 0;
             if (n) {
                 const uint32_t rows = TURNED ? n : (uint32_t)min(g.R - r0, C::BR);
@@ -254,9 +255,9 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 const int row = task / (A_PITCH / 16), first = 8 * (task % (A_PITCH / 16));
                 const bool in = TURNED ? row < (int)n && first < g.R - r0
                                        : r0 + row < g.R && first < (int)n;
-                raw.a[i] = __builtin_bit_cast(
-                    u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                               ra, in ? (uint32_t)row * a_pitch + 2u * (uint32_t)first : kOOB, 0, 0));
+                const uint32_t off = (uint32_t)row * a_pitch + 2u * (uint32_t)first;
+                raw.a[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                         ra, in ? off : kOOB, 0, 0));
             }
             // The last dword of either operand (its rows are near the end of the range).
             if (n && zt + (int)n == g.Z) {
@@ -310,7 +311,8 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
             uint32_t off = a_off;
             if constexpr (TURNED) {
                 const uint32_t n = (uint32_t)min(left, kGradStep);
-                rsrc = make_rsrc(A + (size_t)zt * g.a_stride + r0, n ? (n - 1) * a_pitch + a_last : 0u);
+                rsrc = make_rsrc(A + (size_t)zt * g.a_stride + r0,
+                                 n ? (n - 1) * a_pitch + a_last : 0u);
             } else {
                 // (From column zt on: the last row ends with the range.)
                 rsrc = make_rsrc(A + (size_t)r0 * g.a_stride + zt,
@@ -319,8 +321,9 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
             }
 #pragma unroll
             for (int i = 0; i < C::A_TASKS; ++i)
-                load_chunk_unseen(rsrc, lds0 + stage + (uint32_t)((wave * A_ROWS + i * A_NEXT) * A_PITCH),
-                                  off + (uint32_t)(i * A_NEXT) * a_pitch);
+                load_chunk_unseen(
+                    rsrc, lds0 + stage + (uint32_t)((wave * A_ROWS + i * A_NEXT) * A_PITCH),
+                    off + (uint32_t)(i * A_NEXT) * a_pitch);
         }
     };
     // What request() gave, into its stage: Q's parts i0 .. i1 - 1; A's chunks.
@@ -496,7 +499,8 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
         if (group > 0) {
 #pragma unroll
             for (int v = 0; v < HELD; ++v)
-                part[((group - 1) * HELD + v) * C::NT + tid] = acc[v / 16 / C::FR][v / 16 % C::FR][v % 16];
+                part[((group - 1) * HELD + v) * C::NT + tid] =
+                    acc[v / 16 / C::FR][v / 16 % C::FR][v % 16];
         }
         __syncthreads();
         if (group > 0)
