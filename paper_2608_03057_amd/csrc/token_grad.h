@@ -224,9 +224,11 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
         const rsrc_t rs = make_rsrc(g.s + zt, 4u * n);
         const int8_t *const q0 = g.Q + (size_t)zt * g.C;
         uint32_t bytes = n * (uint32_t)g.C;
+        bool cut = false;       // some chunk of this step reaches past Q's end
         if (!WHOLE && n) {
             const long long rest = q_end - q0;
-            bytes = rest < bytes + 7 ? (uint32_t)rest : bytes + 7;
+            cut = rest < bytes + 7;
+            bytes = cut ? (uint32_t)rest : bytes + 7;
         }
         const rsrc_t rq = make_rsrc(q0, bytes);
 #pragma unroll
@@ -259,8 +261,10 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
                 raw.a[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
                                                          ra, in ? off : kOOB, 0, 0));
             }
-            // The last dword of either operand (its rows are near the end of the range).
-            if (n && zt + (int)n == g.Z) {
+            // The last dword of either operand.  (Chunks of A reach its end from the last
+            // step only, which cuts Q short as well; those of Q, with rows of one code,
+            // from the last rows of the step before too.)
+            if (cut) {
 #pragma unroll
                 for (int i = 0; i < C::Q_TASKS; ++i) {
                     const int z = qz + i * Q_ROWS, c = c0 + qc;
