@@ -189,9 +189,11 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     char *const sm = all + group * C::LDS;
     const T *A = static_cast<const T *>(g.A);
     const int8_t *const q_end = g.Q + (size_t)g.Z * g.C;
+    const bool factors = g.C > 0;       // (the rows' sums alone have none to read)
     int shift = 0;
     if constexpr (sizeof(T) == 2 && __is_same(T, f16_t))
-        shift = range_exponent<C::ALL>(g.s, first, end, reinterpret_cast<float *>(all));
+        shift = range_exponent<C::ALL>(g.s, first, factors ? end : first,
+                                       reinterpret_cast<float *>(all));
 
     // A step's codes and factors (and A's chunks, where they pass through registers)
     // on their way.
@@ -221,7 +223,7 @@ __device__ __forceinline__ void grad_tile(const GradJob &g, int tr, int tc, int 
     auto request = [&](Raw &raw, int t) {
         const int zt = z0 + kGradStep * t;
         const uint32_t n = uniform(max(min(z1 - zt, kGradStep), 0));
-        const rsrc_t rs = make_rsrc(g.s + zt, 4u * n);
+        const rsrc_t rs = make_rsrc(g.s + zt, factors ? 4u * n : 0u);
         const int8_t *const q0 = g.Q + (size_t)zt * g.C;
         uint32_t bytes = n * (uint32_t)g.C;
         bool cut = false;       // some chunk of this step reaches past Q's end
