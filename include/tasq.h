@@ -869,9 +869,13 @@ int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const
  *             wanted.  dbias needs dw (TASQ_ERR_NULL).  X and sx are read for dw only,
  *             W and sw for dx only, and may else be NULL.
  *   workspace 256-byte aligned device scratch or NULL.  With
- *             tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K) bytes, long sums
- *             of small results are cut into ranges that run side by side; a smaller one
- *             runs them uncut.
+ *             tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K) bytes, whatever
+ *             the layout of dy, much work (M N K of 10^10) is done on 16-bit values that
+ *             are written there first, of both codes and of a dy whose rows are not whole
+ *             16-byte chunks, and long sums of small results are cut into ranges that run
+ *             side by side.  With a smaller one or none every tile makes its values from
+ *             codes, and ranges stay uncut where they do not fit: slower, results within
+ *             the same bounds.
  * N and dy_stride multiples of 8, K of 16 and 16-byte aligned dy, X and W take whole
  * vector loads.  Sums of nothing are zeros.  Errors: TASQ_ERR_NULL, _DIM (a negative
  * size, M or N > 2^30, and where M > 1 dy_stride < N or >= TASQ_MAX_GRAD_STRIDE), _BITS, _OVERFLOW (K > TASQ_MAX_K), _KIND, _ALIGN,

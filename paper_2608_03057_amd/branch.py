@@ -231,8 +231,9 @@ def linear_mx4(X: torch.Tensor, sx: torch.Tensor, W: torch.Tensor, sw: torch.Ten
 
 
 def masked_linear_tokens_backward_workspace_bytes(M: int, N: int, K: int) -> int:
-    """Workspace with which masked_linear_tokens_backward of these sizes runs ranges
-    of a long sum side by side."""
+    """Workspace with which masked_linear_tokens_backward of these sizes turns codes
+    into values once where there is much work, and runs ranges of a long sum side by
+    side; enough for any layout of dy.  A call with less is slower."""
     return _lib.lib().tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K)
 
 

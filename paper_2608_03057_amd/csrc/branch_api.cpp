@@ -254,7 +254,9 @@ void plan_values(GradPlan &p, bool bias)
 // Values pay where there is work enough to fill such tiles and to make up for the pass
 // that writes them.  (Codes / values, us of all kernels: 2000 x 1152 x 1152 52 / 52, 4096
 // tokens of it 55 / 64, 8192 tokens 81 / 73; 2048 x 2240 x 2240 87 / 84; 512 x 4608 x 4608
-// 82 / 80; 3001 x 4447 x 982 143 / 128.)
+// 82 / 80; 3001 x 4447 x 982 143 / 128.  With a copy of dy before it, rows at odd
+// addresses: 520 x 4456 x 4408 78 / 90, 2048 x 2240 x 2400 87 / 90, 3000 x 2240 x 2400
+// 114 / 102, 8192 x 3456 x 1152 259 / 169, 4096 x 11200 x 2240 581 / 439.)
 bool values_pay(int M, int N, int K)
 {
     return M >= 512 && N >= 256 && K >= 256 && (double)M * N * K >= 1e10;
@@ -358,22 +360,22 @@ size_t tasq_masked_linear_tokens_backward_workspace_bytes(int M, int N, int K)
 {
     if (!grad_sizes(M, N, K) || K > TASQ_MAX_K)
         return 0;
-    // Of values one product's parts after the other's, of codes both (whichever of the
-    // two ways their rows may lie).
+    // For rows of dy and of codes wherever they lie.  Of values one product's parts after
+    // the other's, and a copy of dy; of codes the parts of both, each of the larger tile.
     GradPlan plan[2] = {grad_plan(M, N, K, false), grad_plan(M, N, K, true)};
     if (values_pay(M, N, K)) {
         plan_values(plan[0], false);
         plan_values(plan[1], true);
         const size_t parts = plan[0].parts > plan[1].parts ? plan[0].parts : plan[1].parts;
-        return parts + value_bytes(M, N, K, true, true, N % 8 != 0).all();
+        return parts + value_bytes(M, N, K, true, true, true).all();
     }
-    size_t most = 0;
+    size_t most[2] = {};
     for (const bool whole : {false, true}) {
         plan_both(plan, true, {whole, whole}, true);
-        const size_t parts = plan[0].parts + plan[1].parts;
-        most = parts > most ? parts : most;
+        for (int i = 0; i < 2; ++i)
+            most[i] = plan[i].parts > most[i] ? plan[i].parts : most[i];
     }
-    return most;
+    return most[0] + most[1];
 }
 
 int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_stride,
