@@ -8,6 +8,7 @@ asynchronous on the current stream, and results carry no autograd graph.
 """
 from __future__ import annotations
 
+import functools
 import struct
 from typing import NamedTuple, Optional
 
@@ -23,10 +24,20 @@ _KINDS = {"layer": _lib.NORM_LAYER, "rms": _lib.NORM_RMS}
 _NONE = (0, 0)                  # strides of a tensor that is not there
 
 
-def _here(t: torch.Tensor, name: str) -> None:
-    """Calls go to the current device's stream: a tensor of another is refused."""
-    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+@functools.lru_cache(maxsize=None)
+def _devices() -> int:
+    """Devices of the process, of which there is one where a GPU tensor is."""
+    return torch.cuda.device_count()
+
+
+def _here(**tensors: Optional[torch.Tensor]) -> None:
+    """Calls go to the current device's stream: a tensor of another is refused.  (Of one
+    device there is nothing to check: a dozen tensors take 1 us of a call's 11.)"""
+    device = torch._C._cuda_getDevice()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"{name} is on device {t.get_device()}, which is not the current "
+                             f"device {device}")
 
 
 class ResidualGrads(NamedTuple):
@@ -59,7 +70,6 @@ def _residual(x, y, gate, weight, scale, shift, post_weight, kind, residual_scal
         raise _too_large(B, S, C)
     code = _type(x, "x")
     xs = _strided(x, dtype, shape, "x")
-    _here(x, "x")
     yat, ys = _rows(y, dtype, shape, "y")
     if kind not in _KINDS:
         raise ValueError(f"kind must be 'layer' or 'rms', got {kind!r}")
@@ -82,6 +92,9 @@ def _residual(x, y, gate, weight, scale, shift, post_weight, kind, residual_scal
         strides.append(0 if one else st[0])
     wat = _at(weight, torch.float32, (C,), "weight")
     pat = _at(post_weight, torch.float32, (C,), "post_weight")
+    if _devices() > 1:
+        _here(x=x, y=y, gate=gate, weight=weight, scale=scale, shift=shift,
+              post_weight=post_weight)
     return (code, _lib.TYPE_F32 if mod_type == torch.float32 else code, _KINDS[kind], shared, B, S,
             C, eps, residual_scale, x.data_ptr(), yat, xs[0], xs[1], ys[0], ys[1], *at, *strides,
             wat, pat), shared
@@ -116,6 +129,8 @@ def residual_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None,
         else:
             _need(out_r, x.dtype, x.shape, "out_r")
         rat = out_r.data_ptr()
+    if _devices() > 1:
+        _here(out_r=out_r, out_h=out_h)
     a = _RESIDUAL.pack(*head, rat, out_h.data_ptr(), 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
     rc = _lib.lib().tasq_residual_norm(a, _stream())
     if rc:
@@ -145,6 +160,8 @@ def residual_norm_backward(dh: torch.Tensor, dr: Optional[torch.Tensor], r: torc
     shape, dtype = r.shape, r.dtype
     hat, hs = _rows(dh, dtype, shape, "dh")
     rat, rs = _rows(dr, dtype, shape, "dr")
+    if _devices() > 1:
+        _here(dh=dh, dr=dr, workspace=workspace)
     dx, dy = _like(r), None if y is None else _like(r)
     B, S, C = shape
     given = (gate, scale, shift, weight, post_weight)
@@ -185,7 +202,6 @@ def quantize_mx4(x: torch.Tensor, out: Optional[torch.Tensor] = None,
     if M > _MOST or K > _MOST:
         raise _too_large(M, K)
     st = _strided(x, x.dtype, shape, "x")
-    _here(x, "x")
     whole = (K + 127) // 128
     if out is None:
         out = torch.empty_strided((M, 64 * whole), (64 * whole, 1), dtype=torch.uint8,
@@ -197,6 +213,8 @@ def quantize_mx4(x: torch.Tensor, out: Optional[torch.Tensor] = None,
                                      device=x.device)
     else:
         _need(scales, torch.uint8, (M, 4 * whole), "scales")
+    if _devices() > 1:
+        _here(x=x, out=out, scales=scales)
     rc = _lib.lib().tasq_quantize_mx4(x.data_ptr(), _type(x, "x"), M, K, st[0], out.data_ptr(),
                                       scales.data_ptr(), _stream())
     if rc:
@@ -217,11 +235,12 @@ def linear_mx4(X: torch.Tensor, sx: torch.Tensor, W: torch.Tensor, sw: torch.Ten
     _need(W, torch.uint8, (N, half), "W")
     _need(sx, torch.uint8, (M, half // 16), "sx")
     _need(sw, torch.uint8, (N, half // 16), "sw")
-    _here(X, "X")
     if y is None:
         y = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=X.device)
     else:
         _need(y, y.dtype, (M, N), "y")
+    if _devices() > 1:
+        _here(X=X, sx=sx, W=W, sw=sw, bias=bias, y=y)
     rc = _lib.lib().tasq_linear_mx4(X.data_ptr(), sx.data_ptr(), W.data_ptr(), sw.data_ptr(),
                                     _at(bias, torch.float32, (N,), "bias"), M, N, 2 * half,
                                     y.data_ptr(), _type(y, "y"), _stream())
@@ -259,7 +278,6 @@ def masked_linear_tokens_backward(dy: torch.Tensor, X: torch.Tensor, W: torch.Te
     if dtype != torch.bfloat16 and dtype != torch.float16:
         raise ValueError(f"dy must be bfloat16 or float16, got {dtype}")
     st = _strided(dy, dtype, shape, "dy")
-    _here(dy, "dy")
     _need(X, torch.int8, (M, K), "X")
     _need(W, torch.int8, (N, K), "W")
     _need(sx, torch.float32, (M,), "sx")
@@ -276,6 +294,8 @@ def masked_linear_tokens_backward(dy: torch.Tensor, X: torch.Tensor, W: torch.Te
     dx, xat = grad(dx, need_input, X, dtype, "dx")
     dw, wat = grad(dw, need_weight, W, dtype, "dw")
     dbias, bat = grad(dbias, need_weight, sw, torch.float32, "dbias")
+    if _devices() > 1:
+        _here(dy=dy, X=X, W=W, sx=sx, sw=sw, dx=dx, dw=dw, dbias=dbias, workspace=workspace)
     L = _lib.lib()
     if workspace is None:
         nbytes = L.tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K)
