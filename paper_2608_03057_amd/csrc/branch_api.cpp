@@ -137,7 +137,6 @@ constexpr size_t round256(size_t v) { return (v + 255) / 256 * 256; }
 // tiles, or of codes as they are.
 struct GradPlan {
     int R, Z, C;
-    bool values;
     int tile, tile_c;           // rows and columns of a tile
     int tiles_r, tiles_c, splits, split_steps;
     size_t parts;               // bytes of the ranges' parts
@@ -187,7 +186,6 @@ void plan_codes(GradPlan &p, bool bias, bool whole, bool cut, int groups = 1)
     const int steps = (int)((p.Z + 63LL) / 64);
     const long long work = (long long)tiles_of(p.R, 64) * tiles_of(p.C, 64) * (steps + 3);
     const int t = work < 9500 ? 64 : work < 36000 || !whole ? 128 : 256;
-    p.values = false;
     p.tile = p.tile_c = t;
     p.tiles_r = tiles_of(p.R, t);
     p.tiles_c = tiles_of(p.C, t);
@@ -230,7 +228,6 @@ void plan_values(GradPlan &p, bool bias)
     double least = 0;
     for (const int c : {256, 192}) {
         GradPlan q = p;
-        q.values = true;
         q.tile = 256;
         q.tile_c = c;
         q.tiles_r = tiles_of(q.R, 256);

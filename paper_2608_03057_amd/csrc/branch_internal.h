@@ -33,7 +33,6 @@ struct NormCall {
     float *part;                // backward: [batch][chunks][3][width]
     bool sums;                  // backward: some of dgate .. dpost are wanted
 };
-constexpr int kMaxNormWidth = TASQ_MAX_RESIDUAL_WIDTH;
 hipError_t launch_residual_norm(const NormCall &c, hipStream_t stream);
 hipError_t launch_residual_norm_backward(const NormCall &c, hipStream_t stream);
 // Waves of a row, rows at a time and workgroups for each batch entry of the gradient.

@@ -634,29 +634,30 @@ __global__ void __launch_bounds__(256) k_join_grad(GradParts one, GradParts two)
     }
 }
 
-template <class T, class C, bool TURNED> hipError_t launch_cfg(const GradJob &g, bool whole,
-                                                              hipStream_t stream)
+template <class T, class C, bool TURNED, bool WHOLE>
+hipError_t launch_cfg(const GradJob &g, hipStream_t stream)
 {
     constexpr long long MOST = 1 << 22;
     const long long units = (long long)g.tiles_r * g.tiles_c * g.splits;
     for (long long u = 0; u < units; u += MOST) {
         const unsigned grid = (unsigned)(units - u < MOST ? units - u : MOST);
-        if (whole)
-            k_token_grad<T, C, TURNED, true><<<grid, C::NT, 0, stream>>>(g, (int)u);
-        else
-            k_token_grad<T, C, TURNED, false><<<grid, C::NT, 0, stream>>>(g, (int)u);
+        k_token_grad<T, C, TURNED, WHOLE><<<grid, C::NT, 0, stream>>>(g, (int)u);
         if (hipError_t e = hipGetLastError())
             return e;
     }
     return hipSuccess;
 }
 
+// (Tiles of 256 are of whole chunks only: passing rows through registers as well, they
+// spill, and are slower than tiles of 128.)
 template <class T, bool TURNED>
 hipError_t launch_product(const GradJob &g, bool whole, hipStream_t stream)
 {
     if (g.tile == 256)
-        return launch_cfg<T, GradCfg<256, 256, 4, 2>, TURNED>(g, whole, stream);
-    return launch_cfg<T, GradCfg<128, 128, 2, 2>, TURNED>(g, whole, stream);
+        return whole ? launch_cfg<T, GradCfg<256, 256, 4, 2>, TURNED, true>(g, stream)
+                     : hipErrorInvalidValue;
+    return whole ? launch_cfg<T, GradCfg<128, 128, 2, 2>, TURNED, true>(g, stream)
+                 : launch_cfg<T, GradCfg<128, 128, 2, 2>, TURNED, false>(g, stream);
 }
 
 // What is left to add up of a product whose range is cut.
