@@ -122,6 +122,8 @@ def residual_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None,
     else:
         _need(out_h, x.dtype, x.shape, "out_h")
     if y is None:
+        if out_r is not None:
+            raise ValueError("out_r needs y: without it r is x, and is not written")
         out_r, rat = x, 0
     else:
         if out_r is None:
