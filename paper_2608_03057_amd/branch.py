@@ -142,6 +142,8 @@ def residual_norm(x: torch.Tensor, y: Optional[torch.Tensor] = None,
 
 def residual_norm_workspace_bytes(x: torch.Tensor) -> int:
     """Workspace of residual_norm_backward for a stream like x [B, S, C]."""
+    if max(x.shape) > _MOST:
+        raise _too_large(*x.shape)
     return _lib.lib().tasq_residual_norm_workspace_bytes(_type(x, "x"), *x.shape)
 
 
@@ -255,6 +257,8 @@ def masked_linear_tokens_backward_workspace_bytes(M: int, N: int, K: int) -> int
     """Workspace with which masked_linear_tokens_backward of these sizes turns codes
     into values once where there is much work, and runs ranges of a long sum side by
     side; enough for any layout of dy.  A call with less is slower."""
+    if M > _MOST or N > _MOST or K > _MOST:
+        raise _too_large(M, N, K)
     return _lib.lib().tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K)
 
 
