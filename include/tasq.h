@@ -866,8 +866,8 @@ int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const
  * fp32 and in a fixed order (the same bits each time), results are rounded once.
  *   dy        [M][N] of type (BF16 or F16), row m at dy + m * dy_stride
  *   dx        [M][K] of type, dw [N][K] of type, dbias fp32 [N], contiguous; NULL: not
- *             wanted.  dbias needs dw (TASQ_ERR_NULL).  X and sx are read for dw only,
- *             W and sw for dx only, and may else be NULL.
+ *             wanted.  dbias needs dw (TASQ_ERR_NULL) unless K is 0.  X and sx are read
+ *             for dw only, W and sw for dx only, and may else be NULL.
  *   workspace 256-byte aligned device scratch or NULL.  With
  *             tasq_masked_linear_tokens_backward_workspace_bytes(M, N, K) bytes, whatever
  *             the layout of dy, much work (M N K of 10^10) is done on 16-bit values that
@@ -878,8 +878,8 @@ int tasq_linear_mx4(const uint8_t *X, const uint8_t *sx, const uint8_t *W, const
  *             the same bounds.
  * N and dy_stride multiples of 8, K of 16 and 16-byte aligned dy, X and W take whole
  * vector loads.  Sums of nothing are zeros.  Errors: TASQ_ERR_NULL, _DIM (a negative
- * size, M or N > 2^30, and where M > 1 dy_stride < N or >= TASQ_MAX_GRAD_STRIDE), _BITS, _OVERFLOW (K > TASQ_MAX_K), _KIND, _ALIGN,
- * _HIP.
+ * size, M or N > 2^30, and where M > 1 dy_stride < N or >= TASQ_MAX_GRAD_STRIDE), _BITS,
+ * _OVERFLOW (K > TASQ_MAX_K), _KIND (also an fp32 dy), _ALIGN, _HIP.
  */
 int tasq_masked_linear_tokens_backward(const void *dy, int type, long long dy_stride,
                                        const int8_t *X, const float *sx, const int8_t *W,

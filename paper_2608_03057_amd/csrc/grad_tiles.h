@@ -7,8 +7,8 @@
 // product is one of two 16-bit matrices whose rows go to LDS directly: no registers and
 // no vector instructions but addresses between memory and the matrix unit.  Bound by the
 // matrix unit at the clock that the power allows it (2.0 to 2.2 GHz, busy 0.42 to 0.48):
-// 8192 tokens of 1152 -> 3456 70 us a product and 9.5 for the values, 4096 of 2240 ->
-// 11200 207 and 18.
+// medians, 8192 tokens of 1152 -> 3456 77 us a product (the least 70) and 10 for the
+// values, 4096 of 2240 -> 11200 206 (by card up to 245) and 19.
 #pragma once
 
 #include "token_grad.h"

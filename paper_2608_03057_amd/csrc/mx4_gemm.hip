@@ -11,9 +11,11 @@
 // rows of 16-byte stores.
 //
 // Bound, where there are many tokens, by what the products wait for: their share of the
-// matrix units' time is 0.45 over long sums (8192^3 in 285 us), 0.27 for 4096x2240 ->
-// 11200 (77 us) and 0.2 for 8192x1152 -> 4608 (41 us), where a tile's results take as
-// long as two steps.  With few tokens it is the launch and one round of loads.
+// matrix units' time is 0.45 over long sums (8192^3 in 278 us where calls follow for
+// long, 296 to 375 in a first dozen, whose clock is still settling), 0.27 for 4096x2240 ->
+// 11200 (77 us, 81 by card) and 0.2 for 8192x1152 -> 4608 (41 us), where a tile's results
+// take as long as two steps and 2.25 rounds of tiles the time of three.  With few tokens
+// it is the launch and one round of loads.
 #include "branch_internal.h"
 #include "floats.h"
 #include "gemm_pers.h"

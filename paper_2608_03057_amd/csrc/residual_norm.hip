@@ -280,8 +280,11 @@ __global__ void __launch_bounds__(WAVE ? 256 : NV == 1 ? 512 : 1024) k_residual_
 }
 
 // Most threads of a workgroup of the gradient: three waves a SIMD, whose registers
-// hold a row of 16-bit values and its sums, or two for fp32.  (The widest rows take
-// what there is.)
+// hold a row of 16-bit values and its sums, or two for fp32.  Wider rows have sixteen
+// channels a lane and the registers of 1024 threads, which are too few: they spill, one
+// row at a time on a compute unit.  (Gradients of 33.5 M elements, channels: bfloat16,
+// 403 MB, 76 us at 4096, 79 at 6144, 557 at 8192, 432 at 16384; fp32, 805 MB, 191 at 4096,
+// 905 at 5120, 648 at 8192, 496 at 16384.)
 template <class T, int NV> constexpr int kBackThreads = NV > 1 ? 1024 : sizeof(T) == 4 ? 512 : 768;
 
 // A workgroup takes rows of one batch entry, every (chunks * groups)-th for each of
@@ -639,7 +642,8 @@ hipError_t backward(const NormCall &c, hipStream_t stream)
 
 // Eight channels a lane up to the workgroups' most, and sixteen.  (Rows of 1152 in
 // bfloat16 with 24 channels a lane, a wave to a row: 17.5 us for 8192, 14.7 with three
-// waves.)
+// waves.  Sixteen spill a little: 33.5 M elements of bfloat16, 268 MB, 45 us at 4096
+// channels, 73 at 5120, 51 at 8192, 65 at 16384; fp32 88, 189, 148, 175.)
 constexpr int kWideForward = 8 * 512;
 
 template <class T, bool FULL> hipError_t forward_width(const NormCall &c, hipStream_t stream)

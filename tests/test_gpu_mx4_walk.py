@@ -123,3 +123,14 @@ def test_walk_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, f())
+
+
+@pytest.mark.parametrize("M,N", [(100, 70), (2500, 1290), (2500, 9008)])
+@pytest.mark.parametrize("y_type", list(HALF))
+def test_no_channels_over_many_tokens(M, N, y_type):
+    """Sums of nothing in tiles of 64, 128 and 256: the bias, or zeros."""
+    x, w = (T.quantize_mx4(torch.zeros(n, 0, device=DEV)) for n in (M, N))
+    bias = operands(1, 32, N, 0)[2]
+    y = T.linear_mx4(*x, *w, bias, out_dtype=y_type)
+    assert torch.equal(y, bias.to(y_type).expand(M, N))
+    assert not T.linear_mx4(*x, *w, out_dtype=y_type).any()
